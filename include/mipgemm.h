@@ -338,6 +338,113 @@ int mipgemm_static_scratch_status(void *stream);
  * the next such call). */
 int mipgemm_release_staging(void);
 
+/* ---- operators of an 8-bit transformer layer (extensions: the paper stops at one scale per matrix) ----
+ *
+ * The paper's scheme (Section 7.3) carries one scale per matrix and leaves activations, residuals and
+ * everything around the integer product to separate floating-point steps.  A transformer layer that
+ * keeps its precision in 8 bits needs a scale per token and per output channel, needs the codes made on
+ * the device, and, to be trained, needs the way back.  These entry points add that:
+ *
+ *   mipgemm_quantize_rows    activations -> codes, one scale per row (also: activation checkpoints)
+ *   mipgemm_dequantize_rows  ... and back
+ *   mipgemm_s8s8_linear      C = act(a_i b_j (A B)_ij + bias_j) + residual_ij
+ *   mipgemm_s8s8_gated       H = act(G) * U, G and U two projections of the same tokens, in one kernel
+ *   mipgemm_s8s8_gated_grad  the gradients of G and U, recomputed from the codes
+ *   mipgemm_bf16s8_product   C = A diag(s) B: gradients times codes whose scales lie along the summed axis
+ *
+ * Common to all of them: device pointers, asynchronous on `stream`, errors and scratch memory as for
+ * mipgemm_s8s8s32.  `type` is the element type of every floating matrix of the call; a pointer to such
+ * a matrix is aligned to its element size, pitches are counted in elements.  The 8-bit sums are exact
+ * in int32 (the K limits of mipgemm_s8s8s32 hold), everything behind them is computed in binary32 and
+ * rounded once, to nearest even, when it is stored.  Scale vectors are float32, 4-byte aligned; NULL
+ * stands for all ones.  Operands with 16-byte aligned bases and pitches are read in place, other 8-bit
+ * operands are re-pitched into scratch memory first.  Inputs and outputs must not overlap, except where
+ * stated.  Empty outputs (M == 0 or N == 0) are no-ops; K == 0 means that every sum is 0.
+ */
+typedef enum { MIPGEMM_TYPE_F32 = 0, MIPGEMM_TYPE_F16 = 1, MIPGEMM_TYPE_BF16 = 2 } mipgemm_type_t;
+
+typedef enum {
+    MIPGEMM_ACT_NONE = 0,
+    MIPGEMM_ACT_RELU = 1,      /* max(x, 0); derivative 0 at 0                                    */
+    MIPGEMM_ACT_GELU = 2,      /* x (1 + erf(x / sqrt 2)) / 2                                     */
+    MIPGEMM_ACT_GELU_TANH = 3, /* x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2                 */
+    MIPGEMM_ACT_SILU = 4       /* x / (1 + e^-x)                                                  */
+} mipgemm_activation_t;
+
+/*
+ * Codes and scales of the rows of X:  scale_i = max_j |x_ij| / 127,  q_ij = rne(x_ij * (127 / max_j |x_ij|)),
+ * both quotients and the product rounded in binary32.  Codes lie in [-127, 127].  A row whose largest
+ * magnitude is below 2^-119 (the all-zero row among them; 127 / max would leave the binary32 range) gets
+ * scale 0 and codes 0; a row that holds an infinity or a NaN gets scale NaN and codes 0, so that whatever
+ * is computed from it is NaN.
+ *
+ *   X : M x N row-major, ldx >= N (read)    Q : M x N codes row-major, ldq >= N (written)
+ *   scale : M values (written)
+ */
+int mipgemm_quantize_rows(int type, int64_t M, int64_t N, const void *X, int64_t ldx,
+                          int8_t *Q, int64_t ldq, float *scale, void *stream);
+
+/* X = diag(scale) Q, rounded to the type: restores a checkpoint.  Arguments as above; Q and scale are read. */
+int mipgemm_dequantize_rows(int type, int64_t M, int64_t N, const int8_t *Q, int64_t ldq, const float *scale,
+                            void *X, int64_t ldx, void *stream);
+
+/*
+ * C = act(a_scale_i * b_scale_j * (A * B)_ij + bias_j) + residual_ij.
+ *   A, B as for mipgemm_s8s8s32 / mipgemm_u8s8s32;  a_scale : M, b_scale : N, bias : N float32 (each may be NULL)
+ *   residual : M x N of the call's type, ldr >= N, or NULL; may be C itself (with ldr == ldc)
+ *   C : M x N of the call's type, ldc >= N (written)
+ */
+int mipgemm_s8s8_linear(int type, int act, int64_t M, int64_t N, int64_t K,
+                        const int8_t *A, int64_t lda, const float *a_scale,
+                        const int8_t *B, int64_t ldb, const float *b_scale, const float *bias,
+                        const void *residual, int64_t ldr, void *C, int64_t ldc, void *stream);
+int mipgemm_u8s8_linear(int type, int act, int64_t M, int64_t N, int64_t K,
+                        const uint8_t *A, int64_t lda, const float *a_scale,
+                        const int8_t *B, int64_t ldb, const float *b_scale, const float *bias,
+                        const void *residual, int64_t ldr, void *C, int64_t ldc, void *stream);
+
+/*
+ * The two projections of a gated feed-forward block, its activation and its product:
+ *   G_ij = x_scale_i g_scale_j (X Wg)_ij,  U_ij = x_scale_i u_scale_j (X Wu)_ij,  H_ij = act(G_ij) * U_ij.
+ *   X : M x K codes row-major, ldx >= K;  Wg, Wu : F runs of K contiguous codes (as B of mipgemm_s8s8s32),
+ *   pitches ldg, ldu >= K;  x_scale : M, g_scale, u_scale : F (each may be NULL)
+ *   H : M x F of the call's type, ldh >= F (written)
+ */
+int mipgemm_s8s8_gated(int type, int act, int64_t M, int64_t F, int64_t K,
+                       const int8_t *X, int64_t ldx, const float *x_scale,
+                       const int8_t *Wg, int64_t ldg, const float *g_scale,
+                       const int8_t *Wu, int64_t ldu, const float *u_scale,
+                       void *H, int64_t ldh, void *stream);
+
+/*
+ * Backward pass of that block up to its projections: with dH the gradient of H,
+ *   dG_ij = dH_ij * U_ij * act'(G_ij),   dU_ij = dH_ij * act(G_ij).
+ * G and U are computed again from the codes (the 8-bit checkpoint of the block's input is all that has to
+ * be kept).  dH, dG, dU : M x F of the call's type, pitches >= F; dG and dU may be the two halves of one
+ * M x 2F matrix (the form mipgemm_bf16s8_product takes); dG or dU may be dH itself.
+ */
+int mipgemm_s8s8_gated_grad(int type, int act, int64_t M, int64_t F, int64_t K,
+                            const int8_t *X, int64_t ldx, const float *x_scale,
+                            const int8_t *Wg, int64_t ldg, const float *g_scale,
+                            const int8_t *Wu, int64_t ldu, const float *u_scale,
+                            const void *dH, int64_t lddh, void *dG, int64_t lddg, void *dU, int64_t lddu,
+                            void *stream);
+
+/*
+ * C = [C +] A diag(b_scale) B with A bfloat16 and B 8-bit codes: the products of a backward pass.
+ *   gradient of the input    dX = dZ diag(w_scale) W      a_order MIPGEMM_K_CONTIGUOUS
+ *   gradient of the weights  dW = dZ^T diag(x_scale) X    a_order MIPGEMM_MN_CONTIGUOUS (dZ as it lies)
+ * where W [outputs][inputs] and X [tokens][inputs] lie as the forward pass reads them.
+ *   A : bfloat16, a(i,k) = A[i*lda + k] (K_CONTIGUOUS, lda >= K) or A[k*lda + i] (MN_CONTIGUOUS, lda >= M)
+ *   B : codes, b(k,j) = B[k*ldb + j], ldb >= N;   b_scale : K float32, or NULL
+ *   C : M x N, float32 or bfloat16 (`type`), ldc >= N;  accumulate != 0 adds to what C holds
+ * Each b_scale_k * b_kj is rounded to bfloat16 (as an operand of the tensor cores; the codes themselves
+ * are exact there); products and sums are held in binary32, the result is rounded once.
+ */
+int mipgemm_bf16s8_product(int type, int a_order, int64_t M, int64_t N, int64_t K,
+                           const void *A, int64_t lda, const int8_t *B, int64_t ldb, const float *b_scale,
+                           void *C, int64_t ldc, int accumulate, void *stream);
+
 /* ---- support calls (no counterpart in the paper) ---- */
 
 /* Number of kernels this library has enqueued since it was loaded (all threads, all devices). */

@@ -52,6 +52,13 @@ SIGNATURES = {
     "mipgemm_s8s8s8_requant_bias": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, ctypes.c_float, _int, _vp, _vp]),
     "mipgemm_u8s8u8_requant_bias": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, ctypes.c_float, _vp, _vp]),
     "mipgemm_conv_u8s8u8_requant_bias": (_int, [_i64] * 5 + [_int] * 8 + [_vp, _vp, _vp, ctypes.c_float, _vp, _vp]),
+    "mipgemm_quantize_rows": (_int, [_int, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "mipgemm_dequantize_rows": (_int, [_int, _i64, _i64, _vp, _i64, _vp, _vp, _i64, _vp]),
+    "mipgemm_s8s8_linear": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64, _vp] * 2 + [_vp, _vp, _i64, _vp, _i64, _vp]),
+    "mipgemm_u8s8_linear": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64, _vp] * 2 + [_vp, _vp, _i64, _vp, _i64, _vp]),
+    "mipgemm_s8s8_gated": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64, _vp] * 3 + [_vp, _i64, _vp]),
+    "mipgemm_s8s8_gated_grad": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64, _vp] * 3 + [_vp, _i64] * 3 + [_vp]),
+    "mipgemm_bf16s8_product": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64] * 2 + [_vp, _vp, _i64, _int, _vp]),
     "mipgemm_host_s8s8s32": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
     "mipgemm_host_u8s8s32": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
     "mipgemm_s8s8s32_static_scratch": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
@@ -230,6 +237,58 @@ def mipgemm_conv_u8s8f32_dequant(Nb, H, W, Cin, Cout, R, S, stride_h, stride_w, 
     return _check(_lib.mipgemm_conv_u8s8f32_dequant(Nb, H, W, Cin, Cout, R, S, stride_h, stride_w, pad_h, pad_w,
                                                     dil_h, dil_w, _ptr(X), _ptr(Wt), _ptr(Y), float(scale),
                                                     _stream(stream)), check)
+
+
+#: mipgemm_type_t and mipgemm_activation_t by name
+TYPES = {"f32": 0, "f16": 1, "bf16": 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def mipgemm_quantize_rows(type, M, N, X, ldx, Q, ldq, scale, stream=None, check=True) -> int:
+    """Q[int8] = rne(X * 127 / rowmax), scale[row] = rowmax / 127."""
+    return _check(_lib.mipgemm_quantize_rows(type, M, N, _ptr(X), ldx, _ptr(Q), ldq, _ptr(scale), _stream(stream)), check)
+
+
+def mipgemm_dequantize_rows(type, M, N, Q, ldq, scale, X, ldx, stream=None, check=True) -> int:
+    """X = diag(scale) Q."""
+    return _check(_lib.mipgemm_dequantize_rows(type, M, N, _ptr(Q), ldq, _ptr(scale), _ptr(X), ldx, _stream(stream)),
+                  check)
+
+
+def mipgemm_s8s8_linear(type, act, M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, residual, ldr, C, ldc, stream=None,
+                        check=True) -> int:
+    """C = act(a_scale[row] * b_scale[column] * (A * B) + bias[column]) + residual; scales, bias and residual may be None."""
+    return _check(_lib.mipgemm_s8s8_linear(type, act, M, N, K, _ptr(A), lda, _ptr(a_scale), _ptr(B), ldb, _ptr(b_scale),
+                                           _ptr(bias), _ptr(residual), ldr, _ptr(C), ldc, _stream(stream)), check)
+
+
+def mipgemm_u8s8_linear(type, act, M, N, K, A, lda, a_scale, B, ldb, b_scale, bias, residual, ldr, C, ldc, stream=None,
+                        check=True) -> int:
+    """Same with unsigned 8-bit A."""
+    return _check(_lib.mipgemm_u8s8_linear(type, act, M, N, K, _ptr(A), lda, _ptr(a_scale), _ptr(B), ldb, _ptr(b_scale),
+                                           _ptr(bias), _ptr(residual), ldr, _ptr(C), ldc, _stream(stream)), check)
+
+
+def mipgemm_s8s8_gated(type, act, M, F, K, X, ldx, x_scale, Wg, ldg, g_scale, Wu, ldu, u_scale, H, ldh, stream=None,
+                       check=True) -> int:
+    """H = act(x_scale[row] * g_scale[column] * (X * Wg)) * (x_scale[row] * u_scale[column] * (X * Wu))."""
+    return _check(_lib.mipgemm_s8s8_gated(type, act, M, F, K, _ptr(X), ldx, _ptr(x_scale), _ptr(Wg), ldg, _ptr(g_scale),
+                                          _ptr(Wu), ldu, _ptr(u_scale), _ptr(H), ldh, _stream(stream)), check)
+
+
+def mipgemm_s8s8_gated_grad(type, act, M, F, K, X, ldx, x_scale, Wg, ldg, g_scale, Wu, ldu, u_scale, dH, lddh, dG, lddg,
+                            dU, lddu, stream=None, check=True) -> int:
+    """dG = dH * U * act'(G), dU = dH * act(G), with G and U recomputed from the codes."""
+    return _check(_lib.mipgemm_s8s8_gated_grad(type, act, M, F, K, _ptr(X), ldx, _ptr(x_scale), _ptr(Wg), ldg,
+                                               _ptr(g_scale), _ptr(Wu), ldu, _ptr(u_scale), _ptr(dH), lddh, _ptr(dG), lddg,
+                                               _ptr(dU), lddu, _stream(stream)), check)
+
+
+def mipgemm_bf16s8_product(type, a_order, M, N, K, A, lda, B, ldb, b_scale, C, ldc, accumulate=0, stream=None,
+                           check=True) -> int:
+    """C (+)= A[bf16] * diag(b_scale) * B[int8, K x N row-major]; a_order K_CONTIGUOUS or MN_CONTIGUOUS."""
+    return _check(_lib.mipgemm_bf16s8_product(type, a_order, M, N, K, _ptr(A), lda, _ptr(B), ldb, _ptr(b_scale), _ptr(C),
+                                              ldc, int(bool(accumulate)), _stream(stream)), check)
 
 
 def mipgemm_host_s8s8s32(M, N, K, A, lda, B, ldb, C, ldc, accumulate=0, stream=None, check=True) -> int:

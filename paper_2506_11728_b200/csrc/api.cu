@@ -1222,6 +1222,85 @@ int host_impl(bool a_unsigned, int64_t M, int64_t N, int64_t K, const void* A, i
     return st;
 }
 
+// ---------------------------------------------------------------------------------------
+// Operators of an 8-bit transformer layer.
+
+size_t type_size(int type) { return type == MIPGEMM_TYPE_F32 ? 4 : 2; }
+bool type_ok(int type) { return type >= MIPGEMM_TYPE_F32 && type <= MIPGEMM_TYPE_BF16; }
+bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// Rows to codes (`quantize`) or codes to rows.
+int rows_impl(bool quantize, int type, int64_t M, int64_t N, void* X, int64_t ldx, int8_t* Q, int64_t ldq, float* scale,
+              void* stream_v) {
+    tl_last_path = MIPGEMM_PATH_NONE;
+    if (!type_ok(type) || M < 0 || N < 0 || M > 0x7FFFFF00LL || N > 0x7FFFFF00LL || ldx < N || ldq < N)
+        return MIPGEMM_ERR_INVALID_ARG;
+    if (M == 0 || (N == 0 && !quantize)) return MIPGEMM_OK;
+    if (!scale || !aligned_to(scale, 4)) return MIPGEMM_ERR_INVALID_ARG;
+    if (N > 0 && (!X || !Q || !aligned_to(X, type_size(type)))) return MIPGEMM_ERR_INVALID_ARG;
+    DeviceState* dev = nullptr;
+    const int st = get_device(&dev);
+    if (st != MIPGEMM_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    const cudaError_t e = quantize ? launch_quantize_rows(type, M, N, X, ldx, Q, ldq, scale, stream)
+                                   : launch_dequantize_rows(type, M, N, Q, ldq, scale, X, ldx, stream);
+    ++g_launches;
+    if (e != cudaSuccess) return cuda_fail(e);
+    return MIPGEMM_OK;
+}
+
+int layer_impl(const LayerArgs& a, void* stream_v) {
+    tl_last_path = MIPGEMM_PATH_NONE;
+    const bool gated = a.op != kOpLinear;
+    if (!type_ok(a.type) || a.act < MIPGEMM_ACT_NONE || a.act > MIPGEMM_ACT_SILU) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.M < 0 || a.N < 0 || a.K < 0 || a.M > 0x7FFFFF00LL || a.N > 0x7FFFFF00LL / 2) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.lda < a.K || a.ldb0 < a.K || (gated && a.ldb1 < a.K) || a.ldc < a.N) return MIPGEMM_ERR_INVALID_ARG;
+    if ((a.R || a.op == kOpGatedGrad) && a.ldr < a.N) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.op == kOpGatedGrad && a.ldc2 < a.N) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.K > (a.a_unsigned ? 65793 : 131071)) return MIPGEMM_ERR_K_TOO_LARGE;
+    if (a.M == 0 || a.N == 0) {
+        tl_last_path = MIPGEMM_PATH_TRIVIAL;
+        return MIPGEMM_OK;
+    }
+    if (!a.C || (a.op == kOpGatedGrad && (!a.C2 || !a.R))) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.K > 0 && (!a.A || !a.B0 || (gated && !a.B1))) return MIPGEMM_ERR_INVALID_ARG;
+    for (const void* p : {static_cast<const void*>(a.C), static_cast<const void*>(a.C2), a.R})
+        if (!aligned_to(p, type_size(a.type))) return MIPGEMM_ERR_INVALID_ARG;
+    for (const float* p : {a.a_scale, a.b0_scale, a.b1_scale, a.bias})
+        if (!aligned_to(p, 4)) return MIPGEMM_ERR_INVALID_ARG;
+    DeviceState* dev = nullptr;
+    const int st = get_device(&dev);
+    if (st != MIPGEMM_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    const cudaError_t e = launch_layer_simple(a, stream);
+    ++g_launches;
+    if (e != cudaSuccess) return cuda_fail(e);
+    tl_last_path = a.K == 0 ? MIPGEMM_PATH_TRIVIAL : MIPGEMM_PATH_DENSE;
+    return MIPGEMM_OK;
+}
+
+int product_impl(const ProductArgs& a, void* stream_v) {
+    tl_last_path = MIPGEMM_PATH_NONE;
+    if ((a.type != MIPGEMM_TYPE_F32 && a.type != MIPGEMM_TYPE_BF16) || (a.a_order & ~1)) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.M < 0 || a.N < 0 || a.K < 0 || a.M > 0x7FFFFF00LL || a.N > 0x7FFFFF00LL || a.K > 0x7FFFFF00LL)
+        return MIPGEMM_ERR_INVALID_ARG;
+    if (a.lda < (a.a_order ? a.M : a.K) || a.ldb < a.N || a.ldc < a.N) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.M == 0 || a.N == 0) {
+        tl_last_path = MIPGEMM_PATH_TRIVIAL;
+        return MIPGEMM_OK;
+    }
+    if (!a.C || !aligned_to(a.C, type_size(a.type)) || !aligned_to(a.b_scale, 4)) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.K > 0 && (!a.A || !a.B || !aligned_to(a.A, 2))) return MIPGEMM_ERR_INVALID_ARG;
+    DeviceState* dev = nullptr;
+    const int st = get_device(&dev);
+    if (st != MIPGEMM_OK) return st;
+    const cudaError_t e = launch_product_simple(a, static_cast<cudaStream_t>(stream_v));
+    ++g_launches;
+    if (e != cudaSuccess) return cuda_fail(e);
+    tl_last_path = a.K == 0 ? MIPGEMM_PATH_TRIVIAL : MIPGEMM_PATH_DENSE;
+    return MIPGEMM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1594,6 +1673,56 @@ int mipgemm_gemm_ex(int a_unsigned, int b_unsigned, int a_order, int b_order, in
                     int accumulate, void* stream) {
     return gemm_ex_impl(a_unsigned, b_unsigned, a_order, b_order, c_col_major, M, N, K, A, lda, B, ldb, C, ldc,
                         accumulate, stream);
+}
+
+int mipgemm_quantize_rows(int type, int64_t M, int64_t N, const void* X, int64_t ldx, int8_t* Q, int64_t ldq,
+                          float* scale, void* stream) {
+    return rows_impl(true, type, M, N, const_cast<void*>(X), ldx, Q, ldq, scale, stream);
+}
+
+int mipgemm_dequantize_rows(int type, int64_t M, int64_t N, const int8_t* Q, int64_t ldq, const float* scale, void* X,
+                            int64_t ldx, void* stream) {
+    return rows_impl(false, type, M, N, X, ldx, const_cast<int8_t*>(Q), ldq, const_cast<float*>(scale), stream);
+}
+
+int mipgemm_s8s8_linear(int type, int act, int64_t M, int64_t N, int64_t K, const int8_t* A, int64_t lda,
+                        const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, const float* bias,
+                        const void* residual, int64_t ldr, void* C, int64_t ldc, void* stream) {
+    const LayerArgs a{kOpLinear, type, act, 0, M, N, K, A, lda, B, ldb, nullptr, 0, a_scale, b_scale, nullptr, bias,
+                      residual, residual ? ldr : N, C, ldc, nullptr, 0};
+    return layer_impl(a, stream);
+}
+
+int mipgemm_u8s8_linear(int type, int act, int64_t M, int64_t N, int64_t K, const uint8_t* A, int64_t lda,
+                        const float* a_scale, const int8_t* B, int64_t ldb, const float* b_scale, const float* bias,
+                        const void* residual, int64_t ldr, void* C, int64_t ldc, void* stream) {
+    const LayerArgs a{kOpLinear, type, act, 1, M, N, K, A, lda, B, ldb, nullptr, 0, a_scale, b_scale, nullptr, bias,
+                      residual, residual ? ldr : N, C, ldc, nullptr, 0};
+    return layer_impl(a, stream);
+}
+
+int mipgemm_s8s8_gated(int type, int act, int64_t M, int64_t F, int64_t K, const int8_t* X, int64_t ldx,
+                       const float* x_scale, const int8_t* Wg, int64_t ldg, const float* g_scale, const int8_t* Wu,
+                       int64_t ldu, const float* u_scale, void* H, int64_t ldh, void* stream) {
+    const LayerArgs a{kOpGated, type, act, 0, M, F, K, X, ldx, Wg, ldg, Wu, ldu, x_scale, g_scale, u_scale, nullptr,
+                      nullptr, 0, H, ldh, nullptr, 0};
+    return layer_impl(a, stream);
+}
+
+int mipgemm_s8s8_gated_grad(int type, int act, int64_t M, int64_t F, int64_t K, const int8_t* X, int64_t ldx,
+                            const float* x_scale, const int8_t* Wg, int64_t ldg, const float* g_scale,
+                            const int8_t* Wu, int64_t ldu, const float* u_scale, const void* dH, int64_t lddh, void* dG,
+                            int64_t lddg, void* dU, int64_t lddu, void* stream) {
+    const LayerArgs a{kOpGatedGrad, type, act, 0, M, F, K, X, ldx, Wg, ldg, Wu, ldu, x_scale, g_scale, u_scale, nullptr,
+                      dH, lddh, dG, lddg, dU, lddu};
+    return layer_impl(a, stream);
+}
+
+int mipgemm_bf16s8_product(int type, int a_order, int64_t M, int64_t N, int64_t K, const void* A, int64_t lda,
+                           const int8_t* B, int64_t ldb, const float* b_scale, void* C, int64_t ldc, int accumulate,
+                           void* stream) {
+    const ProductArgs a{type, a_order, accumulate ? 1 : 0, M, N, K, A, lda, B, ldb, b_scale, C, ldc};
+    return product_impl(a, stream);
 }
 
 uint64_t mipgemm_launch_count(void) { return g_launches.load(); }

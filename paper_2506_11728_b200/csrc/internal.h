@@ -159,6 +159,43 @@ bool skinny_ring16_supported(const SkinnyParams& p, int sm_count);
 cudaError_t skinny_ring16_init();  // once per device
 cudaError_t launch_skinny_ring16(const SkinnyRingParams& p, int sm_count, cudaStream_t stream);
 
+// ---- kernels of the 8-bit transformer layer
+
+// Which transform the exact sums of a layer kernel go through (see layer_math.cuh).
+constexpr int kOpLinear = 0, kOpGated = 1, kOpGatedGrad = 2;
+struct LayerArgs {
+    int op, type, act;               // kOp*, mipgemm_type_t of R / C / C2, mipgemm_activation_t
+    int a_unsigned;
+    long long M, N, K;               // N = output columns (a gated block's width F)
+    const void* A; long long lda;    // 8-bit codes, K contiguous
+    const int8_t* B0; long long ldb0;   // weights; the gate projection of a gated block
+    const int8_t* B1; long long ldb1;   // the other projection of a gated block
+    const float* a_scale;            // per row of A, or NULL (all ones)
+    const float* b0_scale;           // per row of B0 / B1, or NULL
+    const float* b1_scale;
+    const float* bias;               // kOpLinear: per column, or NULL
+    const void* R; long long ldr;    // kOpLinear: residual or NULL; kOpGatedGrad: gradient of the block's output
+    void* C; long long ldc;          // result; kOpGatedGrad: gradient of the gate projection
+    void* C2; long long ldc2;        // kOpGatedGrad: gradient of the other projection
+};
+cudaError_t launch_layer_simple(const LayerArgs& a, cudaStream_t stream);
+
+// C = A diag(b_scale) B [+ C]: A bf16 (K- or M-contiguous), B int8 [K][N]
+struct ProductArgs {
+    int type, a_order, accumulate;
+    long long M, N, K;
+    const void* A; long long lda;
+    const int8_t* B; long long ldb;
+    const float* b_scale;
+    void* C; long long ldc;
+};
+cudaError_t launch_product_simple(const ProductArgs& a, cudaStream_t stream);
+
+cudaError_t launch_quantize_rows(int type, long long M, long long N, const void* X, long long ldx, int8_t* Q,
+                                 long long ldq, float* scale, cudaStream_t stream);
+cudaError_t launch_dequantize_rows(int type, long long M, long long N, const int8_t* Q, long long ldq,
+                                   const float* scale, void* X, long long ldx, cudaStream_t stream);
+
 // Auxiliary kernels.
 cudaError_t launch_repack(const void* src, long long src_pitch, void* dst, long long dst_pitch,
                           long long rows, long long cols, cudaStream_t stream);
