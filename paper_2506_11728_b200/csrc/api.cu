@@ -1,6 +1,7 @@
 // C-ABI entry points of libmipgemm: argument validation, path selection, tensor-map
 // construction, scratch-memory handling and kernel launches.  No arithmetic of the
 // method happens on the host.
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -8,6 +9,7 @@
 #include <atomic>
 #include <map>
 #include <mutex>
+#include <new>
 
 #include "../../include/mipgemm.h"
 #include "internal.h"
@@ -184,6 +186,7 @@ int get_device(DeviceState** out) {
                 g_encode_im2col = reinterpret_cast<EncodeIm2colFn>(fn);
             }
             if ((e = dense_init()) != cudaSuccess) return cuda_fail(e);
+            if ((e = layer_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring16_init()) != cudaSuccess) return cuda_fail(e);
             d.pair_clusters = dense_pair_max_clusters(kSmemBudget);
@@ -1249,6 +1252,171 @@ int rows_impl(bool quantize, int type, int64_t M, int64_t N, void* X, int64_t ld
     return MIPGEMM_OK;
 }
 
+// A row-major matrix of the call's type as the layer kernel's epilogue reads and writes it: boxes of 128 bytes x 32
+// rows, 128-byte swizzle.
+int encode_slots(CUtensorMap* map, const void* base, int type, long long M, long long N, long long ld) {
+    const cuuint64_t size = type_size(type);
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(M)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * size};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), 32};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = g_encode_tiled(map, size == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2,
+                                      const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        tl_last_cuda_error = 100000 + static_cast<int>(r);
+        return MIPGEMM_ERR_CUDA;
+    }
+    return MIPGEMM_OK;
+}
+
+struct LayerPlan {
+    int pair, block_n, grid;
+};
+
+// Tile shape of the dense layer kernel: the main loop's cost per k-block is that of the plain product's kernel
+// (plan_cost_us); a tile's epilogue runs beside the next tile's main loop, the last one is exposed.
+LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
+    const bool gated = a.op != kOpLinear;
+    const bool wide = a.type == MIPGEMM_TYPE_F32;
+    const int k_blocks = static_cast<int>((a.K + 127) / 128);
+    // output columns come in whole 128-byte slots
+    const int step = gated ? (wide ? 64 : 128) : 64;
+    const Tuning tun = tuning_now();
+    LayerPlan best{0, step, 1};
+    double best_clk = 1e30;
+    for (int pair = 0; pair <= 1; ++pair) {
+        if (pair && dev->pair_clusters <= 0) continue;
+        if (tun.force_path == MIPGEMM_PATH_DENSE_PAIR && !pair && dev->pair_clusters > 0) continue;
+        if (tun.force_path == MIPGEMM_PATH_DENSE && pair) continue;
+        for (int bn = step; bn <= 256; bn += step) {
+            if (tun.block_n && bn != std::max(tun.block_n / step, 1) * step) continue;
+            const int out_n = gated ? bn / 2 : bn;
+            const long long rows = pair ? 2 * kBlockM : kBlockM;
+            const long long tiles = ((a.M + rows - 1) / rows) * ((a.N + out_n - 1) / out_n);
+            const long long slots = pair ? dev->pair_clusters : dev->sm_count;
+            const double main = k_blocks * (pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn);
+            const double epi = bn / 32 * (a.op == kOpLinear ? 450.0 : 600.0);
+            const double period = std::max(main, epi) + 0.2 * std::min(main, epi);
+            const long long waves = (tiles + slots - 1) / slots;
+            const double clk = (waves - 1) * period + main + epi + (pair ? 1900.0 : 0.0);
+            if (clk < best_clk) {
+                best_clk = clk;
+                best = LayerPlan{pair, bn, static_cast<int>(std::min(tiles, slots)) * (pair ? 2 : 1)};
+            }
+        }
+    }
+    return best;
+}
+
+// Plans and tensor maps of recent layer calls, as g_plan_cache keeps those of the plain products.
+struct LayerEntry {
+    bool used = false;
+    PlanKey key;
+    LayerParams p;
+    LayerPlan pl;
+};
+constexpr int kLayerCacheSlots = 256;
+LayerEntry* g_layer_cache = nullptr;
+
+int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool cacheable) {
+    LayerParams p;
+    LayerPlan pl;
+    cacheable = cacheable && plan_cache_enabled();
+    PlanKey key;
+    size_t slot = 0;
+    bool hit = false;
+    if (cacheable) {
+        std::memset(&key, 0, sizeof(key));
+        const uint64_t words[] = {
+            reinterpret_cast<uint64_t>(dev), g_tuning_epoch.load(std::memory_order_acquire),
+            static_cast<uint64_t>(a.op) | (static_cast<uint64_t>(a.type) << 8) | (static_cast<uint64_t>(a.a_unsigned) << 16),
+            static_cast<uint64_t>(a.M), static_cast<uint64_t>(a.N), static_cast<uint64_t>(a.K),
+            reinterpret_cast<uint64_t>(a.A), static_cast<uint64_t>(a.lda), reinterpret_cast<uint64_t>(a.B0),
+            static_cast<uint64_t>(a.ldb0), reinterpret_cast<uint64_t>(a.B1), static_cast<uint64_t>(a.ldb1),
+            reinterpret_cast<uint64_t>(a.R), static_cast<uint64_t>(a.ldr), reinterpret_cast<uint64_t>(a.C),
+            static_cast<uint64_t>(a.ldc), reinterpret_cast<uint64_t>(a.C2), static_cast<uint64_t>(a.ldc2)};
+        static_assert(sizeof(words) <= sizeof(key.w), "plan key too small");
+        std::memcpy(key.w, words, sizeof(words));
+        slot = plan_slot(key) % kLayerCacheSlots;
+        std::lock_guard<std::mutex> lock(g_plan_mutex);
+        if (g_layer_cache && g_layer_cache[slot].used && std::memcmp(&g_layer_cache[slot].key, &key, sizeof(key)) == 0) {
+            p = g_layer_cache[slot].p;
+            pl = g_layer_cache[slot].pl;
+            hit = true;
+        }
+    }
+    if (hit) {
+        ++g_plan_hits;
+    } else {
+        const bool gated = a.op != kOpLinear, grad = a.op == kOpGatedGrad;
+        pl = plan_layer(a, dev);
+        std::memset(&p, 0, sizeof(p));
+        p.M = static_cast<int>(a.M);
+        p.N = static_cast<int>(a.N);
+        p.type = a.type;
+        p.k_blocks = static_cast<int>((a.K + 127) / 128);
+        p.block_n = pl.block_n;
+        p.out_n = gated ? pl.block_n / 2 : pl.block_n;
+        const int rows = pl.pair ? 2 * kBlockM : kBlockM;
+        const int b_rows = pl.pair ? pl.block_n / 2 : pl.block_n;
+        p.tiles_m = static_cast<int>((a.M + rows - 1) / rows);
+        p.tiles_n = static_cast<int>((a.N + p.out_n - 1) / p.out_n);
+        p.stages = std::min(kMaxStages, (kSmemBudget - layer_fixed_smem(a.op)) / ((kBlockM + b_rows) * 128));
+        const Tuning tun = tuning_now();
+        if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
+        p.idesc = (2u << 4) | ((a.a_unsigned ? 0u : 1u) << 7) | (1u << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
+                  (static_cast<uint32_t>(rows >> 4) << 24);
+        p.tmem_cols = pow2_at_least(2u * pl.block_n);
+        p.status = dev->status_word;
+        const size_t size = type_size(a.type);
+        p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;
+        // (tile stores clip in 16-byte pieces: a row must end on one)
+        p.c_tma = a.N * size % 16 == 0 && aligned16(a.C, a.ldc * static_cast<long long>(size)) &&
+                  (!grad || aligned16(a.C2, a.ldc2 * static_cast<long long>(size))) ? 1 : 0;
+        int st = encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, kBlockM);
+        if (st == MIPGEMM_OK) st = encode_tiled_2d(&p.tmap_b0, a.B0, a.K, a.N, a.ldb0, 128, gated ? p.out_n : b_rows);
+        if (st == MIPGEMM_OK && gated) st = encode_tiled_2d(&p.tmap_b1, a.B1, a.K, a.N, a.ldb1, 128, p.out_n);
+        if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.R, a.type, a.M, a.N, a.ldr);
+        if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
+        if (st == MIPGEMM_OK && p.c_tma && grad) st = encode_slots(&p.tmap_c2, a.C2, a.type, a.M, a.N, a.ldc2);
+        if (st != MIPGEMM_OK) return st;
+        p.R = a.R; p.ldr = a.ldr;
+        p.C = a.C; p.ldc = a.ldc;
+        p.C2 = a.C2; p.ldc2 = a.ldc2;
+        p.wait_budget_ns = g_wait_budget_ns.load(std::memory_order_relaxed);
+        p.debug_flags = g_debug_flags.load(std::memory_order_relaxed);
+        if (cacheable) {
+            ++g_plan_misses;
+            std::lock_guard<std::mutex> lock(g_plan_mutex);
+            if (!g_layer_cache) g_layer_cache = new (std::nothrow) LayerEntry[kLayerCacheSlots];
+            if (g_layer_cache) {
+                LayerEntry& e = g_layer_cache[slot];
+                e.used = true;
+                e.key = key;
+                e.p = p;
+                e.pl = pl;
+            }
+        }
+    }
+    // (not part of the plan)
+    p.act = a.act;
+    p.a_scale = a.a_scale;
+    p.b0_scale = a.b0_scale;
+    p.b1_scale = a.b1_scale;
+    p.bias = a.bias;
+    const cudaError_t e = launch_layer(p, a.op, pl.pair, pl.grid, stream);
+    ++g_launches;
+    if (e != cudaSuccess) return cuda_fail(e);
+    tl_last_path = pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE;
+    if (log_enabled())
+        std::fprintf(stderr, "mipgemm: layer op=%d M=%d N=%d K=%lld -> dense %s tile=%dx%d stages=%d r_tma=%d c_tma=%d plan=%s\n", a.op,
+                     p.M, p.N, static_cast<long long>(a.K), pl.pair ? "cta-pair" : "one-cta", pl.pair ? 2 * kBlockM : kBlockM,
+                     pl.block_n, p.stages, p.r_tma, p.c_tma, hit ? "cached" : "new");
+    return MIPGEMM_OK;
+}
+
 int layer_impl(const LayerArgs& a, void* stream_v) {
     tl_last_path = MIPGEMM_PATH_NONE;
     const bool gated = a.op != kOpLinear;
@@ -1272,11 +1440,38 @@ int layer_impl(const LayerArgs& a, void* stream_v) {
     const int st = get_device(&dev);
     if (st != MIPGEMM_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    const cudaError_t e = launch_layer_simple(a, stream);
-    ++g_launches;
-    if (e != cudaSuccess) return cuda_fail(e);
-    tl_last_path = a.K == 0 ? MIPGEMM_PATH_TRIVIAL : MIPGEMM_PATH_DENSE;
-    return MIPGEMM_OK;
+    if (a.K == 0) {                      // every sum is 0
+        const cudaError_t e = launch_layer_simple(a, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
+        tl_last_path = MIPGEMM_PATH_TRIVIAL;
+        return MIPGEMM_OK;
+    }
+
+    // 8-bit operands that the TMA cannot address are re-pitched first
+    LayerArgs use = a;
+    const long long pitch = round_up(a.K, 16);
+    struct Operand { const void** ptr; long long* ld; long long rows; };
+    const Operand ops[3] = {{&use.A, &use.lda, a.M}, {reinterpret_cast<const void**>(&use.B0), &use.ldb0, a.N},
+                            {reinterpret_cast<const void**>(&use.B1), &use.ldb1, gated ? a.N : 0}};
+    Scratch scratch(dev, stream);
+    size_t need = 0;
+    for (const Operand& o : ops)
+        if (o.rows && !aligned16(*o.ptr, *o.ld)) need += align256(static_cast<size_t>(o.rows) * pitch);
+    int rc = scratch.reserve(need);
+    if (rc != MIPGEMM_OK) return rc;
+    for (const Operand& o : ops) {
+        if (!o.rows || aligned16(*o.ptr, *o.ld)) continue;
+        void* dst = scratch.take(static_cast<size_t>(o.rows) * pitch);
+        const cudaError_t e = launch_repack(*o.ptr, *o.ld, dst, pitch, o.rows, a.K, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
+        *o.ptr = dst;
+        *o.ld = pitch;
+    }
+    rc = run_layer(use, dev, stream, need == 0);
+    if (rc == MIPGEMM_OK && need) tl_last_path |= MIPGEMM_PATH_REPACK;
+    return rc;
 }
 
 int product_impl(const ProductArgs& a, void* stream_v) {

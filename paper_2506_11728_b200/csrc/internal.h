@@ -180,6 +180,35 @@ struct LayerArgs {
 };
 cudaError_t launch_layer_simple(const LayerArgs& a, cudaStream_t stream);
 
+// The dense layer kernel's parameters; passed by value as a __grid_constant__.
+struct alignas(64) LayerParams {
+    CUtensorMap tmap_a;              // tiled {K, M} byte tensor
+    CUtensorMap tmap_b0, tmap_b1;    // tiled {K, N} byte tensors (b1: gated forms)
+    CUtensorMap tmap_r;              // tiled {N, M} tensors of the call's type: boxes of 128 bytes x 32 rows
+    CUtensorMap tmap_c, tmap_c2;
+    int type, act;
+    int M, N;                        // N = output columns
+    int k_blocks;                    // 128 bytes of K each
+    int block_n;                     // accumulator columns per tile
+    int out_n;                       // output columns per tile: block_n, or half of it (gated forms)
+    int stages, tiles_m, tiles_n;
+    uint32_t idesc, tmem_cols;
+    int r_tma, c_tma;                // 1: R is read / C (and C2) written by TMA tile copies
+    const float* a_scale;
+    const float* b0_scale;
+    const float* b1_scale;
+    const float* bias;
+    const void* R; long long ldr;
+    void* C; long long ldc;
+    void* C2; long long ldc2;
+    unsigned int* status;
+    unsigned long long wait_budget_ns;
+    int debug_flags;                 // test hook (mipgemm_debug_set)
+};
+int layer_fixed_smem(int op);        // shared memory besides the pipeline stages
+cudaError_t layer_init();            // once per device
+cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaStream_t stream);
+
 // C = A diag(b_scale) B [+ C]: A bf16 (K- or M-contiguous), B int8 [K][N]
 struct ProductArgs {
     int type, a_order, accumulate;
