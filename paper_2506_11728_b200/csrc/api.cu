@@ -187,6 +187,7 @@ int get_device(DeviceState** out) {
             }
             if ((e = dense_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = layer_init()) != cudaSuccess) return cuda_fail(e);
+            if ((e = product_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring16_init()) != cudaSuccess) return cuda_fail(e);
             d.pair_clusters = dense_pair_max_clusters(kSmemBudget);
@@ -1320,12 +1321,32 @@ struct LayerEntry {
 constexpr int kLayerCacheSlots = 256;
 LayerEntry* g_layer_cache = nullptr;
 
+bool layer_lookup(const PlanKey& key, LayerParams* p, LayerPlan* pl) {
+    const size_t slot = plan_slot(key) % kLayerCacheSlots;
+    std::lock_guard<std::mutex> lock(g_plan_mutex);
+    if (!g_layer_cache || !g_layer_cache[slot].used || std::memcmp(&g_layer_cache[slot].key, &key, sizeof(key)) != 0) return false;
+    *p = g_layer_cache[slot].p;
+    *pl = g_layer_cache[slot].pl;
+    ++g_plan_hits;
+    return true;
+}
+void layer_store(const PlanKey& key, const LayerParams& p, const LayerPlan& pl) {
+    ++g_plan_misses;
+    std::lock_guard<std::mutex> lock(g_plan_mutex);
+    if (!g_layer_cache) g_layer_cache = new (std::nothrow) LayerEntry[kLayerCacheSlots];
+    if (!g_layer_cache) return;          // (no memory: calls plan every time)
+    LayerEntry& e = g_layer_cache[plan_slot(key) % kLayerCacheSlots];
+    e.used = true;
+    e.key = key;
+    e.p = p;
+    e.pl = pl;
+}
+
 int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool cacheable) {
     LayerParams p;
     LayerPlan pl;
     cacheable = cacheable && plan_cache_enabled();
     PlanKey key;
-    size_t slot = 0;
     bool hit = false;
     if (cacheable) {
         std::memset(&key, 0, sizeof(key));
@@ -1339,22 +1360,15 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
             static_cast<uint64_t>(a.ldc), reinterpret_cast<uint64_t>(a.C2), static_cast<uint64_t>(a.ldc2)};
         static_assert(sizeof(words) <= sizeof(key.w), "plan key too small");
         std::memcpy(key.w, words, sizeof(words));
-        slot = plan_slot(key) % kLayerCacheSlots;
-        std::lock_guard<std::mutex> lock(g_plan_mutex);
-        if (g_layer_cache && g_layer_cache[slot].used && std::memcmp(&g_layer_cache[slot].key, &key, sizeof(key)) == 0) {
-            p = g_layer_cache[slot].p;
-            pl = g_layer_cache[slot].pl;
-            hit = true;
-        }
+        hit = layer_lookup(key, &p, &pl);
     }
-    if (hit) {
-        ++g_plan_hits;
-    } else {
+    if (!hit) {
         const bool gated = a.op != kOpLinear, grad = a.op == kOpGatedGrad;
         pl = plan_layer(a, dev);
         std::memset(&p, 0, sizeof(p));
         p.M = static_cast<int>(a.M);
         p.N = static_cast<int>(a.N);
+        p.K = static_cast<int>(a.K);
         p.type = a.type;
         p.k_blocks = static_cast<int>((a.K + 127) / 128);
         p.block_n = pl.block_n;
@@ -1387,18 +1401,7 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
         p.C2 = a.C2; p.ldc2 = a.ldc2;
         p.wait_budget_ns = g_wait_budget_ns.load(std::memory_order_relaxed);
         p.debug_flags = g_debug_flags.load(std::memory_order_relaxed);
-        if (cacheable) {
-            ++g_plan_misses;
-            std::lock_guard<std::mutex> lock(g_plan_mutex);
-            if (!g_layer_cache) g_layer_cache = new (std::nothrow) LayerEntry[kLayerCacheSlots];
-            if (g_layer_cache) {
-                LayerEntry& e = g_layer_cache[slot];
-                e.used = true;
-                e.key = key;
-                e.p = p;
-                e.pl = pl;
-            }
-        }
+        if (cacheable) layer_store(key, p, pl);
     }
     // (not part of the plan)
     p.act = a.act;
@@ -1474,6 +1477,114 @@ int layer_impl(const LayerArgs& a, void* stream_v) {
     return rc;
 }
 
+int encode_bf16_2d(CUtensorMap* map, const void* base, long long inner, long long outer, long long pitch, int box_outer) {
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
+    cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_outer)};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = g_encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+                                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        tl_last_cuda_error = 100000 + static_cast<int>(r);
+        return MIPGEMM_ERR_CUDA;
+    }
+    return MIPGEMM_OK;
+}
+
+// B as bytes {N, K}: boxes of 128 columns x one stage's rows, not swizzled (warps read them, not the tensor core).
+int encode_codes_rows(CUtensorMap* map, const void* base, long long N, long long K, long long pitch) {
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(K)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch)};
+    cuuint32_t box[2] = {kProductN, kProductK};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = g_encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        tl_last_cuda_error = 100000 + static_cast<int>(r);
+        return MIPGEMM_ERR_CUDA;
+    }
+    return MIPGEMM_OK;
+}
+
+int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, bool cacheable) {
+    LayerParams p;
+    LayerPlan pl;
+    cacheable = cacheable && plan_cache_enabled();
+    PlanKey key;
+    bool hit = false;
+    if (cacheable) {
+        std::memset(&key, 0, sizeof(key));
+        const uint64_t words[] = {
+            reinterpret_cast<uint64_t>(dev), g_tuning_epoch.load(std::memory_order_acquire),
+            static_cast<uint64_t>(kOpProduct) | (static_cast<uint64_t>(a.type) << 8) | (static_cast<uint64_t>(a.a_order) << 16) |
+                (static_cast<uint64_t>(a.accumulate) << 17),
+            static_cast<uint64_t>(a.M), static_cast<uint64_t>(a.N), static_cast<uint64_t>(a.K),
+            reinterpret_cast<uint64_t>(a.A), static_cast<uint64_t>(a.lda), reinterpret_cast<uint64_t>(a.B),
+            static_cast<uint64_t>(a.ldb), reinterpret_cast<uint64_t>(a.C), static_cast<uint64_t>(a.ldc)};
+        std::memcpy(key.w, words, sizeof(words));
+        hit = layer_lookup(key, &p, &pl);
+    }
+    if (!hit) {
+        const Tuning tun = tuning_now();
+        std::memset(&p, 0, sizeof(p));
+        const auto tiles_of = [&](int pair) {
+            const long long rows = pair ? 2 * kBlockM : kBlockM, cols = pair ? 2 * kProductN : kProductN;
+            return ((a.M + rows - 1) / rows) * ((a.N + cols - 1) / cols);
+        };
+        // a pair's tile is four single tiles for the price of two and a half (its warps convert half as much per product)
+        const long long slots1 = dev->sm_count, slots2 = std::max(dev->pair_clusters, 1);
+        const double waves1 = static_cast<double>((tiles_of(0) + slots1 - 1) / slots1);
+        const double waves2 = static_cast<double>((tiles_of(1) + slots2 - 1) / slots2);
+        pl.pair = dev->pair_clusters > 0 && waves2 * 1.6 <= waves1 ? 1 : 0;
+        if (tun.force_path == MIPGEMM_PATH_DENSE_PAIR && dev->pair_clusters > 0) pl.pair = 1;
+        if (tun.force_path == MIPGEMM_PATH_DENSE) pl.pair = 0;
+        const int group = pl.pair ? 2 : 1;
+        pl.block_n = kProductN * group;
+        pl.grid = static_cast<int>(std::min(tiles_of(pl.pair), pl.pair ? slots2 : slots1)) * group;
+        p.M = static_cast<int>(a.M);
+        p.N = static_cast<int>(a.N);
+        p.K = static_cast<int>(a.K);
+        p.type = a.type;
+        p.k_blocks = static_cast<int>((a.K + kProductK - 1) / kProductK);
+        p.block_n = p.out_n = pl.block_n;
+        p.tiles_m = static_cast<int>((a.M + kBlockM * group - 1) / (kBlockM * group));
+        p.tiles_n = static_cast<int>((a.N + pl.block_n - 1) / pl.block_n);
+        p.stages = product_stages();
+        if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
+        // D f32, A and B bf16, B N-major, A K- or M-major
+        p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(a.a_order) << 15) | (1u << 16) |
+                  (static_cast<uint32_t>(pl.block_n >> 3) << 17) | (static_cast<uint32_t>((kBlockM * group) >> 4) << 24);
+        p.tmem_cols = pow2_at_least(2u * pl.block_n);
+        p.status = dev->status_word;
+        const size_t size = type_size(a.type);
+        const bool c_aligned = aligned16(a.C, a.ldc * static_cast<long long>(size));
+        p.r_tma = a.accumulate && c_aligned ? 1 : 0;
+        p.c_tma = a.N * size % 16 == 0 && c_aligned ? 1 : 0;
+        int st = a.a_order ? encode_bf16_2d(&p.tmap_a, a.A, a.M, a.K, a.lda, kProductK)
+                           : encode_bf16_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, kBlockM);
+        if (st == MIPGEMM_OK) st = encode_codes_rows(&p.tmap_b0, a.B, a.N, a.K, a.ldb);
+        if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.C, a.type, a.M, a.N, a.ldc);
+        if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
+        if (st != MIPGEMM_OK) return st;
+        p.R = a.accumulate ? a.C : nullptr; p.ldr = a.ldc;
+        p.C = a.C; p.ldc = a.ldc;
+        p.wait_budget_ns = g_wait_budget_ns.load(std::memory_order_relaxed);
+        p.debug_flags = g_debug_flags.load(std::memory_order_relaxed);
+        if (cacheable) layer_store(key, p, pl);
+    }
+    p.b0_scale = a.b_scale;              // (not part of the plan)
+    const cudaError_t e = launch_product(p, a.a_order, pl.pair, pl.grid, stream);
+    ++g_launches;
+    if (e != cudaSuccess) return cuda_fail(e);
+    tl_last_path = pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE;
+    if (log_enabled())
+        std::fprintf(stderr, "mipgemm: product M=%d N=%d K=%d a_order=%d -> dense %s stages=%d r_tma=%d c_tma=%d plan=%s\n", p.M, p.N, p.K,
+                     a.a_order, pl.pair ? "cta-pair" : "one-cta", p.stages, p.r_tma, p.c_tma, hit ? "cached" : "new");
+    return MIPGEMM_OK;
+}
+
 int product_impl(const ProductArgs& a, void* stream_v) {
     tl_last_path = MIPGEMM_PATH_NONE;
     if ((a.type != MIPGEMM_TYPE_F32 && a.type != MIPGEMM_TYPE_BF16) || (a.a_order & ~1)) return MIPGEMM_ERR_INVALID_ARG;
@@ -1489,11 +1600,42 @@ int product_impl(const ProductArgs& a, void* stream_v) {
     DeviceState* dev = nullptr;
     const int st = get_device(&dev);
     if (st != MIPGEMM_OK) return st;
-    const cudaError_t e = launch_product_simple(a, static_cast<cudaStream_t>(stream_v));
-    ++g_launches;
-    if (e != cudaSuccess) return cuda_fail(e);
-    tl_last_path = a.K == 0 ? MIPGEMM_PATH_TRIVIAL : MIPGEMM_PATH_DENSE;
-    return MIPGEMM_OK;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if (a.K == 0) {                      // every sum is 0
+        const cudaError_t e = launch_product_simple(a, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
+        tl_last_path = MIPGEMM_PATH_TRIVIAL;
+        return MIPGEMM_OK;
+    }
+    ProductArgs use = a;
+    const long long a_rows = a.a_order ? a.K : a.M, a_cols = 2 * (a.a_order ? a.M : a.K);     // bytes of a row of A
+    const bool fix_a = !aligned16(a.A, 2 * a.lda), fix_b = !aligned16(a.B, a.ldb);
+    Scratch scratch(dev, stream);
+    int rc = scratch.reserve((fix_a ? align256(static_cast<size_t>(a_rows) * round_up(a_cols, 16)) : 0) +
+                             (fix_b ? align256(static_cast<size_t>(a.K) * round_up(a.N, 16)) : 0));
+    if (rc != MIPGEMM_OK) return rc;
+    if (fix_a) {
+        const long long pitch = round_up(a_cols, 16);
+        void* dst = scratch.take(static_cast<size_t>(a_rows) * pitch);
+        const cudaError_t e = launch_repack(a.A, 2 * a.lda, dst, pitch, a_rows, a_cols, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
+        use.A = dst;
+        use.lda = pitch / 2;
+    }
+    if (fix_b) {
+        const long long pitch = round_up(a.N, 16);
+        void* dst = scratch.take(static_cast<size_t>(a.K) * pitch);
+        const cudaError_t e = launch_repack(a.B, a.ldb, dst, pitch, a.K, a.N, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
+        use.B = static_cast<const int8_t*>(dst);
+        use.ldb = pitch;
+    }
+    rc = run_product(use, dev, stream, !fix_a && !fix_b);
+    if (rc == MIPGEMM_OK && (fix_a || fix_b)) tl_last_path |= MIPGEMM_PATH_REPACK;
+    return rc;
 }
 
 }  // namespace

@@ -162,7 +162,7 @@ cudaError_t launch_skinny_ring16(const SkinnyRingParams& p, int sm_count, cudaSt
 // ---- kernels of the 8-bit transformer layer
 
 // Which transform the exact sums of a layer kernel go through (see layer_math.cuh).
-constexpr int kOpLinear = 0, kOpGated = 1, kOpGatedGrad = 2;
+constexpr int kOpLinear = 0, kOpGated = 1, kOpGatedGrad = 2, kOpProduct = 3;
 struct LayerArgs {
     int op, type, act;               // kOp*, mipgemm_type_t of R / C / C2, mipgemm_activation_t
     int a_unsigned;
@@ -187,8 +187,8 @@ struct alignas(64) LayerParams {
     CUtensorMap tmap_r;              // tiled {N, M} tensors of the call's type: boxes of 128 bytes x 32 rows
     CUtensorMap tmap_c, tmap_c2;
     int type, act;
-    int M, N;                        // N = output columns
-    int k_blocks;                    // 128 bytes of K each
+    int M, N, K;                     // N = output columns
+    int k_blocks;                    // 128 bytes of A's rows each
     int block_n;                     // accumulator columns per tile
     int out_n;                       // output columns per tile: block_n, or half of it (gated forms)
     int stages, tiles_m, tiles_n;
@@ -219,6 +219,13 @@ struct ProductArgs {
     void* C; long long ldc;
 };
 cudaError_t launch_product_simple(const ProductArgs& a, cudaStream_t stream);
+// Its kernel takes LayerParams: tmap_a = A (bf16: {K, M}, or {M, K} with a_order), tmap_b0 = B ({N, K} bytes), b0_scale =
+// the scales, R = C when it accumulates, k_blocks of kProductK each.
+constexpr int kProductK = 64;        // k per pipeline stage: 128 bytes of a bf16 row
+constexpr int kProductN = 128;       // columns of B staged per CTA
+int product_stages();
+cudaError_t product_init();          // once per device
+cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int grid, cudaStream_t stream);
 
 cudaError_t launch_quantize_rows(int type, long long M, long long N, const void* X, long long ldx, int8_t* Q,
                                  long long ldq, float* scale, cudaStream_t stream);

@@ -1,0 +1,357 @@
+// Epilogue shared by the tensor-core kernels of the 8-bit layer: accumulators in tensor memory -> outputs.
+//
+// Four warps, thread = row.  A slot is 128 bytes of 32 output rows (64 columns of a 16-bit type, 32 of float32): the
+// warp's own swizzled staging buffer.  A matrix that is read (residual, gradient of the output, the sum to add to)
+// arrives in the slot by a TMA tile load asked for before the accumulator is ready, is combined in registers, and
+// the result goes back to the same 16 bytes, from where a TMA tile store takes it: every global access is whole
+// 128-byte lines, no warp waits for another, and reading a matrix in place is safe (each element is read before
+// the same warp writes it).  Matrices the TMA cannot address (16-byte alignment of base and pitch; for stores also
+// whole 16-byte pieces per row, because tile stores clip in those) go through the same slot with one row of
+// element accesses per instruction.  Scales and bias of a slot's columns are fetched one lane per column one slot
+// ahead and broadcast through shared memory.
+#pragma once
+#include "internal.h"
+#include "layer_math.cuh"
+#include "ptx.cuh"
+
+namespace mip {
+
+namespace {
+
+constexpr int kEpiWarps = 4;
+constexpr int kSlot = 4096;                         // 32 rows x 128 bytes
+constexpr int kColBytes = 2 * 64 * 4;               // per warp: two vectors of a slot's columns
+// Slots per warp.  Linear: the four slots of a 256-column tile of a 16-bit type, so that all of its residual can be
+// on its way before the accumulator is ready; gated: nothing comes in, two suffice to store one while the next is
+// computed; gradient: two, each of two buffers (one per result; the incoming gradient lies in the first); product: one
+// (its pipeline stages need the room, and its main loops are long).
+constexpr int slot_count(int op) { return op == kOpLinear ? 4 : (op == kOpProduct ? 1 : 2); }
+constexpr int slot_stride(int op) { return op == kOpGatedGrad ? 2 * kSlot : kSlot; }
+constexpr int slot_bytes_per_warp(int op) { return slot_count(op) * slot_stride(op); }
+
+struct LayerTile {
+    int m0, n0;
+};
+
+__device__ __forceinline__ LayerTile decode_tile(const LayerParams& p, int t, int rows_per_tile) {
+    // groups of 8 tile columns swept top to bottom, column fastest: a group's weights stay in the L2
+    const int per_group = 8 * p.tiles_m;
+    const int g = t / per_group;
+    const int first = g * 8;
+    const int gsize = min(8, p.tiles_n - first);
+    const int r = t - g * per_group;
+    const int tm = r / gsize;
+    LayerTile c;
+    c.m0 = tm * rows_per_tile;
+    c.n0 = (first + (r - tm * gsize)) * p.out_n;
+    return c;
+}
+
+__device__ __forceinline__ uint32_t slot_piece(uint32_t slot, int row, int piece) {
+    return slot + static_cast<uint32_t>(row) * 128u + (static_cast<uint32_t>(piece ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void lds_v4(uint32_t addr, uint32_t (&v)[4]) {
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void lds_f4(uint32_t addr, float (&v)[4]) {
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void sts_f32(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, bool f16) {
+    uint32_t r;
+    if (f16) asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void unpack2(uint32_t w, bool f16, float& lo, float& hi) {
+    if (f16) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        lo = f.x;
+        hi = f.y;
+    } else {
+        lo = __uint_as_float(w << 16);
+        hi = __uint_as_float(w & 0xFFFF0000u);
+    }
+}
+
+// One row of a slot at a time between shared and global memory, element by element (any alignment).
+template <bool kWide>
+__device__ __forceinline__ void slot_rows_in(uint32_t slot, const void* src, long long ld, int row0, int col0, int M, int N, int lane) {
+    const int rows = min(32, M - row0);
+    constexpr int kCols = kWide ? 32 : 64;
+    for (int r = 0; r < rows; ++r) {
+#pragma unroll
+        for (int e = 0; e < kCols; e += 32) {
+            const int c = e + lane;
+            if (col0 + c < N) {
+                const long long i = static_cast<long long>(row0 + r) * ld + col0 + c;
+                if (kWide) {
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(slot_piece(slot, r, c >> 2) + (c & 3) * 4),
+                                 "r"(static_cast<const uint32_t*>(src)[i]) : "memory");
+                } else {
+                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(slot_piece(slot, r, c >> 3) + (c & 7) * 2),
+                                 "h"(static_cast<const uint16_t*>(src)[i]) : "memory");
+                }
+            }
+        }
+    }
+    __syncwarp();
+}
+template <bool kWide>
+__device__ __forceinline__ void slot_rows_out(uint32_t slot, void* dst, long long ld, int row0, int col0, int M, int N, int lane) {
+    __syncwarp();
+    const int rows = min(32, M - row0);
+    constexpr int kCols = kWide ? 32 : 64;
+    for (int r = 0; r < rows; ++r) {
+#pragma unroll
+        for (int e = 0; e < kCols; e += 32) {
+            const int c = e + lane;
+            if (col0 + c < N) {
+                const long long i = static_cast<long long>(row0 + r) * ld + col0 + c;
+                if (kWide) {
+                    uint32_t v;
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(slot_piece(slot, r, c >> 2) + (c & 3) * 4) : "memory");
+                    static_cast<uint32_t*>(dst)[i] = v;
+                } else {
+                    uint16_t v;
+                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(slot_piece(slot, r, c >> 3) + (c & 7) * 2) : "memory");
+                    static_cast<uint16_t*>(dst)[i] = v;
+                }
+            }
+        }
+    }
+    __syncwarp();
+}
+
+// 32 accumulator columns of one row: v0 (and, gated, v1) become outputs in the slot.  `piece0` is the first 16-byte
+// piece of the slot they fill, `cols` the shared-memory address of their first column's scale (second vector 256
+// bytes behind).  The slot's old contents are the residual / the gradient of the output.
+template <int kOp, int kAct, bool kWide>
+__device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uint32_t (&v1)[32], float as, uint32_t cols, uint32_t slot,
+                                             uint32_t slot2, int row, int piece0, bool has_r, bool f16) {
+    constexpr int kPer = kWide ? 4 : 8;             // columns per 16-byte piece
+#pragma unroll
+    for (int g = 0; g < 32 / kPer; ++g) {
+        float b0[kPer], b1[kPer], r[kPer], y[kPer], y2[kPer];
+#pragma unroll
+        for (int h = 0; h < kPer && kOp != kOpProduct; h += 4) {
+            lds_f4(cols + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b0[h]));
+            lds_f4(cols + 256 + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b1[h]));
+        }
+        const uint32_t at = slot_piece(slot, row, piece0 + g);
+        if (has_r) {
+            uint32_t w[4];
+            lds_v4(at, w);
+            if (kWide) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = __uint_as_float(w[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) unpack2(w[j], f16, r[2 * j % kPer], r[(2 * j + 1) % kPer]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) r[j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (kOp == kOpProduct) {
+                y[j] = __uint_as_float(v0[g * kPer + j]) + r[j];
+                continue;
+            }
+            const float z0 = __int2float_rn(static_cast<int>(v0[g * kPer + j])) * as * b0[j];
+            if (kOp == kOpLinear) {
+                y[j] = activation<kAct>(z0 + b1[j]) + r[j];
+            } else {
+                const float z1 = __int2float_rn(static_cast<int>(v1[g * kPer + j])) * as * b1[j];
+                if (kOp == kOpGated) {
+                    y[j] = activation<kAct>(z0) * z1;
+                } else {
+                    float value, slope;
+                    activation_slope<kAct>(z0, value, slope);
+                    y[j] = r[j] * z1 * slope;
+                    y2[j] = r[j] * value;
+                }
+            }
+        }
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y[j]) : pack2(y[2 * j % kPer], y[(2 * j + 1) % kPer], f16);
+        st_shared_v4(at, o);
+        if (kOp == kOpGatedGrad) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y2[j]) : pack2(y2[2 * j % kPer], y2[(2 * j + 1) % kPer], f16);
+            st_shared_v4(slot_piece(slot2, row, piece0 + g), o);
+        }
+    }
+}
+
+// The epilogue role of one warp (e = 0 .. kEpiWarps-1; q = the quarter of the TMEM lanes it may read).  Walks the same
+// tiles as the other roles; `slots`, `colvec` and `bar_in` are the shared-memory addresses of the slots, column
+// vectors and arrival barriers of all warps.
+template <bool kPair, int kOp, bool kWide>
+__device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t slots, uint32_t colvec, uint32_t bar_in, uint32_t bar_tfull,
+                                               uint32_t bar_tempty, volatile uint32_t* abort_flag, uint32_t tmem_base, int e, int q, int lane,
+                                               uint32_t cta_rank, int first_unit, int unit_stride) {
+    constexpr bool kGatedForm = kOp == kOpGated || kOp == kOpGatedGrad;
+    constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
+    constexpr int kSlotCols = kWide ? 32 : 64;
+    constexpr int kBuffers = slot_count(kOp);
+    constexpr int kSlotStride = slot_stride(kOp);
+    constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp);
+    const bool leader = cta_rank == 0;
+    const int total_units = p.tiles_m * p.tiles_n;
+    const uint64_t budget = p.wait_budget_ns;
+    const uint32_t my_slots = slots + static_cast<uint32_t>(e) * kSlotBytesPerWarp;
+    const uint32_t my_cols = colvec + static_cast<uint32_t>(e) * kColBytes;
+    const uint32_t my_bar = bar_in + 8u * static_cast<uint32_t>(e * kBuffers);
+    const bool f16 = p.type == kF16;
+    const bool has_r = p.R != nullptr;
+    const bool r_tma = p.r_tma != 0, c_tma = p.c_tma != 0;
+    uint32_t loads = 0, slot_no = 0;                           // tile loads asked for, slots finished
+    int t = 0;
+    for (int unit = first_unit; unit < total_units; unit += unit_stride, ++t) {
+        const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+        const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
+        const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
+        const int n_here = min(p.out_n, p.N - tc.n0);
+        const bool active = row0 < p.M;                        // (warp-uniform)
+        const int n_slots = active ? (n_here + kSlotCols - 1) / kSlotCols : 0;
+        const int row = row0 + lane;
+        float as = 1.0f;
+        // the slots' first buffers: every store that still reads them has been issued by this warp
+        int asked = 0;                                         // of this tile
+        if (active) {
+            if (p.a_scale && row < p.M) as = __ldg(p.a_scale + row);
+            if (r_tma) {
+                if (elect_one()) tma_store_wait_read<0>();
+                __syncwarp();
+                fence_proxy_async_smem();
+                __syncwarp();
+                for (; asked < kBuffers && asked < n_slots; ++asked, ++loads) {
+                    const uint32_t b = loads % kBuffers;
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(my_bar + 8u * b, kSlot);
+                        tma_load_2d(my_slots + b * kSlotStride, &p.tmap_r, my_bar + 8u * b, tc.n0 + asked * kSlotCols, row0);
+                    }
+                }
+            }
+        }
+        // one lane per column: scales and bias of the first slot
+        float cv[4];
+        auto fetch_columns = [&](int c0) {
+            if (kOp == kOpProduct) return;
+#pragma unroll
+            for (int h = 0; h < kSlotCols / 32; ++h) {
+                const int col = tc.n0 + c0 + h * 32 + lane;
+                const bool in = col < p.N;
+                cv[2 * h] = (in && p.b0_scale) ? __ldg(p.b0_scale + col) : 1.0f;
+                if (kGatedForm) cv[2 * h + 1] = (in && p.b1_scale) ? __ldg(p.b1_scale + col) : 1.0f;
+                else cv[2 * h + 1] = (in && p.bias) ? __ldg(p.bias + col) : 0.0f;
+            }
+        };
+        if (n_slots > 0) fetch_columns(0);
+        // (the lanes of a warp decide together: none may leave while others still expect it at a warp barrier)
+        if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, budget))) break;
+        tc_fence_after();
+        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
+        const uint32_t t_up = t_row + static_cast<uint32_t>(p.block_n >> 1);
+        uint32_t va0[32], va1[32], vb0[32], vb1[32];
+        auto load_acc = [&](uint32_t (&v0)[32], uint32_t (&v1)[32], int c0) {
+            tmem_ld_32x32(t_row + c0, v0);
+            if (kGatedForm) tmem_ld_32x32(t_up + c0, v1);
+        };
+        bool gave_up = false;
+        if (n_slots > 0) load_acc(va0, va1, 0);
+        for (int sl = 0; sl < n_slots; ++sl, ++slot_no) {
+            const int c0 = sl * kSlotCols;
+            const uint32_t b = slot_no % kBuffers;
+            const uint32_t slot = my_slots + b * kSlotStride, slot2 = slot + kSlot;
+            // the slot is free (its last store has been read) or holds the tile that was asked for
+            if (!r_tma) {
+                if (c_tma && elect_one()) tma_store_wait_read<kBuffers - 1>();
+                __syncwarp();
+                if (has_r) slot_rows_in<kWide>(slot, p.R, p.ldr, row0, tc.n0 + c0, p.M, p.N, lane);
+            }
+            if (kOp != kOpProduct) {
+                __syncwarp();                                  // (the last slot's column vectors have been read)
+#pragma unroll
+                for (int h = 0; h < kSlotCols / 32; ++h) {
+                    sts_f32(my_cols + (h * 32 + lane) * 4, cv[2 * h]);
+                    sts_f32(my_cols + 256 + (h * 32 + lane) * 4, cv[2 * h + 1]);
+                }
+                __syncwarp();
+            }
+            if (sl + 1 < n_slots) fetch_columns(c0 + kSlotCols);
+            if (r_tma && !__all_sync(~0u, mbar_wait(my_bar + 8u * b, (slot_no / kBuffers) & 1u, abort_flag, budget))) {
+                gave_up = true;
+                break;
+            }
+            tmem_ld_wait_for(va0);
+            if (kGatedForm) tmem_ld_wait_for(va1);
+            const bool last = sl + 1 == n_slots;
+            if (!kWide) load_acc(vb0, vb1, c0 + 32);
+            with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
+                finish_chunk<kOp, decltype(act)::value, kWide>(va0, va1, as, my_cols, slot, slot2, lane, 0, has_r, f16);
+            });
+            if (kWide) {
+                if (!last) load_acc(va0, va1, c0 + 32);
+            } else {
+                tmem_ld_wait_for(vb0);
+                if (kGatedForm) tmem_ld_wait_for(vb1);
+                if (!last) load_acc(va0, va1, c0 + 64);
+                with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
+                    finish_chunk<kOp, decltype(act)::value, kWide>(vb0, vb1, as, my_cols + 128, slot, slot2, lane, 4, has_r, f16);
+                });
+            }
+            if (c_tma) {
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (elect_one()) {
+                    tma_store_2d(&p.tmap_c, slot, tc.n0 + c0, row0);
+                    if (kOp == kOpGatedGrad) tma_store_2d(&p.tmap_c2, slot2, tc.n0 + c0, row0);
+                    tma_store_commit();
+                }
+            } else {
+                slot_rows_out<kWide>(slot, p.C, p.ldc, row0, tc.n0 + c0, p.M, p.N, lane);
+                if (kOp == kOpGatedGrad) slot_rows_out<kWide>(slot2, p.C2, p.ldc2, row0, tc.n0 + c0, p.M, p.N, lane);
+            }
+            // ask for the tile of a later slot once the buffer it goes to has been read by its store: the one
+            // before last (the last store may still be reading its own), unless there is only one buffer
+            if (r_tma && (kBuffers == 1 || sl > 0) && asked < n_slots) {
+                if (elect_one()) tma_store_wait_read<kBuffers == 1 ? 0 : 1>();
+                __syncwarp();
+                fence_proxy_async_smem();
+                __syncwarp();
+                const uint32_t nb = loads % kBuffers;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(my_bar + 8u * nb, kSlot);
+                    tma_load_2d(my_slots + nb * kSlotStride, &p.tmap_r, my_bar + 8u * nb, tc.n0 + asked * kSlotCols, row0);
+                }
+                ++asked;
+                ++loads;
+            }
+        }
+        if (gave_up) break;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (kPair && !leader) mbar_arrive_remote(bar_tempty + 8u * acc, 0);
+            else mbar_arrive(bar_tempty + 8u * acc);
+        }
+    }
+    // unwinding: tiles still on their way into the slots
+    for (uint32_t i = slot_no; r_tma && i < loads; ++i) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(my_bar + 8u * (i % kBuffers), (i / kBuffers) & 1u)) {
+            if (globaltimer_ns() - t0 > budget) break;
+        }
+    }
+    if (c_tma && elect_one()) tma_store_wait<0>();
+    __syncwarp();
+}
+
+}  // namespace
+
+}  // namespace mip

@@ -1,0 +1,354 @@
+// C = A diag(s) B with A bfloat16 and B 8-bit codes [K][N]: the products of a backward pass through 8-bit weights
+// (dX, scales of the weights' rows) and 8-bit activations (dW, scales of the tokens).
+//
+// The scales lie along the summed axis, so they cannot be applied behind the sum: each code times its row's scale is
+// rounded to bfloat16 on its way to the tensor core (codes alone are exact in bfloat16), and tcgen05.mma.kind::f16
+// multiplies it with A into binary32.  The codes cross HBM and L2 as bytes; nothing is written back in 16 bits.
+//
+// Roles.  Warp 0 loads A (TMA, 128-byte swizzle, K-major or M-major as it lies), warp 1 issues the MMAs, warps 2-5
+// are the epilogue (layer_epilogue.cuh), warp 6 loads B's codes (TMA, 64 rows x 128 bytes, plain rows), warps 7-14
+// convert: a lane takes 16 codes of a row (one 16-byte read, eight lanes a row), scales them and writes the two
+// 16-byte pieces of the N-major 128-byte-swizzled tile the tensor core reads.  Lanes of the row's second half write
+// their pieces in the other order, so that eight lanes cover all banks.  A stage is 64 k: 16 KB of A, 8 KB of codes,
+// 16 KB of converted B per CTA.  In the pair form (256 x 256 tile, cta_group::2) each CTA converts its half of B, so
+// the conversion -- 16 codes per clock and SM at the tensor core's pace, against 32 for a CTA of its own -- hides.
+//
+// Every wait is bounded, with the unwinding of the other dense kernels.
+#include "layer_epilogue.cuh"
+
+namespace mip {
+
+namespace {
+
+constexpr int kConvWarps = 8;
+constexpr int kFirstConvWarp = 3 + kEpiWarps;
+constexpr int kProductThreads = 32 * (kFirstConvWarp + kConvWarps);
+constexpr uint32_t kABytes = kBlockM * kProductK * 2;          // 16 KB
+constexpr uint32_t kBBytes = kProductN * kProductK * 2;        // 16 KB, two blocks of 64 columns
+constexpr uint32_t kRawBytes = kProductN * kProductK;          // 8 KB
+constexpr uint32_t kProductStage = kABytes + kBBytes + kRawBytes;
+constexpr int kProductFixed = kEpiWarps * slot_bytes_per_warp(kOpProduct) + kCtrlBytes + 1024;
+
+// Four codes (the bytes of w) times s, rounded to bfloat16.  A byte with its sign bit flipped, put behind the
+// exponent of 2^23, is the float 2^23 + 128 + code: one byte permutation and one exact subtraction per code instead
+// of a conversion instruction, which runs at a quarter of their rate or less.
+__device__ __forceinline__ void scale_codes(uint32_t w, float s, uint32_t& lo, uint32_t& hi) {
+    w ^= 0x80808080u;
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        f[i] = __fmul_rn(__fsub_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540u + i)), 8388736.0f), s);
+    lo = pack2(f[0], f[1], false);
+    hi = pack2(f[2], f[3], false);
+}
+
+template <bool kPair, bool kAMajorM, bool kWide>
+__global__ void __launch_bounds__(kProductThreads, 1)
+mip_product_kernel(const __grid_constant__ LayerParams p) {
+    constexpr int kGroup = kPair ? 2 : 1;
+    constexpr int kRowsPerTile = kGroup * kBlockM;
+    const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
+    const bool leader = cta_rank == 0;
+    const int first_unit = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
+    const int unit_stride = kPair ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
+    uint8_t* smem = smem_raw + pad;
+    const uint32_t smem_base = raw_addr + pad;
+    const uint32_t stages = static_cast<uint32_t>(p.stages);
+    const uint32_t slots = smem_base + stages * kProductStage;
+    const uint32_t ctrl = slots + kEpiWarps * slot_bytes_per_warp(kOpProduct);
+    // control block, 8 bytes each: A has arrived | B is converted | A and B have been read | codes have arrived | codes
+    // have been read (`stages` of each), accumulators full and empty, drain, arrivals in the slots
+    const uint32_t bar_a = ctrl;
+    const uint32_t bar_b = ctrl + 64u;
+    const uint32_t bar_empty = ctrl + 128u;
+    const uint32_t bar_raw = ctrl + 192u;
+    const uint32_t bar_rawfree = ctrl + 256u;
+    const uint32_t bar_tfull = ctrl + 320u;
+    const uint32_t bar_tempty = ctrl + 336u;
+    const uint32_t bar_drain = ctrl + 352u;
+    const uint32_t bar_in = ctrl + 384u;
+    uint8_t* ctrl_ptr = smem + (ctrl - smem_base);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr + 360);
+    volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + 364);
+
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < stages; ++s) {
+            mbar_init(bar_a + 8u * s, 1);
+            mbar_init(bar_b + 8u * s, kGroup * kConvWarps);
+            mbar_init(bar_empty + 8u * s, 1);
+            mbar_init(bar_raw + 8u * s, 1);
+            mbar_init(bar_rawfree + 8u * s, kConvWarps);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(bar_tfull + 8u * a, 1);
+            mbar_init(bar_tempty + 8u * a, kGroup * kEpiWarps);
+        }
+        mbar_init(bar_drain, 1);
+        for (int i = 0; i < kEpiWarps * slot_count(kOpProduct); ++i) mbar_init(bar_in + 8u * i, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&p.tmap_a);
+        tma_prefetch_desc(&p.tmap_b0);
+        if (p.c_tma) tma_prefetch_desc(&p.tmap_c);
+    }
+    if (warp == 1) {
+        tmem_alloc<kGroup>(smem_u32(tmem_slot), p.tmem_cols);
+        tmem_relinquish<kGroup>();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (kPair) {
+        cluster_arrive();
+        cluster_wait();
+    }
+    tc_fence_after();
+    pdl_launch_dependents();
+    pdl_wait();          // from here on global memory is touched
+    const uint32_t tmem_base = *tmem_slot;
+    const int total_units = p.tiles_m * p.tiles_n;
+    const uint64_t budget = p.wait_budget_ns;
+    uint32_t issued = 0;       // stages whose copies this warp (0: A, 6: codes) has asked for
+    uint32_t s = 0, phase = 0;
+    const auto advance = [&] { if (++s == stages) { s = 0; phase ^= 1u; } };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ A
+        bool ok = true;
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+            const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+            const int m_cta = tc.m0 + static_cast<int>(cta_rank) * kBlockM;
+            for (int kb = 0; kb < p.k_blocks; ++kb) {
+                if (!mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                const uint32_t local = bar_a + 8u * s;
+                const uint32_t full = kPair ? mapa_u32(local, 0) : local;     // both CTAs' bytes complete on the leader's
+                const uint32_t dst = smem_base + s * kProductStage;
+                if (elect_one()) {
+                    if (leader) mbar_arrive_expect_tx(local, kGroup * kABytes);
+                    if (kAMajorM) {          // two blocks of 64 rows of the tile
+                        for (int i = 0; i < 2; ++i) {
+                            if (kPair) tma_load_2d_pair(dst + i * (kABytes / 2), &p.tmap_a, full, m_cta + 64 * i, kb * kProductK);
+                            else tma_load_2d(dst + i * (kABytes / 2), &p.tmap_a, full, m_cta + 64 * i, kb * kProductK);
+                        }
+                    } else {
+                        if (kPair) tma_load_2d_pair(dst, &p.tmap_a, full, kb * kProductK, m_cta);
+                        else tma_load_2d(dst, &p.tmap_a, full, kb * kProductK, m_cta);
+                    }
+                }
+                ++issued;
+                advance();
+            }
+        }
+    } else if (warp == 2 + kEpiWarps) {
+        // ------------------------------------------------------------ codes of B
+        bool ok = true;
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+            const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+            const int n_cta = tc.n0 + static_cast<int>(cta_rank) * kProductN;
+            for (int kb = 0; kb < p.k_blocks; ++kb) {
+                if (!mbar_wait(bar_rawfree + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(bar_raw + 8u * s, kRawBytes);
+                    tma_load_2d(smem_base + s * kProductStage + kABytes + kBBytes, &p.tmap_b0, bar_raw + 8u * s, n_cta, kb * kProductK);
+                }
+                ++issued;
+                advance();
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer
+        if (leader) {
+            bool ok = true;
+            int t = 0;
+            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++t) {
+                const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
+                if (!mbar_wait<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + acc * p.block_n;
+                for (int kb = 0; kb < p.k_blocks; ++kb) {
+                    if (!mbar_wait(bar_a + 8u * s, phase, abort_flag, budget) ||
+                        !mbar_wait<kPair>(bar_b + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a_addr = smem_base + s * kProductStage;
+                    const uint64_t a_desc = kAMajorM ? make_mnmajor_desc(a_addr, kABytes / 2) : make_kmajor_desc(a_addr, 128);
+                    const uint64_t b_desc = make_mnmajor_desc(a_addr + kABytes, kBBytes / 2);
+                    // 16 k per instruction: 32 bytes of a K-major row, 16 rows of 128 bytes of an M- or N-major block
+                    constexpr uint64_t a_step = kAMajorM ? 128ull : 2ull, b_step = 128ull;
+                    const uint32_t empty_local = bar_empty + 8u * s;
+                    const uint32_t empty_peer = kPair ? mapa_u32(empty_local, 1) : 0u;
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t k = 0; k < kProductK / 16; ++k)
+                            mma_f16<kGroup>(d_tmem, a_desc + a_step * k, b_desc + b_step * k, p.idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                        if (kPair) {
+                            mma_commit_pair(empty_local);
+                            mma_commit_pair(empty_peer);
+                        } else {
+                            mma_commit(empty_local);
+                        }
+                    }
+                    advance();
+                }
+                if (ok && !(p.debug_flags & 1)) {   // (test hook, bit 0: the "accumulator ready" signal is withheld)
+                    const uint32_t tfull_local = bar_tfull + 8u * acc;
+                    const uint32_t tfull_peer = kPair ? mapa_u32(tfull_local, 1) : 0u;
+                    if (elect_one()) {
+                        if (kPair) {
+                            mma_commit_pair(tfull_local);
+                            mma_commit_pair(tfull_peer);
+                        } else {
+                            mma_commit(tfull_local);
+                        }
+                    }
+                }
+            }
+        }
+    } else if (warp >= kFirstConvWarp) {
+        // ------------------------------------------------------------ codes -> bfloat16
+        const int j = lane & 7;                                    // 16 columns of the CTA's 128
+        const int r0 = (warp - kFirstConvWarp) * 8 + (lane >> 3);  // this lane's rows of a stage: r0 and r0 + 4
+        // its two 16-byte pieces inside the block of 64 columns; the second half of a row writes the odd one first
+        const uint32_t block = kABytes + static_cast<uint32_t>(j >> 2) * (kBBytes / 2);
+        const uint32_t flip = static_cast<uint32_t>(j >> 2);
+        const uint32_t piece = static_cast<uint32_t>(j & 3) * 2u;
+        const auto scale_of = [&](int k) { return k < p.K ? scale_at(p.b0_scale, k) : 0.0f; };
+        float s0 = scale_of(r0), s1 = scale_of(r0 + 4);
+        bool ok = true;
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+            for (int kb = 0; kb < p.k_blocks; ++kb) {
+                // (the scales of the next stage travel while this one is converted)
+                const int k_next = (kb + 1 < p.k_blocks ? kb + 1 : 0) * kProductK + r0;
+                const float n0 = scale_of(k_next), n1 = scale_of(k_next + 4);
+                const uint32_t stage = smem_base + s * kProductStage;
+                // codes in place; the tensor core has read what the buffer held.  (Lanes decide together.)
+                const bool ready = mbar_wait(bar_raw + 8u * s, phase, abort_flag, budget) &&
+                                   mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget);
+                if (!__all_sync(~0u, ready)) { ok = false; break; }
+                uint32_t w[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    lds_v4(stage + kABytes + kBBytes + static_cast<uint32_t>(r0 + 4 * i) * 128u + static_cast<uint32_t>(j) * 16u, w[i]);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t r = static_cast<uint32_t>(r0 + 4 * i);
+                    const float sc = i ? s1 : s0;
+                    uint32_t lo[4], hi[4];                         // columns 0-7 and 8-15
+                    scale_codes(w[i][0], sc, lo[0], lo[1]);
+                    scale_codes(w[i][1], sc, lo[2], lo[3]);
+                    scale_codes(w[i][2], sc, hi[0], hi[1]);
+                    scale_codes(w[i][3], sc, hi[2], hi[3]);
+                    uint32_t first[4], second[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        first[c] = flip ? hi[c] : lo[c];
+                        second[c] = flip ? lo[c] : hi[c];
+                    }
+                    const uint32_t row = stage + block + r * 128u;
+                    st_shared_v4(row + (((piece + flip) ^ (r & 7u)) << 4), first);
+                    st_shared_v4(row + (((piece + (flip ^ 1u)) ^ (r & 7u)) << 4), second);
+                }
+                // the writes become visible to the tensor core, and the codes' bytes may be overwritten by the TMA
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (kPair && !leader) mbar_arrive_remote(bar_b + 8u * s, 0);
+                    else mbar_arrive(bar_b + 8u * s);
+                    mbar_arrive(bar_rawfree + 8u * s);
+                }
+                s0 = n0;
+                s1 = n1;
+                advance();
+            }
+        }
+    } else {
+        layer_epilogue<kPair, kOpProduct, kWide>(p, slots, 0, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3, lane,
+                                                 cta_rank, first_unit, unit_stride);
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag != 0) {
+        // copies asked for last: A's complete on the leader's barriers, the codes' on each CTA's own
+        if ((warp == 0 && leader) || warp == 2 + kEpiWarps) {
+            const uint32_t bar = warp == 0 ? bar_a : bar_raw;
+            const uint32_t n = min(issued, stages);
+            for (uint32_t i = 1; i <= n; ++i) {
+                const uint32_t idx = issued - i;
+                const uint64_t t0 = globaltimer_ns();
+                while (!mbar_try_wait(bar + 8u * (idx % stages), (idx / stages) & 1u)) {
+                    if (globaltimer_ns() - t0 > budget) break;
+                }
+            }
+        }
+        if (warp == 1 && leader) {
+            if (elect_one()) {
+                if (kPair) mma_commit_pair(bar_drain); else mma_commit(bar_drain);
+            }
+            const uint64_t t0 = globaltimer_ns();
+            while (!mbar_try_wait(bar_drain, 0)) {
+                if (globaltimer_ns() - t0 > budget) break;
+            }
+            tc_fence_before();
+        }
+        __syncthreads();
+    }
+    if (kPair) {
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc<kGroup>(tmem_base, p.tmem_cols);
+    }
+    if (threadIdx.x == 0 && *abort_flag != 0) atomicOr(p.status, 1u);
+}
+
+template <bool kPair, bool kAMajorM, bool kWide>
+cudaError_t product_init_t() {
+    return cudaFuncSetAttribute(mip_product_kernel<kPair, kAMajorM, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudget);
+}
+
+}  // namespace
+
+int product_stages() { return (kSmemBudget - kProductFixed) / static_cast<int>(kProductStage); }
+
+cudaError_t product_init() {
+    for (cudaError_t e : {product_init_t<false, false, false>(), product_init_t<false, false, true>(), product_init_t<false, true, false>(),
+                          product_init_t<false, true, true>(), product_init_t<true, false, false>(), product_init_t<true, false, true>(),
+                          product_init_t<true, true, false>(), product_init_t<true, true, true>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+
+cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int grid, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
+    cfg.blockDim = dim3(kProductThreads, 1, 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * kProductStage + kProductFixed;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pair ? 2 : 1;
+    switch ((pair ? 4 : 0) + (a_order ? 2 : 0) + (p.type == kF32 ? 1 : 0)) {
+        case 0: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, false, false>, p);
+        case 1: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, false, true>, p);
+        case 2: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, true, false>, p);
+        case 3: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, true, true>, p);
+        case 4: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, false, false>, p);
+        case 5: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, false, true>, p);
+        case 6: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, true, false>, p);
+        default: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, true, true>, p);
+    }
+}
+
+}  // namespace mip
