@@ -134,10 +134,12 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
 #pragma unroll
     for (int g = 0; g < 32 / kPer; ++g) {
         float b0[kPer], b1[kPer], r[kPer], y[kPer], y2[kPer];
+        if constexpr (kOp != kOpProduct) {
 #pragma unroll
-        for (int h = 0; h < kPer && kOp != kOpProduct; h += 4) {
-            lds_f4(cols + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b0[h]));
-            lds_f4(cols + 256 + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b1[h]));
+            for (int h = 0; h < kPer; h += 4) {
+                lds_f4(cols + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b0[h]));
+                lds_f4(cols + 256 + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b1[h]));
+            }
         }
         const uint32_t at = slot_piece(slot, row, piece0 + g);
         if (has_r) {

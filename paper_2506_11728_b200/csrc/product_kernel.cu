@@ -7,7 +7,7 @@
 //
 // Roles.  Warp 0 loads A (TMA, 128-byte swizzle, K-major or M-major as it lies), warp 1 issues the MMAs, warps 2-5
 // are the epilogue (layer_epilogue.cuh), warp 6 loads B's codes (TMA, 64 rows x 128 bytes, plain rows), warps 7-14
-// convert: a lane takes 16 codes of a row (one 16-byte read, eight lanes a row), scales them and writes the two
+// convert, two groups by turns: a lane takes 16 codes of a row (one 16-byte read, eight lanes a row), scales them and writes the two
 // 16-byte pieces of the N-major 128-byte-swizzled tile the tensor core reads.  Lanes of the row's second half write
 // their pieces in the other order, so that eight lanes cover all banks.  A stage is 64 k: 16 KB of A, 8 KB of codes,
 // 16 KB of converted B per CTA.  In the pair form (256 x 256 tile, cta_group::2) each CTA converts its half of B, so
@@ -27,6 +27,7 @@ constexpr uint32_t kABytes = kBlockM * kProductK * 2;          // 16 KB
 constexpr uint32_t kBBytes = kProductN * kProductK * 2;        // 16 KB, two blocks of 64 columns
 constexpr uint32_t kRawBytes = kProductN * kProductK;          // 8 KB
 constexpr uint32_t kProductStage = kABytes + kBBytes + kRawBytes;
+constexpr uint32_t kScaleBytes = kProductK * 4;                // the rows' scales, behind the stages
 constexpr int kProductFixed = kEpiWarps * slot_bytes_per_warp(kOpProduct) + kCtrlBytes + 1024;
 
 // Four codes (the bytes of w) times s, rounded to bfloat16.  A byte with its sign bit flipped, put behind the
@@ -58,7 +59,8 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     const uint32_t smem_base = raw_addr + pad;
     const uint32_t stages = static_cast<uint32_t>(p.stages);
     const uint32_t slots = smem_base + stages * kProductStage;
-    const uint32_t ctrl = slots + kEpiWarps * slot_bytes_per_warp(kOpProduct);
+    const uint32_t scales = slots + kEpiWarps * slot_bytes_per_warp(kOpProduct);
+    const uint32_t ctrl = scales + stages * kScaleBytes;
     // control block, 8 bytes each: A has arrived | B is converted | A and B have been read | codes have arrived | codes
     // have been read (`stages` of each), accumulators full and empty, drain, arrivals in the slots
     const uint32_t bar_a = ctrl;
@@ -79,10 +81,10 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < stages; ++s) {
             mbar_init(bar_a + 8u * s, 1);
-            mbar_init(bar_b + 8u * s, kGroup * kConvWarps);
+            mbar_init(bar_b + 8u * s, kGroup * kConvWarps / 2);
             mbar_init(bar_empty + 8u * s, 1);
-            mbar_init(bar_raw + 8u * s, 1);
-            mbar_init(bar_rawfree + 8u * s, kConvWarps);
+            mbar_init(bar_raw + 8u * s, 33);     // the copy of the codes, and every lane's copy of two scales
+            mbar_init(bar_rawfree + 8u * s, kConvWarps / 2);
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(bar_tfull + 8u * a, 1);
@@ -146,6 +148,8 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     } else if (warp == 2 + kEpiWarps) {
         // ------------------------------------------------------------ codes of B
         bool ok = true;
+        if (!p.b0_scale)         // no scales: ones, written once
+            for (uint32_t i = lane; i < stages * kProductK; i += 32) sts_f32(scales + i * 4u, 1.0f);
         for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int n_cta = tc.n0 + static_cast<int>(cta_rank) * kProductN;
@@ -154,6 +158,21 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
                 if (elect_one()) {
                     mbar_arrive_expect_tx(bar_raw + 8u * s, kRawBytes);
                     tma_load_2d(smem_base + s * kProductStage + kABytes + kBBytes, &p.tmap_b0, bar_raw + 8u * s, n_cta, kb * kProductK);
+                }
+                // the rows' scales: 4-byte asynchronous copies (the vector has no alignment beyond that), two per lane,
+                // rows beyond K zero; every lane's arrival follows its copies
+                if (p.b0_scale) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int k = kb * kProductK + h * 32 + lane;
+                        const uint32_t bytes = k < p.K ? 4u : 0u;
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;"
+                                     ::"r"(scales + s * kScaleBytes + static_cast<uint32_t>(h * 32 + lane) * 4u),
+                                       "l"(__cvta_generic_to_global(p.b0_scale + (k < p.K ? k : 0))), "r"(bytes) : "memory");
+                    }
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_raw + 8u * s) : "memory");
+                } else {
+                    mbar_arrive(bar_raw + 8u * s);
                 }
                 ++issued;
                 advance();
@@ -209,59 +228,56 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         }
     } else if (warp >= kFirstConvWarp) {
         // ------------------------------------------------------------ codes -> bfloat16
+        // Two groups of four warps take the stages in turn: the chain of one stage -- wait, read, convert, write, proxy
+        // fence, arrive -- may then last as long as two of the tensor core's stages.
+        const int cw = warp - kFirstConvWarp;
         const int j = lane & 7;                                    // 16 columns of the CTA's 128
-        const int r0 = (warp - kFirstConvWarp) * 8 + (lane >> 3);  // this lane's rows of a stage: r0 and r0 + 4
+        const int r0 = (cw & 3) * 16 + (lane >> 3);                // this lane's rows of a stage: r0 + 4 i, i < 4
         // its two 16-byte pieces inside the block of 64 columns; the second half of a row writes the odd one first
-        const uint32_t block = kABytes + static_cast<uint32_t>(j >> 2) * (kBBytes / 2);
         const uint32_t flip = static_cast<uint32_t>(j >> 2);
+        const uint32_t block = kABytes + flip * (kBBytes / 2);
         const uint32_t piece = static_cast<uint32_t>(j & 3) * 2u;
-        const auto scale_of = [&](int k) { return k < p.K ? scale_at(p.b0_scale, k) : 0.0f; };
-        float s0 = scale_of(r0), s1 = scale_of(r0 + 4);
-        bool ok = true;
-        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
-                // (the scales of the next stage travel while this one is converted)
-                const int k_next = (kb + 1 < p.k_blocks ? kb + 1 : 0) * kProductK + r0;
-                const float n0 = scale_of(k_next), n1 = scale_of(k_next + 4);
-                const uint32_t stage = smem_base + s * kProductStage;
-                // codes in place; the tensor core has read what the buffer held.  (Lanes decide together.)
-                const bool ready = mbar_wait(bar_raw + 8u * s, phase, abort_flag, budget) &&
-                                   mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget);
-                if (!__all_sync(~0u, ready)) { ok = false; break; }
-                uint32_t w[2][4];
+        const uint32_t my_units = first_unit < total_units ? static_cast<uint32_t>((total_units - first_unit + unit_stride - 1) / unit_stride) : 0u;
+        const uint32_t total = my_units * static_cast<uint32_t>(p.k_blocks);      // stages this CTA converts
+        for (uint32_t it = static_cast<uint32_t>(cw >> 2); it < total; it += 2) {
+            const uint32_t st = it % stages, ph = (it / stages) & 1u;
+            const uint32_t stage = smem_base + st * kProductStage;
+            // codes and scales in place; the tensor core has read what the buffer held.  (Lanes decide together.)
+            const bool ready = mbar_wait(bar_raw + 8u * st, ph, abort_flag, budget) &&
+                               mbar_wait(bar_empty + 8u * st, ph ^ 1u, abort_flag, budget);
+            if (!__all_sync(~0u, ready)) break;
+            uint32_t w[4][4];
+            float sc[4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    lds_v4(stage + kABytes + kBBytes + static_cast<uint32_t>(r0 + 4 * i) * 128u + static_cast<uint32_t>(j) * 16u, w[i]);
+            for (int i = 0; i < 4; ++i) {
+                lds_v4(stage + kABytes + kBBytes + static_cast<uint32_t>(r0 + 4 * i) * 128u + static_cast<uint32_t>(j) * 16u, w[i]);
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sc[i]) : "r"(scales + st * kScaleBytes + static_cast<uint32_t>(r0 + 4 * i) * 4u) : "memory");
+            }
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t r = static_cast<uint32_t>(r0 + 4 * i);
-                    const float sc = i ? s1 : s0;
-                    uint32_t lo[4], hi[4];                         // columns 0-7 and 8-15
-                    scale_codes(w[i][0], sc, lo[0], lo[1]);
-                    scale_codes(w[i][1], sc, lo[2], lo[3]);
-                    scale_codes(w[i][2], sc, hi[0], hi[1]);
-                    scale_codes(w[i][3], sc, hi[2], hi[3]);
-                    uint32_t first[4], second[4];
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = static_cast<uint32_t>(r0 + 4 * i);
+                uint32_t lo[4], hi[4];                             // columns 0-7 and 8-15
+                scale_codes(w[i][0], sc[i], lo[0], lo[1]);
+                scale_codes(w[i][1], sc[i], lo[2], lo[3]);
+                scale_codes(w[i][2], sc[i], hi[0], hi[1]);
+                scale_codes(w[i][3], sc[i], hi[2], hi[3]);
+                uint32_t first[4], second[4];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        first[c] = flip ? hi[c] : lo[c];
-                        second[c] = flip ? lo[c] : hi[c];
-                    }
-                    const uint32_t row = stage + block + r * 128u;
-                    st_shared_v4(row + (((piece + flip) ^ (r & 7u)) << 4), first);
-                    st_shared_v4(row + (((piece + (flip ^ 1u)) ^ (r & 7u)) << 4), second);
+                for (int c = 0; c < 4; ++c) {
+                    first[c] = flip ? hi[c] : lo[c];
+                    second[c] = flip ? lo[c] : hi[c];
                 }
-                // the writes become visible to the tensor core, and the codes' bytes may be overwritten by the TMA
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) {
-                    if (kPair && !leader) mbar_arrive_remote(bar_b + 8u * s, 0);
-                    else mbar_arrive(bar_b + 8u * s);
-                    mbar_arrive(bar_rawfree + 8u * s);
-                }
-                s0 = n0;
-                s1 = n1;
-                advance();
+                const uint32_t row = stage + block + r * 128u;
+                st_shared_v4(row + (((piece + flip) ^ (r & 7u)) << 4), first);
+                st_shared_v4(row + (((piece + (flip ^ 1u)) ^ (r & 7u)) << 4), second);
+            }
+            // the writes become visible to the tensor core, and the codes' bytes may be overwritten by the TMA
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (kPair && !leader) mbar_arrive_remote(bar_b + 8u * st, 0);
+                else mbar_arrive(bar_b + 8u * st);
+                mbar_arrive(bar_rawfree + 8u * st);
             }
         }
     } else {
@@ -314,7 +330,7 @@ cudaError_t product_init_t() {
 
 }  // namespace
 
-int product_stages() { return (kSmemBudget - kProductFixed) / static_cast<int>(kProductStage); }
+int product_stages() { return (kSmemBudget - kProductFixed) / static_cast<int>(kProductStage + kScaleBytes); }
 
 cudaError_t product_init() {
     for (cudaError_t e : {product_init_t<false, false, false>(), product_init_t<false, false, true>(), product_init_t<false, true, false>(),
@@ -328,7 +344,7 @@ cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int grid
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(kProductThreads, 1, 1);
-    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * kProductStage + kProductFixed;
+    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kProductStage + kScaleBytes) + kProductFixed;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
