@@ -30,17 +30,23 @@ constexpr uint32_t kProductStage = kABytes + kBBytes + kRawBytes;
 constexpr uint32_t kScaleBytes = kProductK * 4;                // the rows' scales, behind the stages
 constexpr int kProductFixed = kEpiWarps * slot_bytes_per_warp(kOpProduct) + kCtrlBytes + 1024;
 
-// Four codes (the bytes of w) times s, rounded to bfloat16.  A byte with its sign bit flipped, put behind the
-// exponent of 2^23, is the float 2^23 + 128 + code: one byte permutation and one exact subtraction per code instead
-// of a conversion instruction, which runs at a quarter of their rate or less.
-__device__ __forceinline__ void scale_codes(uint32_t w, float s, uint32_t& lo, uint32_t& hi) {
+// Four codes (the bytes of w) times s (twice, packed), rounded to bfloat16.  A byte with its sign bit flipped, put
+// behind the exponent of 2^23, is the float 2^23 + 128 + code: one byte permutation per code and one exact packed
+// subtraction per two instead of conversion instructions, which run at a quarter of their rate or less.
+__device__ __forceinline__ void scale_codes(uint32_t w, uint64_t ss, uint32_t& lo, uint32_t& hi) {
+    constexpr uint64_t kBias = 0xCB000080CB000080ull;              // -(2^23 + 128), twice
     w ^= 0x80808080u;
-    float f[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        f[i] = __fmul_rn(__fsub_rn(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540u + i)), 8388736.0f), s);
-    lo = pack2(f[0], f[1], false);
-    hi = pack2(f[2], f[3], false);
+    for (int h = 0; h < 2; ++h) {
+        uint64_t v;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(__byte_perm(w, 0x4B000000u, 0x7540u + 2 * h)),
+            "r"(__byte_perm(w, 0x4B000000u, 0x7541u + 2 * h)));
+        asm("add.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(kBias));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(ss));
+        float a, b;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+        (h ? hi : lo) = pack2(a, b, false);
+    }
 }
 
 template <bool kPair, bool kAMajorM, bool kWide>
@@ -246,36 +252,35 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
             const bool ready = mbar_wait(bar_raw + 8u * st, ph, abort_flag, budget) &&
                                mbar_wait(bar_empty + 8u * st, ph ^ 1u, abort_flag, budget);
             if (!__all_sync(~0u, ready)) break;
+            // (the second half of a row reads its two halves in the other order too, so no register is chosen by lane)
             uint32_t w[4][4];
-            float sc[4];
+            uint64_t ss[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                lds_v4(stage + kABytes + kBBytes + static_cast<uint32_t>(r0 + 4 * i) * 128u + static_cast<uint32_t>(j) * 16u, w[i]);
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sc[i]) : "r"(scales + st * kScaleBytes + static_cast<uint32_t>(r0 + 4 * i) * 4u) : "memory");
+                const uint32_t src = stage + kABytes + kBBytes + static_cast<uint32_t>(r0 + 4 * i) * 128u + static_cast<uint32_t>(j) * 16u;
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[i][0]), "=r"(w[i][1]) : "r"(src + flip * 8u) : "memory");
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[i][2]), "=r"(w[i][3]) : "r"(src + (flip ^ 1u) * 8u) : "memory");
+                uint32_t sc;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(sc) : "r"(scales + st * kScaleBytes + static_cast<uint32_t>(r0 + 4 * i) * 4u) : "memory");
+                asm("mov.b64 %0, {%1, %1};" : "=l"(ss[i]) : "r"(sc));
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t r = static_cast<uint32_t>(r0 + 4 * i);
-                uint32_t lo[4], hi[4];                             // columns 0-7 and 8-15
-                scale_codes(w[i][0], sc[i], lo[0], lo[1]);
-                scale_codes(w[i][1], sc[i], lo[2], lo[3]);
-                scale_codes(w[i][2], sc[i], hi[0], hi[1]);
-                scale_codes(w[i][3], sc[i], hi[2], hi[3]);
-                uint32_t first[4], second[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    first[c] = flip ? hi[c] : lo[c];
-                    second[c] = flip ? lo[c] : hi[c];
-                }
+                uint32_t first[4], second[4];                      // eight columns each
+                scale_codes(w[i][0], ss[i], first[0], first[1]);
+                scale_codes(w[i][1], ss[i], first[2], first[3]);
                 const uint32_t row = stage + block + r * 128u;
                 st_shared_v4(row + (((piece + flip) ^ (r & 7u)) << 4), first);
+                scale_codes(w[i][2], ss[i], second[0], second[1]);
+                scale_codes(w[i][3], ss[i], second[2], second[3]);
                 st_shared_v4(row + (((piece + (flip ^ 1u)) ^ (r & 7u)) << 4), second);
             }
             // the writes become visible to the tensor core, and the codes' bytes may be overwritten by the TMA
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
-                if (kPair && !leader) mbar_arrive_remote(bar_b + 8u * st, 0);
+                if (kPair && !leader) mbar_arrive_remote_fenced(bar_b + 8u * st, 0);
                 else mbar_arrive(bar_b + 8u * st);
                 mbar_arrive(bar_rawfree + 8u * st);
             }

@@ -73,6 +73,16 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar, uint32_t cta) {
         "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n\t}"
         ::"r"(bar), "r"(cta) : "memory");
 }
+// Arrives on CTA `cta`'s barrier for writes to the arriving CTA's OWN shared memory that a proxy fence has already
+// made visible to the tensor core: nothing is left for the arrival itself to order beyond its own CTA.  (The
+// cluster-scope release of mbar_arrive_remote, behind a warp's shared-memory stores, costs it ~1300 clocks.)
+__device__ __forceinline__ void mbar_arrive_remote_fenced(uint32_t bar, uint32_t cta) {
+    asm volatile(
+        "{\n\t.reg .b32 ra;\n\t"
+        "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+        "mbarrier.arrive.release.cta.shared::cluster.b64 _, [ra];\n\t}"
+        ::"r"(bar), "r"(cta) : "memory");
+}
 __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
