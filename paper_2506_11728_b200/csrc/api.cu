@@ -188,6 +188,7 @@ int get_device(DeviceState** out) {
             if ((e = dense_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = layer_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = product_init()) != cudaSuccess) return cuda_fail(e);
+            if ((e = stream_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring16_init()) != cudaSuccess) return cuda_fail(e);
             d.pair_clusters = dense_pair_max_clusters(kSmemBudget);
@@ -1274,6 +1275,7 @@ int encode_slots(CUtensorMap* map, const void* base, int type, long long M, long
 
 struct LayerPlan {
     int pair, block_n, grid;
+    int split, stages;                   // split > 0: the few-token kernel, K split over so many CTAs
 };
 
 // Tile shape of the dense layer kernel: the main loop's cost per k-block is that of the plain product's kernel
@@ -1285,7 +1287,7 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
     // output columns come in whole 128-byte slots
     const int step = gated ? (wide ? 64 : 128) : 64;
     const Tuning tun = tuning_now();
-    LayerPlan best{0, step, 1};
+    LayerPlan best{0, step, 1, 0, 0};
     double best_clk = 1e30;
     for (int pair = 0; pair <= 1; ++pair) {
         if (pair && dev->pair_clusters <= 0) continue;
@@ -1304,11 +1306,36 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
             const double clk = (waves - 1) * period + main + epi + (pair ? 1900.0 : 0.0);
             if (clk < best_clk) {
                 best_clk = clk;
-                best = LayerPlan{pair, bn, static_cast<int>(std::min(tiles, slots)) * (pair ? 2 : 1)};
+                best = LayerPlan{pair, bn, static_cast<int>(std::min(tiles, slots)) * (pair ? 2 : 1), 0, 0};
             }
         }
     }
     return best;
+}
+
+// Few tokens: the weights stream through once, whatever M is, so what counts is that every SM has enough of them on
+// its way, and that all CTAs (two per SM when their stages fit) are resident at once.  K is split over the CTAs of a
+// cluster while that holds and the CTAs would otherwise leave a quarter of the SMs without one, or each still gets
+// eight k-blocks.  Measured, one token, us for split 1 / 2 / 4 / 8 (N x K): 4096 x 4096 10.2 / 7.9 / 6.7 / 7.2,
+// 4096 x 11008 21.1 / 14.5 / 11.6 / 10.8, 14336 x 4096 14.1 / 13.6 / 18.0 / 24.5, gated 11008 x 4096 18.9 / 23.0 / 23.4
+// / 35.0, gated 4096 x 1024 4.9 / 4.8 / 5.5 / 7.1.
+LayerPlan plan_stream(const LayerArgs& a, const DeviceState* dev) {
+    const int out_n = a.op == kOpLinear ? kStreamRows : kStreamRows / 2;
+    const long long tiles = (a.N + out_n - 1) / out_n;
+    const int k_blocks = static_cast<int>((a.K + 127) / 128);
+    LayerPlan pl{0, static_cast<int>(round_up(a.M, 16)), 0, 1, 0};
+    const int per_sm = 2 * stream_smem(pl.block_n, 3) <= 224 * 1024 ? 2 : 1;
+    while (pl.split < 8 && 2 * pl.split * tiles <= static_cast<long long>(dev->sm_count) * per_sm && k_blocks / (2 * pl.split) >= 2 &&
+           (4 * tiles * pl.split < 3 * dev->sm_count || k_blocks / (2 * pl.split) >= 8))
+        pl.split *= 2;
+    const Tuning tun = tuning_now();
+    if (tun.split_k == 1 || tun.split_k == 2 || tun.split_k == 4 || tun.split_k == 8) pl.split = tun.split_k;
+    pl.grid = static_cast<int>(tiles) * pl.split;
+    const int budget = per_sm == 2 ? 113 * 1024 : kSmemBudget;
+    pl.stages = kMaxStages;
+    while (pl.stages > 2 && stream_smem(pl.block_n, pl.stages) > budget) --pl.stages;
+    pl.stages = std::max(2, std::min(pl.stages, (k_blocks + pl.split - 1) / pl.split));
+    return pl;
 }
 
 // Plans and tensor maps of recent layer calls, as g_plan_cache keeps those of the plain products.
@@ -1364,7 +1391,11 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
     }
     if (!hit) {
         const bool gated = a.op != kOpLinear, grad = a.op == kOpGatedGrad;
-        pl = plan_layer(a, dev);
+        const Tuning tun = tuning_now();
+        // Few tokens, or few tiles of a deep K (M = 48, us here / dense kernel: 4096 x 11008 13.1 / 19.0, 4096 x 4096 9.4 /
+        // 9.4, 14336 x 4096 18.5 / 16.1, gated 11008 x 4096 22.3 / 22.4; M = 24: 11.8 / 18.7, 7.8 / 9.4, 15.4 / 16.1, 19.9 / 22.4)
+        const bool few = (a.M <= 32 || (a.M <= 64 && a.N * (gated ? 2 : 1) <= 64 * dev->sm_count && a.K >= 48 * 128)) && tun.force_path != MIPGEMM_PATH_DENSE && tun.force_path != MIPGEMM_PATH_DENSE_PAIR;
+        pl = few ? plan_stream(a, dev) : plan_layer(a, dev);
         std::memset(&p, 0, sizeof(p));
         p.M = static_cast<int>(a.M);
         p.N = static_cast<int>(a.N);
@@ -1372,29 +1403,44 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
         p.type = a.type;
         p.k_blocks = static_cast<int>((a.K + 127) / 128);
         p.block_n = pl.block_n;
-        p.out_n = gated ? pl.block_n / 2 : pl.block_n;
-        const int rows = pl.pair ? 2 * kBlockM : kBlockM;
-        const int b_rows = pl.pair ? pl.block_n / 2 : pl.block_n;
-        p.tiles_m = static_cast<int>((a.M + rows - 1) / rows);
-        p.tiles_n = static_cast<int>((a.N + p.out_n - 1) / p.out_n);
-        p.stages = std::min(kMaxStages, (kSmemBudget - layer_fixed_smem(a.op)) / ((kBlockM + b_rows) * 128));
-        const Tuning tun = tuning_now();
-        if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
-        p.idesc = (2u << 4) | ((a.a_unsigned ? 0u : 1u) << 7) | (1u << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
-                  (static_cast<uint32_t>(rows >> 4) << 24);
-        p.tmem_cols = pow2_at_least(2u * pl.block_n);
         p.status = dev->status_word;
-        const size_t size = type_size(a.type);
-        p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;
-        // (tile stores clip in 16-byte pieces: a row must end on one)
-        p.c_tma = a.N * size % 16 == 0 && aligned16(a.C, a.ldc * static_cast<long long>(size)) &&
-                  (!grad || aligned16(a.C2, a.ldc2 * static_cast<long long>(size))) ? 1 : 0;
-        int st = encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, kBlockM);
-        if (st == MIPGEMM_OK) st = encode_tiled_2d(&p.tmap_b0, a.B0, a.K, a.N, a.ldb0, 128, gated ? p.out_n : b_rows);
-        if (st == MIPGEMM_OK && gated) st = encode_tiled_2d(&p.tmap_b1, a.B1, a.K, a.N, a.ldb1, 128, p.out_n);
-        if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.R, a.type, a.M, a.N, a.ldr);
-        if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
-        if (st == MIPGEMM_OK && p.c_tma && grad) st = encode_slots(&p.tmap_c2, a.C2, a.type, a.M, a.N, a.ldc2);
+        p.split = pl.split;
+        int st;
+        if (few) {
+            p.out_n = gated ? kStreamRows / 2 : kStreamRows;
+            p.tiles_n = static_cast<int>((a.N + p.out_n - 1) / p.out_n);
+            p.stages = pl.stages;
+            // weights are the 128-row operand, tokens the columns
+            p.idesc = (2u << 4) | (1u << 7) | ((a.a_unsigned ? 0u : 1u) << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
+                      (static_cast<uint32_t>(kStreamRows >> 4) << 24);
+            p.tmem_cols = pow2_at_least(pl.block_n);
+            st = encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, static_cast<int>(a.M));
+            if (st == MIPGEMM_OK) st = encode_tiled_2d(&p.tmap_b0, a.B0, a.K, a.N, a.ldb0, 128, p.out_n);
+            if (st == MIPGEMM_OK && gated) st = encode_tiled_2d(&p.tmap_b1, a.B1, a.K, a.N, a.ldb1, 128, p.out_n);
+        } else {
+            p.out_n = gated ? pl.block_n / 2 : pl.block_n;
+            const int rows = pl.pair ? 2 * kBlockM : kBlockM;
+            const int b_rows = pl.pair ? pl.block_n / 2 : pl.block_n;
+            p.tiles_m = static_cast<int>((a.M + rows - 1) / rows);
+            p.tiles_n = static_cast<int>((a.N + p.out_n - 1) / p.out_n);
+            p.stages = std::min(kMaxStages, (kSmemBudget - layer_fixed_smem(a.op)) / ((kBlockM + b_rows) * 128));
+            if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
+            p.idesc = (2u << 4) | ((a.a_unsigned ? 0u : 1u) << 7) | (1u << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
+                      (static_cast<uint32_t>(rows >> 4) << 24);
+            p.tmem_cols = pow2_at_least(2u * pl.block_n);
+            const size_t size = type_size(a.type);
+            p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;
+            // (tile stores clip in 16-byte pieces: a row must end on one)
+            p.c_tma = a.N * size % 16 == 0 && aligned16(a.C, a.ldc * static_cast<long long>(size)) &&
+                      (!grad || aligned16(a.C2, a.ldc2 * static_cast<long long>(size))) ? 1 : 0;
+            p.a_rows = std::min(p.M, kBlockM);
+            st = encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, p.a_rows);
+            if (st == MIPGEMM_OK) st = encode_tiled_2d(&p.tmap_b0, a.B0, a.K, a.N, a.ldb0, 128, gated ? p.out_n : b_rows);
+            if (st == MIPGEMM_OK && gated) st = encode_tiled_2d(&p.tmap_b1, a.B1, a.K, a.N, a.ldb1, 128, p.out_n);
+            if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.R, a.type, a.M, a.N, a.ldr);
+            if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
+            if (st == MIPGEMM_OK && p.c_tma && grad) st = encode_slots(&p.tmap_c2, a.C2, a.type, a.M, a.N, a.ldc2);
+        }
         if (st != MIPGEMM_OK) return st;
         p.R = a.R; p.ldr = a.ldr;
         p.C = a.C; p.ldc = a.ldc;
@@ -1409,11 +1455,24 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
     p.b0_scale = a.b0_scale;
     p.b1_scale = a.b1_scale;
     p.bias = a.bias;
-    const cudaError_t e = launch_layer(p, a.op, pl.pair, pl.grid, stream);
+    cudaError_t e;
+    if (pl.split) {
+        // (a promise about the weights, not part of the plan either)
+        p.b_constant = g_weights_constant.load() ||
+                       (inside_constant_range(a.B0, static_cast<size_t>(a.N - 1) * a.ldb0 + a.K) &&
+                        (a.op == kOpLinear || inside_constant_range(a.B1, static_cast<size_t>(a.N - 1) * a.ldb1 + a.K)));
+        e = launch_layer_stream(p, a.op, pl.grid, stream);
+        tl_last_path = MIPGEMM_PATH_SKINNY | (pl.split > 1 ? MIPGEMM_PATH_SPLITK : 0);
+    } else {
+        e = launch_layer(p, a.op, pl.pair, pl.grid, stream);
+        tl_last_path = pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE;
+    }
     ++g_launches;
     if (e != cudaSuccess) return cuda_fail(e);
-    tl_last_path = pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE;
-    if (log_enabled())
+    if (log_enabled() && pl.split)
+        std::fprintf(stderr, "mipgemm: layer op=%d M=%d N=%d K=%d -> few tokens, %d CTAs, split=%d stages=%d%s plan=%s\n", a.op, p.M, p.N, p.K,
+                     pl.grid, pl.split, p.stages, p.b_constant ? " (constant weights: early fetch)" : "", hit ? "cached" : "new");
+    else if (log_enabled())
         std::fprintf(stderr, "mipgemm: layer op=%d M=%d N=%d K=%lld -> dense %s tile=%dx%d stages=%d r_tma=%d c_tma=%d plan=%s\n", a.op,
                      p.M, p.N, static_cast<long long>(a.K), pl.pair ? "cta-pair" : "one-cta", pl.pair ? 2 * kBlockM : kBlockM,
                      pl.block_n, p.stages, p.r_tma, p.c_tma, hit ? "cached" : "new");
@@ -1537,6 +1596,7 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
         const long long slots1 = dev->sm_count, slots2 = std::max(dev->pair_clusters, 1);
         const double waves1 = static_cast<double>((tiles_of(0) + slots1 - 1) / slots1);
         const double waves2 = static_cast<double>((tiles_of(1) + slots2 - 1) / slots2);
+        pl = LayerPlan{};
         pl.pair = dev->pair_clusters > 0 && waves2 * 1.6 <= waves1 ? 1 : 0;
         if (tun.force_path == MIPGEMM_PATH_DENSE_PAIR && dev->pair_clusters > 0) pl.pair = 1;
         if (tun.force_path == MIPGEMM_PATH_DENSE) pl.pair = 0;

@@ -192,6 +192,7 @@ struct alignas(64) LayerParams {
     int block_n;                     // accumulator columns per tile
     int out_n;                       // output columns per tile: block_n, or half of it (gated forms)
     int stages, tiles_m, tiles_n;
+    int a_rows;                      // rows of A per tile copy: 128, or M where it is less
     uint32_t idesc, tmem_cols;
     int r_tma, c_tma;                // 1: R is read / C (and C2) written by TMA tile copies
     const float* a_scale;
@@ -204,7 +205,13 @@ struct alignas(64) LayerParams {
     unsigned int* status;
     unsigned long long wait_budget_ns;
     int debug_flags;                 // test hook (mipgemm_debug_set)
+    int split, b_constant;           // few-token kernel: CTAs that share K; weights may be fetched early
 };
+// Few-token form: the weights' rows on the accumulator's lanes, K split over a cluster.
+constexpr int kStreamRows = 128;     // weight rows per CTA (gated forms: 64 of each projection)
+int stream_smem(int tokens, int stages);
+cudaError_t stream_init();           // once per device
+cudaError_t launch_layer_stream(const LayerParams& p, int op, int grid, cudaStream_t stream);
 int layer_fixed_smem(int op);        // shared memory besides the pipeline stages
 cudaError_t layer_init();            // once per device
 cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaStream_t stream);

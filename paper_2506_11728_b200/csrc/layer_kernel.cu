@@ -102,7 +102,9 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
         uint32_t s = 0, phase = 0;
         bool ok = true;
         const bool side_a = warp == 0;
-        const uint32_t tx_bytes = kGroup * (side_a ? a_bytes : b_bytes);
+        // (fewer than 128 rows in all: only those are copied -- rows a TMA copy has to fill with zeros cost it several
+        // times those it reads -- and the accumulator rows behind them, never stored, add up what lies there)
+        const uint32_t tx_bytes = kGroup * (side_a ? static_cast<uint32_t>(p.a_rows) * 128u : b_bytes);
         for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int m_cta = tc.m0 + static_cast<int>(cta_rank) * kBlockM;
