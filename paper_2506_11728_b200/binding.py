@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmipgemm.so")
@@ -104,6 +105,10 @@ def _ptr(x) -> int:
 
 def _stream(stream) -> int:
     if stream is None:
+        # the current stream's handle without a Stream object around it (0.3 us a call instead of 4)
+        torch = sys.modules.get("torch")
+        if torch is not None and torch.cuda.is_initialized():
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         import torch
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
