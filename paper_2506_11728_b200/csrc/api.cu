@@ -97,6 +97,7 @@ struct DeviceState {
     bool host_events_ready = false;
     void* lent = nullptr;
     size_t lent_bytes = 0;
+    cudaMemPool_t pool = nullptr;          // scratch of the calls; keeps what it has been given back (see Scratch)
 };
 DeviceState g_dev[kMaxDevices];
 std::mutex g_mutex;
@@ -201,6 +202,18 @@ int get_device(DeviceState** out) {
             if (cudaStreamCreateWithFlags(&d.copy_in, cudaStreamNonBlocking) != cudaSuccess) d.copy_in = nullptr;
             if (cudaStreamCreateWithFlags(&d.copy_out, cudaStreamNonBlocking) != cudaSuccess) d.copy_out = nullptr;
             (void)cudaGetLastError();
+            // Scratch comes from a pool of the library's own that keeps up to 1 GiB between calls: the default pool gives
+            // everything back at every synchronisation, and the next call pays for mapping it again (0.5 ms and more).
+            cudaMemPoolProps props = {};
+            props.allocType = cudaMemAllocationTypePinned;
+            props.location.type = cudaMemLocationTypeDevice;
+            props.location.id = dev;
+            unsigned long long keep = 1ull << 30;
+            if (cudaMemPoolCreate(&d.pool, &props) != cudaSuccess ||
+                cudaMemPoolSetAttribute(d.pool, cudaMemPoolAttrReleaseThreshold, &keep) != cudaSuccess) {
+                d.pool = nullptr;                    // (the default pool then)
+                (void)cudaGetLastError();
+            }
             d.status = MIPGEMM_OK;
         }
         d.ready = true;
@@ -223,7 +236,10 @@ struct Scratch {
             if (bytes > dev->lent_bytes) return MIPGEMM_ERR_WORKSPACE;
             base = dev->lent;
         } else {
-            cudaError_t e = cudaMallocAsync(&base, bytes, stream);
+            // (a captured call allocates from the graph's memory)
+            cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+            const bool own = dev->pool && cudaStreamIsCapturing(stream, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone;
+            cudaError_t e = own ? cudaMallocFromPoolAsync(&base, bytes, dev->pool, stream) : cudaMallocAsync(&base, bytes, stream);
             if (e != cudaSuccess) {
                 tl_last_cuda_error = static_cast<int>(e);
                 (void)cudaGetLastError();
@@ -1273,9 +1289,11 @@ int encode_slots(CUtensorMap* map, const void* base, int type, long long M, long
     return MIPGEMM_OK;
 }
 
+constexpr int kMaxSplit = 16;
 struct LayerPlan {
     int pair, block_n, grid;
-    int split, stages;                   // split > 0: the few-token kernel, K split over so many CTAs
+    int few;                             // 1: the few-token kernel
+    int split, stages;                   // K is split over so many units (few-token kernel: CTAs of a cluster)
 };
 
 // Tile shape of the dense layer kernel: the main loop's cost per k-block is that of the plain product's kernel
@@ -1287,7 +1305,7 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
     // output columns come in whole 128-byte slots
     const int step = gated ? (wide ? 64 : 128) : 64;
     const Tuning tun = tuning_now();
-    LayerPlan best{0, step, 1, 0, 0};
+    LayerPlan best{0, step, 1, 0, 1, 0};
     double best_clk = 1e30;
     for (int pair = 0; pair <= 1; ++pair) {
         if (pair && dev->pair_clusters <= 0) continue;
@@ -1299,14 +1317,25 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
             const long long rows = pair ? 2 * kBlockM : kBlockM;
             const long long tiles = ((a.M + rows - 1) / rows) * ((a.N + out_n - 1) / out_n);
             const long long slots = pair ? dev->pair_clusters : dev->sm_count;
-            const double main = k_blocks * (pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn);
+            const double kb_clk = pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn;
             const double epi = bn / 32 * (a.op == kOpLinear ? 450.0 : 600.0);
-            const double period = std::max(main, epi) + 0.2 * std::min(main, epi);
-            const long long waves = (tiles + slots - 1) / slots;
-            const double clk = (waves - 1) * period + main + epi + (pair ? 1900.0 : 0.0);
-            if (clk < best_clk) {
-                best_clk = clk;
-                best = LayerPlan{pair, bn, static_cast<int>(std::min(tiles, slots)) * (pair ? 2 : 1), 0, 0};
+            for (int split = 1; split <= kMaxSplit; ++split) {
+                // K in `split` shares whose partial sums a second kernel adds: only while there are more SMs than tiles
+                // (not in lent scratch: what a call may need of it stays what the queries say)
+                if (split > 1 && (dev->lent || tiles * (split - 1) >= slots || k_blocks / split < 4 || (gated && bn % 64 != 0))) break;
+                const int share = (k_blocks + split - 1) / split;
+                if ((k_blocks + share - 1) / share != split) continue;
+                const double main = share * kb_clk;
+                const double period = std::max(main, epi) + 0.2 * std::min(main, epi);
+                const long long waves = (tiles * split + slots - 1) / slots;
+                double clk = (waves - 1) * period + main + epi + (pair ? 1900.0 : 0.0);
+                // (a launch, and the planes written and read at the L2's pace)
+                if (split > 1) clk += 5500.0 + 8.0 * split * static_cast<double>(a.M) * a.N * (gated ? 2 : 1) / 3500.0;
+                if (tun.split_k) { if (split != std::min(tun.split_k, k_blocks)) continue; }
+                if (clk < best_clk) {
+                    best_clk = clk;
+                    best = LayerPlan{pair, bn, static_cast<int>(std::min(tiles * split, slots)) * (pair ? 2 : 1), 0, split, 0};
+                }
             }
         }
     }
@@ -1323,13 +1352,14 @@ LayerPlan plan_stream(const LayerArgs& a, const DeviceState* dev) {
     const int out_n = a.op == kOpLinear ? kStreamRows : kStreamRows / 2;
     const long long tiles = (a.N + out_n - 1) / out_n;
     const int k_blocks = static_cast<int>((a.K + 127) / 128);
-    LayerPlan pl{0, static_cast<int>(round_up(a.M, 16)), 0, 1, 0};
+    LayerPlan pl{0, static_cast<int>(round_up(a.M, 16)), 0, 1, 1, 0};
     const int per_sm = 2 * stream_smem(pl.block_n, 3) <= 224 * 1024 ? 2 : 1;
     while (pl.split < 8 && 2 * pl.split * tiles <= static_cast<long long>(dev->sm_count) * per_sm && k_blocks / (2 * pl.split) >= 2 &&
            (4 * tiles * pl.split < 3 * dev->sm_count || k_blocks / (2 * pl.split) >= 8))
         pl.split *= 2;
     const Tuning tun = tuning_now();
     if (tun.split_k == 1 || tun.split_k == 2 || tun.split_k == 4 || tun.split_k == 8) pl.split = tun.split_k;
+    pl.few = 1;
     pl.grid = static_cast<int>(tiles) * pl.split;
     const int budget = per_sm == 2 ? 113 * 1024 : kSmemBudget;
     pl.stages = kMaxStages;
@@ -1379,7 +1409,8 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
         std::memset(&key, 0, sizeof(key));
         const uint64_t words[] = {
             reinterpret_cast<uint64_t>(dev), g_tuning_epoch.load(std::memory_order_acquire),
-            static_cast<uint64_t>(a.op) | (static_cast<uint64_t>(a.type) << 8) | (static_cast<uint64_t>(a.a_unsigned) << 16),
+            static_cast<uint64_t>(a.op) | (static_cast<uint64_t>(a.type) << 8) | (static_cast<uint64_t>(a.a_unsigned) << 16) |
+                (static_cast<uint64_t>(dev->lent != nullptr) << 17),
             static_cast<uint64_t>(a.M), static_cast<uint64_t>(a.N), static_cast<uint64_t>(a.K),
             reinterpret_cast<uint64_t>(a.A), static_cast<uint64_t>(a.lda), reinterpret_cast<uint64_t>(a.B0),
             static_cast<uint64_t>(a.ldb0), reinterpret_cast<uint64_t>(a.B1), static_cast<uint64_t>(a.ldb1),
@@ -1428,6 +1459,9 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
             p.idesc = (2u << 4) | ((a.a_unsigned ? 0u : 1u) << 7) | (1u << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
                       (static_cast<uint32_t>(rows >> 4) << 24);
             p.tmem_cols = pow2_at_least(2u * pl.block_n);
+            p.kb_share = (p.k_blocks + pl.split - 1) / pl.split;
+            p.plane_rows = static_cast<int>(round_up(a.M, 32));
+            p.plane_second = gated ? static_cast<int>(round_up(a.N, 32)) : 0;
             const size_t size = type_size(a.type);
             p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;
             // (tile stores clip in 16-byte pieces: a row must end on one)
@@ -1438,8 +1472,8 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
             if (st == MIPGEMM_OK) st = encode_tiled_2d(&p.tmap_b0, a.B0, a.K, a.N, a.ldb0, 128, gated ? p.out_n : b_rows);
             if (st == MIPGEMM_OK && gated) st = encode_tiled_2d(&p.tmap_b1, a.B1, a.K, a.N, a.ldb1, 128, p.out_n);
             if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.R, a.type, a.M, a.N, a.ldr);
-            if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
-            if (st == MIPGEMM_OK && p.c_tma && grad) st = encode_slots(&p.tmap_c2, a.C2, a.type, a.M, a.N, a.ldc2);
+            if (st == MIPGEMM_OK && p.c_tma && pl.split == 1) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
+            if (st == MIPGEMM_OK && p.c_tma && grad && pl.split == 1) st = encode_slots(&p.tmap_c2, a.C2, a.type, a.M, a.N, a.ldc2);
         }
         if (st != MIPGEMM_OK) return st;
         p.R = a.R; p.ldr = a.ldr;
@@ -1456,26 +1490,42 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
     p.b1_scale = a.b1_scale;
     p.bias = a.bias;
     cudaError_t e;
-    if (pl.split) {
+    if (pl.few) {
         // (a promise about the weights, not part of the plan either)
         p.b_constant = g_weights_constant.load() ||
                        (inside_constant_range(a.B0, static_cast<size_t>(a.N - 1) * a.ldb0 + a.K) &&
                         (a.op == kOpLinear || inside_constant_range(a.B1, static_cast<size_t>(a.N - 1) * a.ldb1 + a.K)));
         e = launch_layer_stream(p, a.op, pl.grid, stream);
         tl_last_path = MIPGEMM_PATH_SKINNY | (pl.split > 1 ? MIPGEMM_PATH_SPLITK : 0);
+    } else if (pl.split > 1) {
+        const bool gated = a.op != kOpLinear;
+        PartialPlanes planes{nullptr, pl.split, p.plane_rows, round_up(a.N, 32) * (gated ? 2 : 1), p.plane_second};
+        Scratch scratch(dev, stream);
+        int st = scratch.reserve(static_cast<size_t>(pl.split) * planes.plane_rows * planes.pitch * 4);
+        if (st != MIPGEMM_OK) return st;
+        planes.base = scratch.base;
+        st = encode_slots(&p.tmap_c, scratch.base, MIPGEMM_TYPE_F32, pl.split * planes.plane_rows, planes.pitch, planes.pitch);
+        if (st != MIPGEMM_OK) return st;
+        p.R = nullptr;
+        p.r_tma = 0;
+        p.c_tma = 1;
+        e = launch_layer(p, gated ? kOpRawGated : kOpRaw, pl.pair, pl.grid, stream);
+        ++g_launches;
+        if (e == cudaSuccess) e = launch_layer_finish(a, planes, stream);
+        tl_last_path = (pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE) | MIPGEMM_PATH_SPLITK;
     } else {
         e = launch_layer(p, a.op, pl.pair, pl.grid, stream);
         tl_last_path = pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE;
     }
     ++g_launches;
     if (e != cudaSuccess) return cuda_fail(e);
-    if (log_enabled() && pl.split)
+    if (log_enabled() && pl.few)
         std::fprintf(stderr, "mipgemm: layer op=%d M=%d N=%d K=%d -> few tokens, %d CTAs, split=%d stages=%d%s plan=%s\n", a.op, p.M, p.N, p.K,
                      pl.grid, pl.split, p.stages, p.b_constant ? " (constant weights: early fetch)" : "", hit ? "cached" : "new");
     else if (log_enabled())
-        std::fprintf(stderr, "mipgemm: layer op=%d M=%d N=%d K=%lld -> dense %s tile=%dx%d stages=%d r_tma=%d c_tma=%d plan=%s\n", a.op,
+        std::fprintf(stderr, "mipgemm: layer op=%d M=%d N=%d K=%lld -> dense %s tile=%dx%d stages=%d split=%d r_tma=%d c_tma=%d plan=%s\n", a.op,
                      p.M, p.N, static_cast<long long>(a.K), pl.pair ? "cta-pair" : "one-cta", pl.pair ? 2 * kBlockM : kBlockM,
-                     pl.block_n, p.stages, p.r_tma, p.c_tma, hit ? "cached" : "new");
+                     pl.block_n, p.stages, pl.split, p.r_tma, p.c_tma, hit ? "cached" : "new");
     return MIPGEMM_OK;
 }
 
@@ -1503,7 +1553,7 @@ int layer_impl(const LayerArgs& a, void* stream_v) {
     if (st != MIPGEMM_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     if (a.K == 0) {                      // every sum is 0
-        const cudaError_t e = launch_layer_simple(a, stream);
+        const cudaError_t e = launch_layer_finish(a, PartialPlanes{}, stream);
         ++g_launches;
         if (e != cudaSuccess) return cuda_fail(e);
         tl_last_path = MIPGEMM_PATH_TRIVIAL;
@@ -1578,7 +1628,7 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
         const uint64_t words[] = {
             reinterpret_cast<uint64_t>(dev), g_tuning_epoch.load(std::memory_order_acquire),
             static_cast<uint64_t>(kOpProduct) | (static_cast<uint64_t>(a.type) << 8) | (static_cast<uint64_t>(a.a_order) << 16) |
-                (static_cast<uint64_t>(a.accumulate) << 17),
+                (static_cast<uint64_t>(a.accumulate) << 17) | (static_cast<uint64_t>(dev->lent != nullptr) << 18),
             static_cast<uint64_t>(a.M), static_cast<uint64_t>(a.N), static_cast<uint64_t>(a.K),
             reinterpret_cast<uint64_t>(a.A), static_cast<uint64_t>(a.lda), reinterpret_cast<uint64_t>(a.B),
             static_cast<uint64_t>(a.ldb), reinterpret_cast<uint64_t>(a.C), static_cast<uint64_t>(a.ldc)};
@@ -1592,22 +1642,42 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
             const long long rows = pair ? 2 * kBlockM : kBlockM, cols = pair ? 2 * kProductN : kProductN;
             return ((a.M + rows - 1) / rows) * ((a.N + cols - 1) / cols);
         };
-        // a pair's tile is four single tiles for the price of two and a half (its warps convert half as much per product)
-        const long long slots1 = dev->sm_count, slots2 = std::max(dev->pair_clusters, 1);
-        const double waves1 = static_cast<double>((tiles_of(0) + slots1 - 1) / slots1);
-        const double waves2 = static_cast<double>((tiles_of(1) + slots2 - 1) / slots2);
         pl = LayerPlan{};
-        pl.pair = dev->pair_clusters > 0 && waves2 * 1.6 <= waves1 ? 1 : 0;
-        if (tun.force_path == MIPGEMM_PATH_DENSE_PAIR && dev->pair_clusters > 0) pl.pair = 1;
-        if (tun.force_path == MIPGEMM_PATH_DENSE) pl.pair = 0;
+        double best_clk = 1e30;
+        const int k_blocks = static_cast<int>((a.K + kProductK - 1) / kProductK);
+        for (int pair = 0; pair <= 1; ++pair) {
+            if (pair && dev->pair_clusters <= 0) continue;
+            if (tun.force_path == MIPGEMM_PATH_DENSE_PAIR && !pair && dev->pair_clusters > 0) continue;
+            if (tun.force_path == MIPGEMM_PATH_DENSE && pair) continue;
+            const long long slots = pair ? dev->pair_clusters : dev->sm_count;
+            for (int split = 1; split <= kMaxSplit; ++split) {
+                if (split > 1 && (dev->lent || k_blocks / split < 4)) break;
+                const int share = (k_blocks + split - 1) / split;
+                if ((k_blocks + share - 1) / share != split) continue;
+                if (tun.split_k && split != std::min(tun.split_k, k_blocks)) continue;
+                // a stage costs a CTA the same 670 clocks in either form (its warps convert 128 columns x 64 k); a pair does
+                // four times a single CTA's products with it
+                const long long waves = (tiles_of(pair) * split + slots - 1) / slots;
+                double clk = static_cast<double>(waves) * (share * 670.0 + 1500.0) + 4000.0 + (pair ? 1900.0 : 0.0);
+                if (split > 1) clk += 5500.0 + 8.0 * split * static_cast<double>(a.M) * a.N / 3500.0;
+                if (clk < best_clk) {
+                    best_clk = clk;
+                    pl.pair = pair;
+                    pl.split = split;
+                    pl.grid = static_cast<int>(std::min(tiles_of(pair) * split, slots)) * (pair ? 2 : 1);
+                }
+            }
+        }
         const int group = pl.pair ? 2 : 1;
         pl.block_n = kProductN * group;
-        pl.grid = static_cast<int>(std::min(tiles_of(pl.pair), pl.pair ? slots2 : slots1)) * group;
         p.M = static_cast<int>(a.M);
         p.N = static_cast<int>(a.N);
         p.K = static_cast<int>(a.K);
         p.type = a.type;
-        p.k_blocks = static_cast<int>((a.K + kProductK - 1) / kProductK);
+        p.k_blocks = k_blocks;
+        p.split = pl.split;
+        p.kb_share = (k_blocks + pl.split - 1) / pl.split;
+        p.plane_rows = static_cast<int>(round_up(a.M, 32));
         p.block_n = p.out_n = pl.block_n;
         p.tiles_m = static_cast<int>((a.M + kBlockM * group - 1) / (kBlockM * group));
         p.tiles_n = static_cast<int>((a.N + pl.block_n - 1) / pl.block_n);
@@ -1626,7 +1696,7 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
                            : encode_bf16_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, kBlockM);
         if (st == MIPGEMM_OK) st = encode_codes_rows(&p.tmap_b0, a.B, a.N, a.K, a.ldb);
         if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.C, a.type, a.M, a.N, a.ldc);
-        if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
+        if (st == MIPGEMM_OK && p.c_tma && pl.split == 1) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
         if (st != MIPGEMM_OK) return st;
         p.R = a.accumulate ? a.C : nullptr; p.ldr = a.ldc;
         p.C = a.C; p.ldc = a.ldc;
@@ -1635,13 +1705,30 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
         if (cacheable) layer_store(key, p, pl);
     }
     p.b0_scale = a.b_scale;              // (not part of the plan)
-    const cudaError_t e = launch_product(p, a.a_order, pl.pair, pl.grid, stream);
+    cudaError_t e;
+    if (pl.split > 1) {
+        PartialPlanes planes{nullptr, pl.split, p.plane_rows, round_up(a.N, 32), 0};
+        Scratch scratch(dev, stream);
+        int st = scratch.reserve(static_cast<size_t>(pl.split) * planes.plane_rows * planes.pitch * 4);
+        if (st != MIPGEMM_OK) return st;
+        planes.base = scratch.base;
+        st = encode_slots(&p.tmap_c, scratch.base, MIPGEMM_TYPE_F32, pl.split * planes.plane_rows, planes.pitch, planes.pitch);
+        if (st != MIPGEMM_OK) return st;
+        p.R = nullptr;
+        p.r_tma = 0;
+        p.c_tma = 1;
+        e = launch_product(p, a.a_order, pl.pair, 1, pl.grid, stream);
+        ++g_launches;
+        if (e == cudaSuccess) e = launch_product_finish(a, planes, stream);
+    } else {
+        e = launch_product(p, a.a_order, pl.pair, 0, pl.grid, stream);
+    }
     ++g_launches;
     if (e != cudaSuccess) return cuda_fail(e);
-    tl_last_path = pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE;
+    tl_last_path = (pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE) | (pl.split > 1 ? MIPGEMM_PATH_SPLITK : 0);
     if (log_enabled())
-        std::fprintf(stderr, "mipgemm: product M=%d N=%d K=%d a_order=%d -> dense %s stages=%d r_tma=%d c_tma=%d plan=%s\n", p.M, p.N, p.K,
-                     a.a_order, pl.pair ? "cta-pair" : "one-cta", p.stages, p.r_tma, p.c_tma, hit ? "cached" : "new");
+        std::fprintf(stderr, "mipgemm: product M=%d N=%d K=%d a_order=%d -> dense %s stages=%d split=%d r_tma=%d c_tma=%d plan=%s\n", p.M, p.N, p.K,
+                     a.a_order, pl.pair ? "cta-pair" : "one-cta", p.stages, pl.split, p.r_tma, p.c_tma, hit ? "cached" : "new");
     return MIPGEMM_OK;
 }
 
@@ -1662,7 +1749,7 @@ int product_impl(const ProductArgs& a, void* stream_v) {
     if (st != MIPGEMM_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     if (a.K == 0) {                      // every sum is 0
-        const cudaError_t e = launch_product_simple(a, stream);
+        const cudaError_t e = launch_product_finish(a, PartialPlanes{}, stream);
         ++g_launches;
         if (e != cudaSuccess) return cuda_fail(e);
         tl_last_path = MIPGEMM_PATH_TRIVIAL;
@@ -2133,6 +2220,10 @@ int mipgemm_release_staging(void) {
         cudaError_t e = cudaFree(dev->staging);
         dev->staging = nullptr;
         dev->staging_bytes = 0;
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
+    if (dev->pool) {
+        const cudaError_t e = cudaMemPoolTrimTo(dev->pool, 0);
         if (e != cudaSuccess) return cuda_fail(e);
     }
     return MIPGEMM_OK;

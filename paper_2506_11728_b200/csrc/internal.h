@@ -163,6 +163,8 @@ cudaError_t launch_skinny_ring16(const SkinnyRingParams& p, int sm_count, cudaSt
 
 // Which transform the exact sums of a layer kernel go through (see layer_math.cuh).
 constexpr int kOpLinear = 0, kOpGated = 1, kOpGatedGrad = 2, kOpProduct = 3;
+// Partial sums as they are, for a K split over units of the grid (a second kernel adds and finishes them).
+constexpr int kOpRaw = 4, kOpRawGated = 5;
 struct LayerArgs {
     int op, type, act;               // kOp*, mipgemm_type_t of R / C / C2, mipgemm_activation_t
     int a_unsigned;
@@ -177,8 +179,24 @@ struct LayerArgs {
     const void* R; long long ldr;    // kOpLinear: residual or NULL; kOpGatedGrad: gradient of the block's output
     void* C; long long ldc;          // result; kOpGatedGrad: gradient of the gate projection
     void* C2; long long ldc2;        // kOpGatedGrad: gradient of the other projection
+    // Moves everything that is indexed by row (besides A) `rows` rows on.
+    void advance(long long rows) {
+        const long long size = type == 0 ? 4 : 2;
+        if (a_scale) a_scale += rows;
+        if (R) R = static_cast<const char*>(R) + rows * ldr * size;
+        C = static_cast<char*>(C) + rows * ldc * size;
+        if (C2) C2 = static_cast<char*>(C2) + rows * ldc2 * size;
+    }
 };
-cudaError_t launch_layer_simple(const LayerArgs& a, cudaStream_t stream);
+
+// The transforms alone: adds `split` planes of partial sums ([split][plane_rows][pitch] int32; the second projection's
+// columns start at `second`) and finishes them.  split = 0: every sum is 0 (K == 0).
+struct PartialPlanes {
+    const void* base;
+    int split;
+    long long plane_rows, pitch, second;
+};
+cudaError_t launch_layer_finish(const LayerArgs& a, const PartialPlanes& s, cudaStream_t stream);
 
 // The dense layer kernel's parameters; passed by value as a __grid_constant__.
 struct alignas(64) LayerParams {
@@ -205,7 +223,10 @@ struct alignas(64) LayerParams {
     unsigned int* status;
     unsigned long long wait_budget_ns;
     int debug_flags;                 // test hook (mipgemm_debug_set)
-    int split, b_constant;           // few-token kernel: CTAs that share K; weights may be fetched early
+    int split;                       // > 1: K is split over so many units (few-token kernel: over the CTAs of a cluster)
+    int kb_share;                    // dense kernels: k-blocks per unit
+    int plane_rows, plane_second;    // partial sums: rows per plane, first column of the second projection
+    int b_constant;                  // few-token kernel: weights may be fetched early
 };
 // Few-token form: the weights' rows on the accumulator's lanes, K split over a cluster.
 constexpr int kStreamRows = 128;     // weight rows per CTA (gated forms: 64 of each projection)
@@ -224,15 +245,17 @@ struct ProductArgs {
     const int8_t* B; long long ldb;
     const float* b_scale;
     void* C; long long ldc;
+    void advance(long long rows) { C = static_cast<char*>(C) + rows * ldc * (type == 0 ? 4 : 2); }   // (see LayerArgs)
 };
-cudaError_t launch_product_simple(const ProductArgs& a, cudaStream_t stream);
+// The same for its float32 partial sums, added in the order of K.
+cudaError_t launch_product_finish(const ProductArgs& a, const PartialPlanes& s, cudaStream_t stream);
 // Its kernel takes LayerParams: tmap_a = A (bf16: {K, M}, or {M, K} with a_order), tmap_b0 = B ({N, K} bytes), b0_scale =
 // the scales, R = C when it accumulates, k_blocks of kProductK each.
 constexpr int kProductK = 64;        // k per pipeline stage: 128 bytes of a bf16 row
 constexpr int kProductN = 128;       // columns of B staged per CTA
 int product_stages();
 cudaError_t product_init();          // once per device
-cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int grid, cudaStream_t stream);
+cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int raw, int grid, cudaStream_t stream);
 
 cudaError_t launch_quantize_rows(int type, long long M, long long N, const void* X, long long ldx, int8_t* Q,
                                  long long ldq, float* scale, cudaStream_t stream);

@@ -25,27 +25,39 @@ constexpr int kColBytes = 2 * 64 * 4;               // per warp: two vectors of 
 // on its way before the accumulator is ready; gated: nothing comes in, two suffice to store one while the next is
 // computed; gradient: two, each of two buffers (one per result; the incoming gradient lies in the first); product: one
 // (its pipeline stages need the room, and its main loops are long).
-constexpr int slot_count(int op) { return op == kOpLinear ? 4 : (op == kOpProduct ? 1 : 2); }
+constexpr int slot_count(int op) { return op == kOpLinear || op == kOpRaw ? 4 : (op == kOpProduct ? 1 : 2); }
 constexpr int slot_stride(int op) { return op == kOpGatedGrad ? 2 * kSlot : kSlot; }
 constexpr int slot_bytes_per_warp(int op) { return slot_count(op) * slot_stride(op); }
 
 struct LayerTile {
     int m0, n0;
+    int kb0, kb1;        // k-blocks of this unit
+    int plane;           // first row of its plane of partial sums
 };
 
-__device__ __forceinline__ LayerTile decode_tile(const LayerParams& p, int t, int rows_per_tile) {
-    // groups of 8 tile columns swept top to bottom, column fastest: a group's weights stay in the L2
+__device__ __forceinline__ LayerTile decode_tile(const LayerParams& p, int unit, int rows_per_tile) {
+    // the units of a tile (K split) follow one another; tiles: groups of 8 tile columns swept top to bottom, column
+    // fastest, so that a group's weights stay in the L2
+    LayerTile c;
+    int t = unit, ks = 0;
+    if (p.split > 1) {
+        t = unit / p.split;
+        ks = unit - t * p.split;
+    }
     const int per_group = 8 * p.tiles_m;
     const int g = t / per_group;
     const int first = g * 8;
     const int gsize = min(8, p.tiles_n - first);
     const int r = t - g * per_group;
     const int tm = r / gsize;
-    LayerTile c;
     c.m0 = tm * rows_per_tile;
     c.n0 = (first + (r - tm * gsize)) * p.out_n;
+    c.kb0 = ks * p.kb_share;
+    c.kb1 = min(p.k_blocks, c.kb0 + p.kb_share);
+    c.plane = ks * p.plane_rows;
     return c;
 }
+__device__ __forceinline__ int layer_units(const LayerParams& p) { return p.tiles_m * p.tiles_n * max(p.split, 1); }
 
 __device__ __forceinline__ uint32_t slot_piece(uint32_t slot, int row, int piece) {
     return slot + static_cast<uint32_t>(row) * 128u + (static_cast<uint32_t>(piece ^ (row & 7)) << 4);
@@ -75,51 +87,65 @@ __device__ __forceinline__ void unpack2(uint32_t w, bool f16, float& lo, float& 
     }
 }
 
-// One row of a slot at a time between shared and global memory, element by element (any alignment).
+// A slot between shared and global memory, one row per instruction, element by element (any alignment): eight rows'
+// accesses at a time, so that a load's latency is paid once per eight rows.
 template <bool kWide>
 __device__ __forceinline__ void slot_rows_in(uint32_t slot, const void* src, long long ld, int row0, int col0, int M, int N, int lane) {
+    using Raw = std::conditional_t<kWide, uint32_t, uint16_t>;
+    constexpr int kHalves = kWide ? 1 : 2, kPer = kWide ? 4 : 8;
     const int rows = min(32, M - row0);
-    constexpr int kCols = kWide ? 32 : 64;
-    for (int r = 0; r < rows; ++r) {
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        Raw v[8][kHalves];
 #pragma unroll
-        for (int e = 0; e < kCols; e += 32) {
-            const int c = e + lane;
-            if (col0 + c < N) {
-                const long long i = static_cast<long long>(row0 + r) * ld + col0 + c;
-                if (kWide) {
-                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(slot_piece(slot, r, c >> 2) + (c & 3) * 4),
-                                 "r"(static_cast<const uint32_t*>(src)[i]) : "memory");
-                } else {
-                    asm volatile("st.shared.b16 [%0], %1;" ::"r"(slot_piece(slot, r, c >> 3) + (c & 7) * 2),
-                                 "h"(static_cast<const uint16_t*>(src)[i]) : "memory");
-                }
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int c = h * 32 + lane;
+                v[r][h] = r0 + r < rows && col0 + c < N ? static_cast<const Raw*>(src)[static_cast<long long>(row0 + r0 + r) * ld + col0 + c] : Raw(0);
             }
-        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int c = h * 32 + lane;
+                const uint32_t at = slot_piece(slot, r0 + r, c / kPer) + static_cast<uint32_t>(c % kPer) * static_cast<uint32_t>(sizeof(Raw));
+                if (kWide) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(static_cast<uint32_t>(v[r][h])) : "memory");
+                else asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(v[r][h])) : "memory");
+            }
     }
     __syncwarp();
 }
 template <bool kWide>
 __device__ __forceinline__ void slot_rows_out(uint32_t slot, void* dst, long long ld, int row0, int col0, int M, int N, int lane) {
+    using Raw = std::conditional_t<kWide, uint32_t, uint16_t>;
+    constexpr int kHalves = kWide ? 1 : 2, kPer = kWide ? 4 : 8;
     __syncwarp();
     const int rows = min(32, M - row0);
-    constexpr int kCols = kWide ? 32 : 64;
-    for (int r = 0; r < rows; ++r) {
+    for (int r0 = 0; r0 < rows; r0 += 8) {
+        Raw v[8][kHalves];
 #pragma unroll
-        for (int e = 0; e < kCols; e += 32) {
-            const int c = e + lane;
-            if (col0 + c < N) {
-                const long long i = static_cast<long long>(row0 + r) * ld + col0 + c;
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int c = h * 32 + lane;
+                const uint32_t at = slot_piece(slot, r0 + r, c / kPer) + static_cast<uint32_t>(c % kPer) * static_cast<uint32_t>(sizeof(Raw));
                 if (kWide) {
-                    uint32_t v;
-                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(slot_piece(slot, r, c >> 2) + (c & 3) * 4) : "memory");
-                    static_cast<uint32_t*>(dst)[i] = v;
+                    uint32_t x;
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+                    v[r][h] = static_cast<Raw>(x);
                 } else {
-                    uint16_t v;
-                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(slot_piece(slot, r, c >> 3) + (c & 7) * 2) : "memory");
-                    static_cast<uint16_t*>(dst)[i] = v;
+                    uint16_t x;
+                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at) : "memory");
+                    v[r][h] = static_cast<Raw>(x);
                 }
             }
-        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                const int c = h * 32 + lane;
+                if (r0 + r < rows && col0 + c < N) static_cast<Raw*>(dst)[static_cast<long long>(row0 + r0 + r) * ld + col0 + c] = v[r][h];
+            }
     }
     __syncwarp();
 }
@@ -189,6 +215,56 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
     }
 }
 
+// Partial sums as they are (32-bit words): slots of 32 accumulator columns to the unit's plane by TMA tile stores.
+// kSlots: slots of the warp's staging; kHalves: the accumulator holds two projections side by side.
+template <bool kPair, int kSlots, bool kHalves>
+__device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_slots, uint32_t bar_tfull, uint32_t bar_tempty,
+                                             volatile uint32_t* abort_flag, uint32_t tmem_base, int q, int lane, uint32_t cta_rank,
+                                             int first_unit, int unit_stride) {
+    constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
+    const bool leader = cta_rank == 0;
+    const int total_units = layer_units(p);
+    uint32_t slot_no = 0;
+    int t = 0;
+    for (int unit = first_unit; unit < total_units; unit += unit_stride, ++t) {
+        const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+        const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
+        const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
+        const int n_here = min(p.out_n, p.N - tc.n0);
+        if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, p.wait_budget_ns))) break;
+        tc_fence_after();
+        const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
+        for (int c0 = 0; c0 < p.block_n && row0 < p.M; c0 += 32) {
+            const bool second = kHalves && c0 >= p.out_n;
+            const int c = second ? c0 - p.out_n : c0;
+            if (c >= n_here) continue;
+            uint32_t v[32];
+            tmem_ld_32x32(t_row + c0, v);
+            if (elect_one()) tma_store_wait_read<kSlots - 1>();
+            __syncwarp();
+            tmem_ld_wait_for(v);
+            const uint32_t slot = my_slots + (slot_no % kSlots) * kSlot;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) st_shared_v4(slot_piece(slot, lane, j), &v[4 * j]);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (elect_one()) {
+                tma_store_2d(&p.tmap_c, slot, (second ? p.plane_second : 0) + tc.n0 + c, tc.plane + row0);
+                tma_store_commit();
+            }
+            ++slot_no;
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (kPair && !leader) mbar_arrive_remote(bar_tempty + 8u * acc, 0);
+            else mbar_arrive(bar_tempty + 8u * acc);
+        }
+    }
+    if (elect_one()) tma_store_wait<0>();
+    __syncwarp();
+}
+
 // The epilogue role of one warp (e = 0 .. kEpiWarps-1; q = the quarter of the TMEM lanes it may read).  Walks the same
 // tiles as the other roles; `slots`, `colvec` and `bar_in` are the shared-memory addresses of the slots, column
 // vectors and arrival barriers of all warps.
@@ -203,7 +279,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
     constexpr int kSlotStride = slot_stride(kOp);
     constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp);
     const bool leader = cta_rank == 0;
-    const int total_units = p.tiles_m * p.tiles_n;
+    const int total_units = layer_units(p);
     const uint64_t budget = p.wait_budget_ns;
     const uint32_t my_slots = slots + static_cast<uint32_t>(e) * kSlotBytesPerWarp;
     const uint32_t my_cols = colvec + static_cast<uint32_t>(e) * kColBytes;

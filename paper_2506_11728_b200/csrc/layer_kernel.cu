@@ -27,7 +27,8 @@ template <bool kPair, int kOp, bool kWide>
 __global__ void __launch_bounds__(kLayerThreads, 1)
 mip_layer_kernel(const __grid_constant__ LayerParams p) {
     constexpr int kGroup = kPair ? 2 : 1;
-    constexpr bool kGatedForm = kOp != kOpLinear;
+    constexpr bool kGatedForm = kOp == kOpGated || kOp == kOpGatedGrad || kOp == kOpRawGated;
+    constexpr bool kRaw = kOp == kOpRaw || kOp == kOpRawGated;
     constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
     constexpr int kBuffers = slot_count(kOp);
     constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp);
@@ -93,7 +94,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
     pdl_launch_dependents();
     pdl_wait();          // from here on global memory is touched
     const uint32_t tmem_base = *tmem_slot;
-    const int total_units = p.tiles_m * p.tiles_n;
+    const int total_units = layer_units(p);
     const uint64_t budget = p.wait_budget_ns;
     uint32_t issued = 0;
 
@@ -109,7 +110,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int m_cta = tc.m0 + static_cast<int>(cta_rank) * kBlockM;
             const int half = p.block_n >> 1;
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
+            for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
                 if (!mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 const uint32_t full_local = bar_full + 8u * s;
                 const uint32_t full = kPair ? mapa_u32(full_local, 0) : full_local;
@@ -141,11 +142,12 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
             bool ok = true;
             int t = 0;
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++t) {
+                const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
                 const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
                 if (!mbar_wait<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * p.block_n;
-                for (int kb = 0; kb < p.k_blocks; ++kb) {
+                for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
                     if (!mbar_wait(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a_addr = smem_base + s * stage_bytes;
@@ -156,7 +158,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
                     if (elect_one()) {
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k)
-                            mma_i8<kGroup>(d_tmem, a_desc + 2ull * k, b_desc + 2ull * k, p.idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                            mma_i8<kGroup>(d_tmem, a_desc + 2ull * k, b_desc + 2ull * k, p.idesc, (kb > tc.kb0 || k > 0) ? 1u : 0u);
                         if (kPair) {
                             mma_commit_pair(empty_local);
                             mma_commit_pair(empty_peer);
@@ -181,8 +183,12 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
             }
         }
     } else {
-        layer_epilogue<kPair, kOp, kWide>(p, slots, colvec, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3, lane,
-                                          cta_rank, first_unit, unit_stride);
+        if constexpr (kRaw)
+            raw_epilogue<kPair, kBuffers, kGatedForm>(p, slots + static_cast<uint32_t>(warp - 2) * kSlotBytesPerWarp, bar_tfull, bar_tempty,
+                                                      abort_flag, tmem_base, warp & 3, lane, cta_rank, first_unit, unit_stride);
+        else
+            layer_epilogue<kPair, kOp, kWide>(p, slots, colvec, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
+                                              lane, cta_rank, first_unit, unit_stride);
     }
 
     tc_fence_before();
@@ -241,7 +247,8 @@ int layer_fixed_smem(int op) { return kEpiWarps * (slot_bytes_per_warp(op) + kCo
 
 cudaError_t layer_init() {
     for (cudaError_t e : {init_op<false, kOpLinear>(), init_op<true, kOpLinear>(), init_op<false, kOpGated>(),
-                          init_op<true, kOpGated>(), init_op<false, kOpGatedGrad>(), init_op<true, kOpGatedGrad>()})
+                          init_op<true, kOpGated>(), init_op<false, kOpGatedGrad>(), init_op<true, kOpGatedGrad>(), init_t<false, kOpRaw, true>(),
+                          init_t<true, kOpRaw, true>(), init_t<false, kOpRawGated, true>(), init_t<true, kOpRawGated, true>()})
         if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
@@ -261,6 +268,8 @@ cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaS
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pair ? 2 : 1;
+    if (op == kOpRaw) return pair ? launch_t<true, kOpRaw, true>(p, cfg) : launch_t<false, kOpRaw, true>(p, cfg);
+    if (op == kOpRawGated) return pair ? launch_t<true, kOpRawGated, true>(p, cfg) : launch_t<false, kOpRawGated, true>(p, cfg);
     const bool wide = p.type == kF32;
     switch (op * 4 + (pair ? 2 : 0) + (wide ? 1 : 0)) {
         case kOpLinear * 4 + 0: return launch_t<false, kOpLinear, false>(p, cfg);

@@ -49,7 +49,7 @@ __device__ __forceinline__ void scale_codes(uint32_t w, uint64_t ss, uint32_t& l
     }
 }
 
-template <bool kPair, bool kAMajorM, bool kWide>
+template <bool kPair, bool kAMajorM, bool kWide, bool kRaw>
 __global__ void __launch_bounds__(kProductThreads, 1)
 mip_product_kernel(const __grid_constant__ LayerParams p) {
     constexpr int kGroup = kPair ? 2 : 1;
@@ -118,7 +118,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     pdl_launch_dependents();
     pdl_wait();          // from here on global memory is touched
     const uint32_t tmem_base = *tmem_slot;
-    const int total_units = p.tiles_m * p.tiles_n;
+    const int total_units = layer_units(p);
     const uint64_t budget = p.wait_budget_ns;
     uint32_t issued = 0;       // stages whose copies this warp (0: A, 6: codes) has asked for
     uint32_t s = 0, phase = 0;
@@ -130,7 +130,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int m_cta = tc.m0 + static_cast<int>(cta_rank) * kBlockM;
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
+            for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
                 if (!mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 const uint32_t local = bar_a + 8u * s;
                 const uint32_t full = kPair ? mapa_u32(local, 0) : local;     // both CTAs' bytes complete on the leader's
@@ -159,7 +159,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int n_cta = tc.n0 + static_cast<int>(cta_rank) * kProductN;
-            for (int kb = 0; kb < p.k_blocks; ++kb) {
+            for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
                 if (!mbar_wait(bar_rawfree + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 if (elect_one()) {
                     mbar_arrive_expect_tx(bar_raw + 8u * s, kRawBytes);
@@ -190,11 +190,12 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
             bool ok = true;
             int t = 0;
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++t) {
+                const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
                 const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
                 if (!mbar_wait<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * p.block_n;
-                for (int kb = 0; kb < p.k_blocks; ++kb) {
+                for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
                     if (!mbar_wait(bar_a + 8u * s, phase, abort_flag, budget) ||
                         !mbar_wait<kPair>(bar_b + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
                     tc_fence_after();
@@ -208,7 +209,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
                     if (elect_one()) {
 #pragma unroll
                         for (uint32_t k = 0; k < kProductK / 16; ++k)
-                            mma_f16<kGroup>(d_tmem, a_desc + a_step * k, b_desc + b_step * k, p.idesc, (kb > 0 || k > 0) ? 1u : 0u);
+                            mma_f16<kGroup>(d_tmem, a_desc + a_step * k, b_desc + b_step * k, p.idesc, (kb > tc.kb0 || k > 0) ? 1u : 0u);
                         if (kPair) {
                             mma_commit_pair(empty_local);
                             mma_commit_pair(empty_peer);
@@ -243,8 +244,11 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         const uint32_t flip = static_cast<uint32_t>(j >> 2);
         const uint32_t block = kABytes + flip * (kBBytes / 2);
         const uint32_t piece = static_cast<uint32_t>(j & 3) * 2u;
-        const uint32_t my_units = first_unit < total_units ? static_cast<uint32_t>((total_units - first_unit + unit_stride - 1) / unit_stride) : 0u;
-        const uint32_t total = my_units * static_cast<uint32_t>(p.k_blocks);      // stages this CTA converts
+        uint32_t total = 0;                                        // stages this CTA converts
+        for (int unit = first_unit; unit < total_units; unit += unit_stride) {
+            const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+            total += static_cast<uint32_t>(tc.kb1 - tc.kb0);
+        }
         for (uint32_t it = static_cast<uint32_t>(cw >> 2); it < total; it += 2) {
             const uint32_t st = it % stages, ph = (it / stages) & 1u;
             const uint32_t stage = smem_base + st * kProductStage;
@@ -286,8 +290,13 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
             }
         }
     } else {
-        layer_epilogue<kPair, kOpProduct, kWide>(p, slots, 0, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3, lane,
-                                                 cta_rank, first_unit, unit_stride);
+        if constexpr (kRaw)
+            raw_epilogue<kPair, slot_count(kOpProduct), false>(p, slots + static_cast<uint32_t>(warp - 2) * slot_bytes_per_warp(kOpProduct),
+                                                               bar_tfull, bar_tempty, abort_flag, tmem_base, warp & 3, lane, cta_rank,
+                                                               first_unit, unit_stride);
+        else
+            layer_epilogue<kPair, kOpProduct, kWide>(p, slots, 0, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
+                                                     lane, cta_rank, first_unit, unit_stride);
     }
 
     tc_fence_before();
@@ -328,9 +337,22 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     if (threadIdx.x == 0 && *abort_flag != 0) atomicOr(p.status, 1u);
 }
 
-template <bool kPair, bool kAMajorM, bool kWide>
+template <bool kPair, bool kAMajorM, bool kWide, bool kRaw>
 cudaError_t product_init_t() {
-    return cudaFuncSetAttribute(mip_product_kernel<kPair, kAMajorM, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudget);
+    return cudaFuncSetAttribute(mip_product_kernel<kPair, kAMajorM, kWide, kRaw>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudget);
+}
+template <bool kPair, bool kAMajorM>
+cudaError_t product_init_form() {
+    for (cudaError_t e : {product_init_t<kPair, kAMajorM, false, false>(), product_init_t<kPair, kAMajorM, true, false>(),
+                          product_init_t<kPair, kAMajorM, true, true>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+template <bool kPair, bool kAMajorM>
+cudaError_t product_launch_form(const LayerParams& p, int raw, const cudaLaunchConfig_t& cfg) {
+    if (raw) return cudaLaunchKernelEx(&cfg, mip_product_kernel<kPair, kAMajorM, true, true>, p);
+    if (p.type == kF32) return cudaLaunchKernelEx(&cfg, mip_product_kernel<kPair, kAMajorM, true, false>, p);
+    return cudaLaunchKernelEx(&cfg, mip_product_kernel<kPair, kAMajorM, false, false>, p);
 }
 
 }  // namespace
@@ -338,14 +360,13 @@ cudaError_t product_init_t() {
 int product_stages() { return (kSmemBudget - kProductFixed) / static_cast<int>(kProductStage + kScaleBytes); }
 
 cudaError_t product_init() {
-    for (cudaError_t e : {product_init_t<false, false, false>(), product_init_t<false, false, true>(), product_init_t<false, true, false>(),
-                          product_init_t<false, true, true>(), product_init_t<true, false, false>(), product_init_t<true, false, true>(),
-                          product_init_t<true, true, false>(), product_init_t<true, true, true>()})
+    for (cudaError_t e : {product_init_form<false, false>(), product_init_form<false, true>(), product_init_form<true, false>(),
+                          product_init_form<true, true>()})
         if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
 
-cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int grid, cudaStream_t stream) {
+cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int raw, int grid, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(kProductThreads, 1, 1);
@@ -360,16 +381,8 @@ cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int grid
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pair ? 2 : 1;
-    switch ((pair ? 4 : 0) + (a_order ? 2 : 0) + (p.type == kF32 ? 1 : 0)) {
-        case 0: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, false, false>, p);
-        case 1: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, false, true>, p);
-        case 2: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, true, false>, p);
-        case 3: return cudaLaunchKernelEx(&cfg, mip_product_kernel<false, true, true>, p);
-        case 4: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, false, false>, p);
-        case 5: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, false, true>, p);
-        case 6: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, true, false>, p);
-        default: return cudaLaunchKernelEx(&cfg, mip_product_kernel<true, true, true>, p);
-    }
+    if (pair) return a_order ? product_launch_form<true, true>(p, raw, cfg) : product_launch_form<true, false>(p, raw, cfg);
+    return a_order ? product_launch_form<false, true>(p, raw, cfg) : product_launch_form<false, false>(p, raw, cfg);
 }
 
 }  // namespace mip
