@@ -1,6 +1,6 @@
 // Epilogue shared by the tensor-core kernels of the 8-bit layer: accumulators in tensor memory -> outputs.
 //
-// Four warps, thread = row.  A slot is 128 bytes of 32 output rows (64 columns of a 16-bit type, 32 of float32): the
+// Thread = row.  A slot is 128 bytes of 32 output rows (64 columns of a 16-bit type, 32 of float32): the
 // warp's own swizzled staging buffer.  A matrix that is read (residual, gradient of the output, the sum to add to)
 // arrives in the slot by a TMA tile load asked for before the accumulator is ready, is combined in registers, and
 // the result goes back to the same 16 bytes, from where a TMA tile store takes it: every global access is whole
@@ -18,14 +18,17 @@ namespace mip {
 
 namespace {
 
-constexpr int kEpiWarps = 4;
 constexpr int kSlot = 4096;                         // 32 rows x 128 bytes
 constexpr int kColBytes = 2 * 64 * 4;               // per warp: two vectors of a slot's columns
-// Slots per warp.  Linear: the four slots of a 256-column tile of a 16-bit type, so that all of its residual can be
-// on its way before the accumulator is ready; gated: nothing comes in, two suffice to store one while the next is
-// computed; gradient: two, each of two buffers (one per result; the incoming gradient lies in the first); product: one
-// (its pipeline stages need the room, and its main loops are long).
-constexpr int slot_count(int op) { return op == kOpLinear || op == kOpRaw ? 4 : (op == kOpProduct ? 1 : 2); }
+// Epilogue warps: one or two per quarter of the accumulator's lanes (two take the slots of a tile by turns; the gated
+// forms' exponentials and the 16-bit residual sums keep one warp per scheduler from hiding its own latencies).  The
+// product has none to spare: its conversion warps take the registers.
+constexpr int epi_warps(int op) { return op == kOpProduct ? 4 : 8; }
+// Slots per warp.  Linear: two, with both warps of a quarter the four slots of a 256-column tile of a 16-bit type, so
+// that all of its residual can be on its way before the accumulator is ready; gated forms: one, all a warp has of a
+// tile of 16-bit outputs (gradient: of two buffers, one per result; the incoming gradient lies in the first); product:
+// one (its pipeline stages need the room, and its main loops are long).
+constexpr int slot_count(int op) { return op == kOpLinear || op == kOpRaw ? 2 : 1; }
 constexpr int slot_stride(int op) { return op == kOpGatedGrad ? 2 * kSlot : kSlot; }
 constexpr int slot_bytes_per_warp(int op) { return slot_count(op) * slot_stride(op); }
 
@@ -85,6 +88,43 @@ __device__ __forceinline__ void unpack2(uint32_t w, bool f16, float& lo, float& 
         lo = __uint_as_float(w << 16);
         hi = __uint_as_float(w & 0xFFFF0000u);
     }
+}
+
+// Two binary32 values in a register pair, for the packed instructions.
+__device__ __forceinline__ uint64_t pack_f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack_f2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Two int32 sums as binary32, rounded to nearest even.  kByParts: without the conversion instruction, which shares its
+// quarter-rate unit with the exponential and the reciprocal: the upper half (biased by 2^15) and the lower half are put
+// behind the exponent of 2^23, both differences are exact, and one fused multiply-add rounds once, like the conversion.
+template <bool kByParts>
+__device__ __forceinline__ uint64_t ints_to_f2(uint32_t a, uint32_t b) {
+    if (!kByParts) return pack_f2(__int2float_rn(static_cast<int>(a)), __int2float_rn(static_cast<int>(b)));
+    constexpr uint32_t kExp = 0x4B000000u;
+    const uint64_t lo = pack_f2(__uint_as_float(__byte_perm(a, kExp, 0x7410)), __uint_as_float(__byte_perm(b, kExp, 0x7410)));
+    const uint64_t hi = pack_f2(__uint_as_float(__byte_perm(a ^ 0x80000000u, kExp, 0x7432)), __uint_as_float(__byte_perm(b ^ 0x80000000u, kExp, 0x7432)));
+    const uint64_t lo_exact = add_f2(lo, pack_f2(-8388608.0f, -8388608.0f));
+    const uint64_t hi_exact = add_f2(hi, pack_f2(-8421376.0f, -8421376.0f));       // 2^23 + 2^15
+    return fma_f2(hi_exact, pack_f2(65536.0f, 65536.0f), lo_exact);
 }
 
 // A slot between shared and global memory, one row per instruction, element by element (any alignment): eight rows'
@@ -157,6 +197,7 @@ template <int kOp, int kAct, bool kWide>
 __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uint32_t (&v1)[32], float as, uint32_t cols, uint32_t slot,
                                              uint32_t slot2, int row, int piece0, bool has_r, bool f16) {
     constexpr int kPer = kWide ? 4 : 8;             // columns per 16-byte piece
+    constexpr bool kMufu = kAct == kActGeluTanh || kAct == kActSilu || (kAct == kActGelu && kOp == kOpGatedGrad);
 #pragma unroll
     for (int g = 0; g < 32 / kPer; ++g) {
         float b0[kPer], b1[kPer], r[kPer], y[kPer], y2[kPer];
@@ -182,24 +223,30 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
 #pragma unroll
             for (int j = 0; j < kPer; ++j) r[j] = 0.0f;
         }
+        if constexpr (kOp == kOpProduct) {
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            if (kOp == kOpProduct) {
-                y[j] = __uint_as_float(v0[g * kPer + j]) + r[j];
-                continue;
-            }
-            const float z0 = __int2float_rn(static_cast<int>(v0[g * kPer + j])) * as * b0[j];
-            if (kOp == kOpLinear) {
-                y[j] = activation<kAct>(z0 + b1[j]) + r[j];
-            } else {
-                const float z1 = __int2float_rn(static_cast<int>(v1[g * kPer + j])) * as * b1[j];
-                if (kOp == kOpGated) {
-                    y[j] = activation<kAct>(z0) * z1;
-                } else {
-                    float value, slope;
-                    activation_slope<kAct>(z0, value, slope);
-                    y[j] = r[j] * z1 * slope;
-                    y2[j] = r[j] * value;
+            for (int j = 0; j < kPer; ++j) y[j] = __uint_as_float(v0[g * kPer + j]) + r[j];
+        } else {
+            // two columns at a time: (sum * row scale) * column scale
+            const uint64_t as2 = pack_f2(as, as);
+#pragma unroll
+            for (int j = 0; j < kPer; j += 2) {
+                float z0[2], z1[2];
+                unpack_f2(mul_f2(mul_f2(ints_to_f2<kMufu>(v0[g * kPer + j], v0[g * kPer + j + 1]), as2), pack_f2(b0[j], b0[j + 1])), z0[0], z0[1]);
+                if constexpr (kOp != kOpLinear)
+                    unpack_f2(mul_f2(mul_f2(ints_to_f2<kMufu>(v1[g * kPer + j], v1[g * kPer + j + 1]), as2), pack_f2(b1[j], b1[j + 1])), z1[0], z1[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (kOp == kOpLinear) {
+                        y[j + h] = activation<kAct>(z0[h] + b1[j + h]) + r[j + h];
+                    } else if (kOp == kOpGated) {
+                        y[j + h] = activation<kAct>(z0[h]) * z1[h];
+                    } else {
+                        float value, slope;
+                        activation_slope<kAct>(z0[h], value, slope);
+                        y[j + h] = r[j + h] * z1[h] * slope;
+                        y2[j + h] = r[j + h] * value;
+                    }
                 }
             }
         }
@@ -216,9 +263,10 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
 }
 
 // Partial sums as they are (32-bit words): slots of 32 accumulator columns to the unit's plane by TMA tile stores.
-// kSlots: slots of the warp's staging; kHalves: the accumulator holds two projections side by side.
-template <bool kPair, int kSlots, bool kHalves>
-__device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_slots, uint32_t bar_tfull, uint32_t bar_tempty,
+// kSlots: slots of the warp's staging; kHalves: the accumulator holds two projections side by side; kSubs warps take
+// the slots of a tile by turns, this one every kSubs-th from `sub`.
+template <bool kPair, int kSlots, bool kHalves, int kSubs>
+__device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_slots, int sub, uint32_t bar_tfull, uint32_t bar_tempty,
                                              volatile uint32_t* abort_flag, uint32_t tmem_base, int q, int lane, uint32_t cta_rank,
                                              int first_unit, int unit_stride) {
     constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
@@ -234,7 +282,7 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
         if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, p.wait_budget_ns))) break;
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
-        for (int c0 = 0; c0 < p.block_n && row0 < p.M; c0 += 32) {
+        for (int c0 = 32 * sub; c0 < p.block_n && row0 < p.M; c0 += 32 * kSubs) {
             const bool second = kHalves && c0 >= p.out_n;
             const int c = second ? c0 - p.out_n : c0;
             if (c >= n_here) continue;
@@ -265,7 +313,7 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
     __syncwarp();
 }
 
-// The epilogue role of one warp (e = 0 .. kEpiWarps-1; q = the quarter of the TMEM lanes it may read).  Walks the same
+// The epilogue role of one warp (e = 0 .. epi_warps(kOp)-1; q = the quarter of the TMEM lanes it may read).  Walks the same
 // tiles as the other roles; `slots`, `colvec` and `bar_in` are the shared-memory addresses of the slots, column
 // vectors and arrival barriers of all warps.
 template <bool kPair, int kOp, bool kWide>
@@ -278,6 +326,8 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
     constexpr int kBuffers = slot_count(kOp);
     constexpr int kSlotStride = slot_stride(kOp);
     constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp);
+    constexpr int kSubs = epi_warps(kOp) / 4;
+    const int sub = e >> 2;
     const bool leader = cta_rank == 0;
     const int total_units = layer_units(p);
     const uint64_t budget = p.wait_budget_ns;
@@ -295,7 +345,8 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
         const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
         const int n_here = min(p.out_n, p.N - tc.n0);
         const bool active = row0 < p.M;                        // (warp-uniform)
-        const int n_slots = active ? (n_here + kSlotCols - 1) / kSlotCols : 0;
+        const int n_slots = active ? ((n_here + kSlotCols - 1) / kSlotCols - sub + kSubs - 1) / kSubs : 0;     // this warp's
+        const auto slot_col = [&](int i) { return (sub + i * kSubs) * kSlotCols; };
         const int row = row0 + lane;
         float as = 1.0f;
         // the slots' first buffers: every store that still reads them has been issued by this warp
@@ -311,7 +362,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                     const uint32_t b = loads % kBuffers;
                     if (elect_one()) {
                         mbar_arrive_expect_tx(my_bar + 8u * b, kSlot);
-                        tma_load_2d(my_slots + b * kSlotStride, &p.tmap_r, my_bar + 8u * b, tc.n0 + asked * kSlotCols, row0);
+                        tma_load_2d(my_slots + b * kSlotStride, &p.tmap_r, my_bar + 8u * b, tc.n0 + slot_col(asked), row0);
                     }
                 }
             }
@@ -329,21 +380,21 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 else cv[2 * h + 1] = (in && p.bias) ? __ldg(p.bias + col) : 0.0f;
             }
         };
-        if (n_slots > 0) fetch_columns(0);
+        if (n_slots > 0) fetch_columns(slot_col(0));
         // (the lanes of a warp decide together: none may leave while others still expect it at a warp barrier)
         if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, budget))) break;
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
         const uint32_t t_up = t_row + static_cast<uint32_t>(p.block_n >> 1);
-        uint32_t va0[32], va1[32], vb0[32], vb1[32];
+        uint32_t va0[32], va1[32], vb0[32];
         auto load_acc = [&](uint32_t (&v0)[32], uint32_t (&v1)[32], int c0) {
             tmem_ld_32x32(t_row + c0, v0);
             if (kGatedForm) tmem_ld_32x32(t_up + c0, v1);
         };
         bool gave_up = false;
-        if (n_slots > 0) load_acc(va0, va1, 0);
+        if (!kGatedForm && n_slots > 0) load_acc(va0, va0, slot_col(0));
         for (int sl = 0; sl < n_slots; ++sl, ++slot_no) {
-            const int c0 = sl * kSlotCols;
+            const int c0 = slot_col(sl);
             const uint32_t b = slot_no % kBuffers;
             const uint32_t slot = my_slots + b * kSlotStride, slot2 = slot + kSlot;
             // the slot is free (its last store has been read) or holds the tile that was asked for
@@ -361,27 +412,38 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 }
                 __syncwarp();
             }
-            if (sl + 1 < n_slots) fetch_columns(c0 + kSlotCols);
+            if (sl + 1 < n_slots) fetch_columns(slot_col(sl + 1));
             if (r_tma && !__all_sync(~0u, mbar_wait(my_bar + 8u * b, (slot_no / kBuffers) & 1u, abort_flag, budget))) {
                 gave_up = true;
                 break;
             }
-            tmem_ld_wait_for(va0);
-            if (kGatedForm) tmem_ld_wait_for(va1);
-            const bool last = sl + 1 == n_slots;
-            if (!kWide) load_acc(vb0, vb1, c0 + 32);
-            with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
-                finish_chunk<kOp, decltype(act)::value, kWide>(va0, va1, as, my_cols, slot, slot2, lane, 0, has_r, f16);
-            });
-            if (kWide) {
-                if (!last) load_acc(va0, va1, c0 + 32);
-            } else {
-                tmem_ld_wait_for(vb0);
-                if (kGatedForm) tmem_ld_wait_for(vb1);
-                if (!last) load_acc(va0, va1, c0 + 64);
+            const auto finish = [&](const uint32_t (&v0)[32], const uint32_t (&v1)[32], int h) {
                 with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
-                    finish_chunk<kOp, decltype(act)::value, kWide>(vb0, vb1, as, my_cols + 128, slot, slot2, lane, 4, has_r, f16);
+                    finish_chunk<kOp, decltype(act)::value, kWide>(v0, v1, as, my_cols + h * 128, slot, slot2, lane, 4 * h, has_r, f16);
                 });
+            };
+            if constexpr (kGatedForm) {
+                // (two accumulators' columns in registers; the quarter's other warp covers the load's latency)
+#pragma unroll 1
+                for (int h = 0; h < kSlotCols / 32; ++h) {
+                    load_acc(va0, va1, c0 + 32 * h);
+                    tmem_ld_wait_for(va0);
+                    tmem_ld_wait_for(va1);
+                    finish(va0, va1, h);
+                }
+            } else {
+                // the next 32 columns travel while these are finished
+                const bool last = sl + 1 == n_slots;
+                tmem_ld_wait_for(va0);
+                if (!kWide) load_acc(vb0, vb0, c0 + 32);
+                finish(va0, va0, 0);
+                if (kWide) {
+                    if (!last) load_acc(va0, va0, slot_col(sl + 1));
+                } else {
+                    tmem_ld_wait_for(vb0);
+                    if (!last) load_acc(va0, va0, slot_col(sl + 1));
+                    finish(vb0, vb0, 1);
+                }
             }
             if (c_tma) {
                 fence_proxy_async_smem();
@@ -405,7 +467,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 const uint32_t nb = loads % kBuffers;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(my_bar + 8u * nb, kSlot);
-                    tma_load_2d(my_slots + nb * kSlotStride, &p.tmap_r, my_bar + 8u * nb, tc.n0 + asked * kSlotCols, row0);
+                    tma_load_2d(my_slots + nb * kSlotStride, &p.tmap_r, my_bar + 8u * nb, tc.n0 + slot_col(asked), row0);
                 }
                 ++asked;
                 ++loads;

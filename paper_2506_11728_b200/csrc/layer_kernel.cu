@@ -21,6 +21,7 @@ namespace mip {
 
 namespace {
 
+constexpr int kEpiWarps = epi_warps(kOpLinear);     // (the same for all of this kernel's operators)
 constexpr int kLayerThreads = 32 * (3 + kEpiWarps);
 
 template <bool kPair, int kOp, bool kWide>
@@ -184,8 +185,9 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
         }
     } else {
         if constexpr (kRaw)
-            raw_epilogue<kPair, kBuffers, kGatedForm>(p, slots + static_cast<uint32_t>(warp - 2) * kSlotBytesPerWarp, bar_tfull, bar_tempty,
-                                                      abort_flag, tmem_base, warp & 3, lane, cta_rank, first_unit, unit_stride);
+            raw_epilogue<kPair, kBuffers, kGatedForm, kEpiWarps / 4>(
+                p, slots + static_cast<uint32_t>(warp - 2) * kSlotBytesPerWarp, (warp - 2) >> 2, bar_tfull, bar_tempty, abort_flag,
+                tmem_base, warp & 3, lane, cta_rank, first_unit, unit_stride);
         else
             layer_epilogue<kPair, kOp, kWide>(p, slots, colvec, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
                                               lane, cta_rank, first_unit, unit_stride);

@@ -20,6 +20,7 @@ namespace mip {
 
 namespace {
 
+constexpr int kEpiWarps = epi_warps(kOpProduct);
 constexpr int kConvWarps = 8;
 constexpr int kFirstConvWarp = 3 + kEpiWarps;
 constexpr int kProductThreads = 32 * (kFirstConvWarp + kConvWarps);
@@ -291,8 +292,8 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         }
     } else {
         if constexpr (kRaw)
-            raw_epilogue<kPair, slot_count(kOpProduct), false>(p, slots + static_cast<uint32_t>(warp - 2) * slot_bytes_per_warp(kOpProduct),
-                                                               bar_tfull, bar_tempty, abort_flag, tmem_base, warp & 3, lane, cta_rank,
+            raw_epilogue<kPair, slot_count(kOpProduct), false, 1>(p, slots + static_cast<uint32_t>(warp - 2) * slot_bytes_per_warp(kOpProduct), 0,
+                                                                  bar_tfull, bar_tempty, abort_flag, tmem_base, warp & 3, lane, cta_rank,
                                                                first_unit, unit_stride);
         else
             layer_epilogue<kPair, kOpProduct, kWide>(p, slots, 0, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
