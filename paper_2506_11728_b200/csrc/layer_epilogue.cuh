@@ -197,48 +197,65 @@ template <int kOp, int kAct, bool kWide>
 __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uint32_t (&v1)[32], float as, uint32_t cols, uint32_t slot,
                                              uint32_t slot2, int row, int piece0, bool has_r, bool f16) {
     constexpr int kPer = kWide ? 4 : 8;             // columns per 16-byte piece
-    constexpr bool kMufu = kAct == kActGeluTanh || kAct == kActSilu || (kAct == kActGelu && kOp == kOpGatedGrad);
-#pragma unroll
-    for (int g = 0; g < 32 / kPer; ++g) {
-        float b0[kPer], b1[kPer], r[kPer], y[kPer], y2[kPer];
+    constexpr int kPieces = 32 / kPer;
+    struct Inputs {
+        float b0[kPer], b1[kPer];
+        uint32_t r[4];
+    };
+    const auto fetch = [&](int g) {
+        Inputs in;
         if constexpr (kOp != kOpProduct) {
 #pragma unroll
             for (int h = 0; h < kPer; h += 4) {
-                lds_f4(cols + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b0[h]));
-                lds_f4(cols + 256 + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(b1[h]));
+                lds_f4(cols + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(in.b0[h]));
+                lds_f4(cols + 256 + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(in.b1[h]));
             }
         }
-        const uint32_t at = slot_piece(slot, row, piece0 + g);
-        if (has_r) {
-            uint32_t w[4];
-            lds_v4(at, w);
-            if (kWide) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r[j] = __uint_as_float(w[j]);
+        if (kOp != kOpGated) {
+            if (has_r) {
+                lds_v4(slot_piece(slot, row, piece0 + g), in.r);
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) unpack2(w[j], f16, r[2 * j % kPer], r[(2 * j + 1) % kPer]);
+                for (int j = 0; j < 4; ++j) in.r[j] = 0u;
             }
-        } else {
+        }
+        return in;
+    };
+    // (the next piece's reads go out before this piece's writes: shared-memory accesses keep their order)
+    Inputs next = fetch(0);
+    const uint64_t as2 = pack_f2(as, as);
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) r[j] = 0.0f;
+    for (int g = 0; g < kPieces; ++g) {
+        const Inputs in = next;
+        if (g + 1 < kPieces) next = fetch(g + 1);
+        float r[kPer], y[kPer], y2[kPer];
+        if constexpr (kOp != kOpGated) {
+            if constexpr (kWide) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[j] = __uint_as_float(in.r[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) unpack2(in.r[j], f16, r[2 * j], r[2 * j + 1]);
+            }
         }
         if constexpr (kOp == kOpProduct) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j) y[j] = __uint_as_float(v0[g * kPer + j]) + r[j];
         } else {
             // two columns at a time: (sum * row scale) * column scale
-            const uint64_t as2 = pack_f2(as, as);
 #pragma unroll
             for (int j = 0; j < kPer; j += 2) {
                 float z0[2], z1[2];
-                unpack_f2(mul_f2(mul_f2(ints_to_f2<kMufu>(v0[g * kPer + j], v0[g * kPer + j + 1]), as2), pack_f2(b0[j], b0[j + 1])), z0[0], z0[1]);
+                constexpr bool kByParts = kAct >= kActGelu;        // the activation keeps the quarter-rate unit busy
+                unpack_f2(mul_f2(mul_f2(ints_to_f2<kByParts>(v0[g * kPer + j], v0[g * kPer + j + 1]), as2), pack_f2(in.b0[j], in.b0[j + 1])),
+                          z0[0], z0[1]);
                 if constexpr (kOp != kOpLinear)
-                    unpack_f2(mul_f2(mul_f2(ints_to_f2<kMufu>(v1[g * kPer + j], v1[g * kPer + j + 1]), as2), pack_f2(b1[j], b1[j + 1])), z1[0], z1[1]);
+                    unpack_f2(mul_f2(mul_f2(ints_to_f2<kByParts>(v1[g * kPer + j], v1[g * kPer + j + 1]), as2), pack_f2(in.b1[j], in.b1[j + 1])),
+                              z1[0], z1[1]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     if (kOp == kOpLinear) {
-                        y[j + h] = activation<kAct>(z0[h] + b1[j + h]) + r[j + h];
+                        y[j + h] = activation<kAct>(z0[h] + in.b1[j + h]) + r[j + h];
                     } else if (kOp == kOpGated) {
                         y[j + h] = activation<kAct>(z0[h]) * z1[h];
                     } else {
@@ -253,7 +270,7 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
         uint32_t o[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y[j]) : pack2(y[2 * j % kPer], y[(2 * j + 1) % kPer], f16);
-        st_shared_v4(at, o);
+        st_shared_v4(slot_piece(slot, row, piece0 + g), o);
         if (kOp == kOpGatedGrad) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y2[j]) : pack2(y2[2 * j % kPer], y2[(2 * j + 1) % kPer], f16);
@@ -338,22 +355,49 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
     const bool has_r = p.R != nullptr;
     const bool r_tma = p.r_tma != 0, c_tma = p.c_tma != 0;
     uint32_t loads = 0, slot_no = 0;                           // tile loads asked for, slots finished
+    // slots of a tile this warp finishes, and the column of its i-th
+    const auto slots_of = [&](const LayerTile& c) {
+        const int n_here = min(p.out_n, p.N - c.n0);
+        const bool active = c.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32 < p.M;       // (warp-uniform)
+        return active ? ((n_here + kSlotCols - 1) / kSlotCols - sub + kSubs - 1) / kSubs : 0;
+    };
+    const auto slot_col = [&](int i) { return (sub + i * kSubs) * kSlotCols; };
+    // a tile's row scale and a slot's column vectors, one lane per row / column; asked for one slot or tile ahead
+    float cv[4], as = 1.0f;
+    const auto fetch_columns = [&](const LayerTile& c, int i) {
+        if (kOp == kOpProduct) return;
+#pragma unroll
+        for (int h = 0; h < kSlotCols / 32; ++h) {
+            const int col = c.n0 + slot_col(i) + h * 32 + lane;
+            const bool in = col < p.N;
+            cv[2 * h] = (in && p.b0_scale) ? __ldg(p.b0_scale + col) : 1.0f;
+            if (kGatedForm) cv[2 * h + 1] = (in && p.b1_scale) ? __ldg(p.b1_scale + col) : 1.0f;
+            else cv[2 * h + 1] = (in && p.bias) ? __ldg(p.bias + col) : 0.0f;
+        }
+    };
+    const auto fetch_row = [&](const LayerTile& c) {
+        const int row = c.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32 + lane;
+        return (kOp != kOpProduct && p.a_scale && row < p.M) ? __ldg(p.a_scale + row) : 1.0f;
+    };
+    LayerTile next = {};
+    if (first_unit < total_units) {
+        next = decode_tile(p, first_unit, kRowsPerTile);
+        as = fetch_row(next);
+        fetch_columns(next, 0);
+    }
     int t = 0;
     for (int unit = first_unit; unit < total_units; unit += unit_stride, ++t) {
-        const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+        const LayerTile tc = next;
+        const bool more = unit + unit_stride < total_units;
+        if (more) next = decode_tile(p, unit + unit_stride, kRowsPerTile);
         const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
         const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
-        const int n_here = min(p.out_n, p.N - tc.n0);
-        const bool active = row0 < p.M;                        // (warp-uniform)
-        const int n_slots = active ? ((n_here + kSlotCols - 1) / kSlotCols - sub + kSubs - 1) / kSubs : 0;     // this warp's
-        const auto slot_col = [&](int i) { return (sub + i * kSubs) * kSlotCols; };
-        const int row = row0 + lane;
-        float as = 1.0f;
+        const int n_slots = slots_of(tc);
+        const float as_here = as;
         // the slots' first buffers: every store that still reads them has been issued by this warp
         int asked = 0;                                         // of this tile
-        if (active) {
-            if (p.a_scale && row < p.M) as = __ldg(p.a_scale + row);
-            if (r_tma) {
+        if (r_tma) {
+            if (n_slots > 0) {
                 if (elect_one()) tma_store_wait_read<0>();
                 __syncwarp();
                 fence_proxy_async_smem();
@@ -366,21 +410,18 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                     }
                 }
             }
+            // the L2 is asked for what the next tile will read: its loads cannot start before this tile's stores have
+            // left their buffers
+            const int ahead = more ? slots_of(next) : 0;
+            if (elect_one())
+                for (int i = 0; i < ahead; ++i)
+                    tma_prefetch_l2_2d(&p.tmap_r, next.n0 + slot_col(i), next.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32);
+            __syncwarp();
         }
-        // one lane per column: scales and bias of the first slot
-        float cv[4];
-        auto fetch_columns = [&](int c0) {
-            if (kOp == kOpProduct) return;
-#pragma unroll
-            for (int h = 0; h < kSlotCols / 32; ++h) {
-                const int col = tc.n0 + c0 + h * 32 + lane;
-                const bool in = col < p.N;
-                cv[2 * h] = (in && p.b0_scale) ? __ldg(p.b0_scale + col) : 1.0f;
-                if (kGatedForm) cv[2 * h + 1] = (in && p.b1_scale) ? __ldg(p.b1_scale + col) : 1.0f;
-                else cv[2 * h + 1] = (in && p.bias) ? __ldg(p.bias + col) : 0.0f;
-            }
-        };
-        if (n_slots > 0) fetch_columns(slot_col(0));
+        if (n_slots == 0 && more) {
+            as = fetch_row(next);
+            fetch_columns(next, 0);
+        }
         // (the lanes of a warp decide together: none may leave while others still expect it at a warp barrier)
         if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, budget))) break;
         tc_fence_after();
@@ -412,14 +453,19 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 }
                 __syncwarp();
             }
-            if (sl + 1 < n_slots) fetch_columns(slot_col(sl + 1));
+            if (sl + 1 < n_slots) {
+                fetch_columns(tc, sl + 1);
+            } else if (more) {
+                as = fetch_row(next);
+                fetch_columns(next, 0);
+            }
             if (r_tma && !__all_sync(~0u, mbar_wait(my_bar + 8u * b, (slot_no / kBuffers) & 1u, abort_flag, budget))) {
                 gave_up = true;
                 break;
             }
             const auto finish = [&](const uint32_t (&v0)[32], const uint32_t (&v1)[32], int h) {
                 with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
-                    finish_chunk<kOp, decltype(act)::value, kWide>(v0, v1, as, my_cols + h * 128, slot, slot2, lane, 4 * h, has_r, f16);
+                    finish_chunk<kOp, decltype(act)::value, kWide>(v0, v1, as_here, my_cols + h * 128, slot, slot2, lane, 4 * h, has_r, f16);
                 });
             };
             if constexpr (kGatedForm) {

@@ -13,19 +13,53 @@ namespace mip {
 constexpr int kF32 = 0, kF16 = 1, kBF16 = 2;
 constexpr int kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4;
 
-// 1 / (1 + e^-x).  The fast exponential is off by 2 + |1.16 x| units in the last place, at most 1e-5
-// relative where the result is above 1e-35; e^-x = infinity gives the limit 0.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
+// The hardware's 2^x and 1/x without the steps that keep subnormal numbers: one instruction each, 2 units in the last
+// place and 1.  (The library forms of the exponential and the quotient are four to six: half of an epilogue's time.)
+__device__ __forceinline__ float fast_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+constexpr float kLog2E = 1.4426950408889634f;
+
+// 1 / (1 + e^-x): the rounded product x log2(e) puts 0.7 |x| units in the last place into the exponential, at most
+// 1e-5 relative where the result is above 1e-35; e^-x = infinity gives the limit 0.
+__device__ __forceinline__ float sigmoid(float x) { return fast_rcp(1.0f + fast_exp2(-kLog2E * x)); }
 
 // 2 sqrt(2/pi) (x + 0.044715 x^3): tanh(y/2) = 2 sigmoid(y) - 1 turns the tanh form of the Gaussian
 // error unit, x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2, into x sigmoid(gelu_inner(x)).
 constexpr float kGeluC = 1.5957691216057308f, kGeluC3 = 0.044715f;
 __device__ __forceinline__ float gelu_inner(float x) { return kGeluC * x * (1.0f + kGeluC3 * x * x); }
 
+// The normal distribution's integral Phi(x) = (1 + erf(x / sqrt 2)) / 2 and e^(-x^2 / 2), which its density shares.
+// Abramowitz and Stegun 7.1.26: 1 - erf(y) = (a1 t + ... + a5 t^5) e^(-y^2), t = 1 / (1 + p y), y >= 0, within 1.5e-7;
+// for x < 0 the complement is the answer itself, so small values keep their relative size.  No branch, one exponential
+// and one reciprocal (erff: two polynomials by case and its own exponential, twice the time of a whole epilogue).
+__device__ __forceinline__ float normal_cdf(float x, float& gauss) {
+    const float y = fabsf(x) * 0.70710678118654752f;
+    gauss = fast_exp2((-0.5f * kLog2E) * x * x);
+    const float t = fast_rcp(1.0f + 0.3275911f * y);
+    float q = 1.061405429f;
+    q = q * t - 1.453152027f;
+    q = q * t + 1.421413741f;
+    q = q * t - 0.284496736f;
+    q = q * t + 0.254829592f;
+    const float tail = 0.5f * q * t * gauss;
+    return x < 0.0f ? tail : 1.0f - tail;
+}
+
 template <int kAct>
 __device__ __forceinline__ float activation(float x) {
     if (kAct == kActRelu) return x < 0.0f ? 0.0f : x;           // (NaN stays NaN)
-    if (kAct == kActGelu) return 0.5f * x * (1.0f + erff(x * 0.70710678118654752f));
+    if (kAct == kActGelu) {
+        float gauss;
+        return x * normal_cdf(x, gauss);
+    }
     if (kAct == kActGeluTanh) return x * sigmoid(gelu_inner(x));
     if (kAct == kActSilu) return x * sigmoid(x);
     return x;
@@ -38,9 +72,10 @@ __device__ __forceinline__ void activation_slope(float x, float& value, float& s
         value = x < 0.0f ? 0.0f : x;
         slope = x > 0.0f ? 1.0f : 0.0f;                         // (0 at 0)
     } else if (kAct == kActGelu) {
-        const float cdf = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+        float gauss;
+        const float cdf = normal_cdf(x, gauss);
         value = x * cdf;
-        slope = cdf + x * 0.3989422804014327f * __expf(-0.5f * x * x);
+        slope = cdf + x * 0.3989422804014327f * gauss;
     } else if (kAct == kActGeluTanh) {
         const float e = sigmoid(gelu_inner(x));
         value = x * e;
