@@ -1270,17 +1270,17 @@ int rows_impl(bool quantize, int type, int64_t M, int64_t N, void* X, int64_t ld
     return MIPGEMM_OK;
 }
 
-// A row-major matrix of the call's type as the layer kernel's epilogue reads and writes it: boxes of 128 bytes x 32
-// rows, 128-byte swizzle.
+// A row-major matrix of the call's type as the layer kernel's epilogue reads and writes it: boxes of 32 columns x 32
+// rows, swizzled over the box's row.
 int encode_slots(CUtensorMap* map, const void* base, int type, long long M, long long N, long long ld) {
     const cuuint64_t size = type_size(type);
     cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(M)};
     cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld) * size};
-    cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / size), 32};
+    cuuint32_t box[2] = {32, 32};
     cuuint32_t estr[2] = {1, 1};
     const CUresult r = g_encode_tiled(map, size == 4 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2,
                                       const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                                      size == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         tl_last_cuda_error = 100000 + static_cast<int>(r);
@@ -1300,10 +1300,8 @@ struct LayerPlan {
 // (plan_cost_us); a tile's epilogue runs beside the next tile's main loop, the last one is exposed.
 LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
     const bool gated = a.op != kOpLinear;
-    const bool wide = a.type == MIPGEMM_TYPE_F32;
     const int k_blocks = static_cast<int>((a.K + 127) / 128);
-    // output columns come in whole 128-byte slots
-    const int step = gated ? (wide ? 64 : 128) : 64;
+    const int step = 64;                 // output columns come in whole slots of 32
     const Tuning tun = tuning_now();
     LayerPlan best{0, step, 1, 0, 1, 0};
     double best_clk = 1e30;
@@ -1454,7 +1452,9 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
             const int b_rows = pl.pair ? pl.block_n / 2 : pl.block_n;
             p.tiles_m = static_cast<int>((a.M + rows - 1) / rows);
             p.tiles_n = static_cast<int>((a.N + p.out_n - 1) / p.out_n);
-            p.stages = std::min(kMaxStages, (kSmemBudget - layer_fixed_smem(a.op)) / ((kBlockM + b_rows) * 128));
+            const bool wide = a.type == MIPGEMM_TYPE_F32;
+            const int fixed = pl.split > 1 ? layer_fixed_smem(gated ? kOpRawGated : kOpRaw, true) : layer_fixed_smem(a.op, wide);
+            p.stages = std::min(kMaxStages, (kSmemBudget - fixed) / ((kBlockM + b_rows) * 128));
             if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
             p.idesc = (2u << 4) | ((a.a_unsigned ? 0u : 1u) << 7) | (1u << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
                       (static_cast<uint32_t>(rows >> 4) << 24);

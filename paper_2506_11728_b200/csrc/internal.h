@@ -202,7 +202,7 @@ cudaError_t launch_layer_finish(const LayerArgs& a, const PartialPlanes& s, cuda
 struct alignas(64) LayerParams {
     CUtensorMap tmap_a;              // tiled {K, M} byte tensor
     CUtensorMap tmap_b0, tmap_b1;    // tiled {K, N} byte tensors (b1: gated forms)
-    CUtensorMap tmap_r;              // tiled {N, M} tensors of the call's type: boxes of 128 bytes x 32 rows
+    CUtensorMap tmap_r;              // tiled {N, M} tensors of the call's type: boxes of 32 columns x 32 rows
     CUtensorMap tmap_c, tmap_c2;
     int type, act;
     int M, N, K;                     // N = output columns
@@ -233,7 +233,7 @@ constexpr int kStreamRows = 128;     // weight rows per CTA (gated forms: 64 of 
 int stream_smem(int tokens, int stages);
 cudaError_t stream_init();           // once per device
 cudaError_t launch_layer_stream(const LayerParams& p, int op, int grid, cudaStream_t stream);
-int layer_fixed_smem(int op);        // shared memory besides the pipeline stages
+int layer_fixed_smem(int op, bool wide);        // shared memory besides the pipeline stages
 cudaError_t layer_init();            // once per device
 cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaStream_t stream);
 

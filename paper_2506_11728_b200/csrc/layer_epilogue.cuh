@@ -1,14 +1,19 @@
 // Epilogue shared by the tensor-core kernels of the 8-bit layer: accumulators in tensor memory -> outputs.
 //
-// Thread = row.  A slot is 128 bytes of 32 output rows (64 columns of a 16-bit type, 32 of float32): the
-// warp's own swizzled staging buffer.  A matrix that is read (residual, gradient of the output, the sum to add to)
-// arrives in the slot by a TMA tile load asked for before the accumulator is ready, is combined in registers, and
-// the result goes back to the same 16 bytes, from where a TMA tile store takes it: every global access is whole
-// 128-byte lines, no warp waits for another, and reading a matrix in place is safe (each element is read before
-// the same warp writes it).  Matrices the TMA cannot address (16-byte alignment of base and pitch; for stores also
-// whole 16-byte pieces per row, because tile stores clip in those) go through the same slot with one row of
-// element accesses per instruction.  Scales and bias of a slot's columns are fetched one lane per column one slot
-// ahead and broadcast through shared memory.
+// Thread = row.  A slot is 32 output columns of 32 rows (64 bytes a row in a 16-bit type, 128 in float32): the warp's
+// own swizzled staging buffer.  A matrix that is read (residual, gradient of the output, the sum to add to) arrives in
+// the slot by a TMA tile load asked for before the accumulator is ready, is combined in registers, and the result
+// goes back to the same 16 bytes, from where a TMA tile store takes it: no global access is narrower than a row of the
+// slot, no warp waits for another, and reading a matrix in place is safe (each element is read before the same warp
+// writes it).  Matrices the TMA cannot address (16-byte alignment of base and pitch; for stores also whole 16-byte
+// pieces per row, because tile stores clip in those) go through the same slot with one row of element accesses per
+// instruction.  Scales and bias of a slot's columns are fetched one lane per column one slot ahead and broadcast
+// through shared memory.
+//
+// What bounds it.  An output of a gated or activated layer takes 25 to 30 instructions and two on the quarter-rate
+// unit; beside a short main loop that is the kernel's time, and what counts is how well the schedulers are fed: one
+// warp each issues every fifth clock or so, so 16-bit outputs have four epilogue warps per scheduler, which take the
+// slots of a tile by turns.
 #pragma once
 #include "internal.h"
 #include "layer_math.cuh"
@@ -18,19 +23,18 @@ namespace mip {
 
 namespace {
 
-constexpr int kSlot = 4096;                         // 32 rows x 128 bytes
-constexpr int kColBytes = 2 * 64 * 4;               // per warp: two vectors of a slot's columns
-// Epilogue warps: one or two per quarter of the accumulator's lanes (two take the slots of a tile by turns; the gated
-// forms' exponentials and the 16-bit residual sums keep one warp per scheduler from hiding its own latencies).  The
-// product has none to spare: its conversion warps take the registers.
-constexpr int epi_warps(int op) { return op == kOpProduct ? 4 : 8; }
-// Slots per warp.  Linear: two, with both warps of a quarter the four slots of a 256-column tile of a 16-bit type, so
-// that all of its residual can be on its way before the accumulator is ready; gated forms: one, all a warp has of a
-// tile of 16-bit outputs (gradient: of two buffers, one per result; the incoming gradient lies in the first); product:
-// one (its pipeline stages need the room, and its main loops are long).
+constexpr int kSlotCols = 32;
+constexpr int slot_bytes(bool wide) { return wide ? 4096 : 2048; }
+constexpr int kColBytes = 2 * kSlotCols * 4;        // per warp: two vectors of a slot's columns
+// Epilogue warps (a multiple of four: a warp reads one quarter of the accumulator's lanes).  float32 outputs need twice
+// the staging and half the instructions per byte; the product's conversion warps take the registers of more.
+constexpr int epi_warps(int op, bool wide) { return op == kOpProduct ? 4 : (wide ? 8 : 16); }
+// Slots per warp: what a warp has of a 256-column tile where there is something to wait for or nothing else to do
+// meanwhile; gated forms have half the output columns (gradient: two buffers per slot, one per result; the incoming
+// gradient lies in the first), the product's pipeline stages need the room.
 constexpr int slot_count(int op) { return op == kOpLinear || op == kOpRaw ? 2 : 1; }
-constexpr int slot_stride(int op) { return op == kOpGatedGrad ? 2 * kSlot : kSlot; }
-constexpr int slot_bytes_per_warp(int op) { return slot_count(op) * slot_stride(op); }
+constexpr int slot_stride(int op, bool wide) { return op == kOpGatedGrad ? 2 * slot_bytes(wide) : slot_bytes(wide); }
+constexpr int slot_bytes_per_warp(int op, bool wide) { return slot_count(op) * slot_stride(op, wide); }
 
 struct LayerTile {
     int m0, n0;
@@ -62,8 +66,11 @@ __device__ __forceinline__ LayerTile decode_tile(const LayerParams& p, int unit,
 }
 __device__ __forceinline__ int layer_units(const LayerParams& p) { return p.tiles_m * p.tiles_n * max(p.split, 1); }
 
+// Shared-memory address of 16 bytes of a slot's row, in the swizzle of a TMA box of 64- or 128-byte rows.
+template <bool kWide>
 __device__ __forceinline__ uint32_t slot_piece(uint32_t slot, int row, int piece) {
-    return slot + static_cast<uint32_t>(row) * 128u + (static_cast<uint32_t>(piece ^ (row & 7)) << 4);
+    if (kWide) return slot + static_cast<uint32_t>(row) * 128u + (static_cast<uint32_t>(piece ^ (row & 7)) << 4);
+    return slot + static_cast<uint32_t>(row) * 64u + (static_cast<uint32_t>(piece ^ ((row >> 1) & 3)) << 4);
 }
 __device__ __forceinline__ void lds_v4(uint32_t addr, uint32_t (&v)[4]) {
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
@@ -127,77 +134,68 @@ __device__ __forceinline__ uint64_t ints_to_f2(uint32_t a, uint32_t b) {
     return fma_f2(hi_exact, pack_f2(65536.0f, 65536.0f), lo_exact);
 }
 
-// A slot between shared and global memory, one row per instruction, element by element (any alignment): eight rows'
-// accesses at a time, so that a load's latency is paid once per eight rows.
+// A slot between shared and global memory, one row per instruction (lane = column), element by element: any alignment.
+// Eight rows' accesses at a time, so that a load's latency is paid once per eight rows.
+template <bool kWide>
+__device__ __forceinline__ uint32_t slot_element(uint32_t slot, int row, int col) {
+    constexpr int kPer = kWide ? 4 : 8;
+    return slot_piece<kWide>(slot, row, col / kPer) + static_cast<uint32_t>(col % kPer) * (kWide ? 4u : 2u);
+}
 template <bool kWide>
 __device__ __forceinline__ void slot_rows_in(uint32_t slot, const void* src, long long ld, int row0, int col0, int M, int N, int lane) {
     using Raw = std::conditional_t<kWide, uint32_t, uint16_t>;
-    constexpr int kHalves = kWide ? 1 : 2, kPer = kWide ? 4 : 8;
     const int rows = min(32, M - row0);
+    const Raw* at = static_cast<const Raw*>(src) + static_cast<long long>(row0) * ld + col0 + lane;
+    const bool in = col0 + lane < N;
     for (int r0 = 0; r0 < rows; r0 += 8) {
-        Raw v[8][kHalves];
+        Raw v[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int r = 0; r < 8; ++r) v[r] = in && r0 + r < rows ? at[static_cast<long long>(r0 + r) * ld] : Raw(0);
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const int c = h * 32 + lane;
-                v[r][h] = r0 + r < rows && col0 + c < N ? static_cast<const Raw*>(src)[static_cast<long long>(row0 + r0 + r) * ld + col0 + c] : Raw(0);
-            }
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const int c = h * 32 + lane;
-                const uint32_t at = slot_piece(slot, r0 + r, c / kPer) + static_cast<uint32_t>(c % kPer) * static_cast<uint32_t>(sizeof(Raw));
-                if (kWide) asm volatile("st.shared.b32 [%0], %1;" ::"r"(at), "r"(static_cast<uint32_t>(v[r][h])) : "memory");
-                else asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(v[r][h])) : "memory");
-            }
+        for (int r = 0; r < 8; ++r) {
+            if (kWide) asm volatile("st.shared.b32 [%0], %1;" ::"r"(slot_element<kWide>(slot, r0 + r, lane)), "r"(static_cast<uint32_t>(v[r])) : "memory");
+            else asm volatile("st.shared.b16 [%0], %1;" ::"r"(slot_element<kWide>(slot, r0 + r, lane)), "h"(static_cast<uint16_t>(v[r])) : "memory");
+        }
     }
     __syncwarp();
 }
 template <bool kWide>
 __device__ __forceinline__ void slot_rows_out(uint32_t slot, void* dst, long long ld, int row0, int col0, int M, int N, int lane) {
     using Raw = std::conditional_t<kWide, uint32_t, uint16_t>;
-    constexpr int kHalves = kWide ? 1 : 2, kPer = kWide ? 4 : 8;
     __syncwarp();
     const int rows = min(32, M - row0);
+    Raw* at = static_cast<Raw*>(dst) + static_cast<long long>(row0) * ld + col0 + lane;
+    const bool in = col0 + lane < N;
     for (int r0 = 0; r0 < rows; r0 += 8) {
-        Raw v[8][kHalves];
+        Raw v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            if (kWide) {
+                uint32_t x;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(slot_element<kWide>(slot, r0 + r, lane)) : "memory");
+                v[r] = static_cast<Raw>(x);
+            } else {
+                uint16_t x;
+                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(slot_element<kWide>(slot, r0 + r, lane)) : "memory");
+                v[r] = static_cast<Raw>(x);
+            }
+        }
 #pragma unroll
         for (int r = 0; r < 8; ++r)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const int c = h * 32 + lane;
-                const uint32_t at = slot_piece(slot, r0 + r, c / kPer) + static_cast<uint32_t>(c % kPer) * static_cast<uint32_t>(sizeof(Raw));
-                if (kWide) {
-                    uint32_t x;
-                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-                    v[r][h] = static_cast<Raw>(x);
-                } else {
-                    uint16_t x;
-                    asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at) : "memory");
-                    v[r][h] = static_cast<Raw>(x);
-                }
-            }
-#pragma unroll
-        for (int r = 0; r < 8; ++r)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const int c = h * 32 + lane;
-                if (r0 + r < rows && col0 + c < N) static_cast<Raw*>(dst)[static_cast<long long>(row0 + r0 + r) * ld + col0 + c] = v[r][h];
-            }
+            if (in && r0 + r < rows) at[static_cast<long long>(r0 + r) * ld] = v[r];
     }
     __syncwarp();
 }
 
-// 32 accumulator columns of one row: v0 (and, gated, v1) become outputs in the slot.  `piece0` is the first 16-byte
-// piece of the slot they fill, `cols` the shared-memory address of their first column's scale (second vector 256
-// bytes behind).  The slot's old contents are the residual / the gradient of the output.
-template <int kOp, int kAct, bool kWide>
-__device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uint32_t (&v1)[32], float as, uint32_t cols, uint32_t slot,
-                                             uint32_t slot2, int row, int piece0, bool has_r, bool f16) {
+// kN accumulator columns of one row: v0 (and, gated, v1) become outputs in the slot.  `col` is the first of them in the
+// slot, `cols` the shared-memory address of the slot's column vectors.  The slot's old contents are the residual / the
+// gradient of the output.
+template <int kOp, int kAct, bool kWide, int kN>
+__device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[kN], const uint32_t (&v1)[kN], float as, uint32_t cols, uint32_t slot,
+                                             uint32_t slot2, int row, int col, bool has_r, bool f16) {
     constexpr int kPer = kWide ? 4 : 8;             // columns per 16-byte piece
-    constexpr int kPieces = 32 / kPer;
+    constexpr int kPieces = kN / kPer;
+    const int piece0 = col / kPer;
     struct Inputs {
         float b0[kPer], b1[kPer];
         uint32_t r[4];
@@ -207,13 +205,13 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
         if constexpr (kOp != kOpProduct) {
 #pragma unroll
             for (int h = 0; h < kPer; h += 4) {
-                lds_f4(cols + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(in.b0[h]));
-                lds_f4(cols + 256 + (g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(in.b1[h]));
+                lds_f4(cols + (col + g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(in.b0[h]));
+                lds_f4(cols + kSlotCols * 4 + (col + g * kPer + h) * 4, reinterpret_cast<float (&)[4]>(in.b1[h]));
             }
         }
         if (kOp != kOpGated) {
             if (has_r) {
-                lds_v4(slot_piece(slot, row, piece0 + g), in.r);
+                lds_v4(slot_piece<kWide>(slot, row, piece0 + g), in.r);
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) in.r[j] = 0u;
@@ -221,13 +219,10 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
         }
         return in;
     };
-    // (the next piece's reads go out before this piece's writes: shared-memory accesses keep their order)
-    Inputs next = fetch(0);
     const uint64_t as2 = pack_f2(as, as);
 #pragma unroll
     for (int g = 0; g < kPieces; ++g) {
-        const Inputs in = next;
-        if (g + 1 < kPieces) next = fetch(g + 1);
+        const Inputs in = fetch(g);
         float r[kPer], y[kPer], y2[kPer];
         if constexpr (kOp != kOpGated) {
             if constexpr (kWide) {
@@ -270,18 +265,18 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[32], const uin
         uint32_t o[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y[j]) : pack2(y[2 * j % kPer], y[(2 * j + 1) % kPer], f16);
-        st_shared_v4(slot_piece(slot, row, piece0 + g), o);
+        st_shared_v4(slot_piece<kWide>(slot, row, piece0 + g), o);
         if (kOp == kOpGatedGrad) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y2[j]) : pack2(y2[2 * j % kPer], y2[(2 * j + 1) % kPer], f16);
-            st_shared_v4(slot_piece(slot2, row, piece0 + g), o);
+            st_shared_v4(slot_piece<kWide>(slot2, row, piece0 + g), o);
         }
     }
 }
 
-// Partial sums as they are (32-bit words): slots of 32 accumulator columns to the unit's plane by TMA tile stores.
-// kSlots: slots of the warp's staging; kHalves: the accumulator holds two projections side by side; kSubs warps take
-// the slots of a tile by turns, this one every kSubs-th from `sub`.
+// Partial sums as they are (32-bit words) to the unit's plane, by TMA tile stores.  kSlots: slots of the warp's staging;
+// kHalves: the accumulator holds two projections side by side; kSubs warps take the slots of a tile by turns, this one
+// every kSubs-th from `sub`.
 template <bool kPair, int kSlots, bool kHalves, int kSubs>
 __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_slots, int sub, uint32_t bar_tfull, uint32_t bar_tempty,
                                              volatile uint32_t* abort_flag, uint32_t tmem_base, int q, int lane, uint32_t cta_rank,
@@ -308,9 +303,9 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
             if (elect_one()) tma_store_wait_read<kSlots - 1>();
             __syncwarp();
             tmem_ld_wait_for(v);
-            const uint32_t slot = my_slots + (slot_no % kSlots) * kSlot;
+            const uint32_t slot = my_slots + (slot_no % kSlots) * slot_bytes(true);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) st_shared_v4(slot_piece(slot, lane, j), &v[4 * j]);
+            for (int j = 0; j < 8; ++j) st_shared_v4(slot_piece<true>(slot, lane, j), &v[4 * j]);
             fence_proxy_async_smem();
             __syncwarp();
             if (elect_one()) {
@@ -330,8 +325,8 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
     __syncwarp();
 }
 
-// The epilogue role of one warp (e = 0 .. epi_warps(kOp)-1; q = the quarter of the TMEM lanes it may read).  Walks the same
-// tiles as the other roles; `slots`, `colvec` and `bar_in` are the shared-memory addresses of the slots, column
+// The epilogue role of one warp (e = 0 .. epi_warps(kOp, kWide)-1; q = the quarter of the TMEM lanes it may read).  Walks
+// the same tiles as the other roles; `slots`, `colvec` and `bar_in` are the shared-memory addresses of the slots, column
 // vectors and arrival barriers of all warps.
 template <bool kPair, int kOp, bool kWide>
 __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t slots, uint32_t colvec, uint32_t bar_in, uint32_t bar_tfull,
@@ -339,11 +334,10 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                                                uint32_t cta_rank, int first_unit, int unit_stride) {
     constexpr bool kGatedForm = kOp == kOpGated || kOp == kOpGatedGrad;
     constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
-    constexpr int kSlotCols = kWide ? 32 : 64;
     constexpr int kBuffers = slot_count(kOp);
-    constexpr int kSlotStride = slot_stride(kOp);
-    constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp);
-    constexpr int kSubs = epi_warps(kOp) / 4;
+    constexpr int kSlotStride = slot_stride(kOp, kWide);
+    constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp, kWide);
+    constexpr int kSubs = epi_warps(kOp, kWide) / 4;
     const int sub = e >> 2;
     const bool leader = cta_rank == 0;
     const int total_units = layer_units(p);
@@ -363,17 +357,14 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
     };
     const auto slot_col = [&](int i) { return (sub + i * kSubs) * kSlotCols; };
     // a tile's row scale and a slot's column vectors, one lane per row / column; asked for one slot or tile ahead
-    float cv[4], as = 1.0f;
+    float cv0 = 1.0f, cv1 = 0.0f, as = 1.0f;
     const auto fetch_columns = [&](const LayerTile& c, int i) {
         if (kOp == kOpProduct) return;
-#pragma unroll
-        for (int h = 0; h < kSlotCols / 32; ++h) {
-            const int col = c.n0 + slot_col(i) + h * 32 + lane;
-            const bool in = col < p.N;
-            cv[2 * h] = (in && p.b0_scale) ? __ldg(p.b0_scale + col) : 1.0f;
-            if (kGatedForm) cv[2 * h + 1] = (in && p.b1_scale) ? __ldg(p.b1_scale + col) : 1.0f;
-            else cv[2 * h + 1] = (in && p.bias) ? __ldg(p.bias + col) : 0.0f;
-        }
+        const int col = c.n0 + slot_col(i) + lane;
+        const bool in = col < p.N;
+        cv0 = (in && p.b0_scale) ? __ldg(p.b0_scale + col) : 1.0f;
+        if (kGatedForm) cv1 = (in && p.b1_scale) ? __ldg(p.b1_scale + col) : 1.0f;
+        else cv1 = (in && p.bias) ? __ldg(p.bias + col) : 0.0f;
     };
     const auto fetch_row = [&](const LayerTile& c) {
         const int row = c.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32 + lane;
@@ -396,19 +387,22 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
         const float as_here = as;
         // the slots' first buffers: every store that still reads them has been issued by this warp
         int asked = 0;                                         // of this tile
+        const auto ask = [&] {
+            const uint32_t b = loads % kBuffers;
+            if (elect_one()) {
+                mbar_arrive_expect_tx(my_bar + 8u * b, slot_bytes(kWide));
+                tma_load_2d(my_slots + b * kSlotStride, &p.tmap_r, my_bar + 8u * b, tc.n0 + slot_col(asked), row0);
+            }
+            ++asked;
+            ++loads;
+        };
         if (r_tma) {
             if (n_slots > 0) {
                 if (elect_one()) tma_store_wait_read<0>();
                 __syncwarp();
                 fence_proxy_async_smem();
                 __syncwarp();
-                for (; asked < kBuffers && asked < n_slots; ++asked, ++loads) {
-                    const uint32_t b = loads % kBuffers;
-                    if (elect_one()) {
-                        mbar_arrive_expect_tx(my_bar + 8u * b, kSlot);
-                        tma_load_2d(my_slots + b * kSlotStride, &p.tmap_r, my_bar + 8u * b, tc.n0 + slot_col(asked), row0);
-                    }
-                }
+                while (asked < kBuffers && asked < n_slots) ask();
             }
             // the L2 is asked for what the next tile will read: its loads cannot start before this tile's stores have
             // left their buffers
@@ -427,17 +421,13 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
         const uint32_t t_up = t_row + static_cast<uint32_t>(p.block_n >> 1);
-        uint32_t va0[32], va1[32], vb0[32];
-        auto load_acc = [&](uint32_t (&v0)[32], uint32_t (&v1)[32], int c0) {
-            tmem_ld_32x32(t_row + c0, v0);
-            if (kGatedForm) tmem_ld_32x32(t_up + c0, v1);
-        };
         bool gave_up = false;
-        if (!kGatedForm && n_slots > 0) load_acc(va0, va0, slot_col(0));
         for (int sl = 0; sl < n_slots; ++sl, ++slot_no) {
             const int c0 = slot_col(sl);
             const uint32_t b = slot_no % kBuffers;
-            const uint32_t slot = my_slots + b * kSlotStride, slot2 = slot + kSlot;
+            const uint32_t slot = my_slots + b * kSlotStride, slot2 = slot + slot_bytes(kWide);
+            uint32_t v[kGatedForm ? 16 : 32], v1[16];
+            if constexpr (!kGatedForm) tmem_ld_32x32(t_row + c0, v);
             // the slot is free (its last store has been read) or holds the tile that was asked for
             if (!r_tma) {
                 if (c_tma && elect_one()) tma_store_wait_read<kBuffers - 1>();
@@ -446,11 +436,8 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
             }
             if (kOp != kOpProduct) {
                 __syncwarp();                                  // (the last slot's column vectors have been read)
-#pragma unroll
-                for (int h = 0; h < kSlotCols / 32; ++h) {
-                    sts_f32(my_cols + (h * 32 + lane) * 4, cv[2 * h]);
-                    sts_f32(my_cols + 256 + (h * 32 + lane) * 4, cv[2 * h + 1]);
-                }
+                sts_f32(my_cols + lane * 4, cv0);
+                sts_f32(my_cols + kSlotCols * 4 + lane * 4, cv1);
                 __syncwarp();
             }
             if (sl + 1 < n_slots) {
@@ -463,33 +450,22 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 gave_up = true;
                 break;
             }
-            const auto finish = [&](const uint32_t (&v0)[32], const uint32_t (&v1)[32], int h) {
-                with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
-                    finish_chunk<kOp, decltype(act)::value, kWide>(v0, v1, as_here, my_cols + h * 128, slot, slot2, lane, 4 * h, has_r, f16);
-                });
-            };
             if constexpr (kGatedForm) {
-                // (two accumulators' columns in registers; the quarter's other warp covers the load's latency)
+                // (16 columns of both projections at a time: registers for four epilogue warps per scheduler)
 #pragma unroll 1
-                for (int h = 0; h < kSlotCols / 32; ++h) {
-                    load_acc(va0, va1, c0 + 32 * h);
-                    tmem_ld_wait_for(va0);
-                    tmem_ld_wait_for(va1);
-                    finish(va0, va1, h);
+                for (int c = 0; c < kSlotCols; c += 16) {
+                    tmem_ld_32x16(t_row + c0 + c, v);
+                    tmem_ld_32x16(t_up + c0 + c, v1);
+                    tmem_ld_wait_for16(v, v1);
+                    with_activation(p.act, [&](auto act) {
+                        finish_chunk<kOp, decltype(act)::value, kWide, 16>(v, v1, as_here, my_cols, slot, slot2, lane, c, has_r, f16);
+                    });
                 }
             } else {
-                // the next 32 columns travel while these are finished
-                const bool last = sl + 1 == n_slots;
-                tmem_ld_wait_for(va0);
-                if (!kWide) load_acc(vb0, vb0, c0 + 32);
-                finish(va0, va0, 0);
-                if (kWide) {
-                    if (!last) load_acc(va0, va0, slot_col(sl + 1));
-                } else {
-                    tmem_ld_wait_for(vb0);
-                    if (!last) load_acc(va0, va0, slot_col(sl + 1));
-                    finish(vb0, vb0, 1);
-                }
+                tmem_ld_wait_for(v);
+                with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
+                    finish_chunk<kOp, decltype(act)::value, kWide, 32>(v, v, as_here, my_cols, slot, slot2, lane, 0, has_r, f16);
+                });
             }
             if (c_tma) {
                 fence_proxy_async_smem();
@@ -510,13 +486,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 __syncwarp();
                 fence_proxy_async_smem();
                 __syncwarp();
-                const uint32_t nb = loads % kBuffers;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(my_bar + 8u * nb, kSlot);
-                    tma_load_2d(my_slots + nb * kSlotStride, &p.tmap_r, my_bar + 8u * nb, tc.n0 + slot_col(asked), row0);
-                }
-                ++asked;
-                ++loads;
+                ask();
             }
         }
         if (gave_up) break;

@@ -21,18 +21,18 @@ namespace mip {
 
 namespace {
 
-constexpr int kEpiWarps = epi_warps(kOpLinear);     // (the same for all of this kernel's operators)
-constexpr int kLayerThreads = 32 * (3 + kEpiWarps);
+constexpr int layer_threads(int op, bool wide) { return 32 * (3 + epi_warps(op, wide)); }
 
 template <bool kPair, int kOp, bool kWide>
-__global__ void __launch_bounds__(kLayerThreads, 1)
+__global__ void __launch_bounds__(layer_threads(kOp, kWide), 1)
 mip_layer_kernel(const __grid_constant__ LayerParams p) {
     constexpr int kGroup = kPair ? 2 : 1;
     constexpr bool kGatedForm = kOp == kOpGated || kOp == kOpGatedGrad || kOp == kOpRawGated;
     constexpr bool kRaw = kOp == kOpRaw || kOp == kOpRawGated;
     constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
     constexpr int kBuffers = slot_count(kOp);
-    constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp);
+    constexpr int kEpiWarps = epi_warps(kOp, kWide);
+    constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp, kWide);
     const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
     const bool leader = cta_rank == 0;
     const int first_unit = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
@@ -245,7 +245,7 @@ cudaError_t init_op() {
 
 }  // namespace
 
-int layer_fixed_smem(int op) { return kEpiWarps * (slot_bytes_per_warp(op) + kColBytes) + kCtrlBytes + 1024; }
+int layer_fixed_smem(int op, bool wide) { return epi_warps(op, wide) * (slot_bytes_per_warp(op, wide) + kColBytes) + kCtrlBytes + 1024; }
 
 cudaError_t layer_init() {
     for (cudaError_t e : {init_op<false, kOpLinear>(), init_op<true, kOpLinear>(), init_op<false, kOpGated>(),
@@ -258,8 +258,9 @@ cudaError_t layer_init() {
 cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
-    cfg.blockDim = dim3(kLayerThreads, 1, 1);
-    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kBlockM + (pair ? p.block_n / 2 : p.block_n)) * 128 + layer_fixed_smem(op);
+    const bool wide = p.type == kF32 || op == kOpRaw || op == kOpRawGated;      // (partial sums are words)
+    cfg.blockDim = dim3(layer_threads(op, wide), 1, 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kBlockM + (pair ? p.block_n / 2 : p.block_n)) * 128 + layer_fixed_smem(op, wide);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -272,7 +273,6 @@ cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaS
     cfg.numAttrs = pair ? 2 : 1;
     if (op == kOpRaw) return pair ? launch_t<true, kOpRaw, true>(p, cfg) : launch_t<false, kOpRaw, true>(p, cfg);
     if (op == kOpRawGated) return pair ? launch_t<true, kOpRawGated, true>(p, cfg) : launch_t<false, kOpRawGated, true>(p, cfg);
-    const bool wide = p.type == kF32;
     switch (op * 4 + (pair ? 2 : 0) + (wide ? 1 : 0)) {
         case kOpLinear * 4 + 0: return launch_t<false, kOpLinear, false>(p, cfg);
         case kOpLinear * 4 + 1: return launch_t<false, kOpLinear, true>(p, cfg);

@@ -20,7 +20,7 @@ namespace mip {
 
 namespace {
 
-constexpr int kEpiWarps = epi_warps(kOpProduct);
+constexpr int kEpiWarps = epi_warps(kOpProduct, false);
 constexpr int kConvWarps = 8;
 constexpr int kFirstConvWarp = 3 + kEpiWarps;
 constexpr int kProductThreads = 32 * (kFirstConvWarp + kConvWarps);
@@ -29,7 +29,7 @@ constexpr uint32_t kBBytes = kProductN * kProductK * 2;        // 16 KB, two blo
 constexpr uint32_t kRawBytes = kProductN * kProductK;          // 8 KB
 constexpr uint32_t kProductStage = kABytes + kBBytes + kRawBytes;
 constexpr uint32_t kScaleBytes = kProductK * 4;                // the rows' scales, behind the stages
-constexpr int kProductFixed = kEpiWarps * slot_bytes_per_warp(kOpProduct) + kCtrlBytes + 1024;
+constexpr int kProductFixed = kEpiWarps * slot_bytes_per_warp(kOpProduct, true) + kCtrlBytes + 1024;
 
 // Four codes (the bytes of w) times s (twice, packed), rounded to bfloat16.  A byte with its sign bit flipped, put
 // behind the exponent of 2^23, is the float 2^23 + 128 + code: one byte permutation per code and one exact packed
@@ -66,7 +66,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     const uint32_t smem_base = raw_addr + pad;
     const uint32_t stages = static_cast<uint32_t>(p.stages);
     const uint32_t slots = smem_base + stages * kProductStage;
-    const uint32_t scales = slots + kEpiWarps * slot_bytes_per_warp(kOpProduct);
+    const uint32_t scales = slots + kEpiWarps * slot_bytes_per_warp(kOpProduct, true);
     const uint32_t ctrl = scales + stages * kScaleBytes;
     // control block, 8 bytes each: A has arrived | B is converted | A and B have been read | codes have arrived | codes
     // have been read (`stages` of each), accumulators full and empty, drain, arrivals in the slots
@@ -292,7 +292,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         }
     } else {
         if constexpr (kRaw)
-            raw_epilogue<kPair, slot_count(kOpProduct), false, 1>(p, slots + static_cast<uint32_t>(warp - 2) * slot_bytes_per_warp(kOpProduct), 0,
+            raw_epilogue<kPair, slot_count(kOpProduct), false, 1>(p, slots + static_cast<uint32_t>(warp - 2) * slot_bytes_per_warp(kOpProduct, true), 0,
                                                                   bar_tfull, bar_tempty, abort_flag, tmem_base, warp & 3, lane, cta_rank,
                                                                first_unit, unit_stride);
         else
