@@ -1296,12 +1296,24 @@ struct LayerPlan {
     int split, stages;                   // K is split over so many units (few-token kernel: CTAs of a cluster)
 };
 
+// Epilogue warps: 16 where they set the pace, i.e. 16-bit outputs behind a short K (K = 1024: linear 16384 x 4096 with an
+// activation 115 -> 98 us; K = 4096 and more: 8, whose staging leaves room for a stage more).
+int layer_epi_warps(const LayerArgs& a) { return a.type != MIPGEMM_TYPE_F32 && a.K <= 2048 ? 16 : 8; }
+int layer_stages(const LayerArgs& a, int pair, int block_n, bool raw) {
+    const int op = raw ? (a.op == kOpLinear ? kOpRaw : kOpRawGated) : a.op;
+    const int fixed = layer_fixed_smem(op, a.type == MIPGEMM_TYPE_F32, raw ? 8 : layer_epi_warps(a));
+    return std::min(kMaxStages, (kSmemBudget - fixed) / ((kBlockM + (pair ? block_n / 2 : block_n)) * 128));
+}
+
 // Tile shape of the dense layer kernel: the main loop's cost per k-block is that of the plain product's kernel
 // (plan_cost_us); a tile's epilogue runs beside the next tile's main loop, the last one is exposed.
 LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
     const bool gated = a.op != kOpLinear;
     const int k_blocks = static_cast<int>((a.K + 127) / 128);
     const int step = 64;                 // output columns come in whole slots of 32
+    const int warps = layer_epi_warps(a);
+    const long long size = type_size(a.type);
+    const bool unaligned = a.N * size % 16 != 0 || !aligned16(a.C, a.ldc * size) || (a.R && !aligned16(a.R, a.ldr * size));
     const Tuning tun = tuning_now();
     LayerPlan best{0, step, 1, 0, 1, 0};
     double best_clk = 1e30;
@@ -1315,8 +1327,14 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
             const long long rows = pair ? 2 * kBlockM : kBlockM;
             const long long tiles = ((a.M + rows - 1) / rows) * ((a.N + out_n - 1) / out_n);
             const long long slots = pair ? dev->pair_clusters : dev->sm_count;
-            const double kb_clk = pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn;
-            const double epi = bn / 32 * (a.op == kOpLinear ? 450.0 : 600.0);
+            const int stages = layer_stages(a, pair, bn, false);
+            if (stages < 2) continue;
+            // (a k-block cannot come faster than its copy's latency over the stages on their way)
+            const double kb_clk = std::max(pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn, 2000.0 / stages);
+            // the schedulers' time for the tile's outputs, and at least each warp's rounds of slots
+            const double rounds = (out_n / 32 + warps / 4 - 1) / (warps / 4);
+            const double per_col = a.op == kOpGatedGrad ? 42.0 : (gated ? 30.0 : (a.act >= MIPGEMM_ACT_GELU ? 27.0 : 14.0));
+            const double epi = std::max(out_n * per_col, rounds * (a.op == kOpGatedGrad ? 2600.0 : 1700.0)) * (unaligned ? 2.5 : 1.0);
             for (int split = 1; split <= kMaxSplit; ++split) {
                 // K in `split` shares whose partial sums a second kernel adds: only while there are more SMs than tiles
                 // (not in lent scratch: what a call may need of it stays what the queries say)
@@ -1452,9 +1470,8 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
             const int b_rows = pl.pair ? pl.block_n / 2 : pl.block_n;
             p.tiles_m = static_cast<int>((a.M + rows - 1) / rows);
             p.tiles_n = static_cast<int>((a.N + p.out_n - 1) / p.out_n);
-            const bool wide = a.type == MIPGEMM_TYPE_F32;
-            const int fixed = pl.split > 1 ? layer_fixed_smem(gated ? kOpRawGated : kOpRaw, true) : layer_fixed_smem(a.op, wide);
-            p.stages = std::min(kMaxStages, (kSmemBudget - fixed) / ((kBlockM + b_rows) * 128));
+            p.epi_warps = pl.split > 1 ? 8 : layer_epi_warps(a);
+            p.stages = layer_stages(a, pl.pair, pl.block_n, pl.split > 1);
             if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
             p.idesc = (2u << 4) | ((a.a_unsigned ? 0u : 1u) << 7) | (1u << 10) | (static_cast<uint32_t>(pl.block_n >> 3) << 17) |
                       (static_cast<uint32_t>(rows >> 4) << 24);
@@ -1572,14 +1589,19 @@ int layer_impl(const LayerArgs& a, void* stream_v) {
         if (o.rows && !aligned16(*o.ptr, *o.ld)) need += align256(static_cast<size_t>(o.rows) * pitch);
     int rc = scratch.reserve(need);
     if (rc != MIPGEMM_OK) return rc;
+    RepackPart parts[3];
+    int count = 0;
     for (const Operand& o : ops) {
         if (!o.rows || aligned16(*o.ptr, *o.ld)) continue;
         void* dst = scratch.take(static_cast<size_t>(o.rows) * pitch);
-        const cudaError_t e = launch_repack(*o.ptr, *o.ld, dst, pitch, o.rows, a.K, stream);
-        ++g_launches;
-        if (e != cudaSuccess) return cuda_fail(e);
+        parts[count++] = RepackPart{*o.ptr, *o.ld, dst, pitch, o.rows, a.K};
         *o.ptr = dst;
         *o.ld = pitch;
+    }
+    if (count) {
+        const cudaError_t e = launch_repack_parts(parts, count, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
     }
     rc = run_layer(use, dev, stream, need == 0);
     if (rc == MIPGEMM_OK && need) tl_last_path |= MIPGEMM_PATH_REPACK;
@@ -1762,23 +1784,26 @@ int product_impl(const ProductArgs& a, void* stream_v) {
     int rc = scratch.reserve((fix_a ? align256(static_cast<size_t>(a_rows) * round_up(a_cols, 16)) : 0) +
                              (fix_b ? align256(static_cast<size_t>(a.K) * round_up(a.N, 16)) : 0));
     if (rc != MIPGEMM_OK) return rc;
+    RepackPart parts[2];
+    int count = 0;
     if (fix_a) {
         const long long pitch = round_up(a_cols, 16);
         void* dst = scratch.take(static_cast<size_t>(a_rows) * pitch);
-        const cudaError_t e = launch_repack(a.A, 2 * a.lda, dst, pitch, a_rows, a_cols, stream);
-        ++g_launches;
-        if (e != cudaSuccess) return cuda_fail(e);
+        parts[count++] = RepackPart{a.A, 2 * a.lda, dst, pitch, a_rows, a_cols};
         use.A = dst;
         use.lda = pitch / 2;
     }
     if (fix_b) {
         const long long pitch = round_up(a.N, 16);
         void* dst = scratch.take(static_cast<size_t>(a.K) * pitch);
-        const cudaError_t e = launch_repack(a.B, a.ldb, dst, pitch, a.K, a.N, stream);
-        ++g_launches;
-        if (e != cudaSuccess) return cuda_fail(e);
+        parts[count++] = RepackPart{a.B, a.ldb, dst, pitch, a.K, a.N};
         use.B = static_cast<const int8_t*>(dst);
         use.ldb = pitch;
+    }
+    if (count) {
+        const cudaError_t e = launch_repack_parts(parts, count, stream);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_fail(e);
     }
     rc = run_product(use, dev, stream, !fix_a && !fix_b);
     if (rc == MIPGEMM_OK && (fix_a || fix_b)) tl_last_path |= MIPGEMM_PATH_REPACK;

@@ -64,6 +64,68 @@ cudaError_t launch_repack(const void* src, long long src_pitch, void* dst, long 
     return launch_repack2(src, src_pitch, dst, rows, nullptr, 0, nullptr, 0, dst_pitch, cols, stream);
 }
 
+// The same for the layer operators' operands: up to three matrices of their own shapes, block y = matrix.  A warp takes
+// 512 bytes of a row (16 per lane), so no index needs a division.
+struct RepackArgs {
+    RepackPart part[3];
+};
+__global__ void __launch_bounds__(256)
+mip_repack_parts_kernel(const RepackArgs a) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const RepackPart& p = a.part[blockIdx.y];
+    const int segments = static_cast<int>((p.cols + 511) / 512);
+    const long long warps = static_cast<long long>(gridDim.x) * 8;
+    const int lane = threadIdx.x & 31;
+    long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    // (row, segment) advance by a fixed step
+    long long r = w / segments;
+    int sgm = static_cast<int>(w - r * segments);
+    const long long dr = warps / segments;
+    const int ds = static_cast<int>(warps - dr * segments);
+    while (r < p.rows) {
+        const long long c = static_cast<long long>(sgm) * 512 + lane * 16;
+        if (c < p.cols) {
+            const int nvalid = static_cast<int>(min(16LL, p.cols - c));
+            const uint8_t* s = static_cast<const uint8_t*>(p.src) + r * p.src_pitch + c;
+            const unsigned off = static_cast<unsigned>(reinterpret_cast<uintptr_t>(s) & 3u);
+            const uint32_t* word = reinterpret_cast<const uint32_t*>(s - off);
+            const int nwords = (static_cast<int>(off) + nvalid + 3) >> 2;
+            uint32_t x[5];
+#pragma unroll
+            for (int j = 0; j < 5; ++j) x[j] = (j < nwords) ? __ldg(word + j) : 0u;
+            uint4 o;
+            o.x = __funnelshift_r(x[0], x[1], off * 8);
+            o.y = __funnelshift_r(x[1], x[2], off * 8);
+            o.z = __funnelshift_r(x[2], x[3], off * 8);
+            o.w = __funnelshift_r(x[3], x[4], off * 8);
+            *reinterpret_cast<uint4*>(static_cast<uint8_t*>(p.dst) + r * p.dst_pitch + c) = o;
+        }
+        r += dr;
+        sgm += ds;
+        if (sgm >= segments) { sgm -= segments; ++r; }
+    }
+}
+
+cudaError_t launch_repack_parts(const RepackPart* parts, int count, cudaStream_t stream) {
+    RepackArgs a = {};
+    long long most = 1;
+    for (int i = 0; i < count; ++i) {
+        a.part[i] = parts[i];
+        most = max(most, (parts[i].rows * ((parts[i].cols + 511) / 512) + 7) / 8);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(min(most, 148LL * 16)), static_cast<unsigned>(count));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, mip_repack_parts_kernel, a);
+}
+
 // ---------------------------------------------------------------- transposing repack
 // dst[i][k] = src[k*src_pitch + i] for i < rows_out, k < cols_out: turns an M- (or N-) contiguous
 // operand into the K-contiguous form the default path reads, through 32 x 32 byte tiles in shared

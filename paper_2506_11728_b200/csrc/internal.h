@@ -210,6 +210,7 @@ struct alignas(64) LayerParams {
     int block_n;                     // accumulator columns per tile
     int out_n;                       // output columns per tile: block_n, or half of it (gated forms)
     int stages, tiles_m, tiles_n;
+    int epi_warps;                   // 8 or 16
     int a_rows;                      // rows of A per tile copy: 128, or M where it is less
     uint32_t idesc, tmem_cols;
     int r_tma, c_tma;                // 1: R is read / C (and C2) written by TMA tile copies
@@ -233,7 +234,7 @@ constexpr int kStreamRows = 128;     // weight rows per CTA (gated forms: 64 of 
 int stream_smem(int tokens, int stages);
 cudaError_t stream_init();           // once per device
 cudaError_t launch_layer_stream(const LayerParams& p, int op, int grid, cudaStream_t stream);
-int layer_fixed_smem(int op, bool wide);        // shared memory besides the pipeline stages
+int layer_fixed_smem(int op, bool wide, int epi_warps);   // shared memory besides the pipeline stages
 cudaError_t layer_init();            // once per device
 cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaStream_t stream);
 
@@ -268,6 +269,13 @@ cudaError_t launch_repack(const void* src, long long src_pitch, void* dst, long 
 cudaError_t launch_repack2(const void* src0, long long src_pitch0, void* dst0, long long rows0, const void* src1,
                            long long src_pitch1, void* dst1, long long rows1, long long dst_pitch, long long cols,
                            cudaStream_t stream);
+// Up to three byte matrices of their own sizes to 16-byte aligned rows, in one launch.
+struct RepackPart {
+    const void* src; long long src_pitch;
+    void* dst; long long dst_pitch;      // (a multiple of 16)
+    long long rows, cols;
+};
+cudaError_t launch_repack_parts(const RepackPart* parts, int count, cudaStream_t stream);
 cudaError_t launch_transpose_repack(const void* src, long long src_pitch, void* dst, long long dst_pitch,
                                     long long rows_out, long long cols_out, cudaStream_t stream);
 // Weights [rows][R][seg] -> [rows][R][slot], zero padded (slot >= seg, slot % 16 == 0).

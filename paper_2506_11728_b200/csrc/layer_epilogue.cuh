@@ -12,8 +12,8 @@
 //
 // What bounds it.  An output of a gated or activated layer takes 25 to 30 instructions and two on the quarter-rate
 // unit; beside a short main loop that is the kernel's time, and what counts is how well the schedulers are fed: one
-// warp each issues every fifth clock or so, so 16-bit outputs have four epilogue warps per scheduler, which take the
-// slots of a tile by turns.
+// warp each issues every fifth clock or so, so there are two or four per scheduler, which take the slots of a tile by
+// turns.
 #pragma once
 #include "internal.h"
 #include "layer_math.cuh"
@@ -26,12 +26,14 @@ namespace {
 constexpr int kSlotCols = 32;
 constexpr int slot_bytes(bool wide) { return wide ? 4096 : 2048; }
 constexpr int kColBytes = 2 * kSlotCols * 4;        // per warp: two vectors of a slot's columns
-// Epilogue warps (a multiple of four: a warp reads one quarter of the accumulator's lanes).  float32 outputs need twice
-// the staging and half the instructions per byte; the product's conversion warps take the registers of more.
-constexpr int epi_warps(int op, bool wide) { return op == kOpProduct ? 4 : (wide ? 8 : 16); }
-// Slots per warp: what a warp has of a 256-column tile where there is something to wait for or nothing else to do
-// meanwhile; gated forms have half the output columns (gradient: two buffers per slot, one per result; the incoming
-// gradient lies in the first), the product's pipeline stages need the room.
+// Epilogue warps (a multiple of four: a warp reads one quarter of the accumulator's lanes): 8, or 16 for 16-bit outputs
+// behind a short K, where they set the pace.  Behind a long one their staging is better spent on pipeline stages.  (The
+// float32 forms' slots are twice as large; the product's conversion warps take the registers of more.)
+constexpr int kFewEpiWarps = 8, kManyEpiWarps = 16;
+constexpr int product_epi_warps(bool wide) { return wide ? 4 : 8; }
+// Slots per warp: two where there is something to wait for or nothing else to do meanwhile; gated forms have half the
+// output columns (gradient: two buffers per slot, one per result; the incoming gradient lies in the first), the
+// product's pipeline stages need the room.
 constexpr int slot_count(int op) { return op == kOpLinear || op == kOpRaw ? 2 : 1; }
 constexpr int slot_stride(int op, bool wide) { return op == kOpGatedGrad ? 2 * slot_bytes(wide) : slot_bytes(wide); }
 constexpr int slot_bytes_per_warp(int op, bool wide) { return slot_count(op) * slot_stride(op, wide); }
@@ -135,7 +137,7 @@ __device__ __forceinline__ uint64_t ints_to_f2(uint32_t a, uint32_t b) {
 }
 
 // A slot between shared and global memory, one row per instruction (lane = column), element by element: any alignment.
-// Eight rows' accesses at a time, so that a load's latency is paid once per eight rows.
+// Sixteen rows' accesses at a time, so that a load's latency is paid once per sixteen rows.
 template <bool kWide>
 __device__ __forceinline__ uint32_t slot_element(uint32_t slot, int row, int col) {
     constexpr int kPer = kWide ? 4 : 8;
@@ -147,12 +149,15 @@ __device__ __forceinline__ void slot_rows_in(uint32_t slot, const void* src, lon
     const int rows = min(32, M - row0);
     const Raw* at = static_cast<const Raw*>(src) + static_cast<long long>(row0) * ld + col0 + lane;
     const bool in = col0 + lane < N;
-    for (int r0 = 0; r0 < rows; r0 += 8) {
-        Raw v[8];
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+        Raw v[16];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = in && r0 + r < rows ? at[static_cast<long long>(r0 + r) * ld] : Raw(0);
+        for (int r = 0; r < 16; ++r) {
+            v[r] = Raw(0);
+            if (in && r0 + r < rows) v[r] = at[static_cast<long long>(r0 + r) * ld];
+        }
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < 16; ++r) {
             if (kWide) asm volatile("st.shared.b32 [%0], %1;" ::"r"(slot_element<kWide>(slot, r0 + r, lane)), "r"(static_cast<uint32_t>(v[r])) : "memory");
             else asm volatile("st.shared.b16 [%0], %1;" ::"r"(slot_element<kWide>(slot, r0 + r, lane)), "h"(static_cast<uint16_t>(v[r])) : "memory");
         }
@@ -166,10 +171,10 @@ __device__ __forceinline__ void slot_rows_out(uint32_t slot, void* dst, long lon
     const int rows = min(32, M - row0);
     Raw* at = static_cast<Raw*>(dst) + static_cast<long long>(row0) * ld + col0 + lane;
     const bool in = col0 + lane < N;
-    for (int r0 = 0; r0 < rows; r0 += 8) {
-        Raw v[8];
+    for (int r0 = 0; r0 < rows; r0 += 16) {
+        Raw v[16];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = 0; r < 16; ++r) {
             if (kWide) {
                 uint32_t x;
                 asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(slot_element<kWide>(slot, r0 + r, lane)) : "memory");
@@ -181,7 +186,7 @@ __device__ __forceinline__ void slot_rows_out(uint32_t slot, void* dst, long lon
             }
         }
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
+        for (int r = 0; r < 16; ++r)
             if (in && r0 + r < rows) at[static_cast<long long>(r0 + r) * ld] = v[r];
     }
     __syncwarp();
@@ -325,10 +330,10 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
     __syncwarp();
 }
 
-// The epilogue role of one warp (e = 0 .. epi_warps(kOp, kWide)-1; q = the quarter of the TMEM lanes it may read).  Walks
+// The epilogue role of one warp (e = 0 .. kWarps-1; q = the quarter of the TMEM lanes it may read).  Walks
 // the same tiles as the other roles; `slots`, `colvec` and `bar_in` are the shared-memory addresses of the slots, column
 // vectors and arrival barriers of all warps.
-template <bool kPair, int kOp, bool kWide>
+template <bool kPair, int kOp, bool kWide, int kWarps>
 __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t slots, uint32_t colvec, uint32_t bar_in, uint32_t bar_tfull,
                                                uint32_t bar_tempty, volatile uint32_t* abort_flag, uint32_t tmem_base, int e, int q, int lane,
                                                uint32_t cta_rank, int first_unit, int unit_stride) {
@@ -337,7 +342,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
     constexpr int kBuffers = slot_count(kOp);
     constexpr int kSlotStride = slot_stride(kOp, kWide);
     constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp, kWide);
-    constexpr int kSubs = epi_warps(kOp, kWide) / 4;
+    constexpr int kSubs = kWarps / 4;
     const int sub = e >> 2;
     const bool leader = cta_rank == 0;
     const int total_units = layer_units(p);

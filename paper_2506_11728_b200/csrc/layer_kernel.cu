@@ -21,17 +21,15 @@ namespace mip {
 
 namespace {
 
-constexpr int layer_threads(int op, bool wide) { return 32 * (3 + epi_warps(op, wide)); }
 
-template <bool kPair, int kOp, bool kWide>
-__global__ void __launch_bounds__(layer_threads(kOp, kWide), 1)
+template <bool kPair, int kOp, bool kWide, int kEpiWarps>
+__global__ void __launch_bounds__(32 * (3 + kEpiWarps), 1)
 mip_layer_kernel(const __grid_constant__ LayerParams p) {
     constexpr int kGroup = kPair ? 2 : 1;
     constexpr bool kGatedForm = kOp == kOpGated || kOp == kOpGatedGrad || kOp == kOpRawGated;
     constexpr bool kRaw = kOp == kOpRaw || kOp == kOpRawGated;
     constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
     constexpr int kBuffers = slot_count(kOp);
-    constexpr int kEpiWarps = epi_warps(kOp, kWide);
     constexpr int kSlotBytesPerWarp = slot_bytes_per_warp(kOp, kWide);
     const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
     const bool leader = cta_rank == 0;
@@ -189,7 +187,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
                 p, slots + static_cast<uint32_t>(warp - 2) * kSlotBytesPerWarp, (warp - 2) >> 2, bar_tfull, bar_tempty, abort_flag,
                 tmem_base, warp & 3, lane, cta_rank, first_unit, unit_stride);
         else
-            layer_epilogue<kPair, kOp, kWide>(p, slots, colvec, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
+            layer_epilogue<kPair, kOp, kWide, kEpiWarps>(p, slots, colvec, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
                                               lane, cta_rank, first_unit, unit_stride);
     }
 
@@ -229,28 +227,38 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
     if (threadIdx.x == 0 && *abort_flag != 0) atomicOr(p.status, 1u);
 }
 
-template <bool kPair, int kOp, bool kWide>
+template <bool kPair, int kOp, bool kWide, int kEpiWarps>
 cudaError_t launch_t(const LayerParams& p, const cudaLaunchConfig_t& cfg) {
-    return cudaLaunchKernelEx(&cfg, mip_layer_kernel<kPair, kOp, kWide>, p);
+    return cudaLaunchKernelEx(&cfg, mip_layer_kernel<kPair, kOp, kWide, kEpiWarps>, p);
 }
-template <bool kPair, int kOp, bool kWide>
+template <bool kPair, int kOp, bool kWide, int kEpiWarps>
 cudaError_t init_t() {
-    return cudaFuncSetAttribute(mip_layer_kernel<kPair, kOp, kWide>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudget);
+    return cudaFuncSetAttribute(mip_layer_kernel<kPair, kOp, kWide, kEpiWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudget);
 }
 template <bool kPair, int kOp>
 cudaError_t init_op() {
-    const cudaError_t e = init_t<kPair, kOp, false>();
-    return e != cudaSuccess ? e : init_t<kPair, kOp, true>();
+    for (cudaError_t e : {init_t<kPair, kOp, false, kFewEpiWarps>(), init_t<kPair, kOp, false, kManyEpiWarps>(), init_t<kPair, kOp, true, kFewEpiWarps>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+template <bool kPair, int kOp>
+cudaError_t launch_op(const LayerParams& p, const cudaLaunchConfig_t& cfg) {
+    if (p.type == kF32) return launch_t<kPair, kOp, true, kFewEpiWarps>(p, cfg);
+    return p.epi_warps == kManyEpiWarps ? launch_t<kPair, kOp, false, kManyEpiWarps>(p, cfg) : launch_t<kPair, kOp, false, kFewEpiWarps>(p, cfg);
 }
 
 }  // namespace
 
-int layer_fixed_smem(int op, bool wide) { return epi_warps(op, wide) * (slot_bytes_per_warp(op, wide) + kColBytes) + kCtrlBytes + 1024; }
+// (partial sums are words: the float32 form's slots)
+int layer_fixed_smem(int op, bool wide, int epi_warps) {
+    return epi_warps * (slot_bytes_per_warp(op, wide || op == kOpRaw || op == kOpRawGated) + kColBytes) + kCtrlBytes + 1024;
+}
 
 cudaError_t layer_init() {
-    for (cudaError_t e : {init_op<false, kOpLinear>(), init_op<true, kOpLinear>(), init_op<false, kOpGated>(),
-                          init_op<true, kOpGated>(), init_op<false, kOpGatedGrad>(), init_op<true, kOpGatedGrad>(), init_t<false, kOpRaw, true>(),
-                          init_t<true, kOpRaw, true>(), init_t<false, kOpRawGated, true>(), init_t<true, kOpRawGated, true>()})
+    for (cudaError_t e : {init_op<false, kOpLinear>(), init_op<true, kOpLinear>(), init_op<false, kOpGated>(), init_op<true, kOpGated>(),
+                          init_op<false, kOpGatedGrad>(), init_op<true, kOpGatedGrad>(), init_t<false, kOpRaw, true, kFewEpiWarps>(),
+                          init_t<true, kOpRaw, true, kFewEpiWarps>(), init_t<false, kOpRawGated, true, kFewEpiWarps>(),
+                          init_t<true, kOpRawGated, true, kFewEpiWarps>()})
         if (e != cudaSuccess) return e;
     return cudaSuccess;
 }
@@ -258,9 +266,9 @@ cudaError_t layer_init() {
 cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
-    const bool wide = p.type == kF32 || op == kOpRaw || op == kOpRawGated;      // (partial sums are words)
-    cfg.blockDim = dim3(layer_threads(op, wide), 1, 1);
-    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kBlockM + (pair ? p.block_n / 2 : p.block_n)) * 128 + layer_fixed_smem(op, wide);
+    cfg.blockDim = dim3(static_cast<unsigned>(32 * (3 + p.epi_warps)), 1, 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kBlockM + (pair ? p.block_n / 2 : p.block_n)) * 128 +
+                           layer_fixed_smem(op, p.type == kF32, p.epi_warps);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -271,21 +279,12 @@ cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaS
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pair ? 2 : 1;
-    if (op == kOpRaw) return pair ? launch_t<true, kOpRaw, true>(p, cfg) : launch_t<false, kOpRaw, true>(p, cfg);
-    if (op == kOpRawGated) return pair ? launch_t<true, kOpRawGated, true>(p, cfg) : launch_t<false, kOpRawGated, true>(p, cfg);
-    switch (op * 4 + (pair ? 2 : 0) + (wide ? 1 : 0)) {
-        case kOpLinear * 4 + 0: return launch_t<false, kOpLinear, false>(p, cfg);
-        case kOpLinear * 4 + 1: return launch_t<false, kOpLinear, true>(p, cfg);
-        case kOpLinear * 4 + 2: return launch_t<true, kOpLinear, false>(p, cfg);
-        case kOpLinear * 4 + 3: return launch_t<true, kOpLinear, true>(p, cfg);
-        case kOpGated * 4 + 0: return launch_t<false, kOpGated, false>(p, cfg);
-        case kOpGated * 4 + 1: return launch_t<false, kOpGated, true>(p, cfg);
-        case kOpGated * 4 + 2: return launch_t<true, kOpGated, false>(p, cfg);
-        case kOpGated * 4 + 3: return launch_t<true, kOpGated, true>(p, cfg);
-        case kOpGatedGrad * 4 + 0: return launch_t<false, kOpGatedGrad, false>(p, cfg);
-        case kOpGatedGrad * 4 + 1: return launch_t<false, kOpGatedGrad, true>(p, cfg);
-        case kOpGatedGrad * 4 + 2: return launch_t<true, kOpGatedGrad, false>(p, cfg);
-        default: return launch_t<true, kOpGatedGrad, true>(p, cfg);
+    switch (op) {
+        case kOpRaw: return pair ? launch_t<true, kOpRaw, true, kFewEpiWarps>(p, cfg) : launch_t<false, kOpRaw, true, kFewEpiWarps>(p, cfg);
+        case kOpRawGated: return pair ? launch_t<true, kOpRawGated, true, kFewEpiWarps>(p, cfg) : launch_t<false, kOpRawGated, true, kFewEpiWarps>(p, cfg);
+        case kOpLinear: return pair ? launch_op<true, kOpLinear>(p, cfg) : launch_op<false, kOpLinear>(p, cfg);
+        case kOpGated: return pair ? launch_op<true, kOpGated>(p, cfg) : launch_op<false, kOpGated>(p, cfg);
+        default: return pair ? launch_op<true, kOpGatedGrad>(p, cfg) : launch_op<false, kOpGatedGrad>(p, cfg);
     }
 }
 

@@ -5,9 +5,9 @@
 // rounded to bfloat16 on its way to the tensor core (codes alone are exact in bfloat16), and tcgen05.mma.kind::f16
 // multiplies it with A into binary32.  The codes cross HBM and L2 as bytes; nothing is written back in 16 bits.
 //
-// Roles.  Warp 0 loads A (TMA, 128-byte swizzle, K-major or M-major as it lies), warp 1 issues the MMAs, warps 2-5
-// are the epilogue (layer_epilogue.cuh), warp 6 loads B's codes (TMA, 64 rows x 128 bytes, plain rows), warps 7-14
-// convert, two groups by turns: a lane takes 16 codes of a row (one 16-byte read, eight lanes a row), scales them and writes the two
+// Roles.  Warp 0 loads A (TMA, 128-byte swizzle, K-major or M-major as it lies), warp 1 issues the MMAs, then four or eight
+// (16-bit results) epilogue warps (layer_epilogue.cuh), one that loads B's codes (TMA, 64 rows x 128 bytes, plain rows),
+// and eight that convert, two groups by turns: a lane takes 16 codes of a row (one 16-byte read, eight lanes a row), scales them and writes the two
 // 16-byte pieces of the N-major 128-byte-swizzled tile the tensor core reads.  Lanes of the row's second half write
 // their pieces in the other order, so that eight lanes cover all banks.  A stage is 64 k: 16 KB of A, 8 KB of codes,
 // 16 KB of converted B per CTA.  In the pair form (256 x 256 tile, cta_group::2) each CTA converts its half of B, so
@@ -20,16 +20,16 @@ namespace mip {
 
 namespace {
 
-constexpr int kEpiWarps = epi_warps(kOpProduct, false);
 constexpr int kConvWarps = 8;
-constexpr int kFirstConvWarp = 3 + kEpiWarps;
-constexpr int kProductThreads = 32 * (kFirstConvWarp + kConvWarps);
+constexpr int product_threads(bool wide) { return 32 * (3 + product_epi_warps(wide) + kConvWarps); }
 constexpr uint32_t kABytes = kBlockM * kProductK * 2;          // 16 KB
 constexpr uint32_t kBBytes = kProductN * kProductK * 2;        // 16 KB, two blocks of 64 columns
 constexpr uint32_t kRawBytes = kProductN * kProductK;          // 8 KB
 constexpr uint32_t kProductStage = kABytes + kBBytes + kRawBytes;
 constexpr uint32_t kScaleBytes = kProductK * 4;                // the rows' scales, behind the stages
-constexpr int kProductFixed = kEpiWarps * slot_bytes_per_warp(kOpProduct, true) + kCtrlBytes + 1024;
+constexpr int kProductSlots = 4 * slot_bytes_per_warp(kOpProduct, true);       // (as much as 8 warps' 16-bit slots)
+static_assert(product_epi_warps(false) * slot_bytes_per_warp(kOpProduct, false) <= kProductSlots && product_epi_warps(true) == 4, "slots");
+constexpr int kProductFixed = kProductSlots + kCtrlBytes + 1024;
 
 // Four codes (the bytes of w) times s (twice, packed), rounded to bfloat16.  A byte with its sign bit flipped, put
 // behind the exponent of 2^23, is the float 2^23 + 128 + code: one byte permutation per code and one exact packed
@@ -51,9 +51,11 @@ __device__ __forceinline__ void scale_codes(uint32_t w, uint64_t ss, uint32_t& l
 }
 
 template <bool kPair, bool kAMajorM, bool kWide, bool kRaw>
-__global__ void __launch_bounds__(kProductThreads, 1)
+__global__ void __launch_bounds__(product_threads(kWide), 1)
 mip_product_kernel(const __grid_constant__ LayerParams p) {
     constexpr int kGroup = kPair ? 2 : 1;
+    constexpr int kEpiWarps = product_epi_warps(kWide);
+    constexpr int kFirstConvWarp = 3 + kEpiWarps;
     constexpr int kRowsPerTile = kGroup * kBlockM;
     const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
     const bool leader = cta_rank == 0;
@@ -66,7 +68,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     const uint32_t smem_base = raw_addr + pad;
     const uint32_t stages = static_cast<uint32_t>(p.stages);
     const uint32_t slots = smem_base + stages * kProductStage;
-    const uint32_t scales = slots + kEpiWarps * slot_bytes_per_warp(kOpProduct, true);
+    const uint32_t scales = slots + kProductSlots;
     const uint32_t ctrl = scales + stages * kScaleBytes;
     // control block, 8 bytes each: A has arrived | B is converted | A and B have been read | codes have arrived | codes
     // have been read (`stages` of each), accumulators full and empty, drain, arrivals in the slots
@@ -296,7 +298,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
                                                                   bar_tfull, bar_tempty, abort_flag, tmem_base, warp & 3, lane, cta_rank,
                                                                first_unit, unit_stride);
         else
-            layer_epilogue<kPair, kOpProduct, kWide>(p, slots, 0, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
+            layer_epilogue<kPair, kOpProduct, kWide, kEpiWarps>(p, slots, 0, bar_in, bar_tfull, bar_tempty, abort_flag, tmem_base, warp - 2, warp & 3,
                                                      lane, cta_rank, first_unit, unit_stride);
     }
 
@@ -370,7 +372,7 @@ cudaError_t product_init() {
 cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int raw, int grid, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
-    cfg.blockDim = dim3(kProductThreads, 1, 1);
+    cfg.blockDim = dim3(product_threads(raw || p.type == kF32), 1, 1);
     cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kProductStage + kScaleBytes) + kProductFixed;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];

@@ -122,6 +122,24 @@ mip_quantize_rows_kernel(long long M, int vectors, const uint8_t* X, long long l
     }
 }
 
+// Eight elements of a row, kRowThreads apart, as floats (0 beyond N).  Raw loads first: a conversion beside each load
+// would wait for it.
+__device__ __forceinline__ void load_strided8(float (&v)[8], const void* X, long long row_at, long long j0, long long N, int type) {
+    if (type == kF32) {
+        const float* x = static_cast<const float*>(X) + row_at;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = j0 + i * kRowThreads < N ? x[j0 + i * kRowThreads] : 0.0f;
+        return;
+    }
+    const uint16_t* x = static_cast<const uint16_t*>(X) + row_at;
+    uint16_t raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i] = j0 + i * kRowThreads < N ? x[j0 + i * kRowThreads] : uint16_t(0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = type == kF16 ? __half2float(__ushort_as_half(raw[i])) : __uint_as_float(static_cast<uint32_t>(raw[i]) << 16);
+}
+
 // Element form: any alignment, any length.
 __global__ void mip_quantize_elements_kernel(int type, long long N, const void* X, long long ldx, int8_t* Q, long long ldq, float* scale) {
     __shared__ float part[kRowThreads / 32];
@@ -131,11 +149,19 @@ __global__ void mip_quantize_elements_kernel(int type, long long N, const void* 
     const long long row = blockIdx.x;
     float top = 0.0f;
     int bad = 0;
-    for (long long j = threadIdx.x; j < N; j += kRowThreads) {
-        const float v = fabsf(load_element(X, row * ldx + j, type));
+    const auto each = [&](auto&& body) {                 // eight elements at a time: their loads travel together
+        for (long long j0 = threadIdx.x; j0 < N; j0 += 8 * kRowThreads) {
+            float v[8];
+            load_strided8(v, X, row * ldx, j0, N, type);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) body(j0 + i * kRowThreads, v[i]);
+        }
+    };
+    each([&](long long, float x) {                       // (0 beyond the row)
+        const float v = fabsf(x);
         bad |= !(v <= 3.402823466e38f);
         top = fmaxf(top, v);
-    }
+    });
     top = __uint_as_float(__reduce_max_sync(~0u, __float_as_uint(top)));
     bad = __any_sync(~0u, bad);
     if ((threadIdx.x & 31) == 0) { part[threadIdx.x >> 5] = top; odd[threadIdx.x >> 5] = bad; }
@@ -143,8 +169,9 @@ __global__ void mip_quantize_elements_kernel(int type, long long N, const void* 
     for (int w = 0; w < kRowThreads / 32; ++w) { top = fmaxf(top, part[w]); bad |= odd[w]; }
     const RowScale s = row_scale(bad ? __int_as_float(0x7FFFFFFF) : top);
     if (threadIdx.x == 0) scale[row] = s.scale;
-    for (long long j = threadIdx.x; j < N; j += kRowThreads)
-        Q[row * ldq + j] = s.mult == 0.0f ? 0 : static_cast<int8_t>(__float2int_rn(__fmul_rn(load_element(X, row * ldx + j, type), s.mult)));
+    each([&](long long j, float x) {
+        if (j < N) Q[row * ldq + j] = s.mult == 0.0f ? 0 : static_cast<int8_t>(__float2int_rn(__fmul_rn(x, s.mult)));
+    });
 }
 
 // 16 codes per thread and row -> 16 elements; kRows rows per thread, their loads together.
@@ -190,8 +217,15 @@ __global__ void mip_dequantize_elements_kernel(int type, long long N, const int8
     pdl_wait();
     const long long row = blockIdx.x;
     const float s = scale[row];
-    for (long long j = threadIdx.x; j < N; j += kRowThreads)
-        store_element(X, row * ldx + j, type, __fmul_rn(s, static_cast<float>(Q[row * ldq + j])));
+    for (long long j0 = static_cast<long long>(blockIdx.y) * 8 * kRowThreads + threadIdx.x; j0 < N;
+         j0 += static_cast<long long>(gridDim.y) * 8 * kRowThreads) {
+        int8_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = j0 + i * kRowThreads < N ? Q[row * ldq + j0 + i * kRowThreads] : int8_t(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j0 + i * kRowThreads < N) store_element(X, row * ldx + j0 + i * kRowThreads, type, __fmul_rn(s, static_cast<float>(q[i])));
+    }
 }
 
 bool aligned_rows(const void* p, long long pitch_bytes, int bytes) {
@@ -265,7 +299,8 @@ cudaError_t launch_dequantize_rows(int type, long long M, long long N, const int
         if (type == kF16) return dequantize_t<kF16>(M, vectors, Q, ldq, scale, x, ldx_bytes, stream);
         return dequantize_t<kBF16>(M, vectors, Q, ldq, scale, x, ldx_bytes, stream);
     }
-    const RowsLaunch l(dim3(static_cast<unsigned>(M)), dim3(kRowThreads), stream);
+    const long long parts = (N + 8 * kRowThreads - 1) / (8 * kRowThreads);
+    const RowsLaunch l(dim3(static_cast<unsigned>(M), static_cast<unsigned>(parts < 64 ? parts : 64)), dim3(kRowThreads), stream);
     return cudaLaunchKernelEx(&l.cfg, mip_dequantize_elements_kernel, type, N, Q, ldq, scale, X, ldx);
 }
 
