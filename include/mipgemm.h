@@ -52,8 +52,10 @@
  * Some calls need global scratch memory (operand re-pitching, slot-padded
  * filters for convolutions gathered in software, the explicit im2col matrix
  * for the few convolutions neither the TMA nor the gather warps can handle).
- * By default it is taken with cudaMallocAsync on the call's stream and
- * released with cudaFreeAsync after the last kernel of the call.  A caller may instead lend a buffer with mipgemm_set_workspace(); calls
+ * By default it comes from blocks that the library allocates with cudaMalloc when a stream's calls first need
+ * them (or need more) and keeps for later calls on the same stream; mipgemm_release_staging() frees those not
+ * in use.  Calls captured into a CUDA graph take it with cudaMallocAsync from the graph's memory instead.
+ * A caller may instead lend a buffer with mipgemm_set_workspace(); calls
  * that need more than was lent fail with MIPGEMM_ERR_WORKSPACE.  A lent buffer
  * is shared by all calls: calls that use it must be ordered on one stream.
  */
@@ -334,8 +336,8 @@ int mipgemm_s8s8s32_static_scratch(int64_t M, int64_t N, int64_t K,
  * (C is then incomplete; the flag is cleared), or MIPGEMM_ERR_CUDA. */
 int mipgemm_static_scratch_status(void *stream);
 
-/* Frees the current device's staging buffer of the host-buffer variants (it is allocated again by
- * the next such call). */
+/* Frees the current device's staging buffer of the host-buffer variants and the scratch blocks kept between
+ * calls (they are allocated again by the next calls that need them).  Waits for the device. */
 int mipgemm_release_staging(void);
 
 /* ---- operators of an 8-bit transformer layer (extensions: the paper stops at one scale per matrix) ----

@@ -10,6 +10,7 @@
 #include <map>
 #include <mutex>
 #include <new>
+#include <vector>
 
 #include "../../include/mipgemm.h"
 #include "internal.h"
@@ -83,6 +84,13 @@ typedef CUresult (*EncodeIm2colFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t
 constexpr int kMaxDevices = 64;
 constexpr int kHostBlocks = 8;                                    // host-buffer calls: up to 8 x 8 blocks of C
 constexpr int kHostEvents = 2 * kHostBlocks + kHostBlocks * kHostBlocks + 3;
+// Scratch memory kept between calls: a block that nobody holds may be taken by a call on the stream that used it last,
+// whose work it is then ordered behind.
+struct ScratchBlock {
+    void* base;
+    size_t bytes;
+    unsigned long long stream_id;
+};
 struct DeviceState {
     bool ready = false;
     int status = MIPGEMM_OK;
@@ -97,7 +105,8 @@ struct DeviceState {
     bool host_events_ready = false;
     void* lent = nullptr;
     size_t lent_bytes = 0;
-    cudaMemPool_t pool = nullptr;          // scratch of the calls; keeps what it has been given back (see Scratch)
+    std::mutex scratch_mutex;              // scratch blocks kept between calls (see Scratch)
+    std::vector<ScratchBlock> scratch;
 };
 DeviceState g_dev[kMaxDevices];
 std::mutex g_mutex;
@@ -202,18 +211,6 @@ int get_device(DeviceState** out) {
             if (cudaStreamCreateWithFlags(&d.copy_in, cudaStreamNonBlocking) != cudaSuccess) d.copy_in = nullptr;
             if (cudaStreamCreateWithFlags(&d.copy_out, cudaStreamNonBlocking) != cudaSuccess) d.copy_out = nullptr;
             (void)cudaGetLastError();
-            // Scratch comes from a pool of the library's own that keeps up to 1 GiB between calls: the default pool gives
-            // everything back at every synchronisation, and the next call pays for mapping it again (0.5 ms and more).
-            cudaMemPoolProps props = {};
-            props.allocType = cudaMemAllocationTypePinned;
-            props.location.type = cudaMemLocationTypeDevice;
-            props.location.id = dev;
-            unsigned long long keep = 1ull << 30;
-            if (cudaMemPoolCreate(&d.pool, &props) != cudaSuccess ||
-                cudaMemPoolSetAttribute(d.pool, cudaMemPoolAttrReleaseThreshold, &keep) != cudaSuccess) {
-                d.pool = nullptr;                    // (the default pool then)
-                (void)cudaGetLastError();
-            }
             d.status = MIPGEMM_OK;
         }
         d.ready = true;
@@ -222,28 +219,72 @@ int get_device(DeviceState** out) {
     return d.status;
 }
 
-// Scratch memory for one call: a slice of the lent buffer, or a stream-ordered allocation.
+// Scratch memory for one call: a slice of the lent buffer, or a block of the library's own.  Blocks stay with their stream
+// (by its id: handles are reused) and grow with the largest call; only growth reaches the CUDA allocator.  (The
+// stream-ordered allocator maps and unmaps memory around every synchronisation: 0.5 ms and more per call that way, and
+// seconds when a long queue of calls had made its pool grow.)  A captured call allocates from its graph.
 struct Scratch {
     DeviceState* dev;
     cudaStream_t stream;
     void* base = nullptr;
     size_t size = 0, used = 0;
-    bool owned = false;
+    bool owned = false;          // stream-ordered (capture)
+    ScratchBlock block{nullptr, 0, 0};
     Scratch(DeviceState* d, cudaStream_t s) : dev(d), stream(s) {}
+    int fail(cudaError_t e) {
+        tl_last_cuda_error = static_cast<int>(e);
+        (void)cudaGetLastError();
+        return MIPGEMM_ERR_WORKSPACE;
+    }
     int reserve(size_t bytes) {
         if (bytes == 0) return MIPGEMM_OK;
         if (dev->lent) {
             if (bytes > dev->lent_bytes) return MIPGEMM_ERR_WORKSPACE;
             base = dev->lent;
+            size = bytes;
+            return MIPGEMM_OK;
+        }
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        cudaError_t e = cudaStreamIsCapturing(stream, &capture);
+        if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) {
+            unsigned long long id = 0;
+            if ((e = cudaStreamGetId(stream, &id)) != cudaSuccess) return fail(e);
+            {
+                // the smallest of the stream's blocks that is large enough, else its largest, which gives way to a larger
+                std::lock_guard<std::mutex> lock(dev->scratch_mutex);
+                int best = -1;
+                for (int i = 0; i < static_cast<int>(dev->scratch.size()); ++i) {
+                    const ScratchBlock& b = dev->scratch[i];
+                    if (b.stream_id != id) continue;
+                    const bool fits = b.bytes >= bytes;
+                    const bool best_fits = best >= 0 && dev->scratch[best].bytes >= bytes;
+                    if (best < 0 || (fits && !best_fits) || (fits == best_fits && (b.bytes < dev->scratch[best].bytes) == fits)) best = i;
+                }
+                if (best >= 0) {
+                    block = dev->scratch[best];
+                    dev->scratch.erase(dev->scratch.begin() + best);
+                }
+            }
+            if (block.bytes < bytes) {
+                // (another thread may be capturing: these calls do not belong to its graph)
+                cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+                (void)cudaThreadExchangeStreamCaptureMode(&mode);
+                if (block.base) (void)cudaFree(block.base);          // waits for the work that uses it
+                const size_t grown = (bytes + (2u << 20) - 1) & ~static_cast<size_t>((2u << 20) - 1);
+                e = cudaMalloc(&block.base, grown);
+                (void)cudaThreadExchangeStreamCaptureMode(&mode);
+                if (e != cudaSuccess) {
+                    block = ScratchBlock{nullptr, 0, 0};
+                    return fail(e);
+                }
+                block.bytes = grown;
+                block.stream_id = id;
+            }
+            base = block.base;
         } else {
-            // (a captured call allocates from the graph's memory)
-            cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-            const bool own = dev->pool && cudaStreamIsCapturing(stream, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone;
-            cudaError_t e = own ? cudaMallocFromPoolAsync(&base, bytes, dev->pool, stream) : cudaMallocAsync(&base, bytes, stream);
-            if (e != cudaSuccess) {
-                tl_last_cuda_error = static_cast<int>(e);
-                (void)cudaGetLastError();
-                return MIPGEMM_ERR_WORKSPACE;
+            if ((e = cudaMallocAsync(&base, bytes, stream)) != cudaSuccess) {
+                base = nullptr;
+                return fail(e);
             }
             owned = true;
         }
@@ -257,6 +298,14 @@ struct Scratch {
     }
     ~Scratch() {
         if (owned && base) (void)cudaFreeAsync(base, stream);
+        if (!block.base) return;
+        // back to the stream's blocks (everything that uses it has been enqueued)
+        try {
+            std::lock_guard<std::mutex> lock(dev->scratch_mutex);
+            dev->scratch.push_back(block);
+        } catch (...) {
+            (void)cudaFree(block.base);      // (no memory for the list: waits for the block's work)
+        }
     }
 };
 
@@ -1329,8 +1378,11 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
             const long long slots = pair ? dev->pair_clusters : dev->sm_count;
             const int stages = layer_stages(a, pair, bn, false);
             if (stages < 2) continue;
-            // (a k-block cannot come faster than its copy's latency over the stages on their way)
-            const double kb_clk = std::max(pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn, 2000.0 / stages);
+            // (a k-block cannot come faster than its copy's latency over the stages on their way: ~3600 clocks where few
+            // row tiles share the weights, which then come from HBM -- gated_grad 320 x 8192 x 6736, us for pairs of 256
+            // columns in 4 stages / one CTA of 192 in 3 / of 256 in 3: 53 / 66 / 73)
+            const long long row_tiles = (a.M + (pair ? 2 * kBlockM : kBlockM) - 1) / (pair ? 2 * kBlockM : kBlockM);
+            const double kb_clk = std::max(pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn, (row_tiles < 8 ? 3600.0 : 2000.0) / stages);
             // the schedulers' time for the tile's outputs, and at least each warp's rounds of slots
             const double rounds = (out_n / 32 + warps / 4 - 1) / (warps / 4);
             const double per_col = a.op == kOpGatedGrad ? 42.0 : (gated ? 30.0 : (a.act >= MIPGEMM_ACT_GELU ? 27.0 : 14.0));
@@ -1342,7 +1394,8 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
                 const int share = (k_blocks + split - 1) / split;
                 if ((k_blocks + share - 1) / share != split) continue;
                 const double main = share * kb_clk;
-                const double period = std::max(main, epi) + 0.2 * std::min(main, epi);
+                // (a pair waits for both of its CTAs' epilogues: 8 % where they set the pace)
+                const double period = (std::max(main, epi) + 0.2 * std::min(main, epi)) * (pair && epi > main ? 1.08 : 1.0) + 400.0;
                 const long long waves = (tiles * split + slots - 1) / slots;
                 double clk = (waves - 1) * period + main + epi + (pair ? 1900.0 : 0.0);
                 // (a launch, and the planes written and read at the L2's pace)
@@ -2247,8 +2300,13 @@ int mipgemm_release_staging(void) {
         dev->staging_bytes = 0;
         if (e != cudaSuccess) return cuda_fail(e);
     }
-    if (dev->pool) {
-        const cudaError_t e = cudaMemPoolTrimTo(dev->pool, 0);
+    std::vector<ScratchBlock> blocks;
+    {
+        std::lock_guard<std::mutex> lock(dev->scratch_mutex);
+        blocks.swap(dev->scratch);
+    }
+    for (const ScratchBlock& b : blocks) {               // (cudaFree waits for the work that uses it)
+        const cudaError_t e = cudaFree(b.base);
         if (e != cudaSuccess) return cuda_fail(e);
     }
     return MIPGEMM_OK;

@@ -71,8 +71,6 @@ struct RepackArgs {
 };
 __global__ void __launch_bounds__(256)
 mip_repack_parts_kernel(const RepackArgs a) {
-    pdl_launch_dependents();
-    pdl_wait();
     const RepackPart& p = a.part[blockIdx.y];
     const int segments = static_cast<int>((p.cols + 511) / 512);
     const long long warps = static_cast<long long>(gridDim.x) * 8;
@@ -114,16 +112,9 @@ cudaError_t launch_repack_parts(const RepackPart* parts, int count, cudaStream_t
         a.part[i] = parts[i];
         most = max(most, (parts[i].rows * ((parts[i].cols + 511) / 512) + 7) / 8);
     }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(min(most, 148LL * 16)), static_cast<unsigned>(count));
-    cfg.blockDim = dim3(256);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, mip_repack_parts_kernel, a);
+    // (not launched early: see launch_layer_finish)
+    mip_repack_parts_kernel<<<dim3(static_cast<unsigned>(min(most, 148LL * 16)), static_cast<unsigned>(count)), 256, 0, stream>>>(a);
+    return cudaGetLastError();
 }
 
 // ---------------------------------------------------------------- transposing repack

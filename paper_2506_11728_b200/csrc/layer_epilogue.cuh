@@ -296,7 +296,7 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
         const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
         const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
         const int n_here = min(p.out_n, p.N - tc.n0);
-        if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, p.wait_budget_ns))) break;
+        if (!mbar_wait_warp(bar_tfull + 8u * acc, acc_phase, abort_flag, p.wait_budget_ns)) break;
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
         for (int c0 = 32 * sub; c0 < p.block_n && row0 < p.M; c0 += 32 * kSubs) {
@@ -304,6 +304,7 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
             const int c = second ? c0 - p.out_n : c0;
             if (c >= n_here) continue;
             uint32_t v[32];
+            __syncwarp();                                      // tcgen05.ld wants the whole warp: the elected lane is back
             tmem_ld_32x32(t_row + c0, v);
             if (elect_one()) tma_store_wait_read<kSlots - 1>();
             __syncwarp();
@@ -422,7 +423,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
             fetch_columns(next, 0);
         }
         // (the lanes of a warp decide together: none may leave while others still expect it at a warp barrier)
-        if (!__all_sync(~0u, mbar_wait(bar_tfull + 8u * acc, acc_phase, abort_flag, budget))) break;
+        if (!mbar_wait_warp(bar_tfull + 8u * acc, acc_phase, abort_flag, budget)) break;
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
         const uint32_t t_up = t_row + static_cast<uint32_t>(p.block_n >> 1);
@@ -432,6 +433,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
             const uint32_t b = slot_no % kBuffers;
             const uint32_t slot = my_slots + b * kSlotStride, slot2 = slot + slot_bytes(kWide);
             uint32_t v[kGatedForm ? 16 : 32], v1[16];
+            __syncwarp();                                      // tcgen05.ld wants the whole warp: the elected lane is back
             if constexpr (!kGatedForm) tmem_ld_32x32(t_row + c0, v);
             // the slot is free (its last store has been read) or holds the tile that was asked for
             if (!r_tma) {
@@ -451,7 +453,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 as = fetch_row(next);
                 fetch_columns(next, 0);
             }
-            if (r_tma && !__all_sync(~0u, mbar_wait(my_bar + 8u * b, (slot_no / kBuffers) & 1u, abort_flag, budget))) {
+            if (r_tma && !mbar_wait_warp(my_bar + 8u * b, (slot_no / kBuffers) & 1u, abort_flag, budget)) {
                 gave_up = true;
                 break;
             }
@@ -459,6 +461,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                 // (16 columns of both projections at a time: registers for four epilogue warps per scheduler)
 #pragma unroll 1
                 for (int c = 0; c < kSlotCols; c += 16) {
+                    __syncwarp();
                     tmem_ld_32x16(t_row + c0 + c, v);
                     tmem_ld_32x16(t_up + c0 + c, v1);
                     tmem_ld_wait_for16(v, v1);

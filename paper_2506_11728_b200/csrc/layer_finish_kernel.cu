@@ -3,7 +3,6 @@
 // every sum is 0: the case K == 0.
 #include "internal.h"
 #include "layer_math.cuh"
-#include "ptx.cuh"
 
 namespace mip {
 
@@ -15,8 +14,6 @@ constexpr int kCols = 4;             // columns per thread: one 16-byte read per
 template <int kOp>
 __global__ void __launch_bounds__(kThreads)
 mip_layer_finish_kernel(const LayerArgs a, const PartialPlanes s) {
-    pdl_launch_dependents();
-    pdl_wait();
     const long long row = static_cast<long long>(blockIdx.y) * blockDim.y + threadIdx.y;
     const long long col = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) * kCols;
     if (row >= a.M || col >= a.N) return;
@@ -62,8 +59,6 @@ mip_layer_finish_kernel(const LayerArgs a, const PartialPlanes s) {
 
 __global__ void __launch_bounds__(kThreads)
 mip_product_finish_kernel(const ProductArgs a, const PartialPlanes s) {
-    pdl_launch_dependents();
-    pdl_wait();
     const long long row = static_cast<long long>(blockIdx.y) * blockDim.y + threadIdx.y;
     const long long col = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) * kCols;
     if (row >= a.M || col >= a.N) return;
@@ -83,6 +78,9 @@ mip_product_finish_kernel(const ProductArgs a, const PartialPlanes s) {
         if (j < cols) store_element(a.C, row * a.ldc + col + j, a.type, v[j]);
 }
 
+// These kernels are not launched early (programmatic stream serialisation): they come as many small blocks, which would
+// fill the SMs while they wait for a kernel whose clusters may still be looking for room there.  A chain of re-pitch,
+// cluster kernel and finish, all launched early, stopped making progress in long queues.
 template <typename Args>
 cudaError_t finish(void (*kernel)(const Args, const PartialPlanes), const Args& a, const PartialPlanes& s, cudaStream_t stream) {
     int tx = 8;
@@ -96,16 +94,9 @@ cudaError_t finish(void (*kernel)(const Args, const PartialPlanes), const Args& 
         part.M = a.M - row < step ? a.M - row : step;
         part.advance(row);
         if (s.base) planes.base = static_cast<const char*>(s.base) + row * s.pitch * 4;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(static_cast<unsigned>((a.N + tx * kCols - 1) / (tx * kCols)), static_cast<unsigned>((part.M + ty - 1) / ty));
-        cfg.blockDim = dim3(tx, ty);
-        cfg.stream = stream;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, part, planes);
+        const dim3 grid(static_cast<unsigned>((a.N + tx * kCols - 1) / (tx * kCols)), static_cast<unsigned>((part.M + ty - 1) / ty));
+        kernel<<<grid, dim3(tx, ty), 0, stream>>>(part, planes);
+        const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

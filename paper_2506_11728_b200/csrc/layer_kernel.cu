@@ -110,7 +110,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
             const int m_cta = tc.m0 + static_cast<int>(cta_rank) * kBlockM;
             const int half = p.block_n >> 1;
             for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                if (!mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                if (!mbar_wait_warp(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 const uint32_t full_local = bar_full + 8u * s;
                 const uint32_t full = kPair ? mapa_u32(full_local, 0) : full_local;
                 const uint32_t a_dst = smem_base + s * stage_bytes;
@@ -143,11 +143,11 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++t) {
                 const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
                 const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
-                if (!mbar_wait<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                if (!mbar_wait_warp<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * p.block_n;
                 for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                    if (!mbar_wait(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
+                    if (!mbar_wait_warp(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a_addr = smem_base + s * stage_bytes;
                     const uint64_t a_desc = make_kmajor_desc(a_addr, 128);
@@ -191,6 +191,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
                                               lane, cta_rank, first_unit, unit_stride);
     }
 
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (*abort_flag != 0) {

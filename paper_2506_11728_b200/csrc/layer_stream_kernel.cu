@@ -110,7 +110,7 @@ mip_layer_stream_kernel(const __grid_constant__ LayerParams p) {
         pdl_wait();
         uint32_t s = 0, phase = 0;
         for (int i = 0; i < n_kb; ++i) {
-            if (i >= p.stages && !mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) break;
+            if (i >= p.stages && !mbar_wait_warp(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) break;
             if (elect_one()) {
                 const uint32_t dst = smem_base + s * stage_bytes, bar = bar_full + 8u * s;
                 if (!(p.b_constant && i < early)) {
@@ -131,7 +131,7 @@ mip_layer_stream_kernel(const __grid_constant__ LayerParams p) {
         uint32_t s = 0, phase = 0;
         bool ok = true;
         for (int i = 0; i < n_kb; ++i) {
-            if (!mbar_wait(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
+            if (!mbar_wait_warp(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
             tc_fence_after();
             const uint32_t addr = smem_base + s * stage_bytes;
             const uint64_t a_desc = make_kmajor_desc(addr, 128), b_desc = make_kmajor_desc(addr + kWeightTile, 128);

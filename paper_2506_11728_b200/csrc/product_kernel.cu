@@ -134,7 +134,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int m_cta = tc.m0 + static_cast<int>(cta_rank) * kBlockM;
             for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                if (!mbar_wait(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                if (!mbar_wait_warp(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 const uint32_t local = bar_a + 8u * s;
                 const uint32_t full = kPair ? mapa_u32(local, 0) : local;     // both CTAs' bytes complete on the leader's
                 const uint32_t dst = smem_base + s * kProductStage;
@@ -163,7 +163,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
             const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
             const int n_cta = tc.n0 + static_cast<int>(cta_rank) * kProductN;
             for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                if (!mbar_wait(bar_rawfree + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                if (!mbar_wait_warp(bar_rawfree + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 if (elect_one()) {
                     mbar_arrive_expect_tx(bar_raw + 8u * s, kRawBytes);
                     tma_load_2d(smem_base + s * kProductStage + kABytes + kBBytes, &p.tmap_b0, bar_raw + 8u * s, n_cta, kb * kProductK);
@@ -195,12 +195,12 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++t) {
                 const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
                 const uint32_t acc = t & 1, acc_phase = (t >> 1) & 1;
-                if (!mbar_wait<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                if (!mbar_wait_warp<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * p.block_n;
                 for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                    if (!mbar_wait(bar_a + 8u * s, phase, abort_flag, budget) ||
-                        !mbar_wait<kPair>(bar_b + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
+                    if (!mbar_wait_warp(bar_a + 8u * s, phase, abort_flag, budget) ||
+                        !mbar_wait_warp<kPair>(bar_b + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a_addr = smem_base + s * kProductStage;
                     const uint64_t a_desc = kAMajorM ? make_mnmajor_desc(a_addr, kABytes / 2) : make_kmajor_desc(a_addr, 128);
@@ -302,6 +302,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
                                                      lane, cta_rank, first_unit, unit_stride);
     }
 
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (*abort_flag != 0) {

@@ -125,6 +125,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity,
     }
 }
 
+// The same for a whole warp: its lanes decide together.  A lane whose wait has just succeeded must not go on to a warp
+// barrier or an election that lanes which gave up will never reach.
+template <bool kCluster = false>
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint64_t budget_ns) {
+    return __all_sync(0xffffffffu, mbar_wait<kCluster>(bar, parity, abort_flag, budget_ns)) != 0;
+}
+
 // Named barrier over `threads` threads of the CTA that also agrees on a decision: every thread
 // contributes a predicate and all of them receive the OR.  Roles that wait on mbarriers warp by warp
 // use it to decide TOGETHER whether to go on or to unwind, so that no warp can leave while another

@@ -48,8 +48,6 @@ __global__ void __launch_bounds__(1024)
 mip_quantize_rows_kernel(long long M, int vectors, const uint8_t* X, long long ldx_bytes, int8_t* Q, long long ldq, float* scale) {
     constexpr int kElems = kType == kF32 ? 8 : 16;       // per vector
     __shared__ uint32_t part[32];
-    pdl_launch_dependents();
-    pdl_wait();
     const long long row = static_cast<long long>(blockIdx.x) * blockDim.y + threadIdx.y;
     const bool here = row < M;
     const uint8_t* src = X + row * ldx_bytes;
@@ -144,8 +142,6 @@ __device__ __forceinline__ void load_strided8(float (&v)[8], const void* X, long
 __global__ void mip_quantize_elements_kernel(int type, long long N, const void* X, long long ldx, int8_t* Q, long long ldq, float* scale) {
     __shared__ float part[kRowThreads / 32];
     __shared__ int odd[kRowThreads / 32];
-    pdl_launch_dependents();
-    pdl_wait();
     const long long row = blockIdx.x;
     float top = 0.0f;
     int bad = 0;
@@ -178,8 +174,6 @@ __global__ void mip_quantize_elements_kernel(int type, long long N, const void* 
 template <int kType, int kRows>
 __global__ void __launch_bounds__(kRowThreads)
 mip_dequantize_rows_kernel(long long M, int vectors, const int8_t* Q, long long ldq, const float* scale, uint8_t* X, long long ldx_bytes) {
-    pdl_launch_dependents();
-    pdl_wait();
     const int at = blockIdx.y * blockDim.x + threadIdx.x;
     if (at >= vectors) return;
     const long long row0 = (static_cast<long long>(blockIdx.x) * blockDim.y + threadIdx.y) * kRows;
@@ -213,8 +207,6 @@ mip_dequantize_rows_kernel(long long M, int vectors, const int8_t* Q, long long 
 }
 
 __global__ void mip_dequantize_elements_kernel(int type, long long N, const int8_t* Q, long long ldq, const float* scale, void* X, long long ldx) {
-    pdl_launch_dependents();
-    pdl_wait();
     const long long row = blockIdx.x;
     const float s = scale[row];
     for (long long j0 = static_cast<long long>(blockIdx.y) * 8 * kRowThreads + threadIdx.x; j0 < N;
@@ -232,19 +224,12 @@ bool aligned_rows(const void* p, long long pitch_bytes, int bytes) {
     return reinterpret_cast<uintptr_t>(p) % bytes == 0 && pitch_bytes % bytes == 0;
 }
 
-struct RowsLaunch {
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    RowsLaunch(dim3 grid, dim3 block, cudaStream_t stream) {
-        cfg.gridDim = grid;
-        cfg.blockDim = block;
-        cfg.stream = stream;
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-    }
-};
+// (not launched early: see launch_layer_finish)
+template <typename... Formal, typename... Actual>
+cudaError_t launch(void (*kernel)(Formal...), dim3 grid, dim3 block, cudaStream_t stream, Actual... args) {
+    kernel<<<grid, block, 0, stream>>>(args...);
+    return cudaGetLastError();
+}
 
 template <int kType>
 cudaError_t quantize_t(long long M, int vectors, const uint8_t* X, long long ldx_bytes, int8_t* Q, long long ldq, float* scale, cudaStream_t stream) {
@@ -253,10 +238,10 @@ cudaError_t quantize_t(long long M, int vectors, const uint8_t* X, long long ldx
     while (per < 4 && vectors > 1024 * per) per *= 2;
     const int threads = ((vectors + per - 1) / per + 31) / 32 * 32;
     const int rows = threads == 32 ? 4 : 1;
-    const RowsLaunch l(dim3(static_cast<unsigned>((M + rows - 1) / rows)), dim3(threads, rows), stream);
-    if (per == 1) return cudaLaunchKernelEx(&l.cfg, mip_quantize_rows_kernel<kType, 1>, M, vectors, X, ldx_bytes, Q, ldq, scale);
-    if (per == 2) return cudaLaunchKernelEx(&l.cfg, mip_quantize_rows_kernel<kType, 2>, M, vectors, X, ldx_bytes, Q, ldq, scale);
-    return cudaLaunchKernelEx(&l.cfg, mip_quantize_rows_kernel<kType, 4>, M, vectors, X, ldx_bytes, Q, ldq, scale);
+    const dim3 grid = dim3(static_cast<unsigned>((M + rows - 1) / rows)), block = dim3(threads, rows);
+    if (per == 1) return launch(mip_quantize_rows_kernel<kType, 1>, grid, block, stream, M, vectors, X, ldx_bytes, Q, ldq, scale);
+    if (per == 2) return launch(mip_quantize_rows_kernel<kType, 2>, grid, block, stream, M, vectors, X, ldx_bytes, Q, ldq, scale);
+    return launch(mip_quantize_rows_kernel<kType, 4>, grid, block, stream, M, vectors, X, ldx_bytes, Q, ldq, scale);
 }
 
 template <int kType>
@@ -267,9 +252,9 @@ cudaError_t dequantize_t(long long M, int vectors, const int8_t* Q, long long ld
     const int ty = kRowThreads / tx;
     const bool many = M * vectors >= 1 << 20;
     const long long rows = static_cast<long long>(ty) * (many ? 4 : 1);
-    const RowsLaunch l(dim3(static_cast<unsigned>((M + rows - 1) / rows), static_cast<unsigned>((vectors + tx - 1) / tx)), dim3(tx, ty), stream);
-    if (many) return cudaLaunchKernelEx(&l.cfg, mip_dequantize_rows_kernel<kType, 4>, M, vectors, Q, ldq, scale, X, ldx_bytes);
-    return cudaLaunchKernelEx(&l.cfg, mip_dequantize_rows_kernel<kType, 1>, M, vectors, Q, ldq, scale, X, ldx_bytes);
+    const dim3 grid = dim3(static_cast<unsigned>((M + rows - 1) / rows), static_cast<unsigned>((vectors + tx - 1) / tx)), block = dim3(tx, ty);
+    if (many) return launch(mip_dequantize_rows_kernel<kType, 4>, grid, block, stream, M, vectors, Q, ldq, scale, X, ldx_bytes);
+    return launch(mip_dequantize_rows_kernel<kType, 1>, grid, block, stream, M, vectors, Q, ldq, scale, X, ldx_bytes);
 }
 
 }  // namespace
@@ -285,8 +270,8 @@ cudaError_t launch_quantize_rows(int type, long long M, long long N, const void*
         if (type == kF16) return quantize_t<kF16>(M, vectors, x, ldx_bytes, Q, ldq, scale, stream);
         return quantize_t<kBF16>(M, vectors, x, ldx_bytes, Q, ldq, scale, stream);
     }
-    const RowsLaunch l(dim3(static_cast<unsigned>(M)), dim3(kRowThreads), stream);
-    return cudaLaunchKernelEx(&l.cfg, mip_quantize_elements_kernel, type, N, X, ldx, Q, ldq, scale);
+    const dim3 grid = dim3(static_cast<unsigned>(M)), block = dim3(kRowThreads);
+    return launch(mip_quantize_elements_kernel, grid, block, stream, type, N, X, ldx, Q, ldq, scale);
 }
 
 cudaError_t launch_dequantize_rows(int type, long long M, long long N, const int8_t* Q, long long ldq,
@@ -300,8 +285,8 @@ cudaError_t launch_dequantize_rows(int type, long long M, long long N, const int
         return dequantize_t<kBF16>(M, vectors, Q, ldq, scale, x, ldx_bytes, stream);
     }
     const long long parts = (N + 8 * kRowThreads - 1) / (8 * kRowThreads);
-    const RowsLaunch l(dim3(static_cast<unsigned>(M), static_cast<unsigned>(parts < 64 ? parts : 64)), dim3(kRowThreads), stream);
-    return cudaLaunchKernelEx(&l.cfg, mip_dequantize_elements_kernel, type, N, Q, ldq, scale, X, ldx);
+    const dim3 grid = dim3(static_cast<unsigned>(M), static_cast<unsigned>(parts < 64 ? parts : 64)), block = dim3(kRowThreads);
+    return launch(mip_dequantize_elements_kernel, grid, block, stream, type, N, Q, ldq, scale, X, ldx);
 }
 
 }  // namespace mip
