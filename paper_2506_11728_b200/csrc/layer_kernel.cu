@@ -90,8 +90,8 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
         cluster_wait();
     }
     tc_fence_after();
-    pdl_launch_dependents();
     pdl_wait();          // from here on global memory is touched
+    pdl_launch_dependents();      // (only now: one kernel at a time waits for another)
     const uint32_t tmem_base = *tmem_slot;
     const int total_units = layer_units(p);
     const uint64_t budget = p.wait_budget_ns;

@@ -80,7 +80,6 @@ mip_layer_stream_kernel(const __grid_constant__ LayerParams p) {
     __syncthreads();
     tc_fence_after();
     if (split > 1) cluster_arrive();       // "this CTA has started": awaited before anything is sent to it
-    pdl_launch_dependents();
     const uint32_t tmem_base = *tmem_slot;
     const uint64_t budget = p.wait_budget_ns;
     const int share = (p.k_blocks + split - 1) / split;
@@ -108,6 +107,7 @@ mip_layer_stream_kernel(const __grid_constant__ LayerParams p) {
         }
         __syncwarp();
         pdl_wait();
+        pdl_launch_dependents();      // (only now: one kernel at a time waits for another)
         uint32_t s = 0, phase = 0;
         for (int i = 0; i < n_kb; ++i) {
             if (i >= p.stages && !mbar_wait_warp(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) break;
@@ -124,6 +124,7 @@ mip_layer_stream_kernel(const __grid_constant__ LayerParams p) {
         }
     } else {
         pdl_wait();
+        pdl_launch_dependents();
     }
     __syncwarp();
     if (warp == 1 && n_kb > 0) {
