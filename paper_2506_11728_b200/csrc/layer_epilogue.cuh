@@ -99,29 +99,6 @@ __device__ __forceinline__ void unpack2(uint32_t w, bool f16, float& lo, float& 
     }
 }
 
-// Two binary32 values in a register pair, for the packed instructions.
-__device__ __forceinline__ uint64_t pack_f2(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpack_f2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 // Two int32 sums as binary32, rounded to nearest even.  kByParts: without the conversion instruction, which shares its
 // quarter-rate unit with the exponential and the reciprocal: the upper half (biased by 2^15) and the lower half are put
 // behind the exponent of 2^23, both differences are exact, and one fused multiply-add rounds once, like the conversion.
@@ -228,54 +205,60 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[kN], const uin
 #pragma unroll
     for (int g = 0; g < kPieces; ++g) {
         const Inputs in = fetch(g);
-        float r[kPer], y[kPer], y2[kPer];
+        uint64_t r[kPer / 2], y[kPer / 2], y2[kPer / 2];           // two columns each
         if constexpr (kOp != kOpGated) {
-            if constexpr (kWide) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) r[j] = __uint_as_float(in.r[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) unpack2(in.r[j], f16, r[2 * j], r[2 * j + 1]);
+            for (int j = 0; j < kPer / 2; ++j) {
+                if constexpr (kWide) {
+                    r[j] = pack_f2(__uint_as_float(in.r[2 * j]), __uint_as_float(in.r[2 * j + 1]));
+                } else {
+                    float lo, hi;
+                    unpack2(in.r[j], f16, lo, hi);
+                    r[j] = pack_f2(lo, hi);
+                }
             }
         }
-        if constexpr (kOp == kOpProduct) {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) y[j] = __uint_as_float(v0[g * kPer + j]) + r[j];
-        } else {
-            // two columns at a time: (sum * row scale) * column scale
-#pragma unroll
-            for (int j = 0; j < kPer; j += 2) {
-                float z0[2], z1[2];
+        for (int j = 0; j < kPer / 2; ++j) {
+            const int v = g * kPer + 2 * j;
+            if constexpr (kOp == kOpProduct) {
+                y[j] = add_f2(pack_f2(__uint_as_float(v0[v]), __uint_as_float(v0[v + 1])), r[j]);
+            } else {
                 constexpr bool kByParts = kAct >= kActGelu;        // the activation keeps the quarter-rate unit busy
-                unpack_f2(mul_f2(mul_f2(ints_to_f2<kByParts>(v0[g * kPer + j], v0[g * kPer + j + 1]), as2), pack_f2(in.b0[j], in.b0[j + 1])),
-                          z0[0], z0[1]);
-                if constexpr (kOp != kOpLinear)
-                    unpack_f2(mul_f2(mul_f2(ints_to_f2<kByParts>(v1[g * kPer + j], v1[g * kPer + j + 1]), as2), pack_f2(in.b1[j], in.b1[j + 1])),
-                              z1[0], z1[1]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (kOp == kOpLinear) {
-                        y[j + h] = activation<kAct>(z0[h] + in.b1[j + h]) + r[j + h];
-                    } else if (kOp == kOpGated) {
-                        y[j + h] = activation<kAct>(z0[h]) * z1[h];
+                const uint64_t s0 = mul_f2(ints_to_f2<kByParts>(v0[v], v0[v + 1]), as2);
+                const uint64_t b0 = pack_f2(in.b0[2 * j], in.b0[2 * j + 1]), b1 = pack_f2(in.b1[2 * j], in.b1[2 * j + 1]);
+                if constexpr (kOp == kOpLinear) {
+                    y[j] = add_f2(activation_f2<kAct>(fma_f2(s0, b0, b1)), r[j]);
+                } else {
+                    const uint64_t z1 = mul_f2(mul_f2(ints_to_f2<kByParts>(v1[v], v1[v + 1]), as2), b1);
+                    if constexpr (kOp == kOpGated) {
+                        y[j] = mul_f2(activation_f2<kAct>(mul_f2(s0, b0)), z1);
                     } else {
-                        float value, slope;
-                        activation_slope<kAct>(z0[h], value, slope);
-                        y[j + h] = r[j + h] * z1[h] * slope;
-                        y2[j + h] = r[j + h] * value;
+                        uint64_t value, slope;
+                        activation_slope_f2<kAct>(mul_f2(s0, b0), value, slope);
+                        y[j] = mul_f2(mul_f2(r[j], z1), slope);
+                        y2[j] = mul_f2(r[j], value);
                     }
                 }
             }
         }
-        uint32_t o[4];
+        const auto put = [&](uint32_t at, const uint64_t (&x)[kPer / 2]) {
+            uint32_t o[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y[j]) : pack2(y[2 * j % kPer], y[(2 * j + 1) % kPer], f16);
-        st_shared_v4(slot_piece<kWide>(slot, row, piece0 + g), o);
-        if (kOp == kOpGatedGrad) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = kWide ? __float_as_uint(y2[j]) : pack2(y2[2 * j % kPer], y2[(2 * j + 1) % kPer], f16);
-            st_shared_v4(slot_piece<kWide>(slot2, row, piece0 + g), o);
-        }
+            for (int j = 0; j < kPer / 2; ++j) {
+                float lo, hi;
+                unpack_f2(x[j], lo, hi);
+                if constexpr (kWide) {
+                    o[2 * j] = __float_as_uint(lo);
+                    o[2 * j + 1] = __float_as_uint(hi);
+                } else {
+                    o[j] = pack2(lo, hi, f16);
+                }
+            }
+            st_shared_v4(at, o);
+        };
+        put(slot_piece<kWide>(slot, row, piece0 + g), y);
+        if constexpr (kOp == kOpGatedGrad) put(slot_piece<kWide>(slot2, row, piece0 + g), y2);
     }
 }
 

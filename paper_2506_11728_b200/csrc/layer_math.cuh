@@ -90,6 +90,95 @@ __device__ __forceinline__ void activation_slope(float x, float& value, float& s
     }
 }
 
+// Two binary32 values in a register pair, for the packed instructions: half the issue slots.
+__device__ __forceinline__ uint64_t pack_f2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack_f2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t both(float a) { return pack_f2(a, a); }
+template <typename F>
+__device__ __forceinline__ uint64_t each(uint64_t v, F&& f) {
+    float a, b;
+    unpack_f2(v, a, b);
+    return pack_f2(f(a), f(b));
+}
+// 1 / (1 + 2^x)
+__device__ __forceinline__ uint64_t sigmoid_exp2_f2(uint64_t x) {
+    return each(add_f2(each(x, fast_exp2), both(1.0f)), fast_rcp);
+}
+
+__device__ __forceinline__ uint64_t normal_cdf_f2(uint64_t x, uint64_t& gauss) {
+    const uint64_t y = each(x, [](float v) { return fabsf(v); });
+    gauss = each(mul_f2(mul_f2(x, x), both(-0.5f * kLog2E)), fast_exp2);
+    const uint64_t t = each(fma_f2(y, both(0.3275911f * 0.70710678118654752f), both(1.0f)), fast_rcp);
+    uint64_t q = both(0.5f * 1.061405429f);
+    q = fma_f2(q, t, both(0.5f * -1.453152027f));
+    q = fma_f2(q, t, both(0.5f * 1.421413741f));
+    q = fma_f2(q, t, both(0.5f * -0.284496736f));
+    q = fma_f2(q, t, both(0.5f * 0.254829592f));
+    const uint64_t tail = mul_f2(mul_f2(q, t), gauss);
+    const uint64_t rest = fma_f2(tail, both(-1.0f), both(1.0f));
+    float x0, x1, t0, t1, r0, r1;
+    unpack_f2(x, x0, x1);
+    unpack_f2(tail, t0, t1);
+    unpack_f2(rest, r0, r1);
+    return pack_f2(x0 < 0.0f ? t0 : r0, x1 < 0.0f ? t1 : r1);
+}
+
+// The same formulas as activation() and activation_slope(), two values at a time.
+template <int kAct>
+__device__ __forceinline__ uint64_t activation_f2(uint64_t x) {
+    if constexpr (kAct == kActSilu) return mul_f2(x, sigmoid_exp2_f2(mul_f2(x, both(-kLog2E))));
+    else if constexpr (kAct == kActGeluTanh)
+        return mul_f2(x, sigmoid_exp2_f2(mul_f2(x, fma_f2(mul_f2(x, x), both(-kLog2E * kGeluC * kGeluC3), both(-kLog2E * kGeluC)))));
+    else if constexpr (kAct == kActGelu) {
+        uint64_t gauss;
+        return mul_f2(x, normal_cdf_f2(x, gauss));
+    } else if constexpr (kAct == kActRelu) return each(x, [](float v) { return v < 0.0f ? 0.0f : v; });
+    else return x;
+}
+template <int kAct>
+__device__ __forceinline__ void activation_slope_f2(uint64_t x, uint64_t& value, uint64_t& slope) {
+    if constexpr (kAct == kActSilu) {
+        const uint64_t e = sigmoid_exp2_f2(mul_f2(x, both(-kLog2E)));
+        value = mul_f2(x, e);
+        slope = fma_f2(value, fma_f2(e, both(-1.0f), both(1.0f)), e);
+    } else if constexpr (kAct == kActGeluTanh) {
+        const uint64_t xx = mul_f2(x, x);
+        const uint64_t e = sigmoid_exp2_f2(mul_f2(x, fma_f2(xx, both(-kLog2E * kGeluC * kGeluC3), both(-kLog2E * kGeluC))));
+        value = mul_f2(x, e);
+        slope = fma_f2(mul_f2(value, fma_f2(e, both(-1.0f), both(1.0f))), fma_f2(xx, both(3.0f * kGeluC * kGeluC3), both(kGeluC)), e);
+    } else if constexpr (kAct == kActGelu) {
+        uint64_t gauss;
+        const uint64_t cdf = normal_cdf_f2(x, gauss);
+        value = mul_f2(x, cdf);
+        slope = fma_f2(mul_f2(x, gauss), both(0.3989422804014327f), cdf);
+    } else if constexpr (kAct == kActRelu) {
+        value = each(x, [](float v) { return v < 0.0f ? 0.0f : v; });
+        slope = each(x, [](float v) { return v > 0.0f ? 1.0f : 0.0f; });
+    } else {
+        value = x;
+        slope = both(1.0f);
+    }
+}
+
 __device__ __forceinline__ float load_element(const void* base, long long i, int type) {
     if (type == kF32) return static_cast<const float*>(base)[i];
     if (type == kF16) return __half2float(static_cast<const __half*>(base)[i]);
