@@ -306,7 +306,7 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-            if (kPair && !leader) mbar_arrive_remote(bar_tempty + 8u * acc, 0);
+            if (kPair && !leader) mbar_arrive_remote_fenced(bar_tempty + 8u * acc, 0);
             else mbar_arrive(bar_tempty + 8u * acc);
         }
     }
@@ -410,6 +410,16 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
         const uint32_t t_up = t_row + static_cast<uint32_t>(p.block_n >> 1);
+        // the accumulator is the MMA warp's again once this warp has read its last columns of it
+        const auto release = [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (kPair && !leader) mbar_arrive_remote_fenced(bar_tempty + 8u * acc, 0);
+                else mbar_arrive(bar_tempty + 8u * acc);
+            }
+        };
+        if (n_slots == 0) release();
         bool gave_up = false;
         for (int sl = 0; sl < n_slots; ++sl, ++slot_no) {
             const int c0 = slot_col(sl);
@@ -448,12 +458,14 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                     tmem_ld_32x16(t_row + c0 + c, v);
                     tmem_ld_32x16(t_up + c0 + c, v1);
                     tmem_ld_wait_for16(v, v1);
+                    if (sl + 1 == n_slots && c + 16 == kSlotCols) release();
                     with_activation(p.act, [&](auto act) {
                         finish_chunk<kOp, decltype(act)::value, kWide, 16>(v, v1, as_here, my_cols, slot, slot2, lane, c, has_r, f16);
                     });
                 }
             } else {
                 tmem_ld_wait_for(v);
+                if (sl + 1 == n_slots) release();
                 with_activation(kOp == kOpProduct ? kActNone : p.act, [&](auto act) {
                     finish_chunk<kOp, decltype(act)::value, kWide, 32>(v, v, as_here, my_cols, slot, slot2, lane, 0, has_r, f16);
                 });
@@ -481,12 +493,6 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
             }
         }
         if (gave_up) break;
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-            if (kPair && !leader) mbar_arrive_remote(bar_tempty + 8u * acc, 0);
-            else mbar_arrive(bar_tempty + 8u * acc);
-        }
     }
     // unwinding: tiles still on their way into the slots
     for (uint32_t i = slot_no; r_tma && i < loads; ++i) {

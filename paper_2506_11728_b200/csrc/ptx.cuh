@@ -73,8 +73,9 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar, uint32_t cta) {
         "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n\t}"
         ::"r"(bar), "r"(cta) : "memory");
 }
-// Arrives on CTA `cta`'s barrier for writes to the arriving CTA's OWN shared memory that a proxy fence has already
-// made visible to the tensor core: nothing is left for the arrival itself to order beyond its own CTA.  (The
+// Arrives on CTA `cta`'s barrier for accesses to the arriving CTA's OWN shared or tensor memory that a fence has
+// already ordered with the tensor core (fence.proxy.async for writes to shared memory; tcgen05.wait::ld and
+// tcgen05.fence for reads of tensor memory): nothing is left for the arrival itself to order beyond its own CTA.  (The
 // cluster-scope release of mbar_arrive_remote, behind a warp's shared-memory stores, costs it ~1300 clocks.)
 __device__ __forceinline__ void mbar_arrive_remote_fenced(uint32_t bar, uint32_t cta) {
     asm volatile(
