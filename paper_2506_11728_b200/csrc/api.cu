@@ -1385,7 +1385,7 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
             const double kb_clk = std::max(pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn, (row_tiles < 8 ? 3600.0 : 2000.0) / stages);
             // the schedulers' time for the tile's outputs, and at least each warp's rounds of slots
             const double rounds = (out_n / 32 + warps / 4 - 1) / (warps / 4);
-            const double per_col = a.op == kOpGatedGrad ? 42.0 : (gated ? 30.0 : (a.act >= MIPGEMM_ACT_GELU ? 27.0 : 14.0));
+            const double per_col = a.op == kOpGatedGrad ? 46.0 : (gated ? 28.0 : (a.act >= MIPGEMM_ACT_GELU ? 26.0 : 14.0));
             const double epi = std::max(out_n * per_col, rounds * (a.op == kOpGatedGrad ? 2600.0 : 1700.0)) * (unaligned ? 2.5 : 1.0);
             for (int split = 1; split <= kMaxSplit; ++split) {
                 // K in `split` shares whose partial sums a second kernel adds: only while there are more SMs than tiles

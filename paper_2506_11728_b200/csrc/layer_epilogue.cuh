@@ -99,18 +99,10 @@ __device__ __forceinline__ void unpack2(uint32_t w, bool f16, float& lo, float& 
     }
 }
 
-// Two int32 sums as binary32, rounded to nearest even.  kByParts: without the conversion instruction, which shares its
-// quarter-rate unit with the exponential and the reciprocal: the upper half (biased by 2^15) and the lower half are put
-// behind the exponent of 2^23, both differences are exact, and one fused multiply-add rounds once, like the conversion.
-template <bool kByParts>
+// Two int32 sums as binary32, rounded to nearest even.  (The conversion instruction.  Halves behind the exponent of 2^23
+// and one fused multiply-add give the same float on other pipes, and cost the epilogues 15 %.)
 __device__ __forceinline__ uint64_t ints_to_f2(uint32_t a, uint32_t b) {
-    if (!kByParts) return pack_f2(__int2float_rn(static_cast<int>(a)), __int2float_rn(static_cast<int>(b)));
-    constexpr uint32_t kExp = 0x4B000000u;
-    const uint64_t lo = pack_f2(__uint_as_float(__byte_perm(a, kExp, 0x7410)), __uint_as_float(__byte_perm(b, kExp, 0x7410)));
-    const uint64_t hi = pack_f2(__uint_as_float(__byte_perm(a ^ 0x80000000u, kExp, 0x7432)), __uint_as_float(__byte_perm(b ^ 0x80000000u, kExp, 0x7432)));
-    const uint64_t lo_exact = add_f2(lo, pack_f2(-8388608.0f, -8388608.0f));
-    const uint64_t hi_exact = add_f2(hi, pack_f2(-8421376.0f, -8421376.0f));       // 2^23 + 2^15
-    return fma_f2(hi_exact, pack_f2(65536.0f, 65536.0f), lo_exact);
+    return pack_f2(__int2float_rn(static_cast<int>(a)), __int2float_rn(static_cast<int>(b)));
 }
 
 // A slot between shared and global memory, one row per instruction (lane = column), element by element: any alignment.
@@ -224,13 +216,12 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[kN], const uin
             if constexpr (kOp == kOpProduct) {
                 y[j] = add_f2(pack_f2(__uint_as_float(v0[v]), __uint_as_float(v0[v + 1])), r[j]);
             } else {
-                constexpr bool kByParts = kAct >= kActGelu;        // the activation keeps the quarter-rate unit busy
-                const uint64_t s0 = mul_f2(ints_to_f2<kByParts>(v0[v], v0[v + 1]), as2);
+                const uint64_t s0 = mul_f2(ints_to_f2(v0[v], v0[v + 1]), as2);
                 const uint64_t b0 = pack_f2(in.b0[2 * j], in.b0[2 * j + 1]), b1 = pack_f2(in.b1[2 * j], in.b1[2 * j + 1]);
                 if constexpr (kOp == kOpLinear) {
                     y[j] = add_f2(activation_f2<kAct>(fma_f2(s0, b0, b1)), r[j]);
                 } else {
-                    const uint64_t z1 = mul_f2(mul_f2(ints_to_f2<kByParts>(v1[v], v1[v + 1]), as2), b1);
+                    const uint64_t z1 = mul_f2(mul_f2(ints_to_f2(v1[v], v1[v + 1]), as2), b1);
                     if constexpr (kOp == kOpGated) {
                         y[j] = mul_f2(activation_f2<kAct>(mul_f2(s0, b0)), z1);
                     } else {
