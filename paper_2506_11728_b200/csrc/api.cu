@@ -1354,6 +1354,10 @@ int layer_stages(const LayerArgs& a, int pair, int block_n, bool raw) {
     return std::min(kMaxStages, (kSmemBudget - fixed) / ((kBlockM + (pair ? block_n / 2 : block_n)) * 128));
 }
 
+// What a plan with another K split than the one asked for by mipgemm_set_tuning is charged: it is taken only where the
+// size does not allow that split.
+constexpr double kNotAsked = 1e20;
+
 // Tile shape of the dense layer kernel: the main loop's cost per k-block is that of the plain product's kernel
 // (plan_cost_us); a tile's epilogue runs beside the next tile's main loop, the last one is exposed.
 LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
@@ -1400,7 +1404,7 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
                 double clk = (waves - 1) * period + main + epi + (pair ? 1900.0 : 0.0);
                 // (a launch, and the planes written and read at the L2's pace)
                 if (split > 1) clk += 5500.0 + 8.0 * split * static_cast<double>(a.M) * a.N * (gated ? 2 : 1) / 3500.0;
-                if (tun.split_k) { if (split != std::min(tun.split_k, k_blocks)) continue; }
+                if (tun.split_k && split != tun.split_k) clk += kNotAsked;
                 if (clk < best_clk) {
                     best_clk = clk;
                     best = LayerPlan{pair, bn, static_cast<int>(std::min(tiles * split, slots)) * (pair ? 2 : 1), 0, split, 0};
@@ -1729,12 +1733,12 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
                 if (split > 1 && (dev->lent || k_blocks / split < 4)) break;
                 const int share = (k_blocks + split - 1) / split;
                 if ((k_blocks + share - 1) / share != split) continue;
-                if (tun.split_k && split != std::min(tun.split_k, k_blocks)) continue;
                 // a stage costs a CTA the same 670 clocks in either form (its warps convert 128 columns x 64 k); a pair does
                 // four times a single CTA's products with it
                 const long long waves = (tiles_of(pair) * split + slots - 1) / slots;
                 double clk = static_cast<double>(waves) * (share * 670.0 + 1500.0) + 4000.0 + (pair ? 1900.0 : 0.0);
                 if (split > 1) clk += 5500.0 + 8.0 * split * static_cast<double>(a.M) * a.N / 3500.0;
+                if (tun.split_k && split != tun.split_k) clk += kNotAsked;
                 if (clk < best_clk) {
                     best_clk = clk;
                     pl.pair = pair;
