@@ -392,6 +392,18 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
                     tma_prefetch_l2_2d(&p.tmap_r, next.n0 + slot_col(i), next.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32);
             __syncwarp();
         }
+        // the same for a residual that is read element by element: what the buffers hold, before the accumulator is waited for
+        const auto fill = [&] {
+            slot_rows_in<kWide>(my_slots + (loads % kBuffers) * kSlotStride, p.R, p.ldr, row0, tc.n0 + slot_col(asked), p.M, p.N, lane);
+            ++asked;
+            ++loads;
+        };
+        const bool r_rows = has_r && !r_tma;
+        if (r_rows && n_slots > 0) {
+            if (c_tma && elect_one()) tma_store_wait_read<0>();
+            __syncwarp();
+            while (asked < kBuffers && asked < n_slots) fill();
+        }
         if (n_slots == 0 && more) {
             as = fetch_row(next);
             fetch_columns(next, 0);
@@ -423,7 +435,7 @@ __device__ __forceinline__ void layer_epilogue(const LayerParams& p, uint32_t sl
             if (!r_tma) {
                 if (c_tma && elect_one()) tma_store_wait_read<kBuffers - 1>();
                 __syncwarp();
-                if (has_r) slot_rows_in<kWide>(slot, p.R, p.ldr, row0, tc.n0 + c0, p.M, p.N, lane);
+                if (r_rows && asked == sl) fill();
             }
             if (kOp != kOpProduct) {
                 __syncwarp();                                  // (the last slot's column vectors have been read)
