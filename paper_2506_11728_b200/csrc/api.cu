@@ -1472,10 +1472,11 @@ void layer_store(const PlanKey& key, const LayerParams& p, const LayerPlan& pl) 
     e.pl = pl;
 }
 
-int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool cacheable) {
+// as_passed: the operands are the caller's own, not re-pitched copies.
+int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool as_passed) {
     LayerParams p;
     LayerPlan pl;
-    cacheable = cacheable && plan_cache_enabled();
+    const bool cacheable = as_passed && plan_cache_enabled();
     PlanKey key;
     bool hit = false;
     if (cacheable) {
@@ -1565,10 +1566,11 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool ca
     p.bias = a.bias;
     cudaError_t e;
     if (pl.few) {
-        // (a promise about the weights, not part of the plan either)
-        p.b_constant = g_weights_constant.load() ||
+        // (a promise about the weights, not part of the plan either; not about re-pitched copies, which the kernel before
+        // this one writes)
+        p.b_constant = as_passed && (g_weights_constant.load() ||
                        (inside_constant_range(a.B0, static_cast<size_t>(a.N - 1) * a.ldb0 + a.K) &&
-                        (a.op == kOpLinear || inside_constant_range(a.B1, static_cast<size_t>(a.N - 1) * a.ldb1 + a.K)));
+                        (a.op == kOpLinear || inside_constant_range(a.B1, static_cast<size_t>(a.N - 1) * a.ldb1 + a.K))));
         e = launch_layer_stream(p, a.op, pl.grid, stream);
         tl_last_path = MIPGEMM_PATH_SKINNY | (pl.split > 1 ? MIPGEMM_PATH_SPLITK : 0);
     } else if (pl.split > 1) {
