@@ -86,7 +86,7 @@ typedef enum {
     MIPGEMM_PATH_NONE = 0,
     MIPGEMM_PATH_DENSE = 1,       /* TMA + tcgen05.mma.kind::i8, one CTA per tile            */
     MIPGEMM_PATH_DENSE_PAIR = 2,  /* same, CTA pairs (cta_group::2)                          */
-    MIPGEMM_PATH_SKINNY = 3,      /* M <= 16 streaming kernel                                */
+    MIPGEMM_PATH_SKINNY = 3,      /* streaming kernel: M <= 16; layer operators up to 64 tokens */
     MIPGEMM_PATH_TRIVIAL = 4,     /* K == 0 fill or empty problem                            */
     MIPGEMM_PATH_REPACK = 0x100,  /* flag: an operand was re-pitched into scratch first      */
     MIPGEMM_PATH_SPLITK = 0x200,  /* flag: K was split over CTAs (partials added exactly)    */
@@ -294,7 +294,7 @@ int mipgemm_host_u8s8s32(int64_t M, int64_t N, int64_t K,
  * Who needs it: callers that are not allowed to reach the CUDA allocator -- code embedded
  * in a memory-planned inference runtime that owns the whole device, real-time loops that
  * must never block in cudaMalloc/cudaFree, plug-ins running under another framework's
- * memory pool.  The other entry points take scratch memory with cudaMallocAsync whenever
+ * memory pool.  The other entry points take scratch memory (see "Scratch memory") whenever
  * an operand has to be re-pitched for the tensor-memory-accelerator (base or pitch not a
  * multiple of 16 bytes) and allocate one status word per device on first use; this one
  * calls no allocating routine at all.  Its re-pitching scratch is a fixed array of
@@ -360,7 +360,10 @@ int mipgemm_release_staging(void);
  * in int32 (the K limits of mipgemm_s8s8s32 hold), everything behind them is computed in binary32 and
  * rounded once, to nearest even, when it is stored.  Scale vectors are float32, 4-byte aligned; NULL
  * stands for all ones.  Operands with 16-byte aligned bases and pitches are read in place, other 8-bit
- * operands are re-pitched into scratch memory first.  Inputs and outputs must not overlap, except where
+ * operands are re-pitched into scratch memory first.  Sums along a long K with few tiles may be taken in
+ * parts that meet in scratch memory of the library's own (always added in the same order); with a lent
+ * workspace they are not, so that a call needs what its operands' re-pitching needs (M, N or K rows of a
+ * multiple of 16 bytes each, rounded up to 256).  Inputs and outputs must not overlap, except where
  * stated.  Empty outputs (M == 0 or N == 0) are no-ops; K == 0 means that every sum is 0.
  */
 typedef enum { MIPGEMM_TYPE_F32 = 0, MIPGEMM_TYPE_F16 = 1, MIPGEMM_TYPE_BF16 = 2 } mipgemm_type_t;
@@ -502,8 +505,8 @@ int mipgemm_probe_i8_peak(int iters, int *grid_out, double *ops_per_launch,
                           int32_t *sink, void *stream);
 
 /*
- * A promise about the weights of the skinny-M (GEMV-like, paper Section 7.2 batch-1) calls, process
- * wide, off by default: with on != 0 the caller guarantees that the B operand of every later call with
+ * A promise about the weights of the skinny-M (GEMV-like, paper Section 7.2 batch-1) calls, those of
+ * mipgemm_*_linear, _gated and _gated_grad with as few tokens among them, process wide, off by default: with on != 0 the caller guarantees that the B operand of every later call with
  * M <= 16 is not written by any work still pending on the call's stream when it is enqueued (the
  * usual case: B holds inference weights).  The streaming kernel then starts fetching B while the
  * previous kernel on the stream is still draining (programmatic dependent launch); A is read and C is

@@ -1566,9 +1566,9 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool as
     p.bias = a.bias;
     cudaError_t e;
     if (pl.few) {
-        // (a promise about the weights, not part of the plan either; not about re-pitched copies, which the kernel before
-        // this one writes)
-        p.b_constant = as_passed && (g_weights_constant.load() ||
+        // (a promise about the weights, not part of the plan either; it is given for calls of up to 16 tokens, and not about
+        // re-pitched copies, which the kernel before this one writes)
+        p.b_constant = as_passed && a.M <= 16 && (g_weights_constant.load() ||
                        (inside_constant_range(a.B0, static_cast<size_t>(a.N - 1) * a.ldb0 + a.K) &&
                         (a.op == kOpLinear || inside_constant_range(a.B1, static_cast<size_t>(a.N - 1) * a.ldb1 + a.K))));
         e = launch_layer_stream(p, a.op, pl.grid, stream);
