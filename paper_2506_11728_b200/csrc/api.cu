@@ -1580,11 +1580,10 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool as
         int st = scratch.reserve(static_cast<size_t>(pl.split) * planes.plane_rows * planes.pitch * 4);
         if (st != MIPGEMM_OK) return st;
         planes.base = scratch.base;
-        st = encode_slots(&p.tmap_c, scratch.base, MIPGEMM_TYPE_F32, pl.split * planes.plane_rows, planes.pitch, planes.pitch);
-        if (st != MIPGEMM_OK) return st;
+        p.C = scratch.base;
+        p.ldc = planes.pitch;
         p.R = nullptr;
-        p.r_tma = 0;
-        p.c_tma = 1;
+        p.r_tma = p.c_tma = 0;
         e = launch_layer(p, gated ? kOpRawGated : kOpRaw, pl.pair, pl.grid, stream);
         ++g_launches;
         if (e == cudaSuccess) e = launch_layer_finish(a, planes, stream);
@@ -1793,11 +1792,10 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
         int st = scratch.reserve(static_cast<size_t>(pl.split) * planes.plane_rows * planes.pitch * 4);
         if (st != MIPGEMM_OK) return st;
         planes.base = scratch.base;
-        st = encode_slots(&p.tmap_c, scratch.base, MIPGEMM_TYPE_F32, pl.split * planes.plane_rows, planes.pitch, planes.pitch);
-        if (st != MIPGEMM_OK) return st;
+        p.C = scratch.base;
+        p.ldc = planes.pitch;
         p.R = nullptr;
-        p.r_tma = 0;
-        p.c_tma = 1;
+        p.r_tma = p.c_tma = 0;
         e = launch_product(p, a.a_order, pl.pair, 1, pl.grid, stream);
         ++g_launches;
         if (e == cudaSuccess) e = launch_product_finish(a, planes, stream);

@@ -10,10 +10,14 @@
 // instruction.  Scales and bias of a slot's columns are fetched one lane per column one slot ahead and broadcast
 // through shared memory.
 //
-// What bounds it.  An output of a gated or activated layer takes 25 to 30 instructions and two on the quarter-rate
-// unit; beside a short main loop that is the kernel's time, and what counts is how well the schedulers are fed: one
-// warp each issues every fifth clock or so, so there are two or four per scheduler, which take the slots of a tile by
-// turns.
+// What bounds it.  An output of an activated layer takes 14 to 28 scheduler clocks for a warp's 32 (a gradient's two 46),
+// the exponential, the reciprocal and the conversions from integers among them on quarter- and half-rate units; beside a
+// short main loop that is the kernel's time, and what counts is how well the schedulers are fed: one warp each issues
+// every fifth clock or so, so there are two or four per scheduler, which take the slots of a tile by turns.  Measured:
+// linear 16384 x 4096 x 1024 gelu bf16 81 us, 62 without the activation.  Where the pitch of C is not a multiple of 16
+// bytes the element form makes that two to three times as much (linear 11957 x 3640 / 3641 x 112 bf16: 64 / 144 us):
+// every row of a slot begins and ends inside a 32-byte sector, and the memory system completes partly written sectors
+// one by one.
 #pragma once
 #include "internal.h"
 #include "layer_math.cuh"
@@ -34,7 +38,7 @@ constexpr int product_epi_warps(bool wide) { return wide ? 4 : 8; }
 // Slots per warp: two where there is something to wait for or nothing else to do meanwhile; gated forms have half the
 // output columns (gradient: two buffers per slot, one per result; the incoming gradient lies in the first), the
 // product's pipeline stages need the room.
-constexpr int slot_count(int op) { return op == kOpLinear || op == kOpRaw ? 2 : 1; }
+constexpr int slot_count(int op) { return op == kOpRaw || op == kOpRawGated ? 0 : (op == kOpLinear ? 2 : 1); }
 constexpr int slot_stride(int op, bool wide) { return op == kOpGatedGrad ? 2 * slot_bytes(wide) : slot_bytes(wide); }
 constexpr int slot_bytes_per_warp(int op, bool wide) { return slot_count(op) * slot_stride(op, wide); }
 
@@ -253,17 +257,18 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[kN], const uin
     }
 }
 
-// Partial sums as they are (32-bit words) to the unit's plane, by TMA tile stores.  kSlots: slots of the warp's staging;
-// kHalves: the accumulator holds two projections side by side; kSubs warps take the slots of a tile by turns, this one
+// Partial sums as they are (32-bit words) to the unit's plane.  A lane has a row's 32 columns and stores them as four whole
+// 32-byte sectors, straight from registers: as fast as staging and TMA tile stores (product 848 x 5664 x 18608 bf16 193 /
+// 196 us, 1024 x 1024 x 8192 26.8 / 26.9), and the staging's shared memory goes to pipeline stages.
+// kHalves: the accumulator holds two projections side by side; kSubs warps take a tile's columns by turns of 32, this one
 // every kSubs-th from `sub`.
-template <bool kPair, int kSlots, bool kHalves, int kSubs>
-__device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_slots, int sub, uint32_t bar_tfull, uint32_t bar_tempty,
+template <bool kPair, bool kHalves, int kSubs>
+__device__ __forceinline__ void raw_epilogue(const LayerParams& p, int sub, uint32_t bar_tfull, uint32_t bar_tempty,
                                              volatile uint32_t* abort_flag, uint32_t tmem_base, int q, int lane, uint32_t cta_rank,
                                              int first_unit, int unit_stride) {
     constexpr int kRowsPerTile = kPair ? 2 * kBlockM : kBlockM;
     const bool leader = cta_rank == 0;
     const int total_units = layer_units(p);
-    uint32_t slot_no = 0;
     int t = 0;
     for (int unit = first_unit; unit < total_units; unit += unit_stride, ++t) {
         const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
@@ -273,26 +278,17 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
         if (!mbar_wait_warp(bar_tfull + 8u * acc, acc_phase, abort_flag, p.wait_budget_ns)) break;
         tc_fence_after();
         const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * p.block_n;
+        // (planes have whole blocks of 32 rows and columns)
+        int32_t* const out = static_cast<int32_t*>(p.C) + static_cast<long long>(tc.plane + row0 + lane) * p.ldc + tc.n0;
         for (int c0 = 32 * sub; c0 < p.block_n && row0 < p.M; c0 += 32 * kSubs) {
             const bool second = kHalves && c0 >= p.out_n;
             const int c = second ? c0 - p.out_n : c0;
             if (c >= n_here) continue;
             uint32_t v[32];
-            __syncwarp();                                      // tcgen05.ld wants the whole warp: the elected lane is back
             tmem_ld_32x32(t_row + c0, v);
-            if (elect_one()) tma_store_wait_read<kSlots - 1>();
-            __syncwarp();
             tmem_ld_wait_for(v);
-            const uint32_t slot = my_slots + (slot_no % kSlots) * slot_bytes(true);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) st_shared_v4(slot_piece<true>(slot, lane, j), &v[4 * j]);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (elect_one()) {
-                tma_store_2d(&p.tmap_c, slot, (second ? p.plane_second : 0) + tc.n0 + c, tc.plane + row0);
-                tma_store_commit();
-            }
-            ++slot_no;
+            for (int j = 0; j < 4; ++j) st_global_v8(out + (second ? p.plane_second : 0) + c + 8 * j, &v[8 * j]);
         }
         tc_fence_before();
         __syncwarp();
@@ -301,8 +297,6 @@ __device__ __forceinline__ void raw_epilogue(const LayerParams& p, uint32_t my_s
             else mbar_arrive(bar_tempty + 8u * acc);
         }
     }
-    if (elect_one()) tma_store_wait<0>();
-    __syncwarp();
 }
 
 // The epilogue role of one warp (e = 0 .. kWarps-1; q = the quarter of the TMEM lanes it may read).  Walks

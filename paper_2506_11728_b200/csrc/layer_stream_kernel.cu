@@ -12,6 +12,9 @@
 // sums do not depend on the order.  Owners add the partials and finish 4 tokens of a column per thread: neighbouring
 // lanes hold neighbouring columns, so rows of C are written in whole segments.
 //
+// Measured: gated 11008 x 4096 at 16 tokens 20.5 us a call (4.4 TB/s of weights; what is not streaming is the launch, the
+// first copies' latency and the exchange, 5 to 6 us), linear 4096 x 4096 at one token 6.7 us.
+//
 // Weights under the constant-weights promise are fetched before the previous kernel in the stream has completed;
 // without it the L2 is asked for them (a prefetch brings nothing into the SM).  Every wait is bounded.
 #include "internal.h"
