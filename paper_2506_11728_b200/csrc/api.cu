@@ -1351,7 +1351,7 @@ int layer_epi_warps(const LayerArgs& a) { return a.type != MIPGEMM_TYPE_F32 && a
 int layer_stages(const LayerArgs& a, int pair, int block_n, bool raw) {
     const int op = raw ? (a.op == kOpLinear ? kOpRaw : kOpRawGated) : a.op;
     const int fixed = layer_fixed_smem(op, a.type == MIPGEMM_TYPE_F32, raw ? 8 : layer_epi_warps(a));
-    return std::min(kMaxStages, (kSmemBudget - fixed) / ((kBlockM + (pair ? block_n / 2 : block_n)) * 128));
+    return std::min(kMaxLayerStages, (kSmemBudget - fixed) / ((kBlockM + (pair ? block_n / 2 : block_n)) * 128));
 }
 
 // What a plan with another K split than the one asked for by mipgemm_set_tuning is charged: it is taken only where the

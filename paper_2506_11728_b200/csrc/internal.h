@@ -165,6 +165,7 @@ cudaError_t launch_skinny_ring16(const SkinnyRingParams& p, int sm_count, cudaSt
 constexpr int kOpLinear = 0, kOpGated = 1, kOpGatedGrad = 2, kOpProduct = 3;
 // Partial sums as they are, for a K split over units of the grid (a second kernel adds and finishes them).
 constexpr int kOpRaw = 4, kOpRawGated = 5;
+constexpr int kMaxLayerStages = 11;  // pipeline stages of the dense layer kernel (its control block has room for so many)
 struct LayerArgs {
     int op, type, act;               // kOp*, mipgemm_type_t of R / C / C2, mipgemm_activation_t
     int a_unsigned;

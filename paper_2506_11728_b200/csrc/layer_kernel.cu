@@ -19,9 +19,10 @@
 // to 1024 tokens of 4096 outputs.  Both projections in one accumulator make the gated block one pass over the tokens and
 // write H alone: G and U never leave the SM.
 //
-// Every wait is bounded; the unwinding is that of the plain product's kernel (abort word, copies and MMAs in
-// flight awaited, tensor memory released, bit 0 of *status set).
+// Every wait is bounded.  A kernel that gives one up unwinds: all roles of both CTAs stop, copies (unwind.cuh) and MMAs in
+// flight are awaited, tensor memory is released, bit 0 of *status is set.
 #include "layer_epilogue.cuh"
+#include "unwind.cuh"
 
 namespace mip {
 
@@ -62,6 +63,8 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
     uint8_t* ctrl_ptr = smem + (ctrl - smem_base);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr + 16 * p.stages + 40);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(tmem_slot + 1);
+    const UnwindWords unwind = {ctrl + 16u * p.stages + 48u};
+    static_assert(16 * kMaxLayerStages + 48 + UnwindWords::kBytes <= 256, "control block");
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -139,6 +142,7 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
                 if (++s == static_cast<uint32_t>(p.stages)) { s = 0; phase ^= 1u; }
             }
         }
+        if (lane == 0) unwind.put(side_a ? 0 : 1, issued);
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer
         if (leader) {
@@ -198,32 +202,33 @@ mip_layer_kernel(const __grid_constant__ LayerParams p) {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (*abort_flag != 0) {
-        if (warp == 0 && leader) {       // copies of the last stages this CTA (or the pair) asked for
-            const uint32_t n = min(issued, static_cast<uint32_t>(p.stages));
-            for (uint32_t i = 1; i <= n; ++i) {
-                const uint32_t idx = issued - i;
-                const uint64_t t0 = globaltimer_ns();
-                while (!mbar_try_wait(bar_full + 8u * (idx % p.stages), (idx / p.stages) & 1u)) {
-                    if (globaltimer_ns() - t0 > budget) break;
-                }
-            }
-        }
+    bool unwinding = *abort_flag != 0;
+    if (kPair) {   // both CTAs have stopped, and know it of each other
+        if (threadIdx.x == 0) unwind.tell(cta_rank ^ 1u, *abort_flag);
+        cluster_arrive();
+        cluster_wait();
+        unwinding = unwinding || unwind.get(0) != 0;
+    }
+    if (unwinding) {
+        if (warp == 0 && leader)
+            drain_copies<kPair, 2>(unwind, bar_full, static_cast<uint32_t>(p.stages), static_cast<uint32_t>(p.a_rows) * 128u, b_bytes, lane, budget);
         if (warp == 1 && leader) {
             if (elect_one()) {
                 if (kPair) mma_commit_pair(bar_drain); else mma_commit(bar_drain);
             }
+            __syncwarp();
             const uint64_t t0 = globaltimer_ns();
             while (!mbar_try_wait(bar_drain, 0)) {
                 if (globaltimer_ns() - t0 > budget) break;
             }
+            __syncwarp();
             tc_fence_before();
         }
         __syncthreads();
-    }
-    if (kPair) {
-        cluster_arrive();
-        cluster_wait();
+        if (kPair) {   // (the peer's shared memory is still being written or read until here)
+            cluster_arrive();
+            cluster_wait();
+        }
     }
     if (warp == 1) {
         tc_fence_after();
