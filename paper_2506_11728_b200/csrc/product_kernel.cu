@@ -18,8 +18,9 @@
 // 22016 x 4096 x 8192: 1360 TFLOP/s in a short burst, 1120 sustained under the power limit (the library's bf16 product
 // 1620 and 1360).
 //
-// Every wait is bounded, with the unwinding of the other dense kernels.
+// Every wait is bounded, with the unwinding of the dense layer kernel.
 #include "layer_epilogue.cuh"
+#include "unwind.cuh"
 
 namespace mip {
 
@@ -89,6 +90,8 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     uint8_t* ctrl_ptr = smem + (ctrl - smem_base);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr + 360);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl_ptr + 364);
+    const UnwindWords unwind = {bar_in + 8u * kEpiWarps * slot_count(kOpProduct)};
+    static_assert(384 + 8 * kEpiWarps * slot_count(kOpProduct) + UnwindWords::kBytes <= kCtrlBytes, "control block");
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -159,6 +162,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
                 advance();
             }
         }
+        if (lane == 0) unwind.put(0, issued);
     } else if (warp == 2 + kEpiWarps) {
         // ------------------------------------------------------------ codes of B
         bool ok = true;
@@ -309,34 +313,44 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (*abort_flag != 0) {
-        // copies asked for last: A's complete on the leader's barriers, the codes' on each CTA's own
-        if ((warp == 0 && leader) || warp == 2 + kEpiWarps) {
-            const uint32_t bar = warp == 0 ? bar_a : bar_raw;
+    bool unwinding = *abort_flag != 0;
+    if (kPair) {   // both CTAs have stopped, and know it of each other
+        if (threadIdx.x == 0) unwind.tell(cta_rank ^ 1u, *abort_flag);
+        cluster_arrive();
+        cluster_wait();
+        unwinding = unwinding || unwind.get(0) != 0;
+    }
+    if (unwinding) {
+        // A's copies complete on the leader's barriers, the codes', of one producer alone, on each CTA's own
+        if (warp == 0 && leader) drain_copies<kPair, 1>(unwind, bar_a, stages, kABytes, 0, lane, budget);
+        if (warp == 2 + kEpiWarps) {
             const uint32_t n = min(issued, stages);
             for (uint32_t i = 1; i <= n; ++i) {
                 const uint32_t idx = issued - i;
                 const uint64_t t0 = globaltimer_ns();
-                while (!mbar_try_wait(bar + 8u * (idx % stages), (idx / stages) & 1u)) {
+                while (!mbar_try_wait(bar_raw + 8u * (idx % stages), (idx / stages) & 1u)) {
                     if (globaltimer_ns() - t0 > budget) break;
                 }
             }
+            __syncwarp();
         }
         if (warp == 1 && leader) {
             if (elect_one()) {
                 if (kPair) mma_commit_pair(bar_drain); else mma_commit(bar_drain);
             }
+            __syncwarp();
             const uint64_t t0 = globaltimer_ns();
             while (!mbar_try_wait(bar_drain, 0)) {
                 if (globaltimer_ns() - t0 > budget) break;
             }
+            __syncwarp();
             tc_fence_before();
         }
         __syncthreads();
-    }
-    if (kPair) {
-        cluster_arrive();
-        cluster_wait();
+        if (kPair) {   // (the peer's shared memory is still being written or read until here)
+            cluster_arrive();
+            cluster_wait();
+        }
     }
     if (warp == 1) {
         tc_fence_after();

@@ -47,7 +47,7 @@ MIP_HOST_DEVICE uint32_t uses_first(uint32_t last, uint32_t stages) { return las
 namespace mip {
 
 // Uses that a CTA's producers have asked for, by operand (0: A, 1: B), and whether it unwinds, as words in shared memory:
-// [abort of the peer, its A, its B] of the pair forms, then this CTA's A and B.
+// [abort of the peer, its A, its B] of the pair forms, then this CTA's A and B (the product's B is its CTA's own affair).
 struct UnwindWords {
     uint32_t addr;
     static constexpr uint32_t kBytes = 20;

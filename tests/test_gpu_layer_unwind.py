@@ -1,6 +1,7 @@
 """Kernels of the 8-bit layer whose waits run out, in every form: they return, say so once, and what runs after them on the
 same SMs is right.  The "accumulator ready" signal is withheld, so that waits expire after 0.2 ms; with more tiles than
 CTAs the producers are stopped in the middle of their work."""
+import numpy as np
 import pytest
 
 import layer_util as u
@@ -36,3 +37,23 @@ def test_layer_kernel(mg, form, split, kind):
                      lambda: mg.mipgemm_s8s8_gated_grad(t, 4, M, N, K, *block, p["d"].ptr, N, c.ptr, N, c2.ptr, N)):
             expire(mg, call)
         run_all(mg, M, N, K, kind)
+
+
+@pytest.mark.parametrize("order", [0, 1])
+@pytest.mark.parametrize("split", [1, 2])
+@pytest.mark.parametrize("form", ["one", "pair"])
+def test_product_kernel(mg, form, split, order):
+    mg.mipgemm_set_tuning(split_k=split, force_path=mg.PATH_DENSE if form == "one" else mg.PATH_DENSE_PAIR)
+    for M, N, K in [(300, 416, 1000), (4100, 2608, 1000)][:1 if split > 1 else 2]:
+        rng = np.random.default_rng([M, N, K])
+        a = rng.integers(-8, 9, (M, K)).astype(np.float64)
+        b = rng.integers(-128, 128, (K, N)).astype(np.int8)
+        s = 2.0 ** rng.integers(-2, 3, K)
+        A, B = u.Matrix(*((K, M) if order else (M, K)), "bf16", M + 4 if order else K, 0, a.T if order else a), u.Matrix(K, N, "s8", values=b)
+        for kind in ("bf16", "f32"):
+            C = u.Matrix(M, N, kind)
+            call = lambda: mg.mipgemm_bf16s8_product(mg.TYPES[kind], order, M, N, K, A.ptr, A.ld, B.ptr, N, u.vector(s), C.ptr, N)
+            expire(mg, call)
+            call()
+            assert mg.mipgemm_device_status() == mg.OK
+            assert np.array_equal(C.get(), u.rounded(a @ (s[:, None] * b), kind))
