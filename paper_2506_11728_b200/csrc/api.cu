@@ -107,6 +107,7 @@ struct DeviceState {
     size_t lent_bytes = 0;
     std::mutex scratch_mutex;              // scratch blocks kept between calls (see Scratch)
     std::vector<ScratchBlock> scratch;
+    std::atomic<int> families{0};          // kernel families of the layer operators that have been set up
 };
 DeviceState g_dev[kMaxDevices];
 std::mutex g_mutex;
@@ -196,9 +197,6 @@ int get_device(DeviceState** out) {
                 g_encode_im2col = reinterpret_cast<EncodeIm2colFn>(fn);
             }
             if ((e = dense_init()) != cudaSuccess) return cuda_fail(e);
-            if ((e = layer_init()) != cudaSuccess) return cuda_fail(e);
-            if ((e = product_init()) != cudaSuccess) return cuda_fail(e);
-            if ((e = stream_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring_init()) != cudaSuccess) return cuda_fail(e);
             if ((e = skinny_ring16_init()) != cudaSuccess) return cuda_fail(e);
             d.pair_clusters = dense_pair_max_clusters(kSmemBudget);
@@ -217,6 +215,27 @@ int get_device(DeviceState** out) {
     }
     *out = &d;
     return d.status;
+}
+
+// Kernels of the layer operators, set up on a device when one of the family is first launched there: setting an attribute
+// loads the kernel, and loading these with the plain products' made the first call of a program that never uses them
+// 8 to 20 ms longer (9 ms without them).
+constexpr int kFamilyLayer = 1, kFamilyFew = 2, kFamilyProduct = 4;
+int family_ready(DeviceState* dev, int family) {
+    if (dev->families.load(std::memory_order_acquire) & family) return MIPGEMM_OK;
+    std::lock_guard<std::mutex> lock(g_mutex);
+    if (dev->families.load(std::memory_order_relaxed) & family) return MIPGEMM_OK;
+    // (another stream may be captured meanwhile: loading kernels does not belong to its graph)
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+    const cudaError_t e = family == kFamilyLayer ? layer_init() : (family == kFamilyFew ? stream_init() : product_init());
+    (void)cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e != cudaSuccess) return cuda_fail(e);
+    dev->families.fetch_or(family, std::memory_order_release);
+    if (log_enabled())
+        std::fprintf(stderr, "mipgemm: set up %s kernels\n",
+                     family == kFamilyLayer ? "dense layer" : (family == kFamilyFew ? "few-token layer" : "product"));
+    return MIPGEMM_OK;
 }
 
 // Scratch memory for one call: a slice of the lent buffer, or a block of the library's own.  Blocks stay with their stream
@@ -1564,6 +1583,8 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool as
     p.b0_scale = a.b0_scale;
     p.b1_scale = a.b1_scale;
     p.bias = a.bias;
+    const int ready = family_ready(dev, pl.few ? kFamilyFew : kFamilyLayer);
+    if (ready != MIPGEMM_OK) return ready;
     cudaError_t e;
     if (pl.few) {
         // (a promise about the weights, not part of the plan either; it is given for calls of up to 16 tokens, and not about
@@ -1785,6 +1806,8 @@ int run_product(const ProductArgs& a, DeviceState* dev, cudaStream_t stream, boo
         if (cacheable) layer_store(key, p, pl);
     }
     p.b0_scale = a.b_scale;              // (not part of the plan)
+    const int ready = family_ready(dev, kFamilyProduct);
+    if (ready != MIPGEMM_OK) return ready;
     cudaError_t e;
     if (pl.split > 1) {
         PartialPlanes planes{nullptr, pl.split, p.plane_rows, round_up(a.N, 32), 0};
