@@ -1377,6 +1377,9 @@ int layer_stages(const LayerArgs& a, int pair, int block_n, bool raw) {
 // size does not allow that split.
 constexpr double kNotAsked = 1e20;
 
+// Activations that the plan prices alike: with an exponential in a linear layer's epilogue, or without.
+bool costly_activation(const LayerArgs& a) { return a.op == kOpLinear && a.act >= MIPGEMM_ACT_GELU; }
+
 // Tile shape of the dense layer kernel: the main loop's cost per k-block is that of the plain product's kernel
 // (plan_cost_us); a tile's epilogue runs beside the next tile's main loop, the last one is exposed.
 LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
@@ -1408,12 +1411,12 @@ LayerPlan plan_layer(const LayerArgs& a, const DeviceState* dev) {
             const double kb_clk = std::max(pair ? 300.0 + 1.5 * bn : 250.0 + 2.0 * bn, (row_tiles < 8 ? 3600.0 : 2000.0) / stages);
             // the schedulers' time for the tile's outputs, and at least each warp's rounds of slots
             const double rounds = (out_n / 32 + warps / 4 - 1) / (warps / 4);
-            const double per_col = a.op == kOpGatedGrad ? 46.0 : (gated ? 28.0 : (a.act >= MIPGEMM_ACT_GELU ? 26.0 : 14.0));
+            const double per_col = a.op == kOpGatedGrad ? 46.0 : (gated ? 28.0 : (costly_activation(a) ? 26.0 : 14.0));
             const double epi = std::max(out_n * per_col, rounds * (a.op == kOpGatedGrad ? 2600.0 : 1700.0)) * (unaligned ? 2.5 : 1.0);
             for (int split = 1; split <= kMaxSplit; ++split) {
                 // K in `split` shares whose partial sums a second kernel adds: only while there are more SMs than tiles
                 // (not in lent scratch: what a call may need of it stays what the queries say)
-                if (split > 1 && (dev->lent || tiles * (split - 1) >= slots || k_blocks / split < 4 || (gated && bn % 64 != 0))) break;
+                if (split > 1 && (dev->lent || tiles * (split - 1) >= slots || k_blocks / split < 4)) break;
                 const int share = (k_blocks + split - 1) / split;
                 if ((k_blocks + share - 1) / share != split) continue;
                 const double main = share * kb_clk;
@@ -1503,7 +1506,7 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool as
         const uint64_t words[] = {
             reinterpret_cast<uint64_t>(dev), g_tuning_epoch.load(std::memory_order_acquire),
             static_cast<uint64_t>(a.op) | (static_cast<uint64_t>(a.type) << 8) | (static_cast<uint64_t>(a.a_unsigned) << 16) |
-                (static_cast<uint64_t>(dev->lent != nullptr) << 17),
+                (static_cast<uint64_t>(dev->lent != nullptr) << 17) | (static_cast<uint64_t>(costly_activation(a)) << 18),
             static_cast<uint64_t>(a.M), static_cast<uint64_t>(a.N), static_cast<uint64_t>(a.K),
             reinterpret_cast<uint64_t>(a.A), static_cast<uint64_t>(a.lda), reinterpret_cast<uint64_t>(a.B0),
             static_cast<uint64_t>(a.ldb0), reinterpret_cast<uint64_t>(a.B1), static_cast<uint64_t>(a.ldb1),
@@ -1577,7 +1580,7 @@ int run_layer(const LayerArgs& a, DeviceState* dev, cudaStream_t stream, bool as
         p.debug_flags = g_debug_flags.load(std::memory_order_relaxed);
         if (cacheable) layer_store(key, p, pl);
     }
-    // (not part of the plan)
+    // (not part of the plan, but for what costly_activation says of the activation)
     p.act = a.act;
     p.a_scale = a.a_scale;
     p.b0_scale = a.b0_scale;
