@@ -2324,21 +2324,23 @@ int mipgemm_release_staging(void) {
     int st = get_device(&dev);
     if (st != MIPGEMM_OK) return st;
     std::lock_guard<std::mutex> host_lock(dev->host_mutex);
+    cudaError_t first = cudaSuccess;                     // (everything is freed, whatever fails on the way)
+    const auto free_now = [&](void* base) {              // (cudaFree waits for the work that uses it)
+        const cudaError_t e = cudaFree(base);
+        if (first == cudaSuccess) first = e;
+    };
     if (dev->staging) {
-        cudaError_t e = cudaFree(dev->staging);
+        free_now(dev->staging);
         dev->staging = nullptr;
         dev->staging_bytes = 0;
-        if (e != cudaSuccess) return cuda_fail(e);
     }
     std::vector<ScratchBlock> blocks;
     {
         std::lock_guard<std::mutex> lock(dev->scratch_mutex);
         blocks.swap(dev->scratch);
     }
-    for (const ScratchBlock& b : blocks) {               // (cudaFree waits for the work that uses it)
-        const cudaError_t e = cudaFree(b.base);
-        if (e != cudaSuccess) return cuda_fail(e);
-    }
+    for (const ScratchBlock& b : blocks) free_now(b.base);
+    if (first != cudaSuccess) return cuda_fail(first);
     return MIPGEMM_OK;
 }
 

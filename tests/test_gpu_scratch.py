@@ -1,0 +1,80 @@
+"""Scratch memory that the library keeps between calls: how much of it there is, and what a call that needs more does."""
+import ctypes
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def mg():
+    import torch
+    from paper_2506_11728_b200 import binding
+    binding.mipgemm_set_tuning()
+    torch.cuda.synchronize()
+    binding.mipgemm_release_staging()
+    torch.cuda.empty_cache()
+    yield binding
+    torch.cuda.synchronize()
+    binding.mipgemm_release_staging()
+    torch.cuda.empty_cache()
+
+
+class OwnStream:
+    """A stream of its own, destroyed on leaving (torch.cuda.Stream hands out a fixed set of them)."""
+
+    def __enter__(self):
+        import torch
+        handle = ctypes.c_void_p()
+        assert int(torch.cuda.cudart().cudaStreamCreate(ctypes.addressof(handle))) == 0
+        self.handle = handle.value
+        return self.handle
+
+    def __exit__(self, *exc):
+        import torch
+        assert int(torch.cuda.cudart().cudaStreamDestroy(self.handle)) == 0
+
+
+def free_memory():
+    import torch
+    torch.cuda.synchronize()
+    return torch.cuda.mem_get_info()[0]
+
+
+class Call:
+    """A product of ones whose B has an odd pitch: it is re-pitched into N * (K + 15) bytes of scratch."""
+    M = 4
+
+    def __init__(self, mg, N, K=16369):
+        import torch
+        self.mg, self.N, self.K = mg, N, K
+        self.scratch = N * (K + 15)
+        self.A = torch.ones(self.M, K + 15, dtype=torch.int8, device="cuda")
+        self.B = torch.ones(N, K, dtype=torch.int8, device="cuda")
+        self.C = torch.zeros(self.M, N, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+
+    def __call__(self, stream):
+        return self.mg.mipgemm_s8s8s32(self.M, self.N, self.K, self.A, self.K + 15, self.B, self.K, self.C, self.N, stream=stream)
+
+    def check(self):
+        import torch
+        torch.cuda.synchronize()
+        assert bool((self.C == self.K).all())
+
+
+def test_release_frees_every_block(mg):
+    import torch
+    calls = [Call(mg, 4096) for _ in range(3)]
+    streams = [torch.cuda.Stream() for _ in calls]          # (making them takes memory of its own)
+    calls[0](streams[0])
+    calls[0].check()
+    mg.mipgemm_release_staging()
+    before = free_memory()
+    for c, s in zip(calls, streams):
+        c(s)
+    for c in calls:
+        c.check()
+    assert before - free_memory() >= calls[0].scratch
+    mg.mipgemm_release_staging()
+    assert before - free_memory() <= 4 << 20
