@@ -10,6 +10,7 @@
 #include <map>
 #include <mutex>
 #include <new>
+#include <optional>
 #include <vector>
 
 #include "../../include/mipgemm.h"
@@ -85,11 +86,13 @@ constexpr int kMaxDevices = 64;
 constexpr int kHostBlocks = 8;                                    // host-buffer calls: up to 8 x 8 blocks of C
 constexpr int kHostEvents = 2 * kHostBlocks + kHostBlocks * kHostBlocks + 3;
 // Scratch memory kept between calls: a block that nobody holds may be taken by a call on the stream that used it last,
-// whose work it is then ordered behind.
+// whose work it is then ordered behind, and by any other once `done`, if it was recorded behind the last use, has passed.
 struct ScratchBlock {
-    void* base;
-    size_t bytes;
-    unsigned long long stream_id;
+    void* base = nullptr;
+    size_t bytes = 0;
+    unsigned long long stream_id = 0;
+    cudaEvent_t done = nullptr;
+    bool recorded = false;
 };
 struct DeviceState {
     bool ready = false;
@@ -238,9 +241,47 @@ int family_ready(DeviceState* dev, int family) {
     return MIPGEMM_OK;
 }
 
-// Scratch memory for one call: a slice of the lent buffer, or a block of the library's own.  Blocks stay with their stream
-// (by its id: handles are reused) and grow with the largest call; only growth reaches the CUDA allocator.  (The
-// stream-ordered allocator maps and unmaps memory around every synchronisation: 0.5 ms and more per call that way, and
+// Calls that another thread's capture would take for its own are let through while this lives.
+struct RelaxedCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    RelaxedCapture() { (void)cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~RelaxedCapture() { (void)cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
+// Takes a kept block out of the list for a call on stream `id`: the smallest that is large enough, of the stream's own if
+// it has one, else of those that are done with; else the largest of these, which the caller lets grow.  (Memory kept is
+// thus bounded by what calls in flight at the same time need, however many streams come and go.  The stream's own come
+// first, so that a program's usual call asks no event; recording one costs the call 0.3 us of host time, the device none.)
+bool take_block(DeviceState* dev, unsigned long long id, size_t bytes, ScratchBlock* out) {
+    std::lock_guard<std::mutex> lock(dev->scratch_mutex);
+    std::vector<ScratchBlock>& list = dev->scratch;
+    int best = -1;
+    for (const bool own : {true, false}) {
+        std::optional<RelaxedCapture> relaxed;
+        if (!own && !list.empty()) relaxed.emplace();
+        for (int i = 0; i < static_cast<int>(list.size()); ++i) {
+            const ScratchBlock& b = list[i];
+            if ((b.stream_id == id) != own) continue;
+            if (!own && !b.recorded) continue;
+            if (!own && cudaEventQuery(b.done) != cudaSuccess) {
+                (void)cudaGetLastError();            // (not yet passed: no error)
+                continue;
+            }
+            const bool fits = b.bytes >= bytes;
+            const bool best_fits = best >= 0 && list[best].bytes >= bytes;
+            if (best < 0 || (fits && !best_fits) || (fits && b.bytes < list[best].bytes) || (!fits && !best_fits && b.bytes > list[best].bytes)) best = i;
+        }
+        if (best >= 0 && list[best].bytes >= bytes) break;
+    }
+    if (best < 0) return false;
+    *out = list[best];
+    list.erase(list.begin() + best);
+    return true;
+}
+
+// Scratch memory for one call: a slice of the lent buffer, or a block of the library's own.  Blocks are kept between calls
+// (with the id of their stream: handles are reused) and grow with the largest call; only growth reaches the CUDA allocator.
+// (The stream-ordered allocator maps and unmaps memory around every synchronisation: 0.5 ms and more per call that way, and
 // seconds when a long queue of calls had made its pool grow.)  A captured call allocates from its graph.
 struct Scratch {
     DeviceState* dev;
@@ -248,12 +289,19 @@ struct Scratch {
     void* base = nullptr;
     size_t size = 0, used = 0;
     bool owned = false;          // stream-ordered (capture)
-    ScratchBlock block{nullptr, 0, 0};
+    ScratchBlock block;
     Scratch(DeviceState* d, cudaStream_t s) : dev(d), stream(s) {}
     int fail(cudaError_t e) {
         tl_last_cuda_error = static_cast<int>(e);
         (void)cudaGetLastError();
         return MIPGEMM_ERR_WORKSPACE;
+    }
+    // (waits for the block's work)
+    static void drop(ScratchBlock& b) {
+        if (b.base) (void)cudaFree(b.base);
+        if (b.done) (void)cudaEventDestroy(b.done);
+        b = ScratchBlock{};
+        (void)cudaGetLastError();
     }
     int reserve(size_t bytes) {
         if (bytes == 0) return MIPGEMM_OK;
@@ -268,36 +316,18 @@ struct Scratch {
         if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) {
             unsigned long long id = 0;
             if ((e = cudaStreamGetId(stream, &id)) != cudaSuccess) return fail(e);
-            {
-                // the smallest of the stream's blocks that is large enough, else its largest, which gives way to a larger
-                std::lock_guard<std::mutex> lock(dev->scratch_mutex);
-                int best = -1;
-                for (int i = 0; i < static_cast<int>(dev->scratch.size()); ++i) {
-                    const ScratchBlock& b = dev->scratch[i];
-                    if (b.stream_id != id) continue;
-                    const bool fits = b.bytes >= bytes;
-                    const bool best_fits = best >= 0 && dev->scratch[best].bytes >= bytes;
-                    if (best < 0 || (fits && !best_fits) || (fits == best_fits && (b.bytes < dev->scratch[best].bytes) == fits)) best = i;
-                }
-                if (best >= 0) {
-                    block = dev->scratch[best];
-                    dev->scratch.erase(dev->scratch.begin() + best);
-                }
-            }
+            (void)take_block(dev, id, bytes, &block);
+            block.stream_id = id;
             if (block.bytes < bytes) {
-                // (another thread may be capturing: these calls do not belong to its graph)
-                cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
-                (void)cudaThreadExchangeStreamCaptureMode(&mode);
+                const RelaxedCapture relaxed;
                 if (block.base) (void)cudaFree(block.base);          // waits for the work that uses it
+                block.base = nullptr;
                 const size_t grown = (bytes + (2u << 20) - 1) & ~static_cast<size_t>((2u << 20) - 1);
-                e = cudaMalloc(&block.base, grown);
-                (void)cudaThreadExchangeStreamCaptureMode(&mode);
-                if (e != cudaSuccess) {
-                    block = ScratchBlock{nullptr, 0, 0};
+                if ((e = cudaMalloc(&block.base, grown)) != cudaSuccess) {
+                    drop(block);
                     return fail(e);
                 }
                 block.bytes = grown;
-                block.stream_id = id;
             }
             base = block.base;
         } else {
@@ -318,12 +348,16 @@ struct Scratch {
     ~Scratch() {
         if (owned && base) (void)cudaFreeAsync(base, stream);
         if (!block.base) return;
-        // back to the stream's blocks (everything that uses it has been enqueued)
+        // back to the kept blocks: everything that uses it has been enqueued
         try {
             std::lock_guard<std::mutex> lock(dev->scratch_mutex);
+            cudaError_t e = block.done ? cudaSuccess : cudaEventCreateWithFlags(&block.done, cudaEventDisableTiming);
+            if (e == cudaSuccess) e = cudaEventRecord(block.done, stream);
+            block.recorded = e == cudaSuccess;
+            if (e != cudaSuccess) (void)cudaGetLastError();         // (the block stays its stream's)
             dev->scratch.push_back(block);
-        } catch (...) {
-            (void)cudaFree(block.base);      // (no memory for the list: waits for the block's work)
+        } catch (...) {                  // (no memory for the list)
+            drop(block);
         }
     }
 };
@@ -2339,7 +2373,10 @@ int mipgemm_release_staging(void) {
         std::lock_guard<std::mutex> lock(dev->scratch_mutex);
         blocks.swap(dev->scratch);
     }
-    for (const ScratchBlock& b : blocks) free_now(b.base);
+    for (const ScratchBlock& b : blocks) {
+        free_now(b.base);
+        if (b.done) (void)cudaEventDestroy(b.done);
+    }
     if (first != cudaSuccess) return cuda_fail(first);
     return MIPGEMM_OK;
 }

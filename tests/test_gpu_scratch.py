@@ -78,3 +78,39 @@ def test_release_frees_every_block(mg):
     assert before - free_memory() >= calls[0].scratch
     mg.mipgemm_release_staging()
     assert before - free_memory() <= 4 << 20
+
+
+def test_streams_that_come_and_go(mg):
+    """A program that makes a stream for each request keeps the scratch of one, not of all that there were."""
+    c = Call(mg, 4096)
+    with OwnStream() as stream:
+        c(stream)
+        c.check()
+    mg.mipgemm_release_staging()
+    before = free_memory()
+    for _ in range(50):
+        with OwnStream() as stream:
+            c.C.zero_()
+            free_memory()
+            c(stream)
+            c.check()
+    assert before - free_memory() <= 2 * c.scratch
+
+
+def test_a_block_in_use_is_not_handed_on(mg):
+    """Two streams at once, and the same with the roles changed: neither may read the other's copy of its operand."""
+    import torch
+    calls = [Call(mg, 4096 + 16 * i) for i in range(2)]
+    calls[1].B.fill_(-1)
+    streams = [torch.cuda.Stream() for _ in calls]
+    for turn in range(6):
+        for c in calls:
+            c.C.zero_()
+        torch.cuda.synchronize()
+        for i in range(2):
+            s = streams[(i + turn) % 2]
+            with torch.cuda.stream(s):
+                torch.cuda._sleep(2_000_000)            # (about a millisecond: the second call is made while the first waits)
+            calls[i](s)
+        torch.cuda.synchronize()
+        assert bool((calls[0].C == calls[0].K).all()) and bool((calls[1].C == -calls[1].K).all())
