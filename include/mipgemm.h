@@ -52,8 +52,8 @@
  * Some calls need global scratch memory (operand re-pitching, slot-padded
  * filters for convolutions gathered in software, the explicit im2col matrix
  * for the few convolutions neither the TMA nor the gather warps can handle).
- * By default it comes from blocks that the library allocates with cudaMalloc when calls first need
- * them (or need more) and keeps for later calls: of the same stream, or of any other once the work that used
+ * By default it comes from blocks that the library allocates (cudaMallocAsync, on the call's stream) when calls
+ * first need them or need more, and keeps for later calls: of the same stream, or of any other once the work that used
  * them is done, so that what is kept is what calls in flight at the same time needed, however many streams come
  * and go; mipgemm_release_staging() frees the blocks not in use.  Calls captured into a CUDA graph take it with cudaMallocAsync from the graph's memory instead.
  * A caller may instead lend a buffer with mipgemm_set_workspace(); calls

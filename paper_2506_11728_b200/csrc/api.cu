@@ -241,6 +241,16 @@ int family_ready(DeviceState* dev, int family) {
     return MIPGEMM_OK;
 }
 
+// Gives what the current device's pool holds free back to the device (the pool itself does so when it next synchronises).
+cudaError_t trim_pool() {
+    int dev = 0;
+    cudaMemPool_t pool = nullptr;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetMemPool(&pool, dev);
+    if (e == cudaSuccess) e = cudaMemPoolTrimTo(pool, 0);
+    return e;
+}
+
 // Calls that another thread's capture would take for its own are let through while this lives.
 struct RelaxedCapture {
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
@@ -280,9 +290,10 @@ bool take_block(DeviceState* dev, unsigned long long id, size_t bytes, ScratchBl
 }
 
 // Scratch memory for one call: a slice of the lent buffer, or a block of the library's own.  Blocks are kept between calls
-// (with the id of their stream: handles are reused) and grow with the largest call; only growth reaches the CUDA allocator.
-// (The stream-ordered allocator maps and unmaps memory around every synchronisation: 0.5 ms and more per call that way, and
-// seconds when a long queue of calls had made its pool grow.)  A captured call allocates from its graph.
+// (with the id of their stream: handles are reused) and grow with the largest call, by half of themselves at least; only
+// growth reaches the CUDA allocator.  (It maps and unmaps memory around every synchronisation: 0.5 ms and more for calls
+// that take and return memory each time.)  Growth is ordered on the call's stream, so that the call waits for no other
+// work: cudaMalloc and cudaFree would wait for the device.  A captured call allocates from its graph.
 struct Scratch {
     DeviceState* dev;
     cudaStream_t stream;
@@ -296,12 +307,29 @@ struct Scratch {
         (void)cudaGetLastError();
         return MIPGEMM_ERR_WORKSPACE;
     }
-    // (waits for the block's work)
-    static void drop(ScratchBlock& b) {
-        if (b.base) (void)cudaFree(b.base);
+    // Gives a block back, behind its work.
+    void drop(ScratchBlock& b) {
+        if (b.base) (void)cudaFreeAsync(b.base, stream);
         if (b.done) (void)cudaEventDestroy(b.done);
         b = ScratchBlock{};
         (void)cudaGetLastError();
+    }
+    // Memory of at least `bytes` for a block, ordered on the stream.
+    cudaError_t grow(ScratchBlock& b, size_t bytes) {
+        constexpr size_t kStep = 2u << 20;
+        size_t grown = std::max(bytes, b.bytes + b.bytes / 2);
+        if (b.base) (void)cudaFreeAsync(b.base, stream);
+        b.base = nullptr;
+        b.bytes = 0;
+        cudaError_t e = cudaSuccess;
+        for (const size_t want : {grown, bytes}) {
+            grown = (want + kStep - 1) / kStep * kStep;
+            if ((e = cudaMallocAsync(&b.base, grown, stream)) == cudaSuccess) break;
+            b.base = nullptr;
+            (void)cudaGetLastError();
+        }
+        if (e == cudaSuccess) b.bytes = grown;
+        return e;
     }
     int reserve(size_t bytes) {
         if (bytes == 0) return MIPGEMM_OK;
@@ -320,14 +348,10 @@ struct Scratch {
             block.stream_id = id;
             if (block.bytes < bytes) {
                 const RelaxedCapture relaxed;
-                if (block.base) (void)cudaFree(block.base);          // waits for the work that uses it
-                block.base = nullptr;
-                const size_t grown = (bytes + (2u << 20) - 1) & ~static_cast<size_t>((2u << 20) - 1);
-                if ((e = cudaMalloc(&block.base, grown)) != cudaSuccess) {
+                if ((e = grow(block, bytes)) != cudaSuccess) {
                     drop(block);
                     return fail(e);
                 }
-                block.bytes = grown;
             }
             base = block.base;
         } else {
@@ -2359,12 +2383,11 @@ int mipgemm_release_staging(void) {
     if (st != MIPGEMM_OK) return st;
     std::lock_guard<std::mutex> host_lock(dev->host_mutex);
     cudaError_t first = cudaSuccess;                     // (everything is freed, whatever fails on the way)
-    const auto free_now = [&](void* base) {              // (cudaFree waits for the work that uses it)
-        const cudaError_t e = cudaFree(base);
+    const auto note = [&](cudaError_t e) {
         if (first == cudaSuccess) first = e;
     };
     if (dev->staging) {
-        free_now(dev->staging);
+        note(cudaFree(dev->staging));
         dev->staging = nullptr;
         dev->staging_bytes = 0;
     }
@@ -2373,10 +2396,12 @@ int mipgemm_release_staging(void) {
         std::lock_guard<std::mutex> lock(dev->scratch_mutex);
         blocks.swap(dev->scratch);
     }
-    for (const ScratchBlock& b : blocks) {
-        free_now(b.base);
+    for (const ScratchBlock& b : blocks) {               // (cudaFree waits for no work that uses memory of a pool)
+        note(b.recorded ? cudaEventSynchronize(b.done) : cudaDeviceSynchronize());
+        note(cudaFree(b.base));
         if (b.done) (void)cudaEventDestroy(b.done);
     }
+    if (!blocks.empty()) note(trim_pool());
     if (first != cudaSuccess) return cuda_fail(first);
     return MIPGEMM_OK;
 }

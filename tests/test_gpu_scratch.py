@@ -114,3 +114,36 @@ def test_a_block_in_use_is_not_handed_on(mg):
             calls[i](s)
         torch.cuda.synchronize()
         assert bool((calls[0].C == calls[0].K).all()) and bool((calls[1].C == -calls[1].K).all())
+
+
+def test_growing_waits_for_no_other_work(mg):
+    """Calls are asynchronous, those that need more scratch than there is included: they return while another stream, and
+    their own, are busy with what was enqueued before."""
+    import torch
+    small, large = Call(mg, 1024), Call(mg, 4096)
+    other, own = torch.cuda.Stream(), torch.cuda.Stream()
+    small(own)
+    small.check()
+    busy = []
+    for s in (other, own):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(600_000_000)              # (about 0.3 s)
+            busy.append(torch.cuda.Event())
+            busy[-1].record()
+    large(own)
+    assert not any(e.query() for e in busy)
+    large.check()
+
+
+def test_growing_sizes_reach_the_allocator_a_few_times(mg):
+    """Slowly growing calls: blocks grow by half, so that the memory in use never passes 1.5 times the largest need."""
+    c = Call(mg, 4096)
+    free = []
+    for N in range(1024, 4097, 64):
+        c.N = N
+        c.C.zero_()
+        c(None)
+        free.append(free_memory())
+        assert bool((c.C.view(-1)[:c.M * N] == c.K).all())
+    assert len(set(free)) <= 8                          # log(4) / log(1.5) = 3.4 growths, and the caching allocator's own
+    assert free[0] - free[-1] <= 1.5 * c.scratch + (8 << 20)
