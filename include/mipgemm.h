@@ -55,7 +55,8 @@
  * By default it comes from blocks that the library allocates (cudaMallocAsync, on the call's stream) when calls
  * first need them or need more, and keeps for later calls: of the same stream, or of any other once the work that used
  * them is done, so that what is kept is what calls in flight at the same time needed, however many streams come
- * and go; mipgemm_release_staging() frees the blocks not in use.  Calls captured into a CUDA graph take it with cudaMallocAsync from the graph's memory instead.
+ * and go (a call that finds no memory left first has all blocks not in use freed, and waits for that);
+ * mipgemm_release_staging() frees the blocks not in use.  Calls captured into a CUDA graph take it with cudaMallocAsync from the graph's memory instead.
  * A caller may instead lend a buffer with mipgemm_set_workspace(); calls
  * that need more than was lent fail with MIPGEMM_ERR_WORKSPACE.  A lent buffer
  * is shared by all calls: calls that use it must be ordered on one stream.

@@ -289,6 +289,26 @@ bool take_block(DeviceState* dev, unsigned long long id, size_t bytes, ScratchBl
     return true;
 }
 
+// Frees the kept blocks (those that nobody holds), after the work that uses them; the first error.
+cudaError_t free_blocks(DeviceState* dev) {
+    std::vector<ScratchBlock> blocks;
+    {
+        std::lock_guard<std::mutex> lock(dev->scratch_mutex);
+        blocks.swap(dev->scratch);
+    }
+    cudaError_t first = cudaSuccess;                     // (everything is freed, whatever fails on the way)
+    const auto note = [&](cudaError_t e) {
+        if (first == cudaSuccess) first = e;
+    };
+    for (const ScratchBlock& b : blocks) {               // (cudaFree waits for no work that uses memory of a pool)
+        note(b.recorded ? cudaEventSynchronize(b.done) : cudaDeviceSynchronize());
+        note(cudaFree(b.base));
+        if (b.done) (void)cudaEventDestroy(b.done);
+    }
+    if (!blocks.empty()) note(trim_pool());
+    return first;
+}
+
 // Scratch memory for one call: a slice of the lent buffer, or a block of the library's own.  Blocks are kept between calls
 // (with the id of their stream: handles are reused) and grow with the largest call, by half of themselves at least; only
 // growth reaches the CUDA allocator.  (It maps and unmaps memory around every synchronisation: 0.5 ms and more for calls
@@ -314,21 +334,29 @@ struct Scratch {
         b = ScratchBlock{};
         (void)cudaGetLastError();
     }
-    // Memory of at least `bytes` for a block, ordered on the stream.
+    // Memory of at least `bytes` for a block, ordered on the stream.  Where there is none left, all blocks that nobody holds
+    // are given up, and the call waits for that.
     cudaError_t grow(ScratchBlock& b, size_t bytes) {
         constexpr size_t kStep = 2u << 20;
-        size_t grown = std::max(bytes, b.bytes + b.bytes / 2);
+        const size_t sizes[3] = {std::max(bytes, b.bytes + b.bytes / 2), bytes, bytes};
         if (b.base) (void)cudaFreeAsync(b.base, stream);
         b.base = nullptr;
         b.bytes = 0;
         cudaError_t e = cudaSuccess;
-        for (const size_t want : {grown, bytes}) {
-            grown = (want + kStep - 1) / kStep * kStep;
-            if ((e = cudaMallocAsync(&b.base, grown, stream)) == cudaSuccess) break;
+        for (int i = 0; i < 3; ++i) {
+            if (i == 2) {
+                (void)free_blocks(dev);
+                (void)cudaStreamSynchronize(stream);     // (what has been freed on the stream comes back too)
+                (void)trim_pool();
+            }
+            const size_t want = (sizes[i] + kStep - 1) / kStep * kStep;
+            if ((e = cudaMallocAsync(&b.base, want, stream)) == cudaSuccess) {
+                b.bytes = want;
+                break;
+            }
             b.base = nullptr;
             (void)cudaGetLastError();
         }
-        if (e == cudaSuccess) b.bytes = grown;
         return e;
     }
     int reserve(size_t bytes) {
@@ -2382,7 +2410,7 @@ int mipgemm_release_staging(void) {
     int st = get_device(&dev);
     if (st != MIPGEMM_OK) return st;
     std::lock_guard<std::mutex> host_lock(dev->host_mutex);
-    cudaError_t first = cudaSuccess;                     // (everything is freed, whatever fails on the way)
+    cudaError_t first = cudaSuccess;                     // (the blocks are freed even if the staging buffer cannot be)
     const auto note = [&](cudaError_t e) {
         if (first == cudaSuccess) first = e;
     };
@@ -2391,17 +2419,7 @@ int mipgemm_release_staging(void) {
         dev->staging = nullptr;
         dev->staging_bytes = 0;
     }
-    std::vector<ScratchBlock> blocks;
-    {
-        std::lock_guard<std::mutex> lock(dev->scratch_mutex);
-        blocks.swap(dev->scratch);
-    }
-    for (const ScratchBlock& b : blocks) {               // (cudaFree waits for no work that uses memory of a pool)
-        note(b.recorded ? cudaEventSynchronize(b.done) : cudaDeviceSynchronize());
-        note(cudaFree(b.base));
-        if (b.done) (void)cudaEventDestroy(b.done);
-    }
-    if (!blocks.empty()) note(trim_pool());
+    note(free_blocks(dev));
     if (first != cudaSuccess) return cuda_fail(first);
     return MIPGEMM_OK;
 }

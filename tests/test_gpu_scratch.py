@@ -147,3 +147,27 @@ def test_growing_sizes_reach_the_allocator_a_few_times(mg):
         assert bool((c.C.view(-1)[:c.M * N] == c.K).all())
     assert len(set(free)) <= 8                          # log(4) / log(1.5) = 3.4 growths, and the caching allocator's own
     assert free[0] - free[-1] <= 1.5 * c.scratch + (8 << 20)
+
+
+def test_no_memory_left_but_what_idle_blocks_hold(mg):
+    """Two streams' idle blocks hold what a third stream's call needs: it gets it."""
+    import torch
+    calls, large = [Call(mg, 16384) for _ in range(2)], Call(mg, 30000)
+    assert max(c.scratch for c in calls) < large.scratch < sum(c.scratch for c in calls)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for c, s in zip(calls, streams):
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(20_000_000)               # (both at once, so that each has a block of its own)
+        c(s)
+    for c in calls:
+        c.check()
+    held = torch.empty(free_memory() - (100 << 20), dtype=torch.uint8, device="cuda")
+    assert large.scratch > max(c.scratch for c in calls) + free_memory()
+    large(streams[2])
+    large.check()
+    for c, s in zip(calls, streams):                    # the others wait their turn for what is left
+        c.C.zero_()
+        torch.cuda.synchronize()
+        c(s)
+        c.check()
+    del held
