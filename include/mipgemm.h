@@ -360,7 +360,11 @@ int mipgemm_release_staging(void);
  * mipgemm_s8s8s32.  `type` is the element type of every floating matrix of the call; a pointer to such
  * a matrix is aligned to its element size, pitches are counted in elements.  The 8-bit sums are exact
  * in int32 (the K limits of mipgemm_s8s8s32 hold), everything behind them is computed in binary32 and
- * rounded once, to nearest even, when it is stored.  Scale vectors are float32, 4-byte aligned; NULL
+ * rounded once, to nearest even, when it is stored.  The activations use the hardware's approximate
+ * exponential and reciprocal and, for the error function, a fit of their own: relative to their value, small
+ * ones included, they are within (22 + 1.25 x^2) 2^-24 for GELU at x < 0 (16-bit results 4e-6 more), (9 + 1.5 |x|) 2^-24
+ * for SILU and (9 + 7.5 |y|) 2^-24 for GELU_TANH, y = 2 sqrt(2/pi) (x + 0.044715 x^3), until they are below 1e-35
+ * and may be 0; the gradients' terms are as close.  Scale vectors are float32, 4-byte aligned; NULL
  * stands for all ones.  Operands with 16-byte aligned bases and pitches are read in place, other 8-bit
  * operands are re-pitched into scratch memory first.  Sums along a long K with few tiles may be taken in
  * parts that meet in scratch memory of the library's own (always added in the same order); with a lent

@@ -223,14 +223,14 @@ __device__ __forceinline__ void finish_chunk(const uint32_t (&v0)[kN], const uin
                 const uint64_t s0 = mul_f2(ints_to_f2(v0[v], v0[v + 1]), as2);
                 const uint64_t b0 = pack_f2(in.b0[2 * j], in.b0[2 * j + 1]), b1 = pack_f2(in.b1[2 * j], in.b1[2 * j + 1]);
                 if constexpr (kOp == kOpLinear) {
-                    y[j] = add_f2(activation_f2<kAct>(fma_f2(s0, b0, b1)), r[j]);
+                    y[j] = add_f2(activation_f2<kAct, kWide>(fma_f2(s0, b0, b1)), r[j]);
                 } else {
                     const uint64_t z1 = mul_f2(mul_f2(ints_to_f2(v1[v], v1[v + 1]), as2), b1);
                     if constexpr (kOp == kOpGated) {
-                        y[j] = mul_f2(activation_f2<kAct>(mul_f2(s0, b0)), z1);
+                        y[j] = mul_f2(activation_f2<kAct, kWide>(mul_f2(s0, b0)), z1);
                     } else {
                         uint64_t value, slope;
-                        activation_slope_f2<kAct>(mul_f2(s0, b0), value, slope);
+                        activation_slope_f2<kAct, kWide>(mul_f2(s0, b0), value, slope);
                         y[j] = mul_f2(mul_f2(r[j], z1), slope);
                         y2[j] = mul_f2(r[j], value);
                     }
