@@ -35,6 +35,9 @@ __device__ __forceinline__ float sigmoid(float x) { return fast_rcp(1.0f + fast_
 // error unit, x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) / 2, into x sigmoid(gelu_inner(x)).
 constexpr float kGeluC = 1.5957691216057308f, kGeluC3 = 0.044715f;
 __device__ __forceinline__ float gelu_inner(float x) { return kGeluC * x * (1.0f + kGeluC3 * x * x); }
+// x^2 as the factor in its slope takes it: for |x| > 20 what it is multiplied with, x sigmoid (1 - sigmoid), is 0, and has to
+// stay 0 where the square leaves the range of binary32.
+__device__ __forceinline__ float gelu_square(float xx) { return fminf(xx, 1e4f); }
 
 // The normal distribution's integral Phi(x) = (1 + erf(x / sqrt 2)) / 2 and e^(-x^2 / 2), which its density shares.
 // Phi(-|x|) = t P(t) e^(-x^2 / 2), t = 1 / (1 + c |x|): the form of Abramowitz and Stegun 7.1.26, with P and c fitted for the
@@ -92,7 +95,7 @@ __device__ __forceinline__ void activation_slope(float x, float& value, float& s
     } else if (kAct == kActGeluTanh) {
         const float e = sigmoid(gelu_inner(x));
         value = x * e;
-        slope = e + value * (1.0f - e) * kGeluC * (1.0f + 3.0f * kGeluC3 * x * x);
+        slope = e + value * (1.0f - e) * kGeluC * (1.0f + 3.0f * kGeluC3 * gelu_square(x * x));
     } else if (kAct == kActSilu) {
         const float e = sigmoid(x);
         value = x * e;
@@ -177,7 +180,8 @@ __device__ __forceinline__ void activation_slope_f2(uint64_t x, uint64_t& value,
         const uint64_t xx = mul_f2(x, x);
         const uint64_t e = sigmoid_exp2_f2(mul_f2(x, fma_f2(xx, both(-kLog2E * kGeluC * kGeluC3), both(-kLog2E * kGeluC))));
         value = mul_f2(x, e);
-        slope = fma_f2(mul_f2(value, fma_f2(e, both(-1.0f), both(1.0f))), fma_f2(xx, both(3.0f * kGeluC * kGeluC3), both(kGeluC)), e);
+        slope = fma_f2(mul_f2(value, fma_f2(e, both(-1.0f), both(1.0f))),
+                       fma_f2(each(xx, gelu_square), both(3.0f * kGeluC * kGeluC3), both(kGeluC)), e);
     } else if constexpr (kAct == kActGelu) {
         uint64_t gauss;
         const uint64_t cdf = normal_cdf_f2<kFine>(x, gauss);

@@ -89,3 +89,22 @@ def test_the_far_tail_is_zero_or_tiny(mg):
     for act in ("gelu", "gelu_tanh", "silu"):
         mg.mipgemm_s8s8_linear(0, mg.ACTIVATIONS[act], M, N, 1, a.ptr, 1, None, w.ptr, 1, None, None, None, 0, c.ptr, N)
         assert (np.abs(c.get())[z < -110] <= 1e-35).all() and not np.isnan(c.get()).any()
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("act", u.ACTS)
+def test_slopes_at_large_finite_arguments(mg, form, act):
+    """|G| up to 1e30, whose square is beyond binary32: the slopes are 1 and 0 (1 and 1 without an activation), not NaN."""
+    M, N, K, tuning = FORMS[form]
+    mg.mipgemm_set_tuning(**tuning)
+    A, W, V = np.zeros((M, K), np.int8), np.zeros((N, K), np.int8), np.zeros((N, K), np.int8)
+    A[:, 0], W[:, 0], V[:, 0] = 1, np.where(np.arange(N) % 2, -1, 1), 3
+    size = 10.0 ** np.linspace(3, 30, N)
+    a, w, v = (u.Matrix(*x.shape, "s8", values=x) for x in (A, W, V))
+    dh, dg, du = u.Matrix(M, N, "f32", values=np.full((M, N), 2.0)), u.Matrix(M, N, "f32"), u.Matrix(M, N, "f32")
+    mg.mipgemm_s8s8_gated_grad(0, mg.ACTIVATIONS[act], M, N, K, a.ptr, K, None, w.ptr, K, u.vector(size), v.ptr, K, None, dh.ptr, N, dg.ptr, N,
+                               du.ptr, N)
+    positive = W[:, 0] > 0
+    G = W[:, 0] * size.astype(np.float32).astype(np.float64)
+    assert np.array_equal(dg.get(), np.broadcast_to(np.where(positive | (act == "none"), 6.0, 0.0), (M, N)))
+    assert np.array_equal(du.get(), np.broadcast_to((2 * np.where(positive | (act == "none"), G, 0.0)).astype(np.float32), (M, N)))
