@@ -86,7 +86,7 @@ template <int kAct>
 __device__ __forceinline__ void activation_slope(float x, float& value, float& slope) {
     if (kAct == kActRelu) {
         value = x < 0.0f ? 0.0f : x;
-        slope = x > 0.0f ? 1.0f : 0.0f;                         // (0 at 0)
+        slope = x > 0.0f ? 1.0f : value;                        // (0 at 0; NaN stays NaN)
     } else if (kAct == kActGelu) {
         float gauss;
         const float cdf = normal_cdf(x, gauss);
@@ -189,7 +189,10 @@ __device__ __forceinline__ void activation_slope_f2(uint64_t x, uint64_t& value,
         slope = fma_f2(mul_f2(x, gauss), both(0.3989422804014327f), cdf);
     } else if constexpr (kAct == kActRelu) {
         value = each(x, [](float v) { return v < 0.0f ? 0.0f : v; });
-        slope = each(x, [](float v) { return v > 0.0f ? 1.0f : 0.0f; });
+        float x0, x1, v0, v1;
+        unpack_f2(x, x0, x1);
+        unpack_f2(value, v0, v1);
+        slope = pack_f2(x0 > 0.0f ? 1.0f : v0, x1 > 0.0f ? 1.0f : v1);
     } else {
         value = x;
         slope = both(1.0f);

@@ -108,3 +108,22 @@ def test_slopes_at_large_finite_arguments(mg, form, act):
     G = W[:, 0] * size.astype(np.float32).astype(np.float64)
     assert np.array_equal(dg.get(), np.broadcast_to(np.where(positive | (act == "none"), 6.0, 0.0), (M, N)))
     assert np.array_equal(du.get(), np.broadcast_to((2 * np.where(positive | (act == "none"), G, 0.0)).astype(np.float32), (M, N)))
+
+
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_a_nan_of_the_gate_reaches_its_gradient(mg, form, act):
+    """A gate row quantized from an infinity or a NaN has scale NaN: both gradients of its column are NaN, no others."""
+    M, N, K, tuning = FORMS[form]
+    mg.mipgemm_set_tuning(**tuning)
+    A, W = np.zeros((M, K), np.int8), np.zeros((N, K), np.int8)
+    A[:, 0], W[:, 0] = 1, np.where(np.arange(N) % 2, -1, 1)
+    scale = np.ones(N)
+    scale[[3, 10, N - 1]] = np.nan
+    a, w = u.Matrix(M, K, "s8", values=A), u.Matrix(N, K, "s8", values=W)
+    for kind in ("f32", "bf16"):
+        dh, dg, du = u.Matrix(M, N, kind, values=np.ones((M, N))), u.Matrix(M, N, kind), u.Matrix(M, N, kind)
+        mg.mipgemm_s8s8_gated_grad(mg.TYPES[kind], mg.ACTIVATIONS[act], M, N, K, a.ptr, K, None, w.ptr, K, u.vector(scale), w.ptr, K, None,
+                                   dh.ptr, N, dg.ptr, N, du.ptr, N)
+        for got in (dg.get(), du.get()):
+            assert np.array_equal(np.isnan(got), np.broadcast_to(np.isnan(scale), (M, N)))
