@@ -25,6 +25,7 @@
 // multicast form is used anywhere in this file).
 #include "internal.h"
 #include "ptx.cuh"
+#include "unwind.cuh"
 
 namespace mip {
 
@@ -404,6 +405,9 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
     uint8_t* ctrl_ptr = smem + p.stages * stage_bytes + kStagingBytes;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr + 16 * p.stages + 40);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(tmem_slot + 1);
+    // (behind the abort word; beyond the 256 bytes of the gather form's further barriers only in forms without them)
+    const UnwindWords unwind = {ctrl + 16u * p.stages + 48u};
+    static_assert(16 * kMaxStages + 48 + UnwindWords::kBytes <= kCtrlBytes, "control block");
 
     // Broadcasting the warp index makes it provably warp-uniform for the compiler, so each
     // role's loop runs convergently (addresses, counters and descriptors live in uniform
@@ -584,6 +588,7 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
                 if (++s == static_cast<uint32_t>(p.stages)) { s = 0; phase ^= 1u; }
             }
         }
+        if (!kGather && lane == 0) unwind.put(side_a ? 0 : 1, issued);
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (whole warp loops)
         if (leader) {
@@ -1096,13 +1101,20 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
 
     tc_fence_before();
     __syncthreads();
-    if (*abort_flag != 0) {
+    bool unwinding = *abort_flag != 0;
+    if (kPair) {   // neither CTA may leave while the other can still reach its shared memory; both know if one unwinds
+        if (threadIdx.x == 0) unwind.tell(cta_rank ^ 1u, *abort_flag);
+        cluster_arrive();
+        cluster_wait();
+        unwinding = unwinding || unwind.get(0) != 0;
+    }
+    if (unwinding) {
         // Unwinding (uniform: every role has left its loop, so nobody writes the flag any more).  Some role gave
-        // up a wait; whatever is still on its way to this CTA must arrive before shared and tensor memory are
+        // up a wait; whatever is still on its way to the CTAs must arrive before shared and tensor memory are
         // given back, whichever role it was that gave up:
-        //  * the producer warp waits (bounded) until the copies of the last `stages` k-blocks it issued have
-        //    landed (a peer CTA cannot observe its own copies -- they complete on the leader's barrier; it is
-        //    held by the cluster barrier below until the leader has finished here);
+        //  * a warp of the CTA that counts the copies waits (bounded) until all that the producers, of its peer too,
+        //    have asked for have landed (unwind.cuh); in the gather form, whose other writers are this CTA's own
+        //    warps and have stopped, until those of the producer have;
         //  * the MMA warp lets every MMA it issued retire (one more commit, bounded wait).
         if (kGather && warp == 0 && p.g_staged) {       // image rows requested for the last two tiles
             for (uint32_t i = 1; i <= min(rows_tiles, 2u); ++i) {
@@ -1113,7 +1125,7 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
                 }
             }
         }
-        if (warp == 0 && leader) {
+        if (kGather && warp == 0) {
             const uint32_t n = min(issued, static_cast<uint32_t>(p.stages));
             for (uint32_t i = 1; i <= n; ++i) {
                 const uint32_t idx = issued - i;
@@ -1125,23 +1137,29 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
                 }
             }
         }
+        if (!kGather && warp == 0 && leader) {
+            if (kTwoProducers) drain_copies<kPair, 2>(unwind, bar_full, static_cast<uint32_t>(p.stages), a_bytes, b_bytes, lane, budget);
+            else drain_copies<kPair, 1>(unwind, bar_full, static_cast<uint32_t>(p.stages), a_bytes + b_bytes, 0, lane, budget);
+        }
         if (warp == 1 && leader) {
             if (elect_one()) {
                 if (kPair) mma_commit_pair(bar_drain); else mma_commit(bar_drain);
             }
+            __syncwarp();
             const uint64_t t0 = globaltimer_ns();
             while (!mbar_try_wait(bar_drain, 0)) {
                 if (globaltimer_ns() - t0 > budget) break;
             }
+            __syncwarp();
             tc_fence_before();
         }
         __syncthreads();
+        if (kPair) {
+            cluster_arrive();
+            cluster_wait();
+        }
     }
     if (threadIdx.x == 0) MIP_STAMP(8);
-    if (kPair) {   // neither CTA may leave while the other can still reach its shared memory
-        cluster_arrive();
-        cluster_wait();
-    }
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc<kGroup>(tmem_base, p.tmem_cols);
