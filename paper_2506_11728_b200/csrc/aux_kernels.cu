@@ -112,7 +112,7 @@ cudaError_t launch_repack_parts(const RepackPart* parts, int count, cudaStream_t
         a.part[i] = parts[i];
         most = max(most, (parts[i].rows * ((parts[i].cols + 511) / 512) + 7) / 8);
     }
-    // (not launched early: see launch_layer_finish)
+    // (launched in order, as the finishing kernels are)
     mip_repack_parts_kernel<<<dim3(static_cast<unsigned>(min(most, 148LL * 16)), static_cast<unsigned>(count)), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }

@@ -79,9 +79,8 @@ mip_product_finish_kernel(const ProductArgs a, const PartialPlanes s) {
         if (j < cols) store_element(a.C, row * a.ldc + col + j, a.type, v[j]);
 }
 
-// These kernels are not launched early (programmatic stream serialisation): they come as many small blocks, which would
-// fill the SMs while they wait for a kernel whose clusters may still be looking for room there.  A chain of re-pitch,
-// cluster kernel and finish, all launched early, stopped making progress in long queues.
+// These kernels are launched in order (no programmatic stream serialisation): they have nothing to do before the kernel in
+// front of them is over, and as many small blocks they would sit on the SMs until then.
 template <typename Args>
 cudaError_t finish(void (*kernel)(const Args, const PartialPlanes), const Args& a, const PartialPlanes& s, cudaStream_t stream) {
     int tx = 8;

@@ -20,6 +20,7 @@
 //
 // Every wait is bounded, with the unwinding of the dense layer kernel.
 #include "layer_epilogue.cuh"
+#include "stage_waits.h"
 #include "unwind.cuh"
 
 namespace mip {
@@ -264,9 +265,12 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         for (uint32_t it = static_cast<uint32_t>(cw >> 2); it < total; it += 2) {
             const uint32_t st = it % stages, ph = (it / stages) & 1u;
             const uint32_t stage = smem_base + st * kProductStage;
-            // codes and scales in place; the tensor core has read what the buffer held.  (Lanes decide together.)
-            const bool ready = mbar_wait(bar_raw + 8u * st, ph, abort_flag, budget) &&
-                               mbar_wait(bar_empty + 8u * st, ph ^ 1u, abort_flag, budget);
+            // the tensor core has read what the buffer held; codes and scales are in place.  (Lanes decide together.)
+            const auto wait = [&](StageWait what) {
+                return what == kStageFree ? mbar_wait(bar_empty + 8u * st, ph ^ 1u, abort_flag, budget)
+                                          : mbar_wait(bar_raw + 8u * st, ph, abort_flag, budget);
+            };
+            const bool ready = wait(kConverterFirst) && wait(kConverterSecond);
             if (!__all_sync(~0u, ready)) break;
             // (the second half of a row reads its two halves in the other order too, so no register is chosen by lane)
             uint32_t w[4][4];
