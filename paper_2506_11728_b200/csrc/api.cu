@@ -747,9 +747,9 @@ int run_dense(DenseParams& p, const Plan& pl, long long M, long long N, int32_t*
     }
     const long long units = static_cast<long long>(pl.tiles_m) * pl.tiles_n * pl.split_k;
     const int b_rows = pl.pair ? pl.block_n / 2 : pl.block_n;
-    const size_t smem = static_cast<size_t>(pl.stages) * (kBlockM * p.block_k + b_rows * p.block_k) +
-                        kStagingBytes + kCtrlBytes + 1024 +
-                        (p.g_staged ? 64 + 2 * static_cast<size_t>(p.g_rowbuf_stride) + p.g_table_bytes : 0);
+    const size_t smem = std::max(kSmemFloor, static_cast<size_t>(pl.stages) * (kBlockM * p.block_k + b_rows * p.block_k) +
+                                                 kStagingBytes + kCtrlBytes + 1024 +
+                                                 (p.g_staged ? 64 + 2 * static_cast<size_t>(p.g_rowbuf_stride) + p.g_table_bytes : 0));
     if ((p.c_mode == 1 || p.c_mode == 2) && !c_map_ready) {
         cuuint64_t dims[2] = {static_cast<cuuint64_t>(N), static_cast<cuuint64_t>(M)};
         cuuint64_t strides[1] = {static_cast<cuuint64_t>(ldc) * 4};
@@ -1232,7 +1232,7 @@ int batched_impl(bool a_unsigned, int64_t batch, int64_t M, int64_t N, int64_t K
         return st;
     const long long units = tiles_m * pl.tiles_n * batch;
     const int grid = static_cast<int>(units < dev->sm_count ? units : dev->sm_count);
-    const size_t smem = static_cast<size_t>(pl.stages) * stage_bytes + kStagingBytes + kCtrlBytes + 1024;
+    const size_t smem = std::max(kSmemFloor, static_cast<size_t>(pl.stages) * stage_bytes + kStagingBytes + kCtrlBytes + 1024);
     cudaError_t e = launch_dense(p, grid, smem, stream);
     ++g_launches;
     if (e != cudaSuccess) return cuda_fail(e);

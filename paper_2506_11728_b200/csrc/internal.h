@@ -48,6 +48,15 @@ constexpr int kSmemBudget = 226 * 1024;   // leaves room for the static trace ar
 constexpr int kSmemBudget = 227 * 1024;
 #endif
 
+// Shared memory that every launch of a kernel with its accumulators in tensor memory asks for at least, so that no two of
+// them have CTAs on one SM at a time, nor one of them beside the few-token kernel (47 KB at least).  Tensor memory is
+// allocated by waiting for it, without a limit: of two CTA pairs, from two streams, each could hold one SM's and wait for
+// the other's.  The planner's stages leave no room for that anyway where accumulators take more than half of tensor memory;
+// few stages, asked for by mipgemm_set_tuning, do.
+constexpr size_t kSmemFloor = 184 * 1024;
+constexpr size_t kSmemPerSm = 228 * 1024, kSmemReserved = 1024;     // of an SM; of it for each CTA
+static_assert(2 * (kSmemFloor + kSmemReserved) > kSmemPerSm, "two CTAs on an SM");
+
 // Everything the dense kernel needs; passed by value as a __grid_constant__.
 struct alignas(64) DenseParams {
     CUtensorMap tmap_a;      // tiled {K, M} byte tensor, or im2col-mode NHWC tensor

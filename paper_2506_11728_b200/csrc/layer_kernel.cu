@@ -21,6 +21,8 @@
 //
 // Every wait is bounded.  A kernel that gives one up unwinds: all roles of both CTAs stop, copies (unwind.cuh) and MMAs in
 // flight are awaited, tensor memory is released, bit 0 of *status is set.
+#include <algorithm>
+
 #include "layer_epilogue.cuh"
 #include "unwind.cuh"
 
@@ -277,8 +279,8 @@ cudaError_t launch_layer(const LayerParams& p, int op, int pair, int grid, cudaS
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(static_cast<unsigned>(32 * (3 + p.epi_warps)), 1, 1);
-    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kBlockM + (pair ? p.block_n / 2 : p.block_n)) * 128 +
-                           layer_fixed_smem(op, p.type == kF32, p.epi_warps);
+    cfg.dynamicSmemBytes = std::max(kSmemFloor, static_cast<size_t>(p.stages) * (kBlockM + (pair ? p.block_n / 2 : p.block_n)) * 128 +
+                                                    layer_fixed_smem(op, p.type == kF32, p.epi_warps));
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

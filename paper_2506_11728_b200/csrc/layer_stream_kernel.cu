@@ -317,9 +317,11 @@ cudaError_t stream_launch_t(const LayerParams& p, const cudaLaunchConfig_t& cfg)
 
 }  // namespace
 
-int stream_smem(int tokens, int stages) {
+static constexpr int stream_smem_of(int tokens, int stages) {
     return stages * (static_cast<int>(kWeightTile) + tokens * 128) + kStreamRows * (tokens + 4) * 4 + 256 + 1024;
 }
+static_assert(kSmemFloor + stream_smem_of(16, 2) + 2 * kSmemReserved > kSmemPerSm, "a CTA beside one of a dense kernel's");
+int stream_smem(int tokens, int stages) { return stream_smem_of(tokens, stages); }
 
 cudaError_t stream_init() {
     for (cudaError_t e : {stream_init_t<kOpLinear>(), stream_init_t<kOpGated>(), stream_init_t<kOpGatedGrad>()})

@@ -19,6 +19,8 @@
 // 1620 and 1360).
 //
 // Every wait is bounded, with the unwinding of the dense layer kernel.
+#include <algorithm>
+
 #include "layer_epilogue.cuh"
 #include "stage_waits.h"
 #include "unwind.cuh"
@@ -396,7 +398,7 @@ cudaError_t launch_product(const LayerParams& p, int a_order, int pair, int raw,
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(product_threads(raw || p.type == kF32), 1, 1);
-    cfg.dynamicSmemBytes = static_cast<size_t>(p.stages) * (kProductStage + kScaleBytes) + kProductFixed;
+    cfg.dynamicSmemBytes = std::max(kSmemFloor, static_cast<size_t>(p.stages) * (kProductStage + kScaleBytes) + kProductFixed);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
