@@ -437,16 +437,17 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
         tma_prefetch_desc(&p.tmap_b);
         if (p.c_mode == 1 || p.c_mode == 2) tma_prefetch_desc(&p.tmap_c);
     }
+    if (kPair) {   // the peer runs (see tmem_alloc), and its barriers are initialised before anything remote touches them
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
     if (warp == 1) {
         tmem_alloc<kGroup>(smem_u32(tmem_slot), p.tmem_cols);
         tmem_relinquish<kGroup>();
     }
     tc_fence_before();
     __syncthreads();
-    if (kPair) {   // the peer's barriers must be initialised before anything remote touches them
-        cluster_arrive();
-        cluster_wait();
-    }
     tc_fence_after();
     // Programmatic dependent launch: everything so far touched only shared memory, tensor memory
     // and kernel parameters and may overlap the tail of the previous kernel in the stream; from
@@ -1104,6 +1105,7 @@ mip_dense_kernel(const __grid_constant__ DenseParams p) {
     bool unwinding = *abort_flag != 0;
     if (kPair) {   // neither CTA may leave while the other can still reach its shared memory; both know if one unwinds
         if (threadIdx.x == 0) unwind.tell(cta_rank ^ 1u, *abort_flag);
+        __syncwarp();
         cluster_arrive();
         cluster_wait();
         unwinding = unwinding || unwind.get(0) != 0;

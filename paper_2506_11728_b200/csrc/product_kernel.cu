@@ -118,16 +118,17 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
         tma_prefetch_desc(&p.tmap_b0);
         if (p.c_tma) tma_prefetch_desc(&p.tmap_c);
     }
+    if (kPair) {   // the peer runs (see tmem_alloc), and its barriers are initialised before anything remote touches them
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
     if (warp == 1) {
         tmem_alloc<kGroup>(smem_u32(tmem_slot), p.tmem_cols);
         tmem_relinquish<kGroup>();
     }
     tc_fence_before();
     __syncthreads();
-    if (kPair) {
-        cluster_arrive();
-        cluster_wait();
-    }
     tc_fence_after();
     pdl_wait();          // from here on global memory is touched
     pdl_launch_dependents();      // (only now: one kernel at a time waits for another)
@@ -322,6 +323,7 @@ mip_product_kernel(const __grid_constant__ LayerParams p) {
     bool unwinding = *abort_flag != 0;
     if (kPair) {   // both CTAs have stopped, and know it of each other
         if (threadIdx.x == 0) unwind.tell(cta_rank ^ 1u, *abort_flag);
+        __syncwarp();
         cluster_arrive();
         cluster_wait();
         unwinding = unwinding || unwind.get(0) != 0;

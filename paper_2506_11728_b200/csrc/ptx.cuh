@@ -274,6 +274,10 @@ __device__ __forceinline__ uint32_t mapa_u32(uint32_t addr, uint32_t cta) {
 }
 
 // ---------------------------------------------------------------- tcgen05
+// Waits, without a limit, until the columns are there.  For a pair (cta_group::2) it is one operation of both CTAs, and
+// both must be running before either issues it: behind a cluster barrier.  (Issued as soon as a CTA started, ahead of the
+// barrier, the second CTA's could wait for ever where other streams' work had kept its SM busy a little longer: once in
+// some hundred thousand launches.)
 template <int kCtaGroup>
 __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t ncols) {
     if (kCtaGroup == 1)
