@@ -15,7 +15,7 @@
 // short main loop that is the kernel's time, and what counts is how well the schedulers are fed: one warp each issues
 // every fifth clock or so, so there are two or four per scheduler, which take the slots of a tile by turns.  Measured:
 // linear 16384 x 4096 x 1024 gelu bf16 81 us, 62 without the activation.  Where the pitch of C is not a multiple of 16
-// bytes the element form makes that two to three times as much (linear 11957 x 3640 / 3641 x 112 bf16: 64 / 144 us):
+// bytes the element form makes that twice as much and more (linear 11957 x 3640 / 3641 x 112 bf16: 34 / 69 us):
 // every row of a slot begins and ends inside a 32-byte sector, and the memory system completes partly written sectors
 // one by one.
 #pragma once
