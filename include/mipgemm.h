@@ -52,11 +52,13 @@
  * Some calls need global scratch memory (operand re-pitching, slot-padded
  * filters for convolutions gathered in software, the explicit im2col matrix
  * for the few convolutions neither the TMA nor the gather warps can handle).
- * By default it comes from blocks that the library allocates (cudaMallocAsync, on the call's stream) when calls
- * first need them or need more, and keeps for later calls: of the same stream, or of any other once the work that used
- * them is done, so that what is kept is what calls in flight at the same time needed, however many streams come
- * and go (a call that finds no memory left first has all blocks not in use freed, and waits for that);
- * mipgemm_release_staging() frees the blocks not in use.  Calls captured into a CUDA graph take it with cudaMallocAsync from the graph's memory instead.
+ * By default it comes from blocks that the library allocates (cudaMallocAsync, on the
+ * call's stream) when calls first need them or need more, and keeps for later calls: of
+ * the same stream, or of any other once the work that used them is done, so that what is
+ * kept is what calls in flight at the same time needed, however many streams come and go
+ * (a call that finds no memory left first has all blocks not in use freed, and waits for
+ * that).  mipgemm_release_staging() frees the blocks not in use.  Calls captured into a
+ * CUDA graph take it with cudaMallocAsync from the graph's memory instead.
  * A caller may instead lend a buffer with mipgemm_set_workspace(); calls
  * that need more than was lent fail with MIPGEMM_ERR_WORKSPACE.  A lent buffer
  * is shared by all calls: calls that use it must be ordered on one stream.
@@ -361,10 +363,10 @@ int mipgemm_release_staging(void);
  * a matrix is aligned to its element size, pitches are counted in elements.  The 8-bit sums are exact
  * in int32 (the K limits of mipgemm_s8s8s32 hold), everything behind them is computed in binary32 and
  * rounded once, to nearest even, when it is stored.  The activations use the hardware's approximate
- * exponential and reciprocal and, for the error function, a fit of their own: relative to their value, small
- * ones included, they are within (22 + 1.25 x^2) 2^-24 for GELU at x < 0 (16-bit results 4e-6 more), (9 + 1.5 |x|) 2^-24
- * for SILU and (9 + 7.5 |y|) 2^-24 for GELU_TANH, y = 2 sqrt(2/pi) (x + 0.044715 x^3), until they are below 1e-35
- * and may be 0; the gradients' terms are as close.  Scale vectors are float32, 4-byte aligned; NULL
+ * exponential and reciprocal and, for the error function, a fit of their own.  Relative to their value, small
+ * ones included, they are within (22 + 1.25 x^2) 2^-24 for GELU at x < 0 (16-bit results 4e-6 more),
+ * (9 + 1.5 |x|) 2^-24 for SILU and (9 + 7.5 |y|) 2^-24 for GELU_TANH, y = 2 sqrt(2/pi) (x + 0.044715 x^3), until
+ * they are below 1e-35 and may be 0; the terms of the gradients are as close.  Scale vectors are float32, 4-byte aligned; NULL
  * stands for all ones.  Operands with 16-byte aligned bases and pitches are read in place, other 8-bit
  * operands are re-pitched into scratch memory first.  Sums along a long K with few tiles may be taken in
  * parts that meet in scratch memory of the library's own (always added in the same order); with a lent

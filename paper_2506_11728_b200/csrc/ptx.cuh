@@ -1,6 +1,7 @@
 // Thin inline-PTX wrappers for sm_100a: mbarrier, TMA (cp.async.bulk.tensor),
 // tcgen05 (tensor memory, 5th-generation MMA) and a few memory instructions.
-// Every wait offered here is bounded: it returns false instead of spinning forever.
+// Every wait on an mbarrier offered here is bounded: it returns false instead of spinning forever.  (Cluster barriers and
+// the allocation of tensor memory have no bounded form.)
 #pragma once
 #include <cstdint>
 #include <cuda.h>
