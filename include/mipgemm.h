@@ -458,6 +458,144 @@ int mipgemm_bf16s8_product(int type, int a_order, int64_t M, int64_t N, int64_t 
                            const void *A, int64_t lda, const int8_t *B, int64_t ldb, const float *b_scale,
                            void *C, int64_t ldc, int accumulate, void *stream);
 
+/* ---- 8-bit floating point, and the step between two blocks (extensions: the paper's codes are integers) ----
+ *
+ * The same layer with codes of 8-bit floating point, whose scales follow the data in blocks of 128 elements instead of
+ * whole rows, and what stands between its products: norms, gates, dropout and the residual sum.
+ *
+ *   mipgemm_f8_quantize          a matrix -> codes with a scale for each block of 128 along its rows, its columns, or both
+ *   mipgemm_f8_quantize_squares  ... for each square of 128 x 128 (weights: one set of codes serves both passes)
+ *   mipgemm_f8_dequantize        ... and back
+ *   mipgemm_f8f8_product         C = A B of such codes + bias + residual: forward, gradient of the input, of the weights
+ *   mipgemm_norm_step            y = s x + dropout(gate * norm(z)), h = norm(y), h as values and / or as codes
+ *   mipgemm_norm_step_grad       its backward pass
+ *
+ * Common to all of them: what is said above of the operators of an 8-bit transformer layer -- types, alignment to the
+ * element, pitches in elements, binary32 arithmetic rounded once when it is stored, no overlap except where stated,
+ * scratch memory, empty outputs.  A pitch is checked also where the matrix is empty.  Results do not depend on the run: sums are always
+ * taken in the same order (on one device model).
+ */
+typedef enum {
+    MIPGEMM_F8_E4M3 = 0,       /* 4 bits of exponent, 3 of mantissa, largest value 448, no infinity */
+    MIPGEMM_F8_E5M2 = 1        /* 5 and 2, largest finite value 57344                               */
+} mipgemm_f8_format_t;
+
+/* How the blocks that share a scale lie in a matrix of R rows and C columns as it is stored, and where their scales lie. */
+typedef enum {
+    MIPGEMM_F8_ROWS = 0,       /* 1 x 128:    element (r, c) has scale[(c / 128) * lds + r],         lds >= R            */
+    MIPGEMM_F8_COLUMNS = 1,    /* 128 x 1:    element (r, c) has scale[(r / 128) * lds + c],         lds >= C            */
+    MIPGEMM_F8_SQUARES = 2     /* 128 x 128:  element (r, c) has scale[(r / 128) * lds + c / 128],   lds >= ceil(C / 128) */
+} mipgemm_f8_blocks_t;
+
+/*
+ * Codes and scales of the blocks of X:  scale = max|x| / L,  q = rne(x * (L / max|x|)),  L the format's largest finite value,
+ * both quotients and the product rounded in binary32.  Blocks at the edges hold what there is.  A block whose largest
+ * magnitude is below 2^-119 (E4M3) or 2^-112 (E5M2), all zeros among them, gets scale 0 and codes 0; one that holds an
+ * infinity or a NaN gets scale NaN and codes 0, so that whatever is computed from it is NaN.
+ *
+ *   X : M x N row-major, ldx >= N (read)
+ *   Qr, r_scale, ldrs : codes by MIPGEMM_F8_ROWS (ldqr >= N, counted in bytes) and their scales, or both pointers NULL
+ *   Qc, c_scale, ldcs : codes by MIPGEMM_F8_COLUMNS, or both NULL
+ * X is read once, whether one side is wanted or both.
+ */
+int mipgemm_f8_quantize(int type, int format, int64_t M, int64_t N, const void *X, int64_t ldx,
+                        void *Qr, int64_t ldqr, float *r_scale, int64_t ldrs,
+                        void *Qc, int64_t ldqc, float *c_scale, int64_t ldcs, void *stream);
+
+/* The same by MIPGEMM_F8_SQUARES. */
+int mipgemm_f8_quantize_squares(int type, int format, int64_t M, int64_t N, const void *X, int64_t ldx,
+                                void *Q, int64_t ldq, float *scale, int64_t lds, void *stream);
+
+/* X = codes times their scales, the product rounded in binary32, then to the type.  `blocks`: a mipgemm_f8_blocks_t. */
+int mipgemm_f8_dequantize(int type, int format, int blocks, int64_t M, int64_t N, const void *Q, int64_t ldq,
+                          const float *scale, int64_t lds, void *X, int64_t ldx, void *stream);
+
+/*
+ * C_ij = sum over blocks kb of 128 k of  a_scale(kb, i) b_scale(kb, j) sum_k a(i,k) b(k,j)  + bias_j + residual_ij.
+ *   forward                  Y = X W^T        A = X by rows, K_CONTIGUOUS;     B = W by squares, K_CONTIGUOUS
+ *   gradient of the input    dX = dY W        A = dY by rows, K_CONTIGUOUS;    B = W by squares, MN_CONTIGUOUS (as it lies)
+ *   gradient of the weights  dW = dY^T X      A = dY by columns, MN_CONTIGUOUS; B = X by columns, MN_CONTIGUOUS
+ *   A : codes of a_format, a(i,k) = A[i*lda + k] (a_order K_CONTIGUOUS) or A[k*lda + i] (MN_CONTIGUOUS); its blocks lie
+ *       along k: a_scale[kb*ldas + i], ldas >= M
+ *   B : codes of b_format, b(k,j) = B[j*ldb + k] (b_order K_CONTIGUOUS) or B[k*ldb + j] (MN_CONTIGUOUS); b_blocks says how
+ *       its blocks lie in B as it is stored: MIPGEMM_F8_SQUARES, or along k, which is MIPGEMM_F8_ROWS for K_CONTIGUOUS and
+ *       MIPGEMM_F8_COLUMNS for MN_CONTIGUOUS (scales as given there)
+ *   a_scale, b_scale : float32, NULL stands for all ones;  bias : N float32, or NULL
+ *   residual : M x N of the call's type, ldr >= N, or NULL; may be C itself (with ldr == ldc): C += ...
+ *   C : M x N of the call's type, ldc >= N (written)
+ * A block's products are summed on the tensor cores in binary32, the blocks' sums in binary32 behind their scales, in the
+ * order of k or in equal shares of it; the error stays below (K + 8) 2^-23 of the sum of the magnitudes.  Scratch memory: as for
+ * mipgemm_s8s8_linear.
+ */
+int mipgemm_f8f8_product(int type, int a_format, int b_format, int a_order, int b_order, int b_blocks,
+                         int64_t M, int64_t N, int64_t K,
+                         const void *A, int64_t lda, const float *a_scale, int64_t ldas,
+                         const void *B, int64_t ldb, const float *b_scale, int64_t ldbs,
+                         const float *bias, const void *residual, int64_t ldr, void *C, int64_t ldc, void *stream);
+
+typedef enum {
+    MIPGEMM_NORM_NONE = 0,
+    MIPGEMM_NORM_RMS = 1,      /* v w / sqrt(mean(v^2) + eps)                                        */
+    MIPGEMM_NORM_LAYER = 2     /* (v - m) w / sqrt(mean((v - m)^2) + eps) + b,  m = mean(v)          */
+} mipgemm_norm_t;
+
+typedef enum {
+    MIPGEMM_CODES_NONE = 0,
+    MIPGEMM_CODES_S8 = 1,      /* as mipgemm_quantize_rows makes them: q_scale has M values          */
+    MIPGEMM_CODES_E4M3 = 2,    /* as mipgemm_f8_quantize makes them along the rows: q_scale[(j / 128) * ldqs + i] */
+    MIPGEMM_CODES_E5M2 = 3
+} mipgemm_codes_t;
+
+/*
+ * The step between two blocks of a layer, over the rows i of M x N matrices:
+ *   v = dropout(gate * post(Z)),   Y = x_scale X + v,   H = pre(Y),
+ * `post` the norm behind a block, `pre` the one in front of the next (each a mipgemm_norm_t; H is computed from the
+ * unrounded Y).  One pass: X and Z are read once, Y and H or its codes written once, the mask is never stored.
+ *   X, Z : M x N (read); either may be NULL (then 0; without Z no post norm, gate or dropout)
+ *   post_weight, pre_weight : N float32, NULL stands for ones;  post_bias, pre_bias : N float32 or NULL, for
+ *       MIPGEMM_NORM_LAYER only
+ *   gate : ceil(M / gate_rows) x N, row i takes gate row i / gate_rows (1: a gate for each element; M: for each channel;
+ *       a sequence's length: for each sequence and channel), or NULL (no gate)
+ *   drop : rate in [0, 1), taken to the nearest multiple of 2^-16 (below 1 still); kept elements are divided by
+ *       1 - that rate, dropped ones are 0, whatever they were.  Element (i, j) is dropped when the half-word j % 8 (low half
+ *       of a word first) of Philox4x32-10 with key `seed` and counter {i * ceil(N / 8) + j / 8, *counter}, each 64
+ *       bits, low word first, is below rate * 2^16.  counter : device, 8-byte aligned, read when the kernel runs (so that
+ *       a captured graph draws another mask at each replay, if it is raised between them); NULL stands for 0.
+ *   Y : M x N (written), or NULL; may be X or Z itself (with the same pitch)
+ *   H : M x N (written), or NULL;  codes, Q, ldq (bytes), q_scale, ldqs : H's codes (unless MIPGEMM_CODES_NONE), made from the
+ *       unrounded H
+ *   stats : M x 4 float32 (written) or NULL: mean and 1 / sqrt(... + eps) of the post norm, the same of the pre norm (0 where
+ *       there is none; means of MIPGEMM_NORM_RMS are 0); what the backward pass needs
+ * N <= 32768.  Squares are summed in binary32.
+ */
+int mipgemm_norm_step(int type, int post, int pre, int64_t M, int64_t N, float eps,
+                      const void *X, int64_t ldx, float x_scale,
+                      const void *Z, int64_t ldz, const float *post_weight, const float *post_bias,
+                      const void *gate, int64_t ldgate, int64_t gate_rows,
+                      float drop, uint64_t seed, const uint64_t *counter,
+                      const float *pre_weight, const float *pre_bias,
+                      void *Y, int64_t ldy, void *H, int64_t ldh,
+                      int codes, void *Q, int64_t ldq, float *q_scale, int64_t ldqs,
+                      float *stats, void *stream);
+
+/*
+ * Backward pass of the step, from the gradients dY of Y (what reaches it besides H; NULL: nothing does, if there is a pre norm)
+ * and dH of H (with a pre norm only).  Y, Z, gate, the weights, drop, seed and counter as in the forward pass; stats as it
+ * left them.  Every output may be NULL:
+ *   dX, dZ : M x N (written); each may be one of dY, dH, Y and Z (with the same pitch), not both the same
+ *   dgate : as gate (written), summed over the rows that share a gate row
+ *   dpost_weight, dpost_bias, dpre_weight, dpre_bias : N float32 (written), summed over all rows in binary32
+ * M == 0 writes zeros to the four vectors.  Scratch memory: for the sums of the vectors and of dgate.
+ */
+int mipgemm_norm_step_grad(int type, int post, int pre, int64_t M, int64_t N,
+                           const void *dY, int64_t lddy, const void *dH, int64_t lddh,
+                           const void *Y, int64_t ldy, const float *pre_weight, float x_scale,
+                           const void *Z, int64_t ldz, const float *post_weight, const float *post_bias,
+                           const void *gate, int64_t ldgate, int64_t gate_rows,
+                           float drop, uint64_t seed, const uint64_t *counter, const float *stats,
+                           void *dX, int64_t lddx, void *dZ, int64_t lddz, void *dgate, int64_t lddgate,
+                           float *dpost_weight, float *dpost_bias, float *dpre_weight, float *dpre_bias, void *stream);
+
 /* ---- support calls (no counterpart in the paper) ---- */
 
 /* Number of kernels this library has enqueued since it was loaded (all threads, all devices). */

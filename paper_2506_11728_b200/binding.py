@@ -22,6 +22,7 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 _i64, _int, _vp, _sz = ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t
+_f32, _u64 = ctypes.c_float, ctypes.c_uint64
 
 OK, ERR_INVALID_ARG, ERR_K_TOO_LARGE, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(7)
 ERR_STATIC_SCRATCH_LIMIT = 7
@@ -59,6 +60,14 @@ SIGNATURES = {
     "mipgemm_s8s8_gated": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64, _vp] * 3 + [_vp, _i64, _vp]),
     "mipgemm_s8s8_gated_grad": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64, _vp] * 3 + [_vp, _i64] * 3 + [_vp]),
     "mipgemm_bf16s8_product": (_int, [_int] * 2 + [_i64] * 3 + [_vp, _i64] * 2 + [_vp, _vp, _i64, _int, _vp]),
+    "mipgemm_f8_quantize": (_int, [_int] * 2 + [_i64] * 2 + [_vp, _i64] * 5 + [_vp]),
+    "mipgemm_f8_quantize_squares": (_int, [_int] * 2 + [_i64] * 2 + [_vp, _i64] * 3 + [_vp]),
+    "mipgemm_f8_dequantize": (_int, [_int] * 3 + [_i64] * 2 + [_vp, _i64] * 3 + [_vp]),
+    "mipgemm_f8f8_product": (_int, [_int] * 6 + [_i64] * 3 + [_vp, _i64] * 4 + [_vp] + [_vp, _i64] * 2 + [_vp]),
+    "mipgemm_norm_step": (_int, [_int] * 3 + [_i64] * 2 + [_f32, _vp, _i64, _f32, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _f32, _u64, _vp,
+                                                           _vp, _vp, _vp, _i64, _vp, _i64, _int, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "mipgemm_norm_step_grad": (_int, [_int] * 3 + [_i64] * 2 + [_vp, _i64] * 3 + [_vp, _f32, _vp, _i64, _vp, _vp, _vp, _i64, _i64, _f32, _u64,
+                                                                _vp, _vp] + [_vp, _i64] * 3 + [_vp] * 5),
     "mipgemm_host_s8s8s32": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
     "mipgemm_host_u8s8s32": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
     "mipgemm_s8s8s32_static_scratch": (_int, [_i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _int, _vp]),
@@ -299,6 +308,61 @@ def mipgemm_bf16s8_product(type, a_order, M, N, K, A, lda, B, ldb, b_scale, C, l
     """C (+)= A[bf16] * diag(b_scale) * B[int8, K x N row-major]; a_order K_CONTIGUOUS or MN_CONTIGUOUS."""
     return _check(_lib.mipgemm_bf16s8_product(type, a_order, M, N, K, _ptr(A), lda, _ptr(B), ldb, _ptr(b_scale), _ptr(C),
                                               ldc, int(bool(accumulate)), _stream(stream)), check)
+
+
+#: mipgemm_f8_format_t, mipgemm_f8_blocks_t, mipgemm_norm_t and mipgemm_codes_t by name
+F8_FORMATS = {"e4m3": 0, "e5m2": 1}
+F8_BLOCKS = {"rows": 0, "columns": 1, "squares": 2}
+NORMS = {"none": 0, "rms": 1, "layer": 2}
+CODES = {"none": 0, "s8": 1, "e4m3": 2, "e5m2": 3}
+
+
+def mipgemm_f8_quantize(type, format, M, N, X, ldx, Qr, ldqr, r_scale, ldrs, Qc, ldqc, c_scale, ldcs, stream=None, check=True) -> int:
+    """8-bit floating-point codes with a scale for each block of 128 along the rows (Qr), along the columns (Qc), or both."""
+    return _check(_lib.mipgemm_f8_quantize(type, format, M, N, _ptr(X), ldx, _ptr(Qr), ldqr, _ptr(r_scale), ldrs, _ptr(Qc), ldqc,
+                                           _ptr(c_scale), ldcs, _stream(stream)), check)
+
+
+def mipgemm_f8_quantize_squares(type, format, M, N, X, ldx, Q, ldq, scale, lds, stream=None, check=True) -> int:
+    """8-bit floating-point codes with a scale for each square of 128 x 128."""
+    return _check(_lib.mipgemm_f8_quantize_squares(type, format, M, N, _ptr(X), ldx, _ptr(Q), ldq, _ptr(scale), lds, _stream(stream)),
+                  check)
+
+
+def mipgemm_f8_dequantize(type, format, blocks, M, N, Q, ldq, scale, lds, X, ldx, stream=None, check=True) -> int:
+    """X = codes times their blocks' scales."""
+    return _check(_lib.mipgemm_f8_dequantize(type, format, blocks, M, N, _ptr(Q), ldq, _ptr(scale), lds, _ptr(X), ldx, _stream(stream)),
+                  check)
+
+
+def mipgemm_f8f8_product(type, a_format, b_format, a_order, b_order, b_blocks, M, N, K, A, lda, a_scale, ldas, B, ldb, b_scale, ldbs, bias,
+                         residual, ldr, C, ldc, stream=None, check=True) -> int:
+    """C = sum over blocks of 128 k of a_scale * b_scale * (A * B) + bias[column] + residual; scales, bias and residual may be None."""
+    return _check(_lib.mipgemm_f8f8_product(type, a_format, b_format, a_order, b_order, b_blocks, M, N, K, _ptr(A), lda, _ptr(a_scale), ldas,
+                                            _ptr(B), ldb, _ptr(b_scale), ldbs, _ptr(bias), _ptr(residual), ldr, _ptr(C), ldc,
+                                            _stream(stream)), check)
+
+
+def mipgemm_norm_step(type, post, pre, M, N, eps=1e-5, X=None, ldx=0, x_scale=1.0, Z=None, ldz=0, post_weight=None, post_bias=None,
+                      gate=None, ldgate=0, gate_rows=1, drop=0.0, seed=0, counter=None, pre_weight=None, pre_bias=None, Y=None, ldy=0,
+                      H=None, ldh=0, codes=0, Q=None, ldq=0, q_scale=None, ldqs=0, stats=None, stream=None, check=True) -> int:
+    """Y = x_scale * X + dropout(gate * post(Z)), H = pre(Y), as values and / or codes."""
+    return _check(_lib.mipgemm_norm_step(type, post, pre, M, N, eps, _ptr(X), ldx, x_scale, _ptr(Z), ldz, _ptr(post_weight), _ptr(post_bias),
+                                         _ptr(gate), ldgate, gate_rows, drop, seed, _ptr(counter), _ptr(pre_weight), _ptr(pre_bias),
+                                         _ptr(Y), ldy, _ptr(H), ldh, codes, _ptr(Q), ldq, _ptr(q_scale), ldqs, _ptr(stats),
+                                         _stream(stream)), check)
+
+
+def mipgemm_norm_step_grad(type, post, pre, M, N, dY=None, lddy=0, dH=None, lddh=0, Y=None, ldy=0, pre_weight=None, x_scale=1.0, Z=None,
+                           ldz=0, post_weight=None, post_bias=None, gate=None, ldgate=0, gate_rows=1, drop=0.0, seed=0, counter=None,
+                           stats=None, dX=None, lddx=0, dZ=None, lddz=0, dgate=None, lddgate=0, dpost_weight=None, dpost_bias=None,
+                           dpre_weight=None, dpre_bias=None, stream=None, check=True) -> int:
+    """Gradients of that step's X, Z, gate, weights and biases from those of Y and H."""
+    return _check(_lib.mipgemm_norm_step_grad(type, post, pre, M, N, _ptr(dY), lddy, _ptr(dH), lddh, _ptr(Y), ldy, _ptr(pre_weight), x_scale,
+                                              _ptr(Z), ldz, _ptr(post_weight), _ptr(post_bias), _ptr(gate), ldgate, gate_rows, drop, seed,
+                                              _ptr(counter), _ptr(stats), _ptr(dX), lddx, _ptr(dZ), lddz, _ptr(dgate), lddgate,
+                                              _ptr(dpost_weight), _ptr(dpost_bias), _ptr(dpre_weight), _ptr(dpre_bias),
+                                              _stream(stream)), check)
 
 
 def mipgemm_host_s8s8s32(M, N, K, A, lda, B, ldb, C, ldc, accumulate=0, stream=None, check=True) -> int:

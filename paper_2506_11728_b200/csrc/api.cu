@@ -223,7 +223,7 @@ int get_device(DeviceState** out) {
 // Kernels of the layer operators, set up on a device when one of the family is first launched there: setting an attribute
 // loads the kernel, and loading these with the plain products' made the first call of a program that never uses them
 // 8 to 20 ms longer (9 ms without them).
-constexpr int kFamilyLayer = 1, kFamilyFew = 2, kFamilyProduct = 4;
+constexpr int kFamilyLayer = 1, kFamilyFew = 2, kFamilyProduct = 4, kFamilyF8 = 8;
 int family_ready(DeviceState* dev, int family) {
     if (dev->families.load(std::memory_order_acquire) & family) return MIPGEMM_OK;
     std::lock_guard<std::mutex> lock(g_mutex);
@@ -231,13 +231,15 @@ int family_ready(DeviceState* dev, int family) {
     // (another stream may be captured meanwhile: loading kernels does not belong to its graph)
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     (void)cudaThreadExchangeStreamCaptureMode(&mode);
-    const cudaError_t e = family == kFamilyLayer ? layer_init() : (family == kFamilyFew ? stream_init() : product_init());
+    const cudaError_t e = family == kFamilyLayer ? layer_init()
+                          : (family == kFamilyFew ? stream_init() : (family == kFamilyProduct ? product_init() : f8_product_init()));
     (void)cudaThreadExchangeStreamCaptureMode(&mode);
     if (e != cudaSuccess) return cuda_fail(e);
     dev->families.fetch_or(family, std::memory_order_release);
     if (log_enabled())
         std::fprintf(stderr, "mipgemm: set up %s kernels\n",
-                     family == kFamilyLayer ? "dense layer" : (family == kFamilyFew ? "few-token layer" : "product"));
+                     family == kFamilyLayer ? "dense layer"
+                     : (family == kFamilyFew ? "few-token layer" : (family == kFamilyProduct ? "product" : "8-bit floating-point product")));
     return MIPGEMM_OK;
 }
 
@@ -1979,6 +1981,8 @@ int product_impl(const ProductArgs& a, void* stream_v) {
     return rc;
 }
 
+#include "float8_api.cuh"
+
 }  // namespace
 
 extern "C" {
@@ -2404,6 +2408,78 @@ int mipgemm_bf16s8_product(int type, int a_order, int64_t M, int64_t N, int64_t 
 }
 
 uint64_t mipgemm_launch_count(void) { return g_launches.load(); }
+
+int mipgemm_f8_quantize(int type, int format, int64_t M, int64_t N, const void* X, int64_t ldx, void* Qr, int64_t ldqr, float* r_scale, int64_t ldrs,
+                        void* Qc, int64_t ldqc, float* c_scale, int64_t ldcs, void* stream) {
+    const mip::F8Codes out[2] = {{Qr, ldqr, r_scale, ldrs}, {Qc, ldqc, c_scale, ldcs}};
+    return f8_quantize_impl(type, format, false, M, N, X, ldx, out, stream);
+}
+
+int mipgemm_f8_quantize_squares(int type, int format, int64_t M, int64_t N, const void* X, int64_t ldx, void* Q, int64_t ldq, float* scale,
+                                int64_t lds, void* stream) {
+    const mip::F8Codes out[2] = {{Q, ldq, scale, lds}, {nullptr, 0, nullptr, 0}};
+    return f8_quantize_impl(type, format, true, M, N, X, ldx, out, stream);
+}
+
+int mipgemm_f8_dequantize(int type, int format, int blocks, int64_t M, int64_t N, const void* Q, int64_t ldq, const float* scale, int64_t lds,
+                          void* X, int64_t ldx, void* stream) {
+    return f8_dequantize_impl(type, format, blocks, M, N, mip::F8Codes{const_cast<void*>(Q), ldq, const_cast<float*>(scale), lds}, X, ldx, stream);
+}
+
+int mipgemm_f8f8_product(int type, int a_format, int b_format, int a_order, int b_order, int b_blocks, int64_t M, int64_t N, int64_t K,
+                         const void* A, int64_t lda, const float* a_scale, int64_t ldas, const void* B, int64_t ldb, const float* b_scale,
+                         int64_t ldbs, const float* bias, const void* residual, int64_t ldr, void* C, int64_t ldc, void* stream) {
+    return f8_product_impl(mip::F8ProductArgs{type, a_format, b_format, a_order, b_order, b_blocks, M, N, K, A, lda, a_scale, ldas, B, ldb, b_scale,
+                                              ldbs, bias, residual, ldr, C, ldc}, stream);
+}
+
+int mipgemm_norm_step(int type, int post, int pre, int64_t M, int64_t N, float eps, const void* X, int64_t ldx, float x_scale, const void* Z,
+                      int64_t ldz, const float* post_weight, const float* post_bias, const void* gate, int64_t ldgate, int64_t gate_rows, float drop,
+                      uint64_t seed, const uint64_t* counter, const float* pre_weight, const float* pre_bias, void* Y, int64_t ldy, void* H,
+                      int64_t ldh, int codes, void* Q, int64_t ldq, float* q_scale, int64_t ldqs, float* stats, void* stream) {
+    mip::StepArgs a = {};
+    a.M = M; a.N = N;
+    a.post = post; a.pre = pre; a.codes = codes;
+    a.eps = eps; a.x_scale = x_scale;
+    a.X = X; a.ldx = ldx;
+    a.Z = Z; a.ldz = ldz;
+    a.post_w = post_weight; a.post_b = post_bias;
+    a.gate = gate; a.ldgate = ldgate; a.gate_rows = gate_rows;
+    a.seed = seed; a.counter = reinterpret_cast<const unsigned long long*>(counter);
+    a.pre_w = pre_weight; a.pre_b = pre_bias;
+    a.Y = Y; a.ldy = ldy;
+    a.H = H; a.ldh = ldh;
+    a.Q = static_cast<uint8_t*>(Q); a.ldq = ldq;
+    a.q_scale = q_scale; a.ldqs = ldqs;
+    a.stats = stats;
+    return norm_step_impl(type, a, drop, stream);
+}
+
+int mipgemm_norm_step_grad(int type, int post, int pre, int64_t M, int64_t N, const void* dY, int64_t lddy, const void* dH, int64_t lddh,
+                           const void* Y, int64_t ldy, const float* pre_weight, float x_scale, const void* Z, int64_t ldz,
+                           const float* post_weight, const float* post_bias, const void* gate, int64_t ldgate, int64_t gate_rows, float drop,
+                           uint64_t seed, const uint64_t* counter, const float* stats, void* dX, int64_t lddx, void* dZ, int64_t lddz, void* dgate,
+                           int64_t lddgate, float* dpost_weight, float* dpost_bias, float* dpre_weight, float* dpre_bias, void* stream) {
+    mip::StepGradArgs a = {};
+    a.M = M; a.N = N;
+    a.post = post; a.pre = pre;
+    a.x_scale = x_scale;
+    a.dY = dY; a.lddy = lddy;
+    a.dH = dH; a.lddh = lddh;
+    a.Y = Y; a.ldy = ldy;
+    a.pre_w = pre_weight;
+    a.Z = Z; a.ldz = ldz;
+    a.post_w = post_weight; a.post_b = post_bias;
+    a.gate = gate; a.ldgate = ldgate; a.gate_rows = gate_rows;
+    a.seed = seed; a.counter = reinterpret_cast<const unsigned long long*>(counter);
+    a.stats = stats;
+    a.dX = dX; a.lddx = lddx;
+    a.dZ = dZ; a.lddz = lddz;
+    a.dgate = dgate; a.lddgate = lddgate;
+    a.dpost_w = dpost_weight; a.dpost_b = dpost_bias;
+    a.dpre_w = dpre_weight; a.dpre_b = dpre_bias;
+    return norm_step_grad_impl(type, a, drop, stream);
+}
 
 int mipgemm_release_staging(void) {
     DeviceState* dev = nullptr;

@@ -1,0 +1,555 @@
+// C = sum over blocks of 128 k of  sa[kb][i] sb[kb][j] (A B)_kb  + bias + residual, A and B 8-bit floating point: the products of a
+// layer and of its backward pass (operands K- or M/N-contiguous, as they lie).
+//
+// The scales change along the summed axis, so a block's products are summed by the tensor core on their own
+// (tcgen05.mma.kind::f8f6f4, four instructions, binary32 in tensor memory) and added to the tile's sums, which live in
+// registers, behind their two scales.  Eight warps do that: a thread has one row and 128 (CTA pairs, 256 x 256 tiles) or 64
+// (single CTAs, 128 x 128) columns; tensor memory holds two or four blocks' products, so that the tensor core works on the next
+// block meanwhile.  With squares of 128 x 128 on B's side both scales are one number per thread and block: one packed
+// multiply-add for two elements.  With a scale for each column they come through shared memory, and it is one multiplication
+// more.
+//
+// Outputs go through swizzled slots in shared memory as in the layer's kernels (layer_epilogue.cuh).
+//
+// Every wait is bounded, with the unwinding of the dense layer kernel.
+#include <algorithm>
+
+#include "layer_epilogue.cuh"
+#include "unwind.cuh"
+
+namespace mip {
+
+namespace {
+
+constexpr int kSumWarps = 8;
+constexpr int kF8Threads = 32 * (4 + kSumWarps);
+constexpr int kSlotBuffers = 2;
+constexpr int kMaxF8Stages = 8;
+// Registers per thread: the sums take 128 of those of a pair's summing warps.  The block is launched with kLaunchRegs a thread; the
+// four other warps give theirs up (checked against the compiled kernel before its first launch).
+constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 216;
+static_assert(4 * kFewRegs + kSumWarps * kManyRegs <= (4 + kSumWarps) * kLaunchRegs, "register split");
+
+template <int kRegs>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+
+template <int kCtaGroup>
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    if (kCtaGroup == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+__device__ __forceinline__ uint64_t words_f2(uint32_t a, uint32_t b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// kPair: 256 x 256 tiles of CTA pairs, else 128 x 128.  kVec: a scale for each column of B, else for each 128.
+// kWide: 32-bit outputs.  kRaw: the sums go to planes of partial sums.
+template <bool kPair, bool kVec, bool kWide, bool kRaw>
+__global__ void __launch_bounds__(kF8Threads, 1)
+mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
+    constexpr int kGroup = kPair ? 2 : 1;
+    constexpr int kN = kPair ? 256 : 128;                // accumulator columns
+    constexpr int kBuffers = 512 / kN;                   // blocks of products in tensor memory
+    constexpr int kCols = kN / 2;                        // columns per thread
+    constexpr int kRowsPerTile = kGroup * kBlockM;
+    constexpr uint32_t a_bytes = kBlockM * 128, b_bytes = 128 * 128, stage_bytes = a_bytes + b_bytes;
+    constexpr int kSlot = slot_bytes(kWide);
+    const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
+    const bool leader = cta_rank == 0;
+    const int first_unit = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
+    const int unit_stride = kPair ? static_cast<int>(gridDim.x >> 1) : static_cast<int>(gridDim.x);
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
+    uint8_t* smem = smem_raw + pad;
+    const uint32_t smem_base = raw_addr + pad;
+    // shared memory: [stages x (A | B)] [slots of the summing warps] [their column vectors: 128 floats, twice] [control block]
+    const uint32_t slots = smem_base + p.stages * stage_bytes;
+    const uint32_t colvec = slots + (kRaw ? 0u : kSumWarps * kSlotBuffers * kSlot);
+    const uint32_t ctrl = colvec + kSumWarps * kF8ColBytes;
+    const uint32_t bar_full = ctrl, bar_empty = ctrl + 8u * kMaxF8Stages;
+    const uint32_t bar_tfull = ctrl + 16u * kMaxF8Stages, bar_tempty = bar_tfull + 32u, bar_drain = bar_tempty + 32u;
+    const uint32_t bar_in = bar_drain + 8u;              // kSumWarps x kSlotBuffers: a slot's tile has arrived
+    uint8_t* ctrl_ptr = smem + (bar_in + 8u * kSumWarps * kSlotBuffers - smem_base);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr);
+    volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(tmem_slot + 1);
+    const UnwindWords unwind = {bar_in + 8u * kSumWarps * kSlotBuffers + 8u};
+    static_assert(16 * kMaxF8Stages + 72 + 8 * kSumWarps * kSlotBuffers + 8 + UnwindWords::kBytes <= kCtrlBytes, "control block");
+
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(bar_full + 8u * s, 2);                       // two producers
+            mbar_init(bar_empty + 8u * s, 1);
+        }
+        for (int a = 0; a < kBuffers; ++a) {
+            mbar_init(bar_tfull + 8u * a, 1);
+            mbar_init(bar_tempty + 8u * a, kGroup * kSumWarps);
+        }
+        mbar_init(bar_drain, 1);
+        for (int i = 0; i < kSumWarps * kSlotBuffers; ++i) mbar_init(bar_in + 8u * i, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&p.tmap_a);
+        tma_prefetch_desc(&p.tmap_b0);
+        if (p.r_tma) tma_prefetch_desc(&p.tmap_r);
+        if (p.c_tma) tma_prefetch_desc(&p.tmap_c);
+    }
+    if (kPair) {   // the peer runs (see tmem_alloc), and its barriers are initialised before anything remote touches them
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 1) {
+        tmem_alloc<kGroup>(smem_u32(tmem_slot), 512);
+        tmem_relinquish<kGroup>();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();          // from here on global memory is touched
+    pdl_launch_dependents();      // (only now: one kernel at a time waits for another)
+    const uint32_t tmem_base = *tmem_slot;
+    const int total_units = layer_units(p);
+    const uint64_t budget = p.wait_budget_ns;
+
+    if (warp < 4) {
+        if constexpr (kPair) regs_dec<kFewRegs>();
+        if (warp == 0 || warp == 2) {
+            // -------------------------------------------------------- TMA producers: A (warp 0), B (warp 2)
+            uint32_t s = 0, phase = 0, issued = 0;
+            bool ok = true;
+            const bool side_a = warp == 0;
+            const int mn = side_a ? p.a_mn : p.b_mn;
+            // (fewer than 128 K-contiguous rows of A in all: only those are copied, as in the dense layer kernel)
+            const uint32_t tx_bytes = kGroup * (side_a ? static_cast<uint32_t>(p.a_rows) * 128u : b_bytes);
+            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+                const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+                const int at = side_a ? tc.m0 + static_cast<int>(cta_rank) * kBlockM : tc.n0 + static_cast<int>(cta_rank) * 128;
+                for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
+                    if (!mbar_wait_warp(bar_empty + 8u * s, phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                    const uint32_t full_local = bar_full + 8u * s;
+                    const uint32_t full = kPair ? mapa_u32(full_local, 0) : full_local;
+                    const uint32_t dst = smem_base + s * stage_bytes + (side_a ? 0u : a_bytes);
+                    if (elect_one()) {
+                        if (leader) mbar_arrive_expect_tx(full_local, tx_bytes);
+                        const CUtensorMap* map = side_a ? &p.tmap_a : &p.tmap_b0;
+                        const int x = mn ? at : kb * 128, y = mn ? kb * 128 : at;
+                        if (kPair) tma_load_2d_pair(dst, map, full, x, y);
+                        else tma_load_2d(dst, map, full, x, y);
+                    }
+                    ++issued;
+                    if (++s == static_cast<uint32_t>(p.stages)) { s = 0; phase ^= 1u; }
+                }
+            }
+            if (lane == 0) unwind.put(side_a ? 0 : 1, issued);
+        } else if (warp == 1 && leader) {
+            // -------------------------------------------------------- MMA issuer
+            uint32_t s = 0, phase = 0, acc = 0, acc_phase = 0;
+            bool ok = true;
+            // 32 k per instruction: 32 bytes of a K-contiguous row, 32 rows of 128 bytes of an M/N-contiguous block
+            const uint64_t a_step = p.a_mn ? 256ull : 2ull, b_step = p.b_mn ? 256ull : 2ull;
+            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+                const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+                for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
+                    if (!mbar_wait_warp<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget) ||
+                        !mbar_wait_warp(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a_addr = smem_base + s * stage_bytes;
+                    const uint64_t a_desc = p.a_mn ? make_mnmajor_desc(a_addr, a_bytes) : make_kmajor_desc(a_addr, 128);
+                    const uint64_t b_desc = p.b_mn ? make_mnmajor_desc(a_addr + a_bytes, b_bytes) : make_kmajor_desc(a_addr + a_bytes, 128);
+                    const uint32_t empty_local = bar_empty + 8u * s, tfull_local = bar_tfull + 8u * acc;
+                    const uint32_t empty_peer = kPair ? mapa_u32(empty_local, 1) : 0u, tfull_peer = kPair ? mapa_u32(tfull_local, 1) : 0u;
+                    const bool signal = !(p.debug_flags & 1);      // (test hook, bit 0: the "products ready" signal is withheld)
+                    if (elect_one()) {
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k)
+                            mma_f8<kGroup>(tmem_base + acc * kN, a_desc + a_step * k, b_desc + b_step * k, p.idesc, k > 0 ? 1u : 0u);
+                        if (kPair) {
+                            mma_commit_pair(empty_local);
+                            mma_commit_pair(empty_peer);
+                            if (signal) {
+                                mma_commit_pair(tfull_local);
+                                mma_commit_pair(tfull_peer);
+                            }
+                        } else {
+                            mma_commit(empty_local);
+                            if (signal) mma_commit(tfull_local);
+                        }
+                    }
+                    if (++s == static_cast<uint32_t>(p.stages)) { s = 0; phase ^= 1u; }
+                    if (++acc == kBuffers) { acc = 0; acc_phase ^= 1u; }
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ sums and outputs
+        if constexpr (kPair) regs_inc<kManyRegs>();
+        const int e = warp - 4, q = warp & 3, half = e >> 2;
+        const uint32_t my_slots = slots + static_cast<uint32_t>(e) * kSlotBuffers * kSlot;
+        const uint32_t my_cols = colvec + static_cast<uint32_t>(e) * kF8ColBytes;
+        const uint32_t my_bar = bar_in + 8u * static_cast<uint32_t>(e * kSlotBuffers);
+        const uint32_t t_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(half * kCols);
+        const bool f16 = p.type == kF16, has_r = p.R != nullptr, r_tma = p.r_tma != 0, c_tma = p.c_tma != 0;
+        uint32_t acc = 0, acc_phase = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
+        bool ok = true;
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+            const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+            const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32, row = row0 + lane;
+            const int col0 = tc.n0 + half * kCols;
+            const bool active = row0 < p.M && col0 < p.N;          // (warp-uniform)
+            const int n_slots = active ? min(kCols / 32, (p.N - col0 + 31) / 32) : 0;
+            uint64_t sum[kCols / 2];
+#pragma unroll
+            for (int j = 0; j < kCols / 2; ++j) sum[j] = 0ull;
+            // what the slots' first buffers hold in the end: asked for before the sums are there
+            int asked = 0;
+            const auto ask = [&] {
+                const uint32_t b = loads % kSlotBuffers;
+                if (elect_one()) {
+                    mbar_arrive_expect_tx(my_bar + 8u * b, kSlot);
+                    tma_load_2d(my_slots + b * kSlot, &p.tmap_r, my_bar + 8u * b, col0 + asked * 32, row0);
+                }
+                __syncwarp();
+                ++asked;
+                ++loads;
+            };
+            if (!kRaw && r_tma && n_slots > 0) {
+                if (elect_one()) tma_store_wait_read<0>();
+                __syncwarp();
+                fence_proxy_async_smem();
+                __syncwarp();
+                while (asked < kSlotBuffers && asked < n_slots) ask();
+            }
+            // scales of the next two blocks are on their way while one is summed
+            const auto fetch_a = [&](int kb) { return row < p.M && kb < tc.kb1 ? (p.sa ? __ldg(p.sa + static_cast<long long>(kb) * p.lds_a + row) : 1.0f) : 0.0f; };
+            const auto fetch_b = [&](int kb, int i) {              // kVec: of columns lane + 32 i; else of the warp's columns
+                if constexpr (kVec) {
+                    const int col = col0 + lane + 32 * i;
+                    return col < p.N && kb < tc.kb1 ? (p.sb ? __ldg(p.sb + static_cast<long long>(kb) * p.sb_k + col) : 1.0f) : 0.0f;
+                } else {
+                    return active && kb < tc.kb1 ? (p.sb ? __ldg(p.sb + static_cast<long long>(kb) * p.sb_k + (col0 >> 7) * p.sb_n) : 1.0f) : 0.0f;
+                }
+            };
+            constexpr int kB = kVec ? kCols / 32 : 1;
+            float a0 = fetch_a(tc.kb0), a1 = fetch_a(tc.kb0 + 1), b0[kB], b1[kB];
+#pragma unroll
+            for (int i = 0; i < kB; ++i) {
+                b0[i] = fetch_b(tc.kb0, i);
+                b1[i] = fetch_b(tc.kb0 + 1, i);
+            }
+            for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
+                const float a2 = fetch_a(kb + 2);
+                float b2[kB];
+#pragma unroll
+                for (int i = 0; i < kB; ++i) b2[i] = fetch_b(kb + 2, i);
+                const uint32_t cols_at = my_cols + (acc & 1u) * (kF8ColBytes / 2);
+                if constexpr (kVec) {
+#pragma unroll
+                    for (int i = 0; i < kB; ++i) sts_f32(cols_at + static_cast<uint32_t>(lane + 32 * i) * 4u, b0[i]);
+                    __syncwarp();
+                }
+                if (!mbar_wait_warp(bar_tfull + 8u * acc, acc_phase, abort_flag, budget)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t t_at = t_base + acc * kN;
+                if (active) {
+                    const uint64_t s2 = kVec ? pack_f2(a0, a0) : pack_f2(a0 * b0[0], a0 * b0[0]);
+                    uint32_t v[2][32];
+                    tmem_ld_32x32(t_at, v[0]);
+#pragma unroll
+                    for (int c = 0; c < kCols / 32; ++c) {
+                        tmem_ld_wait_for(v[c & 1]);
+                        if (c + 1 < kCols / 32) tmem_ld_32x32(t_at + 32 * (c + 1), v[(c + 1) & 1]);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            const uint64_t x0 = words_f2(v[c & 1][j], v[c & 1][j + 1]), x1 = words_f2(v[c & 1][j + 2], v[c & 1][j + 3]);
+                            uint64_t* to = &sum[16 * c + j / 2];
+                            if constexpr (kVec) {
+                                float b[4];
+                                lds_f4(cols_at + static_cast<uint32_t>(32 * c + j) * 4u, b);
+                                to[0] = fma_f2(mul_f2(x0, pack_f2(b[0], b[1])), s2, to[0]);
+                                to[1] = fma_f2(mul_f2(x1, pack_f2(b[2], b[3])), s2, to[1]);
+                            } else {
+                                to[0] = fma_f2(x0, s2, to[0]);
+                                to[1] = fma_f2(x1, s2, to[1]);
+                            }
+                        }
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (kPair && !leader) mbar_arrive_remote_fenced(bar_tempty + 8u * acc, 0);
+                    else mbar_arrive(bar_tempty + 8u * acc);
+                }
+                if (++acc == kBuffers) { acc = 0; acc_phase ^= 1u; }
+                a0 = a1;
+                a1 = a2;
+#pragma unroll
+                for (int i = 0; i < kB; ++i) {
+                    b0[i] = b1[i];
+                    b1[i] = b2[i];
+                }
+            }
+            if (!ok) break;
+            if constexpr (kRaw) {
+                // (planes have whole blocks of 32 rows and columns)
+                float* out = static_cast<float*>(p.C) + static_cast<long long>(tc.plane + row) * p.ldc + col0;
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    if (c >= n_slots) break;
+                    uint32_t w[32];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(w[2 * j]), "=r"(w[2 * j + 1]) : "l"(sum[16 * c + j]));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) st_global_v8(reinterpret_cast<int32_t*>(out) + 32 * c + 8 * j, &w[8 * j]);
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    if (c >= n_slots) break;
+                    const int col = col0 + 32 * c;
+                    const uint32_t b = taken % kSlotBuffers, at = my_slots + b * kSlot;        // (by turns, from tile to tile)
+                    if (r_tma) {
+                        if (!mbar_wait_warp(my_bar + 8u * b, (taken / kSlotBuffers) & 1u, abort_flag, budget)) { ok = false; break; }
+                    } else {
+                        if (c_tma && elect_one()) tma_store_wait_read<kSlotBuffers - 1>();
+                        __syncwarp();
+                        if (has_r) slot_rows_in<kWide>(at, p.R, p.ldr, row0, col, p.M, p.N, lane);
+                    }
+                    ++taken;
+                    if (p.bias) {
+                        __syncwarp();
+                        sts_f32(my_cols + lane * 4, col + lane < p.N ? __ldg(p.bias + col + lane) : 0.0f);
+                        __syncwarp();
+                    }
+                    constexpr int kPer = kWide ? 4 : 8;            // columns per 16-byte piece
+#pragma unroll
+                    for (int g = 0; g < 32 / kPer; ++g) {
+                        float y[kPer];
+#pragma unroll
+                        for (int j = 0; j < kPer; j += 2) unpack_f2(sum[16 * c + (g * kPer + j) / 2], y[j], y[j + 1]);
+                        if (p.bias) {
+#pragma unroll
+                            for (int j = 0; j < kPer; j += 4) {
+                                float bv[4];
+                                lds_f4(my_cols + static_cast<uint32_t>(g * kPer + j) * 4u, bv);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) y[j + i] += bv[i];
+                            }
+                        }
+                        uint32_t o[4];
+                        if (has_r) {
+                            lds_v4(slot_piece<kWide>(at, lane, g), o);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if constexpr (kWide) {
+                                    y[j] += __uint_as_float(o[j]);
+                                } else {
+                                    float lo, hi;
+                                    unpack2(o[j], f16, lo, hi);
+                                    y[2 * j] += lo;
+                                    y[2 * j + 1] += hi;
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (kWide) o[j] = __float_as_uint(y[j]);
+                            else o[j] = pack2(y[2 * j], y[2 * j + 1], f16);
+                        }
+                        st_shared_v4(slot_piece<kWide>(at, lane, g), o);
+                    }
+                    if (c_tma) {
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (elect_one()) {
+                            tma_store_2d(&p.tmap_c, at, col, row0);
+                            tma_store_commit();
+                        }
+                    } else {
+                        slot_rows_out<kWide>(at, p.C, p.ldc, row0, col, p.M, p.N, lane);
+                    }
+                    // a later slot's tile, once the buffer it goes to has been read by its store (the one before last)
+                    if (r_tma && asked < n_slots && c > 0) {
+                        if (c_tma && elect_one()) tma_store_wait_read<1>();
+                        __syncwarp();
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        ask();
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        // unwinding: tiles still on their way into the slots
+        for (uint32_t i = taken; r_tma && i < loads; ++i) {
+            const uint64_t t0 = globaltimer_ns();
+            while (!mbar_try_wait(my_bar + 8u * (i % kSlotBuffers), (i / kSlotBuffers) & 1u)) {
+                if (globaltimer_ns() - t0 > budget) break;
+            }
+        }
+        __syncwarp();
+        if (!kRaw && c_tma && elect_one()) tma_store_wait<0>();
+    }
+
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    bool unwinding = *abort_flag != 0;
+    if (kPair) {   // both CTAs have stopped, and know it of each other
+        if (threadIdx.x == 0) unwind.tell(cta_rank ^ 1u, *abort_flag);
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        unwinding = unwinding || unwind.get(0) != 0;
+    }
+    if (unwinding) {
+        if (warp == 0 && leader)
+            drain_copies<kPair, 2>(unwind, bar_full, static_cast<uint32_t>(p.stages), static_cast<uint32_t>(p.a_rows) * 128u, b_bytes, lane, budget);
+        if (warp == 1 && leader) {
+            if (elect_one()) {
+                if (kPair) mma_commit_pair(bar_drain); else mma_commit(bar_drain);
+            }
+            __syncwarp();
+            const uint64_t t0 = globaltimer_ns();
+            while (!mbar_try_wait(bar_drain, 0)) {
+                if (globaltimer_ns() - t0 > budget) break;
+            }
+            __syncwarp();
+            tc_fence_before();
+        }
+        __syncthreads();
+        if (kPair) {   // (the peer's shared memory is still being written or read until here)
+            cluster_arrive();
+            cluster_wait();
+        }
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc<kGroup>(tmem_base, 512);
+    }
+    if (threadIdx.x == 0 && *abort_flag != 0) atomicOr(p.status, 1u);
+}
+
+// Adds planes of partial sums in the order of K, the bias and the residual.  Without planes every sum is 0.
+constexpr int kFinishThreads = 256, kFinishCols = 4;
+__global__ void __launch_bounds__(kFinishThreads)
+mip_f8_finish_kernel(const F8ProductArgs a, const PartialPlanes s) {
+    const long long row = static_cast<long long>(blockIdx.y) * blockDim.y + threadIdx.y;
+    const long long col = (static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x) * kFinishCols;
+    if (row >= a.M || col >= a.N) return;
+    float v[kFinishCols] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const float* src = static_cast<const float*>(s.base) + row * s.pitch + col;
+#pragma unroll 4
+    for (int k = 0; k < s.split; ++k) {
+        const float4 x = *reinterpret_cast<const float4*>(src + k * s.plane_rows * s.pitch);
+        v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+    }
+    const int cols = static_cast<int>(min(static_cast<long long>(kFinishCols), a.N - col));
+#pragma unroll
+    for (int j = 0; j < kFinishCols; ++j)
+        if (j < cols) v[j] += (a.bias ? __ldg(a.bias + col + j) : 0.0f) + (a.R ? load_element(a.R, row * a.ldr + col + j, a.type) : 0.0f);
+#pragma unroll
+    for (int j = 0; j < kFinishCols; ++j)
+        if (j < cols) store_element(a.C, row * a.ldc + col + j, a.type, v[j]);
+}
+
+// (checks the register split against what the kernel was compiled to: a warp that asks for more than the block holds waits for ever)
+template <bool kPair, bool kVec, bool kWide, bool kRaw>
+cudaError_t init_t() {
+    const auto kernel = mip_f8_product_kernel<kPair, kVec, kWide, kRaw>;
+    if (kPair) {
+        cudaFuncAttributes attr;
+        const cudaError_t e = cudaFuncGetAttributes(&attr, kernel);
+        if (e != cudaSuccess) return e;
+        if (attr.numRegs < kLaunchRegs) return cudaErrorInvalidKernelImage;
+    }
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBudget);
+}
+template <bool kPair, bool kVec>
+cudaError_t init_form() {
+    for (cudaError_t e : {init_t<kPair, kVec, false, false>(), init_t<kPair, kVec, true, false>(), init_t<kPair, kVec, true, true>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+template <bool kPair, bool kVec>
+cudaError_t launch_form(const F8ProductParams& p, bool raw, const cudaLaunchConfig_t& cfg) {
+    if (raw) return cudaLaunchKernelEx(&cfg, mip_f8_product_kernel<kPair, kVec, true, true>, p);
+    return p.type == kF32 ? cudaLaunchKernelEx(&cfg, mip_f8_product_kernel<kPair, kVec, true, false>, p)
+                          : cudaLaunchKernelEx(&cfg, mip_f8_product_kernel<kPair, kVec, false, false>, p);
+}
+
+size_t smem_of(int type, bool raw, int stages) {
+    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : kSumWarps * kSlotBuffers * slot_bytes(type == kF32)) + kSumWarps * kF8ColBytes + kCtrlBytes + 1024;
+}
+
+}  // namespace
+
+int f8_product_stages(int type, bool raw) {
+    int stages = kMaxF8Stages;
+    while (smem_of(type, raw, stages) > kSmemBudget) --stages;
+    return stages;
+}
+
+cudaError_t f8_product_init() {
+    for (cudaError_t e : {init_form<false, false>(), init_form<false, true>(), init_form<true, false>(), init_form<true, true>()})
+        if (e != cudaSuccess) return e;
+    return cudaSuccess;
+}
+
+cudaError_t launch_f8_product(const F8ProductParams& p, bool pair, bool vec, bool raw, int grid, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
+    cfg.blockDim = dim3(kF8Threads, 1, 1);
+    cfg.dynamicSmemBytes = std::max(kSmemFloor, smem_of(p.type, raw, p.stages));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pair ? 2 : 1;
+    if (pair) return vec ? launch_form<true, true>(p, raw, cfg) : launch_form<true, false>(p, raw, cfg);
+    return vec ? launch_form<false, true>(p, raw, cfg) : launch_form<false, false>(p, raw, cfg);
+}
+
+cudaError_t launch_f8_finish(const F8ProductArgs& a, const PartialPlanes& s, cudaStream_t stream, int* launches) {
+    int tx = 8;
+    while (tx < kFinishThreads && tx * kFinishCols < a.N) tx *= 2;
+    const int ty = kFinishThreads / tx;
+    const long long step = 65535LL * ty, size = a.type == kF32 ? 4 : 2;      // (the grid's second dimension holds 65535 blocks)
+    for (long long row = 0; row < a.M; row += step) {
+        F8ProductArgs part = a;
+        PartialPlanes planes = s;
+        part.M = a.M - row < step ? a.M - row : step;
+        part.C = static_cast<char*>(a.C) + row * a.ldc * size;
+        if (a.R) part.R = static_cast<const char*>(a.R) + row * a.ldr * size;
+        if (s.base) planes.base = static_cast<const char*>(s.base) + row * s.pitch * 4;
+        const dim3 grid(static_cast<unsigned>((a.N + tx * kFinishCols - 1) / (tx * kFinishCols)), static_cast<unsigned>((part.M + ty - 1) / ty));
+        mip_f8_finish_kernel<<<grid, dim3(tx, ty), 0, stream>>>(part, planes);
+        ++*launches;
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace mip

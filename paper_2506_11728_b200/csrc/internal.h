@@ -273,6 +273,99 @@ cudaError_t launch_quantize_rows(int type, long long M, long long N, const void*
 cudaError_t launch_dequantize_rows(int type, long long M, long long N, const int8_t* Q, long long ldq,
                                    const float* scale, void* X, long long ldx, cudaStream_t stream);
 
+// ---- operators in 8-bit floating point, and the step between two blocks
+
+// Codes with a scale for each block of 128 (see mipgemm_f8_quantize).
+struct F8Codes {
+    void* Q; long long ldq;
+    float* scale; long long lds;
+};
+cudaError_t launch_f8_quantize(int type, int format, int form, long long M, long long N, const void* X, long long ldx,
+                               const F8Codes (&out)[2], cudaStream_t stream, int* launches);
+cudaError_t launch_f8_dequantize(int type, int format, int blocks, long long M, long long N, const F8Codes& in, void* X,
+                                 long long ldx, cudaStream_t stream, int* launches);
+
+// C = sum over blocks of 128 k of sa sb (A B)_kb + bias + R
+struct F8ProductArgs {
+    int type, a_format, b_format, a_order, b_order, b_vec;       // b_vec: a scale for each column of B, else for 128 x 128
+    long long M, N, K;
+    const void* A; long long lda;
+    const float* a_scale; long long ldas;
+    const void* B; long long ldb;
+    const float* b_scale; long long ldbs;
+    const float* bias;
+    const void* R; long long ldr;
+    void* C; long long ldc;
+};
+constexpr int kF8ColBytes = 2 * 128 * 4;     // shared memory of a summing warp's column vectors
+struct alignas(64) F8ProductParams : LayerParams {
+    int a_mn, b_mn;
+    const float* sa; long long lds_a;        // or NULL (ones)
+    const float* sb; long long sb_k, sb_n;   // scale of k-block kb and column j (b_vec: 1 apart) or j / 128
+};
+int f8_product_stages(int type, bool raw);
+cudaError_t f8_product_init();               // once per device
+cudaError_t launch_f8_product(const F8ProductParams& p, bool pair, bool vec, bool raw, int grid, cudaStream_t stream);
+cudaError_t launch_f8_finish(const F8ProductArgs& a, const PartialPlanes& s, cudaStream_t stream, int* launches);
+
+constexpr long long kStepColumns = 32768;    // the longest row of the step's kernels
+struct StepArgs {
+    long long M, N;
+    int post, pre, codes;
+    bool wide;                       // 16-byte accesses everywhere (8 bytes of codes)
+    float eps, x_scale;
+    const void* X; long long ldx;    // may be NULL, like most of what follows
+    const void* Z; long long ldz;
+    const float* post_w;
+    const float* post_b;
+    const void* gate; long long ldgate, gate_rows;
+    uint32_t bar; float drop_scale;  // dropout: 16 bits below `bar` are dropped; 0: nothing is
+    unsigned long long seed;
+    const unsigned long long* counter;
+    const float* pre_w;
+    const float* pre_b;
+    void* Y; long long ldy;
+    void* H; long long ldh;
+    uint8_t* Q; long long ldq;
+    float* q_scale; long long ldqs;
+    float* stats;
+};
+cudaError_t launch_norm_step(int type, const StepArgs& a, cudaStream_t stream);
+
+struct StepGradArgs {
+    long long M, N;
+    int post, pre;
+    bool wide;
+    float x_scale;
+    const void* dY; long long lddy;
+    const void* dH; long long lddh;
+    const void* Y; long long ldy;
+    const float* pre_w;
+    const void* Z; long long ldz;
+    const float* post_w;
+    const float* post_b;
+    const void* gate; long long ldgate, gate_rows;
+    uint32_t bar; float drop_scale;
+    unsigned long long seed;
+    const unsigned long long* counter;
+    const float* stats;
+    void* dX; long long lddx;
+    void* dZ; long long lddz;
+    void* dgate; long long lddgate;
+    float* dpost_w;
+    float* dpost_b;
+    float* dpre_w;
+    float* dpre_b;
+    int sums;                        // how many of these four are wanted
+    // filled in by the plan and the launcher
+    int cluster;
+    long long workers, units, parts, part_rows;
+    float* sum_part;
+    float* gate_part;
+};
+size_t plan_norm_step_grad(StepGradArgs& a, int sm_count);       // bytes of scratch
+cudaError_t launch_norm_step_grad(int type, StepGradArgs a, void* scratch, cudaStream_t stream, int* launches);
+
 // Auxiliary kernels.
 cudaError_t launch_repack(const void* src, long long src_pitch, void* dst, long long dst_pitch,
                           long long rows, long long cols, cudaStream_t stream);
