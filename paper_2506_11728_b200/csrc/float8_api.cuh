@@ -133,14 +133,14 @@ int run_f8_product(const mip::F8ProductArgs& a, DeviceState* dev, cudaStream_t s
         p.split = pl.split;
         p.kb_share = (p.k_blocks + pl.split - 1) / pl.split;
         p.plane_rows = static_cast<int>(round_up(a.M, 32));
-        p.stages = mip::f8_product_stages(a.type, pl.split > 1);
+        p.stages = mip::f8_product_stages(a.type, pl.pair != 0, a.b_vec != 0, pl.split > 1);
         if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
         p.a_mn = a.a_order;
         p.b_mn = a.b_order;
         p.a_rows = a.a_order ? mip::kBlockM : std::min(p.M, mip::kBlockM);
-        // D float32, the operands' formats, which of them are M/N-contiguous, the tile
+        // D float32, the operands' formats, which of them are M/N-contiguous, 128 columns, the tile's rows
         p.idesc = (1u << 4) | (static_cast<uint32_t>(a.a_format) << 7) | (static_cast<uint32_t>(a.b_format) << 10) | (static_cast<uint32_t>(a.a_order) << 15) |
-                  (static_cast<uint32_t>(a.b_order) << 16) | (static_cast<uint32_t>(side >> 3) << 17) | (static_cast<uint32_t>(side >> 4) << 24);
+                  (static_cast<uint32_t>(a.b_order) << 16) | (128u >> 3 << 17) | (static_cast<uint32_t>(side >> 4) << 24);
         p.status = dev->status_word;
         const size_t size = type_size(a.type);
         p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;

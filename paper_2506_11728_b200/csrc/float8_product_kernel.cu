@@ -2,10 +2,11 @@
 // layer and of its backward pass (operands K- or M/N-contiguous, as they lie).
 //
 // The scales change along the summed axis, so a block's products are summed by the tensor core on their own
-// (tcgen05.mma.kind::f8f6f4, four instructions, binary32 in tensor memory) and added to the tile's sums, which live in
+// (tcgen05.mma.kind::f8f6f4, binary32 in tensor memory) and added to the tile's sums, which live in
 // registers, behind their two scales.  Eight warps do that: a thread has one row and 128 (CTA pairs, 256 x 256 tiles) or 64
-// (single CTAs, 128 x 128) columns; tensor memory holds two or four blocks' products, so that the tensor core works on the next
-// block meanwhile.  With squares of 128 x 128 on B's side both scales are one number per thread and block: one packed
+// (single CTAs, 128 x 128) columns.  A block's products wait for a signal, are read, and free their buffer by another
+// signal: some 300 clocks of latency beside the reading.  A pair's tile is therefore computed by halves of 128 columns, each
+// with two buffers in tensor memory and four warps of its own: a buffer has the time of a whole block and a half for that.  With squares of 128 x 128 on B's side both scales are one number per thread and block: one packed
 // multiply-add for two elements.  With a scale for each column they come through shared memory, and it is one multiplication
 // more.
 //
@@ -23,11 +24,18 @@ namespace {
 
 constexpr int kSumWarps = 8;
 constexpr int kF8Threads = 32 * (4 + kSumWarps);
-constexpr int kSlotBuffers = 2;
 constexpr int kMaxF8Stages = 8;
+constexpr int slot_buffers(bool wide) { return wide ? 2 : 3; }           // per summing warp
+constexpr int all_slot_bytes(bool wide) { return kSumWarps * slot_buffers(wide) * slot_bytes(wide); }
+// Scales of a k-block: of the tile's 128 rows times those of its squares (each half's two), or of the rows and of the columns.
+// As many blocks as there are buffers of products for a half, twice: a block's place is written when the products of one
+// `depth` blocks before are ready, which says that those of another `depth` blocks before have been summed.
+constexpr int scale_bytes(bool pair, bool vec) { return vec ? (pair ? 1536 : 1024) : (pair ? 1024 : 512); }
+constexpr int scale_places(bool pair) { return pair ? 4 : 8; }
+constexpr int kBiasBytes = kSumWarps * 128;                              // 32 columns for each summing warp
 // Registers per thread: the sums take 128 of those of a pair's summing warps.  The block is launched with kLaunchRegs a thread; the
 // four other warps give theirs up (checked against the compiled kernel before its first launch).
-constexpr int kLaunchRegs = 168, kFewRegs = 56, kManyRegs = 216;
+constexpr int kLaunchRegs = 168, kFewRegs = 120, kManyRegs = 192;
 static_assert(4 * kFewRegs + kSumWarps * kManyRegs <= (4 + kSumWarps) * kLaunchRegs, "register split");
 
 template <int kRegs>
@@ -49,6 +57,28 @@ __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_
             ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// Signals this barrier, in both CTAs of a pair, when all MMAs issued so far are done.
+template <bool kPair>
+__device__ __forceinline__ void commit_all(uint32_t bar) {
+    if (kPair)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
+    else
+        mma_commit(bar);
+}
+__device__ __forceinline__ void tmem_ld_wait_for_16(uint32_t (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+        : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+          "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]) :: "memory");
+}
+// Arrives on a barrier of the cluster (see mbar_arrive_remote_fenced).
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool wait_fast(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, uint64_t budget) {
+    if (__all_sync(~0u, mbar_try_wait(bar, parity))) return true;
+    return mbar_wait_warp(bar, parity, abort_flag, budget);
+}
 __device__ __forceinline__ uint64_t words_f2(uint32_t a, uint32_t b) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
@@ -61,12 +91,14 @@ template <bool kPair, bool kVec, bool kWide, bool kRaw>
 __global__ void __launch_bounds__(kF8Threads, 1)
 mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     constexpr int kGroup = kPair ? 2 : 1;
-    constexpr int kN = kPair ? 256 : 128;                // accumulator columns
-    constexpr int kBuffers = 512 / kN;                   // blocks of products in tensor memory
-    constexpr int kCols = kN / 2;                        // columns per thread
+    // The tile's columns by halves (pair): 64 of each CTA's B tile, so that a half's 128 columns are two runs of 64.
+    constexpr int kHalves = kPair ? 2 : 1;
+    constexpr int kN = 128;                              // accumulator columns of an instruction
+    constexpr int kDepth = 4 / kHalves;                  // blocks of products in tensor memory, for each half
+    constexpr int kCols = kPair ? 128 : 64;              // columns per thread
     constexpr int kRowsPerTile = kGroup * kBlockM;
     constexpr uint32_t a_bytes = kBlockM * 128, b_bytes = 128 * 128, stage_bytes = a_bytes + b_bytes;
-    constexpr int kSlot = slot_bytes(kWide);
+    constexpr int kSlot = slot_bytes(kWide), kSlotBuffers = slot_buffers(kWide);
     const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
     const bool leader = cta_rank == 0;
     const int first_unit = kPair ? static_cast<int>(blockIdx.x >> 1) : static_cast<int>(blockIdx.x);
@@ -76,10 +108,12 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
     uint8_t* smem = smem_raw + pad;
     const uint32_t smem_base = raw_addr + pad;
-    // shared memory: [stages x (A | B)] [slots of the summing warps] [their column vectors: 128 floats, twice] [control block]
+    // shared memory: [stages x (A | B)] [slots of the summing warps] [scales] [bias] [control block]
     const uint32_t slots = smem_base + p.stages * stage_bytes;
-    const uint32_t colvec = slots + (kRaw ? 0u : kSumWarps * kSlotBuffers * kSlot);
-    const uint32_t ctrl = colvec + kSumWarps * kF8ColBytes;
+    const uint32_t scales = slots + (kRaw ? 0u : all_slot_bytes(kWide));
+    constexpr uint32_t kScaleBytes = scale_bytes(kPair, kVec), kPlaces = scale_places(kPair);
+    const uint32_t bias_at = scales + kPlaces * kScaleBytes;
+    const uint32_t ctrl = bias_at + kBiasBytes;
     const uint32_t bar_full = ctrl, bar_empty = ctrl + 8u * kMaxF8Stages;
     const uint32_t bar_tfull = ctrl + 16u * kMaxF8Stages, bar_tempty = bar_tfull + 32u, bar_drain = bar_tempty + 32u;
     const uint32_t bar_in = bar_drain + 8u;              // kSumWarps x kSlotBuffers: a slot's tile has arrived
@@ -87,7 +121,8 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(tmem_slot + 1);
     const UnwindWords unwind = {bar_in + 8u * kSumWarps * kSlotBuffers + 8u};
-    static_assert(16 * kMaxF8Stages + 72 + 8 * kSumWarps * kSlotBuffers + 8 + UnwindWords::kBytes <= kCtrlBytes, "control block");
+    static_assert(16 * kMaxF8Stages + 72 + 8 * kSumWarps * slot_buffers(false) + 8 + UnwindWords::kBytes <= 448, "control block");
+    const uint32_t info = ctrl + 448u;                   // m0, n0 and first plane row of the last four tiles
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -96,9 +131,9 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
             mbar_init(bar_full + 8u * s, 2);                       // two producers
             mbar_init(bar_empty + 8u * s, 1);
         }
-        for (int a = 0; a < kBuffers; ++a) {
-            mbar_init(bar_tfull + 8u * a, 1);
-            mbar_init(bar_tempty + 8u * a, kGroup * kSumWarps);
+        for (int a = 0; a < 4; ++a) {
+            mbar_init(bar_tfull + 8u * a, 2);       // the products, and the scales
+            mbar_init(bar_tempty + 8u * a, kSumWarps);      // warps that read it: four of each CTA's, or all eight
         }
         mbar_init(bar_drain, 1);
         for (int i = 0; i < kSumWarps * kSlotBuffers; ++i) mbar_init(bar_in + 8u * i, 1);
@@ -126,6 +161,12 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     const uint32_t tmem_base = *tmem_slot;
     const int total_units = layer_units(p);
     const uint64_t budget = p.wait_budget_ns;
+    // k-blocks of a unit (without a split, all: no division)
+    const auto unit_blocks = [&](int unit) {
+        if (p.split <= 1) return p.k_blocks;
+        const int kb0 = unit % p.split * p.kb_share;
+        return min(p.k_blocks, kb0 + p.kb_share) - kb0;
+    };
 
     if (warp < 4) {
         if constexpr (kPair) regs_dec<kFewRegs>();
@@ -160,39 +201,106 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         } else if (warp == 1 && leader) {
             // -------------------------------------------------------- MMA issuer
             uint32_t s = 0, phase = 0, acc = 0, acc_phase = 0;
+            // 32 k per instruction: 32 bytes of a K-contiguous row, 32 rows of 128 bytes of an M/N-contiguous block.  The
+            // second half's columns: 64 rows further, or 64 bytes.
+            const uint64_t a_step = p.a_mn ? 256ull : 2ull, b_step = p.b_mn ? 256ull : 2ull, b_half = p.b_mn ? 4ull : 512ull;
+            const uint64_t a_first = p.a_mn ? make_mnmajor_desc(smem_base, a_bytes) : make_kmajor_desc(smem_base, 128);
+            const uint64_t b_first = p.b_mn ? make_mnmajor_desc(smem_base + a_bytes, b_bytes) : make_kmajor_desc(smem_base + a_bytes, 128);
+            const uint32_t stages = p.stages, idesc = p.idesc;
+            const bool signal = !(p.debug_flags & 1);          // (test hook, bit 0: the "products ready" signal is withheld)
             bool ok = true;
-            // 32 k per instruction: 32 bytes of a K-contiguous row, 32 rows of 128 bytes of an M/N-contiguous block
-            const uint64_t a_step = p.a_mn ? 256ull : 2ull, b_step = p.b_mn ? 256ull : 2ull;
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
-                const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
-                for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                    if (!mbar_wait_warp<kPair>(bar_tempty + 8u * acc, acc_phase ^ 1u, abort_flag, budget) ||
-                        !mbar_wait_warp(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t a_addr = smem_base + s * stage_bytes;
-                    const uint64_t a_desc = p.a_mn ? make_mnmajor_desc(a_addr, a_bytes) : make_kmajor_desc(a_addr, 128);
-                    const uint64_t b_desc = p.b_mn ? make_mnmajor_desc(a_addr + a_bytes, b_bytes) : make_kmajor_desc(a_addr + a_bytes, 128);
-                    const uint32_t empty_local = bar_empty + 8u * s, tfull_local = bar_tfull + 8u * acc;
-                    const uint32_t empty_peer = kPair ? mapa_u32(empty_local, 1) : 0u, tfull_peer = kPair ? mapa_u32(tfull_local, 1) : 0u;
-                    const bool signal = !(p.debug_flags & 1);      // (test hook, bit 0: the "products ready" signal is withheld)
-                    if (elect_one()) {
+                for (int left = unit_blocks(unit); left > 0; --left) {
+                    if (!wait_fast(bar_full + 8u * s, phase, abort_flag, budget)) { ok = false; break; }
+                    const uint64_t a_desc = a_first + static_cast<uint64_t>(s * (stage_bytes >> 4));
+                    const uint64_t b_desc = b_first + static_cast<uint64_t>(s * (stage_bytes >> 4));
 #pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k)
-                            mma_f8<kGroup>(tmem_base + acc * kN, a_desc + a_step * k, b_desc + b_step * k, p.idesc, k > 0 ? 1u : 0u);
-                        if (kPair) {
-                            mma_commit_pair(empty_local);
-                            mma_commit_pair(empty_peer);
-                            if (signal) {
-                                mma_commit_pair(tfull_local);
-                                mma_commit_pair(tfull_peer);
-                            }
-                        } else {
-                            mma_commit(empty_local);
-                            if (signal) mma_commit(tfull_local);
+                    for (int h = 0; h < kHalves; ++h) {
+                        const uint32_t buf = h * kDepth + acc;
+                        if (!wait_fast(bar_tempty + 8u * buf, acc_phase ^ 1u, abort_flag, budget)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (uint32_t k = 0; k < 4; ++k)
+                                mma_f8<kGroup>(tmem_base + buf * kN, a_desc + a_step * k, b_desc + b_half * h + b_step * k, idesc, k > 0 ? 1u : 0u);
+                            if (signal) commit_all<kPair>(bar_tfull + 8u * buf);
+                            if (h == kHalves - 1) commit_all<kPair>(bar_empty + 8u * s);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                    if (++s == stages) { s = 0; phase ^= 1u; }
+                    if (++acc == kDepth) { acc = 0; acc_phase ^= 1u; }
+                }
+            }
+        } else if (warp == 3) {
+            // -------------------------------------------------------- scales, and where the tiles lie
+            // (The summing warps go from block to block in the time of two or three hundred instructions: what does not have to be
+            // there is here.)  Loads are two blocks ahead.  Rows, columns and blocks behind the last read the last one's: nothing of
+            // what they give is stored.
+            constexpr int kB = kVec ? kGroup * 4 : kHalves;
+            uint32_t acc = 0, uses = 0, place = 0, tile_no = 0;
+            bool ok = true;
+            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
+                const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+                if (lane == 0)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};"
+                                 ::"r"(info + (tile_no & 3u) * 16u), "r"(tc.m0), "r"(tc.n0), "r"(tc.plane) : "memory");
+                int row[4];
+                long long col[kB];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) row[i] = min(tc.m0 + static_cast<int>(cta_rank) * kBlockM + lane + 32 * i, p.M - 1);
+#pragma unroll
+                for (int i = 0; i < kB; ++i) {
+                    const int c = min(tc.n0 + (kVec ? lane + 32 * i : 128 * i), p.N - 1);
+                    col[i] = kVec ? c : (c >> 7) * p.sb_n;
+                }
+                float a_s[3][4], b_s[3][kB];
+                const auto fetch = [&](int to, int kb) {
+                    const long long k = min(kb, tc.kb1 - 1);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a_s[to][i] = p.sa ? __ldg(p.sa + k * p.lds_a + row[i]) : 1.0f;
+#pragma unroll
+                    for (int i = 0; i < kB; ++i) b_s[to][i] = p.sb ? __ldg(p.sb + k * p.sb_k + col[i]) : 1.0f;
+                };
+                fetch(0, tc.kb0);
+                fetch(1, tc.kb0 + 1);
+                for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
+                    fetch(2, kb + 2);
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+                        if (uses > 0 && ok) ok = wait_fast(bar_tfull + 8u * (h * kDepth + acc), (uses - 1) & 1u, abort_flag, budget);
+                    if (!ok) break;
+                    const uint32_t at = scales + place * kScaleBytes;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t r = static_cast<uint32_t>(lane + 32 * i);
+                        if constexpr (kVec) sts_f32(at + r * 4u, a_s[0][i]);
+                        else if constexpr (kPair)
+                            asm volatile("st.shared.v2.f32 [%0], {%1, %2};" ::"r"(at + r * 8u), "f"(a_s[0][i] * b_s[0][0]), "f"(a_s[0][i] * b_s[0][kB - 1]) : "memory");
+                        else sts_f32(at + r * 4u, a_s[0][i] * b_s[0][0]);
+                    }
+                    if constexpr (kVec) {
+#pragma unroll
+                        for (int i = 0; i < kB; ++i) {             // (pair: by halves, in the order of their columns)
+                            const uint32_t c = static_cast<uint32_t>(lane + 32 * i);
+                            sts_f32(at + 512u + 4u * (kPair ? (c >> 6 & 1u) * 128u + (c & 63u) + (c >> 7) * 64u : c), b_s[0][i]);
                         }
                     }
-                    if (++s == static_cast<uint32_t>(p.stages)) { s = 0; phase ^= 1u; }
-                    if (++acc == kBuffers) { acc = 0; acc_phase ^= 1u; }
+                    __syncwarp();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int h = 0; h < kHalves; ++h) mbar_arrive(bar_tfull + 8u * (h * kDepth + acc));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) a_s[j][i] = a_s[j + 1][i];
+#pragma unroll
+                        for (int i = 0; i < kB; ++i) b_s[j][i] = b_s[j + 1][i];
+                    }
+                    if (++acc == kDepth) { acc = 0; ++uses; }
+                    if (++place == kPlaces) place = 0;
                 }
             }
         }
@@ -201,198 +309,206 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         if constexpr (kPair) regs_inc<kManyRegs>();
         const int e = warp - 4, q = warp & 3, half = e >> 2;
         const uint32_t my_slots = slots + static_cast<uint32_t>(e) * kSlotBuffers * kSlot;
-        const uint32_t my_cols = colvec + static_cast<uint32_t>(e) * kF8ColBytes;
+        const uint32_t my_bias = bias_at + static_cast<uint32_t>(e) * 128u;
         const uint32_t my_bar = bar_in + 8u * static_cast<uint32_t>(e * kSlotBuffers);
-        const uint32_t t_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(half * kCols);
-        const bool f16 = p.type == kF16, has_r = p.R != nullptr, r_tma = p.r_tma != 0, c_tma = p.c_tma != 0;
-        uint32_t acc = 0, acc_phase = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
+        // (pair: this half's buffers, 128 columns each; else half the columns of all)
+        const uint32_t t_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(kPair ? half * kDepth * kN : half * kCols);
+        const uint32_t my_tfull = bar_tfull + (kPair ? 8u * half * kDepth : 0u);
+        uint32_t my_tempty = bar_tempty + (kPair ? 8u * half * kDepth : 0u);
+        if (kPair) my_tempty = mapa_u32(my_tempty, 0);             // the leader's
+        constexpr int kRuns = kCols / 32;
+        // columns of the tile that a thread's c-th run of 32 is
+        const auto run_col = [&](int c) { return kPair ? 64 * half + 32 * (c & 1) + 128 * (c >> 1) : half * kCols + 32 * c; };
+        // where this row's scales lie in a block's place, and those of this warp's columns
+        const uint32_t my_scale = scales + static_cast<uint32_t>(q * 32 + lane) * (kVec || !kPair ? 4u : 8u);
+        const uint32_t my_cols = scales + 512u + static_cast<uint32_t>(half * kCols) * 4u;
+        const bool f16 = p.type == kF16, has_r = p.R != nullptr, r_tma = !kRaw && p.r_tma != 0, c_tma = p.c_tma != 0;
+        uint32_t acc = 0, acc_phase = 0, place = 0, tile_no = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
         bool ok = true;
-        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
-            const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
-            const int row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32, row = row0 + lane;
-            const int col0 = tc.n0 + half * kCols;
-            const bool active = row0 < p.M && col0 < p.N;          // (warp-uniform)
-            const int n_slots = active ? min(kCols / 32, (p.N - col0 + 31) / 32) : 0;
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
+            struct { int m0, n0, plane; } tc = {};
+            int row0 = 0;
+            const auto read_info = [&] {
+                int none;
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(tc.m0), "=r"(tc.n0), "=r"(tc.plane), "=r"(none) : "r"(info + (tile_no & 3u) * 16u) : "memory");
+                row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
+            };
+            const auto run_ok = [&](int c) { return row0 < p.M && tc.n0 + run_col(c) < p.N; };       // (warp-uniform)
+            // what the slots hold in the end: the first of it is asked for beside the first block
+            int asked = 0;                                         // runs
+            const auto ask_round = [&] {
+                fence_proxy_async_smem();
+                __syncwarp();
+                for (int i = 0; i < kSlotBuffers && asked < kRuns && run_ok(asked); ++i) {
+                    const uint32_t b = loads % kSlotBuffers;
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(my_bar + 8u * b, kSlot);
+                        tma_load_2d(my_slots + b * kSlot, &p.tmap_r, my_bar + 8u * b, tc.n0 + run_col(asked), row0);
+                    }
+                    __syncwarp();
+                    ++asked;
+                    ++loads;
+                }
+            };
             uint64_t sum[kCols / 2];
 #pragma unroll
             for (int j = 0; j < kCols / 2; ++j) sum[j] = 0ull;
-            // what the slots' first buffers hold in the end: asked for before the sums are there
-            int asked = 0;
-            const auto ask = [&] {
-                const uint32_t b = loads % kSlotBuffers;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(my_bar + 8u * b, kSlot);
-                    tma_load_2d(my_slots + b * kSlot, &p.tmap_r, my_bar + 8u * b, col0 + asked * 32, row0);
-                }
-                __syncwarp();
-                ++asked;
-                ++loads;
-            };
-            if (!kRaw && r_tma && n_slots > 0) {
-                if (elect_one()) tma_store_wait_read<0>();
-                __syncwarp();
-                fence_proxy_async_smem();
-                __syncwarp();
-                while (asked < kSlotBuffers && asked < n_slots) ask();
-            }
-            // scales of the next two blocks are on their way while one is summed
-            const auto fetch_a = [&](int kb) { return row < p.M && kb < tc.kb1 ? (p.sa ? __ldg(p.sa + static_cast<long long>(kb) * p.lds_a + row) : 1.0f) : 0.0f; };
-            const auto fetch_b = [&](int kb, int i) {              // kVec: of columns lane + 32 i; else of the warp's columns
-                if constexpr (kVec) {
-                    const int col = col0 + lane + 32 * i;
-                    return col < p.N && kb < tc.kb1 ? (p.sb ? __ldg(p.sb + static_cast<long long>(kb) * p.sb_k + col) : 1.0f) : 0.0f;
-                } else {
-                    return active && kb < tc.kb1 ? (p.sb ? __ldg(p.sb + static_cast<long long>(kb) * p.sb_k + (col0 >> 7) * p.sb_n) : 1.0f) : 0.0f;
-                }
-            };
-            constexpr int kB = kVec ? kCols / 32 : 1;
-            float a0 = fetch_a(tc.kb0), a1 = fetch_a(tc.kb0 + 1), b0[kB], b1[kB];
-#pragma unroll
-            for (int i = 0; i < kB; ++i) {
-                b0[i] = fetch_b(tc.kb0, i);
-                b1[i] = fetch_b(tc.kb0 + 1, i);
-            }
-            for (int kb = tc.kb0; kb < tc.kb1; ++kb) {
-                const float a2 = fetch_a(kb + 2);
-                float b2[kB];
-#pragma unroll
-                for (int i = 0; i < kB; ++i) b2[i] = fetch_b(kb + 2, i);
-                const uint32_t cols_at = my_cols + (acc & 1u) * (kF8ColBytes / 2);
-                if constexpr (kVec) {
-#pragma unroll
-                    for (int i = 0; i < kB; ++i) sts_f32(cols_at + static_cast<uint32_t>(lane + 32 * i) * 4u, b0[i]);
-                    __syncwarp();
-                }
-                if (!mbar_wait_warp(bar_tfull + 8u * acc, acc_phase, abort_flag, budget)) { ok = false; break; }
+            const int blocks = unit_blocks(unit);
+            for (int i = 0; i < blocks; ++i) {
+                if (!wait_fast(my_tfull + 8u * acc, acc_phase, abort_flag, budget)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t t_at = t_base + acc * kN;
-                if (active) {
-                    const uint64_t s2 = kVec ? pack_f2(a0, a0) : pack_f2(a0 * b0[0], a0 * b0[0]);
-                    uint32_t v[2][32];
-                    tmem_ld_32x32(t_at, v[0]);
+                const uint32_t t_at = t_base + acc * kN, at = place * kScaleBytes;
+                uint32_t v[2][16];
+                tmem_ld_32x16(t_at, v[0]);
+                uint64_t s2[2];
+                if constexpr (kVec || !kPair) {
+                    float s;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(s) : "r"(my_scale + at) : "memory");
+                    s2[0] = s2[1] = pack_f2(s, s);
+                } else {
+                    float s0, s1;
+                    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(s0), "=f"(s1) : "r"(my_scale + at) : "memory");
+                    s2[0] = pack_f2(s0, s0);
+                    s2[1] = pack_f2(s1, s1);
+                }
 #pragma unroll
-                    for (int c = 0; c < kCols / 32; ++c) {
-                        tmem_ld_wait_for(v[c & 1]);
-                        if (c + 1 < kCols / 32) tmem_ld_32x32(t_at + 32 * (c + 1), v[(c + 1) & 1]);
+                for (int c = 0; c < kCols / 16; ++c) {
+                    tmem_ld_wait_for_16(v[c & 1]);
+                    if (c + 1 < kCols / 16) {
+                        tmem_ld_32x16(t_at + 16 * (c + 1), v[(c + 1) & 1]);
+                    } else {
+                        // the buffer is the tensor core's again: its last columns are in registers
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (kPair) mbar_arrive_cluster(my_tempty + 8u * acc);
+                            else mbar_arrive(my_tempty + 8u * acc);
+                        }
+                    }
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const uint64_t x0 = words_f2(v[c & 1][j], v[c & 1][j + 1]), x1 = words_f2(v[c & 1][j + 2], v[c & 1][j + 3]);
-                            uint64_t* to = &sum[16 * c + j / 2];
-                            if constexpr (kVec) {
-                                float b[4];
-                                lds_f4(cols_at + static_cast<uint32_t>(32 * c + j) * 4u, b);
-                                to[0] = fma_f2(mul_f2(x0, pack_f2(b[0], b[1])), s2, to[0]);
-                                to[1] = fma_f2(mul_f2(x1, pack_f2(b[2], b[3])), s2, to[1]);
-                            } else {
-                                to[0] = fma_f2(x0, s2, to[0]);
-                                to[1] = fma_f2(x1, s2, to[1]);
-                            }
+                    for (int j = 0; j < 16; j += 4) {
+                        const uint64_t x0 = words_f2(v[c & 1][j], v[c & 1][j + 1]), x1 = words_f2(v[c & 1][j + 2], v[c & 1][j + 3]);
+                        uint64_t* to = &sum[8 * c + j / 2];
+                        if constexpr (kVec) {
+                            float b[4];
+                            lds_f4(my_cols + at + static_cast<uint32_t>(16 * c + j) * 4u, b);
+                            to[0] = fma_f2(mul_f2(x0, pack_f2(b[0], b[1])), s2[0], to[0]);
+                            to[1] = fma_f2(mul_f2(x1, pack_f2(b[2], b[3])), s2[0], to[1]);
+                        } else {
+                            to[0] = fma_f2(x0, s2[c / (kRuns)], to[0]);
+                            to[1] = fma_f2(x1, s2[c / (kRuns)], to[1]);
                         }
                     }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (kPair && !leader) mbar_arrive_remote_fenced(bar_tempty + 8u * acc, 0);
-                    else mbar_arrive(bar_tempty + 8u * acc);
-                }
-                if (++acc == kBuffers) { acc = 0; acc_phase ^= 1u; }
-                a0 = a1;
-                a1 = a2;
-#pragma unroll
-                for (int i = 0; i < kB; ++i) {
-                    b0[i] = b1[i];
-                    b1[i] = b2[i];
+                if (++acc == kDepth) { acc = 0; acc_phase ^= 1u; }
+                if (++place == kPlaces) place = 0;
+                if (r_tma && i == 0) {
+                    read_info();
+                    if (run_ok(0)) {
+                        if (elect_one()) tma_store_wait_read<0>();
+                        __syncwarp();
+                        ask_round();
+                    }
                 }
             }
             if (!ok) break;
+            read_info();
             if constexpr (kRaw) {
                 // (planes have whole blocks of 32 rows and columns)
-                float* out = static_cast<float*>(p.C) + static_cast<long long>(tc.plane + row) * p.ldc + col0;
+                float* out = static_cast<float*>(p.C) + static_cast<long long>(tc.plane + row0 + lane) * p.ldc + tc.n0;
 #pragma unroll
-                for (int c = 0; c < kCols / 32; ++c) {
-                    if (c >= n_slots) break;
+                for (int c = 0; c < kRuns; ++c) {
+                    if (!run_ok(c)) continue;
                     uint32_t w[32];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) asm("mov.b64 {%0, %1}, %2;" : "=r"(w[2 * j]), "=r"(w[2 * j + 1]) : "l"(sum[16 * c + j]));
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) st_global_v8(reinterpret_cast<int32_t*>(out) + 32 * c + 8 * j, &w[8 * j]);
+                    for (int j = 0; j < 4; ++j) st_global_v8(reinterpret_cast<int32_t*>(out) + run_col(c) + 8 * j, &w[8 * j]);
                 }
             } else {
+                // by rounds of as many slots as there are: one fence and one wait for a round
 #pragma unroll
-                for (int c = 0; c < kCols / 32; ++c) {
-                    if (c >= n_slots) break;
-                    const int col = col0 + 32 * c;
-                    const uint32_t b = taken % kSlotBuffers, at = my_slots + b * kSlot;        // (by turns, from tile to tile)
-                    if (r_tma) {
-                        if (!mbar_wait_warp(my_bar + 8u * b, (taken / kSlotBuffers) & 1u, abort_flag, budget)) { ok = false; break; }
-                    } else {
-                        if (c_tma && elect_one()) tma_store_wait_read<kSlotBuffers - 1>();
+                for (int c0 = 0; c0 < kRuns; c0 += kSlotBuffers) {
+                    if (!run_ok(c0) || !ok) continue;
+                    if (!r_tma || c0 > 0) {
+                        if (c_tma && elect_one()) tma_store_wait_read<0>();
                         __syncwarp();
-                        if (has_r) slot_rows_in<kWide>(at, p.R, p.ldr, row0, col, p.M, p.N, lane);
+                        if (r_tma) ask_round();
                     }
-                    ++taken;
-                    if (p.bias) {
-                        __syncwarp();
-                        sts_f32(my_cols + lane * 4, col + lane < p.N ? __ldg(p.bias + col + lane) : 0.0f);
-                        __syncwarp();
-                    }
-                    constexpr int kPer = kWide ? 4 : 8;            // columns per 16-byte piece
 #pragma unroll
-                    for (int g = 0; g < 32 / kPer; ++g) {
-                        float y[kPer];
-#pragma unroll
-                        for (int j = 0; j < kPer; j += 2) unpack_f2(sum[16 * c + (g * kPer + j) / 2], y[j], y[j + 1]);
-                        if (p.bias) {
-#pragma unroll
-                            for (int j = 0; j < kPer; j += 4) {
-                                float bv[4];
-                                lds_f4(my_cols + static_cast<uint32_t>(g * kPer + j) * 4u, bv);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) y[j + i] += bv[i];
-                            }
+                    for (int c = c0; c < c0 + kSlotBuffers && c < kRuns; ++c) {
+                        if (!run_ok(c) || !ok) continue;
+                        const int col = tc.n0 + run_col(c);
+                        // (buffers by turns: a round that asks for tiles begins where the last one ended)
+                        const uint32_t b = r_tma ? taken % kSlotBuffers : static_cast<uint32_t>(c - c0), at = my_slots + b * kSlot;
+                        if (r_tma) {
+                            ok = mbar_wait_warp(my_bar + 8u * b, (taken / kSlotBuffers) & 1u, abort_flag, budget);
+                            if (!ok) continue;
+                            ++taken;
+                        } else if (has_r) {
+                            slot_rows_in<kWide>(at, p.R, p.ldr, row0, col, p.M, p.N, lane);
                         }
-                        uint32_t o[4];
-                        if (has_r) {
-                            lds_v4(slot_piece<kWide>(at, lane, g), o);
+                        if (p.bias) {
+                            __syncwarp();
+                            sts_f32(my_bias + lane * 4, col + lane < p.N ? __ldg(p.bias + col + lane) : 0.0f);
+                            __syncwarp();
+                        }
+                        constexpr int kPer = kWide ? 4 : 8;        // columns per 16-byte piece
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                if constexpr (kWide) {
-                                    y[j] += __uint_as_float(o[j]);
-                                } else {
-                                    float lo, hi;
-                                    unpack2(o[j], f16, lo, hi);
-                                    y[2 * j] += lo;
-                                    y[2 * j + 1] += hi;
+                        for (int g = 0; g < 32 / kPer; ++g) {
+                            float y[kPer];
+#pragma unroll
+                            for (int j = 0; j < kPer; j += 2) unpack_f2(sum[16 * c + (g * kPer + j) / 2], y[j], y[j + 1]);
+                            if (p.bias) {
+#pragma unroll
+                                for (int j = 0; j < kPer; j += 4) {
+                                    float bv[4];
+                                    lds_f4(my_bias + static_cast<uint32_t>(g * kPer + j) * 4u, bv);
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) y[j + i] += bv[i];
                                 }
                             }
-                        }
+                            uint32_t o[4];
+                            if (has_r) {
+                                lds_v4(slot_piece<kWide>(at, lane, g), o);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if constexpr (kWide) o[j] = __float_as_uint(y[j]);
-                            else o[j] = pack2(y[2 * j], y[2 * j + 1], f16);
+                                for (int j = 0; j < 4; ++j) {
+                                    if constexpr (kWide) {
+                                        y[j] += __uint_as_float(o[j]);
+                                    } else {
+                                        float lo, hi;
+                                        unpack2(o[j], f16, lo, hi);
+                                        y[2 * j] += lo;
+                                        y[2 * j + 1] += hi;
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                if constexpr (kWide) o[j] = __float_as_uint(y[j]);
+                                else o[j] = pack2(y[2 * j], y[2 * j + 1], f16);
+                            }
+                            st_shared_v4(slot_piece<kWide>(at, lane, g), o);
                         }
-                        st_shared_v4(slot_piece<kWide>(at, lane, g), o);
+                        if (!c_tma) slot_rows_out<kWide>(at, p.C, p.ldc, row0, col, p.M, p.N, lane);
                     }
-                    if (c_tma) {
+                    if (c_tma && ok) {
                         fence_proxy_async_smem();
                         __syncwarp();
+                        const uint32_t first = r_tma ? taken : 0u;             // (of the round's tiles the last one was taken before)
+                        int n = 0;
+#pragma unroll
+                        for (int c = c0; c < c0 + kSlotBuffers && c < kRuns; ++c) n += run_ok(c) ? 1 : 0;
                         if (elect_one()) {
-                            tma_store_2d(&p.tmap_c, at, col, row0);
+                            for (int i = 0; i < n; ++i) {
+                                const uint32_t b = r_tma ? (first - n + i) % kSlotBuffers : static_cast<uint32_t>(i);
+                                tma_store_2d(&p.tmap_c, my_slots + b * kSlot, tc.n0 + run_col(c0 + i), row0);
+                            }
                             tma_store_commit();
                         }
-                    } else {
-                        slot_rows_out<kWide>(at, p.C, p.ldc, row0, col, p.M, p.N, lane);
-                    }
-                    // a later slot's tile, once the buffer it goes to has been read by its store (the one before last)
-                    if (r_tma && asked < n_slots && c > 0) {
-                        if (c_tma && elect_one()) tma_store_wait_read<1>();
                         __syncwarp();
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        ask();
                     }
-                    __syncwarp();
                 }
             }
         }
@@ -494,15 +610,15 @@ cudaError_t launch_form(const F8ProductParams& p, bool raw, const cudaLaunchConf
                           : cudaLaunchKernelEx(&cfg, mip_f8_product_kernel<kPair, kVec, false, false>, p);
 }
 
-size_t smem_of(int type, bool raw, int stages) {
-    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : kSumWarps * kSlotBuffers * slot_bytes(type == kF32)) + kSumWarps * kF8ColBytes + kCtrlBytes + 1024;
+size_t smem_of(int type, bool pair, bool vec, bool raw, int stages) {
+    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : all_slot_bytes(type == kF32)) + scale_places(pair) * scale_bytes(pair, vec) + kBiasBytes + kCtrlBytes + 1024;
 }
 
 }  // namespace
 
-int f8_product_stages(int type, bool raw) {
+int f8_product_stages(int type, bool pair, bool vec, bool raw) {
     int stages = kMaxF8Stages;
-    while (smem_of(type, raw, stages) > kSmemBudget) --stages;
+    while (smem_of(type, pair, vec, raw, stages) > kSmemBudget) --stages;
     return stages;
 }
 
@@ -516,7 +632,7 @@ cudaError_t launch_f8_product(const F8ProductParams& p, bool pair, bool vec, boo
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid), 1, 1);
     cfg.blockDim = dim3(kF8Threads, 1, 1);
-    cfg.dynamicSmemBytes = std::max(kSmemFloor, smem_of(p.type, raw, p.stages));
+    cfg.dynamicSmemBytes = std::max(kSmemFloor, smem_of(p.type, pair, vec, raw, p.stages));
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

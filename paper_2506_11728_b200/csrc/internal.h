@@ -297,13 +297,12 @@ struct F8ProductArgs {
     const void* R; long long ldr;
     void* C; long long ldc;
 };
-constexpr int kF8ColBytes = 2 * 128 * 4;     // shared memory of a summing warp's column vectors
 struct alignas(64) F8ProductParams : LayerParams {
     int a_mn, b_mn;
     const float* sa; long long lds_a;        // or NULL (ones)
     const float* sb; long long sb_k, sb_n;   // scale of k-block kb and column j (b_vec: 1 apart) or j / 128
 };
-int f8_product_stages(int type, bool raw);
+int f8_product_stages(int type, bool pair, bool vec, bool raw);
 cudaError_t f8_product_init();               // once per device
 cudaError_t launch_f8_product(const F8ProductParams& p, bool pair, bool vec, bool raw, int grid, cudaStream_t stream);
 cudaError_t launch_f8_finish(const F8ProductArgs& a, const PartialPlanes& s, cudaStream_t stream, int* launches);
