@@ -330,7 +330,7 @@ int norm_step_impl(int type, mip::StepArgs& a, float drop, void* stream_v) {
     DeviceState* dev = nullptr;
     const int st = get_device(&dev);
     if (st != MIPGEMM_OK) return st;
-    const cudaError_t e = mip::launch_norm_step(type, a, static_cast<cudaStream_t>(stream_v));
+    const cudaError_t e = mip::launch_norm_step(type, a, dev->sm_count, static_cast<cudaStream_t>(stream_v));
     ++g_launches;
     return e == cudaSuccess ? MIPGEMM_OK : cuda_fail(e);
 }

@@ -29,38 +29,54 @@ struct Place {
     static __device__ __forceinline__ int col(int j) { return kWide ? static_cast<int>(threadIdx.x & 7) * 16 + j : static_cast<int>(threadIdx.x & 31) + 32 * j; }
 };
 
-// A thread's elements of a tile, by run; what lies outside the matrix is 0.
+// A thread's elements of a tile as they came (unpacked where they are used: 16-bit elements take half the registers);
+// what lies outside the matrix is 0.
 template <int kType, bool kWide>
 struct Tile {
     using P = Place<kWide>;
-    float v[P::kRuns][P::kLen];
+    Eight<kType> e[P::kRuns][kWide ? 2 : 1];             // (single elements: 4 of the 8 places)
     __device__ __forceinline__ void load(const void* X, long long ldx, long long r0, long long c0, long long M, long long N) {
-        if constexpr (kWide) {
 #pragma unroll
-            for (int i = 0; i < P::kRuns; ++i) {
-                const long long r = r0 + P::row(i), c = c0 + P::col(0);
-                Eight<kType> a, b;
-                a.load(X, r * ldx + c, r < M && c < N ? 8 : 0, true);
-                b.load(X, r * ldx + c + 8, r < M && c + 8 < N ? 8 : 0, true);
-                float x[8];
-                a.values(x);
+        for (int i = 0; i < P::kRuns; ++i) {
+            const long long r = r0 + P::row(i);
+            if constexpr (kWide) {
+                const long long c = c0 + P::col(0);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = x[j];
-                b.values(x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][8 + j] = x[j];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < P::kRuns; ++i)
+                for (int h = 0; h < 2; ++h) e[i][h].load(X, r * ldx + c + 8 * h, r < M && c + 8 * h < N ? 8 : 0, true);
+            } else {
+                float v[8] = {};
 #pragma unroll
                 for (int j = 0; j < P::kLen; ++j) {
-                    const long long r = r0 + P::row(i), c = c0 + P::col(j);
-                    v[i][j] = r < M && c < N ? load_one<kType>(X, r * ldx + c) : 0.0f;
+                    const long long c = c0 + P::col(j);
+                    if (r < M && c < N) v[j] = load_one<kType>(X, r * ldx + c);
                 }
+                e[i][0].set(v);                          // (exact: the elements are of the type)
+            }
+        }
+    }
+    __device__ __forceinline__ void values(int i, float (&v)[P::kLen]) const {
+        float x[8];
+        e[i][0].values(x);
+#pragma unroll
+        for (int j = 0; j < (kWide ? 8 : 4); ++j) v[j] = x[j];
+        if constexpr (kWide) {
+            e[i][1].values(x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[8 + j] = x[j];
         }
     }
 };
+// Magnitudes on the elements' own bits, two of 16 bits at a time (they order like the magnitudes, infinities and NaNs on top).
+template <int kType>
+__device__ __forceinline__ uint32_t word_max(uint32_t top, uint32_t w) {
+    return kType == kF32 ? max(top, w & 0x7FFFFFFFu) : __vmaxu2(top, w & 0x7FFF7FFFu);
+}
+template <int kType>
+__device__ __forceinline__ float word_top(uint32_t top) {            // of the two halves
+    if (kType == kF32) return __uint_as_float(top);
+    const uint32_t m = max(top & 0xFFFFu, top >> 16);
+    return kType == kF16 ? __half2float(__ushort_as_half(static_cast<uint16_t>(m))) : __uint_as_float(m << 16);
+}
 
 // kForm: bit 0 blocks along the rows, bit 1 along the columns; 4: squares.
 struct CodesArgs {
@@ -71,7 +87,7 @@ struct CodesArgs {
 };
 
 template <int kType, int kFormat, int kForm, bool kWide>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kType == kF32 ? 2 : (kForm & 2 ? 3 : 4))
 mip_f8_quantize_kernel(const CodesArgs a) {
     using P = Place<kWide>;
     constexpr bool kRows = kForm & 1, kCols = kForm & 2, kSquare = kForm & 4;
@@ -88,26 +104,25 @@ mip_f8_quantize_kernel(const CodesArgs a) {
         const long long r = r0 + P::row(i);
         if (r >= a.M) return;
         uint8_t* dst = a.Q[side] + r * a.ldq[side] + c0;
+        float v[P::kLen];
+        t.values(i, v);
         if constexpr (kWide) {
             const int c = P::col(0);
             uint32_t q[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if constexpr (kSquare || kRows) {
-                    if (side == 0) {
-                        q[j] = f8_codes4<kFormat>(t.v[i][4 * j], t.v[i][4 * j + 1], t.v[i][4 * j + 2], t.v[i][4 * j + 3], mult_of(0));
-                        continue;
-                    }
+                if (side == 0) {
+                    q[j] = f8_codes4<kFormat>(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3], mult_of(0));
+                    continue;
                 }
                 uint32_t w[4];
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) {
+                    // (a multiplier of 0 stands for "codes 0": an infinity times 0 would be NaN)
                     const float m0 = mult_of(4 * j + e), m1 = mult_of(4 * j + e + 1);
-                    const uint32_t p = f8_pair<kFormat>(__fmul_rn(t.v[i][4 * j + e], m0), __fmul_rn(t.v[i][4 * j + e + 1], m1));
-                    w[e] = m0 == 0.0f ? 0u : p & 0xFFu;
-                    w[e + 1] = m1 == 0.0f ? 0u : p & 0xFF00u;
+                    w[e / 2] = f8_pair<kFormat>(m0 == 0.0f ? 0.0f : __fmul_rn(v[4 * j + e], m0), m1 == 0.0f ? 0.0f : __fmul_rn(v[4 * j + e + 1], m1));
                 }
-                q[j] = w[0] | w[1] | ((w[2] | w[3]) << 16);
+                q[j] = w[0] | (w[1] << 16);
             }
             if (c0 + c + 16 <= a.N) *reinterpret_cast<uint4*>(dst + c) = make_uint4(q[0], q[1], q[2], q[3]);
             else if (c0 + c < a.N) *reinterpret_cast<uint2*>(dst + c) = make_uint2(q[0], q[1]);     // (N is a multiple of 8)
@@ -116,24 +131,29 @@ mip_f8_quantize_kernel(const CodesArgs a) {
             for (int j = 0; j < P::kLen; ++j) {
                 const float m = mult_of(j);
                 if (c0 + P::col(j) < a.N)
-                    dst[P::col(j)] = m == 0.0f ? uint8_t(0) : static_cast<uint8_t>(f8_pair<kFormat>(__fmul_rn(t.v[i][j], m), 0.0f));
+                    dst[P::col(j)] = m == 0.0f ? uint8_t(0) : static_cast<uint8_t>(f8_pair<kFormat>(__fmul_rn(v[j], m), 0.0f));
             }
         }
     };
+    constexpr int kWords = kType == kF32 ? 8 : 4;        // of eight elements
+    constexpr int kUsed = kWide ? kWords : kWords / 2;
 
     if constexpr (kRows) {
 #pragma unroll
         for (int i = 0; i < P::kRuns; ++i) {
             uint32_t top = 0u;
 #pragma unroll
-            for (int j = 0; j < P::kLen; ++j) top = max(top, magnitude_bits(t.v[i][j]));
+            for (int h = 0; h < (kWide ? 2 : 1); ++h)
+#pragma unroll
+                for (int j = 0; j < kUsed; ++j) top = word_max<kType>(top, t.e[i][h].w[j]);
             if constexpr (kWide) {
 #pragma unroll
-                for (int o = 4; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
+                for (int o = 4; o > 0; o >>= 1) top = word_max<kType>(top, __shfl_xor_sync(~0u, top, o));
             } else {
+                if (kType != kF32) top = max(top & 0xFFFFu, top >> 16);
                 top = __reduce_max_sync(~0u, top);
             }
-            const F8Scale s = f8_scale<kFormat>(__uint_as_float(top));
+            const F8Scale s = f8_scale<kFormat>(word_top<kType>(top));
             const long long r = r0 + P::row(i);
             if (r < a.M && (threadIdx.x & (kWide ? 7 : 31)) == 0) a.scale[0][static_cast<long long>(blockIdx.x) * a.lds[0] + r] = s.scale;
             put(0, i, [&](int) { return s.mult; });
@@ -141,17 +161,26 @@ mip_f8_quantize_kernel(const CodesArgs a) {
     }
     if constexpr (kCols) {
         // largest magnitude of each column: over the thread's rows, over the warp's, over the warps'
-        uint32_t top[P::kLen];
 #pragma unroll
-        for (int j = 0; j < P::kLen; ++j) {
-            top[j] = 0u;
+        for (int h = 0; h < (kWide ? 2 : 1); ++h) {
 #pragma unroll
-            for (int i = 0; i < P::kRuns; ++i) top[j] = max(top[j], magnitude_bits(t.v[i][j]));
-            if constexpr (kWide) {
-                top[j] = max(top[j], __shfl_xor_sync(~0u, top[j], 8));
-                top[j] = max(top[j], __shfl_xor_sync(~0u, top[j], 16));
+            for (int j = 0; j < kUsed; ++j) {
+                uint32_t top = 0u;
+#pragma unroll
+                for (int i = 0; i < P::kRuns; ++i) top = word_max<kType>(top, t.e[i][h].w[j]);
+                if constexpr (kWide) {
+                    top = word_max<kType>(top, __shfl_xor_sync(~0u, top, 8));
+                    top = word_max<kType>(top, __shfl_xor_sync(~0u, top, 16));
+                }
+                if (!kWide || lane < 8) {
+                    if constexpr (kType == kF32) {
+                        part[warp][P::col(8 * h + j)] = top;
+                    } else {
+                        part[warp][P::col(8 * h + 2 * j)] = top & 0xFFFFu;
+                        part[warp][P::col(8 * h + 2 * j + 1)] = top >> 16;
+                    }
+                }
             }
-            if (!kWide || lane < 8) part[warp][P::col(j)] = top[j];
         }
         __syncthreads();
         float* mult = reinterpret_cast<float*>(part[0]);
@@ -159,7 +188,7 @@ mip_f8_quantize_kernel(const CodesArgs a) {
             uint32_t m = 0u;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) m = max(m, part[w][threadIdx.x]);
-            const F8Scale s = f8_scale<kFormat>(__uint_as_float(m));
+            const F8Scale s = f8_scale<kFormat>(word_top<kType>(m));
             mult[threadIdx.x] = s.mult;
             if (c0 + threadIdx.x < a.N) a.scale[1][static_cast<long long>(blockIdx.y) * a.lds[1] + c0 + threadIdx.x] = s.scale;
         }
@@ -175,13 +204,16 @@ mip_f8_quantize_kernel(const CodesArgs a) {
 #pragma unroll
         for (int i = 0; i < P::kRuns; ++i)
 #pragma unroll
-            for (int j = 0; j < P::kLen; ++j) top = max(top, magnitude_bits(t.v[i][j]));
+            for (int h = 0; h < (kWide ? 2 : 1); ++h)
+#pragma unroll
+                for (int j = 0; j < kUsed; ++j) top = word_max<kType>(top, t.e[i][h].w[j]);
+        if (kType != kF32) top = max(top & 0xFFFFu, top >> 16);
         top = __reduce_max_sync(~0u, top);
         if (lane == 0) part[0][warp] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) top = max(top, part[0][w]);
-        const F8Scale s = f8_scale<kFormat>(__uint_as_float(top));
+        const F8Scale s = f8_scale<kFormat>(word_top<kType>(top));
         if (threadIdx.x == 0) a.scale[0][static_cast<long long>(blockIdx.y) * a.lds[0] + blockIdx.x] = s.scale;
 #pragma unroll
         for (int i = 0; i < P::kRuns; ++i) put(0, i, [&](int) { return s.mult; });

@@ -122,6 +122,32 @@ struct Eight {
             }
         }
     }
+    // Two neighbours in a register pair, for the packed instructions.
+    __device__ __forceinline__ void pairs(uint64_t (&v)[4]) const {
+        if constexpr (kType == kF32) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = pack_f2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 t = unpack_pair<kType>(w[i]);
+                v[i] = pack_f2(t.x, t.y);
+            }
+        }
+    }
+    __device__ __forceinline__ void set_pairs(const uint64_t (&v)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            unpack_f2(v[i], lo, hi);
+            if constexpr (kType == kF32) {
+                w[2 * i] = __float_as_uint(lo);
+                w[2 * i + 1] = __float_as_uint(hi);
+            } else {
+                w[i] = pack_pair<kType>(lo, hi);
+            }
+        }
+    }
     __device__ __forceinline__ void set(const float (&v)[8]) {
         if constexpr (kType == kF32) {
 #pragma unroll

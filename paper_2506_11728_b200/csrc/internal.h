@@ -329,7 +329,7 @@ struct StepArgs {
     float* q_scale; long long ldqs;
     float* stats;
 };
-cudaError_t launch_norm_step(int type, const StepArgs& a, cudaStream_t stream);
+cudaError_t launch_norm_step(int type, const StepArgs& a, int sm_count, cudaStream_t stream);
 
 struct StepGradArgs {
     long long M, N;

@@ -21,13 +21,13 @@ namespace mip {
 
 namespace {
 
-constexpr int kMaxCluster = 8, kGradThreads = 512, kGradWarps = kGradThreads / 32;
+constexpr int kMaxGradRows = 4, kMaxCluster = 8, kGradThreads = 512, kGradWarps = kGradThreads / 32;
 
 // Sums of two values over a row's threads, over the cluster's CTAs too: every warp leaves its share with every CTA, one
 // barrier, every warp adds the shares up in the same order.  Two slots by turns: a warp that writes a slot again has passed
 // the barrier of the other one, which all warps reach after reading this one.
 struct RowExchange {
-    float2 share[2][kMaxBlockRows][kMaxCluster * kGradWarps];
+    float2 share[2][kMaxGradRows][kMaxCluster * kGradWarps];
 };
 __device__ __forceinline__ float2 exchange(float2 v, RowExchange& x, int slot, int cluster, uint32_t rank) {
     v.x = warp_sum(v.x);
@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 mip_norm_step_grad_kernel(const StepGradArgs a) {
     constexpr bool kAhead = kType != kF32;       // (32-bit elements of two rows leave no registers for the sums)
     __shared__ RowExchange ex;
-    __shared__ float rows_sum[kMaxBlockRows - 1][8 * 64];
+    __shared__ float rows_sum[kMaxGradRows - 1][8 * 64];
     pdl_wait();
     pdl_launch_dependents();
     const int cluster = a.cluster;
@@ -134,7 +134,14 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
             e.set(t);
             e.store(a.dX, row * a.lddx + col, r.count, wide);
         }
-        if (drop.bar) drop.apply(drop.draw(row, col), g);
+        if (drop.bar) {
+            uint64_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) u[j] = pack_f2(g[2 * j], g[2 * j + 1]);
+            drop.apply(drop.draw(row, col), u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) unpack_f2(u[j], g[2 * j], g[2 * j + 1]);
+        }
         float hat[8];
         r.z.values(hat);
         if (kPost) {
@@ -331,7 +338,7 @@ GradShape grad_shape(long long N) {
     GradShape s;
     s.cluster = static_cast<int>((N + 8 * kGradThreads - 1) / (8 * kGradThreads));
     s.threads = static_cast<int>(((N + 8 * s.cluster - 1) / (8 * s.cluster) + 31) / 32 * 32);
-    s.rows = s.threads >= 128 ? 1 : 128 / s.threads;
+    s.rows = s.threads >= 128 ? 1 : 128 / s.threads;             // (up to kMaxGradRows)
     return s;
 }
 

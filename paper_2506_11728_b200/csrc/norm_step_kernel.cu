@@ -3,11 +3,16 @@
 // every part optional.  Two norms, a gate, a mask, the residual sum and the codes in one pass: x and z are read once, y and h
 // (or h's codes) written once, and the mask exists nowhere but in registers.
 //
-// A row stays in the registers of its threads, eight neighbouring columns each and up to four such runs (rows of up to 32768
-// columns).  Means come first, then the squares of what is left, so that a large mean takes no digits from the variance.
-// The dropout mask is a function of (seed, counter, row, column): one draw of a counter-based generator for eight columns.
+// A row stays in the registers of its threads, runs of eight neighbouring columns each (rows of up to 32768 columns).  Means
+// come first, then the squares of what is left, so that a large mean takes no digits from the variance.  The dropout mask is a
+// function of (seed, counter, row, column): one draw of a counter-based generator for eight columns.
 //
-// What bounds it: the bytes of x, z, y and h.
+// What bounds it: the bytes of x, z, y and h, and close behind them the instructions (two norms, a gate and the generator's ten
+// rounds on every eight columns).  Hence packed arithmetic on pairs, 16 columns a thread (a row's exchanges cost a warp the same
+// whatever it holds), blocks that go on from row to row with the norms' weights in registers, and the next row's elements on
+// their way while a row waits for its exchanges.  With few rows each gets a block of its own and eight columns a thread.
+#include <algorithm>
+
 #include "ptx.cuh"
 #include "step_math.cuh"
 
@@ -15,57 +20,87 @@ namespace mip {
 
 namespace {
 
-// Sum over a row's threads; all of them get it.  `slot`: which of the exchange buffers, another one for each use.
-__device__ __forceinline__ float row_sum(float v, float (*part)[kMaxBlockRows][kMaxRowWarps], int slot) {
-    v = warp_sum(v);
+// Sum over a row's threads; all of them get it.  Two exchange buffers by turns: who writes one again has passed the barrier of
+// the other, which all reach after reading this one.
+template <int kThreads>
+struct Exchange {
+    float part[2][kMaxBlockRows][kThreads / 32];
+};
+template <int kThreads, typename F>
+__device__ __forceinline__ float over_warps(float v, Exchange<kThreads>& x, int& slot, const F& join) {
     const int warps = blockDim.x >> 5;
     if (warps == 1) return v;
-    if ((threadIdx.x & 31) == 0) part[slot][threadIdx.y][threadIdx.x >> 5] = v;
+    slot ^= 1;
+    constexpr int kMost = kThreads / 32;
+    if ((threadIdx.x & 31) == 0) x.part[slot][threadIdx.y][threadIdx.x >> 5] = v;
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return warp_sum(lane < warps ? part[slot][threadIdx.y][lane] : 0.0f);
+    const int i = threadIdx.x & (kMost - 1);
+    v = i < warps ? x.part[slot][threadIdx.y][i] : 0.0f;
+#pragma unroll
+    for (int o = kMost / 2; o > 0; o >>= 1) v = join(v, __shfl_xor_sync(~0u, v, o));
+    return v;
 }
-__device__ __forceinline__ uint32_t row_max(uint32_t v, float (*part)[kMaxBlockRows][kMaxRowWarps], int slot) {
-    v = __reduce_max_sync(~0u, v);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return v;
-    if ((threadIdx.x & 31) == 0) part[slot][threadIdx.y][threadIdx.x >> 5] = __uint_as_float(v);
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return __reduce_max_sync(~0u, lane < warps ? __float_as_uint(part[slot][threadIdx.y][lane]) : 0u);
+template <int kThreads>
+__device__ __forceinline__ float row_sum(float v, Exchange<kThreads>& x, int& slot) {
+    return over_warps(warp_sum(v), x, slot, [](float a, float b) { return a + b; });
+}
+// (bits of magnitudes, 0 and up: they order like integers)
+template <int kThreads>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, Exchange<kThreads>& x, int& slot) {
+    return __float_as_uint(over_warps(__uint_as_float(__reduce_max_sync(~0u, v)), x, slot,
+                                      [](float a, float b) { return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b))); }));
 }
 
-// v becomes w (v - mean) / sqrt(var + eps) + b; returns (mean, 1 / sqrt(var + eps)).
-template <int kRuns>
-__device__ __forceinline__ float2 normalize(int kind, float (&v)[kRuns][8], const int (&count)[kRuns], const float* w, const float* b, bool wide,
-                                            const long long (&col)[kRuns], long long N, float eps, float (*part)[kMaxBlockRows][kMaxRowWarps], int slot) {
+// v becomes (v - mean) / sqrt(var + eps); returns (mean, 1 / sqrt(var + eps)).
+template <int kRuns, int kThreads>
+__device__ __forceinline__ float2 normalize(int kind, uint64_t (&v)[kRuns][4], const int (&count)[kRuns], float n, float eps, Exchange<kThreads>& x, int& slot) {
     float mean = 0.0f;
     if (kind == kNormLayer) {
-        float s = 0.0f;
+        uint64_t s = 0ull;
 #pragma unroll
         for (int c = 0; c < kRuns; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += v[c][j];                  // (columns that do not exist hold 0)
-        mean = __fdiv_rn(row_sum(s, part, slot), static_cast<float>(N));
+            for (int j = 0; j < 4; ++j) s = add_f2(s, v[c][j]);        // (columns that do not exist hold 0)
+        mean = __fdiv_rn(row_sum(sum_pair(s), x, slot), n);
+        const uint64_t m = pack_f2(-mean, -mean);
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[c][j] = add_f2(v[c][j], m);
+            clear_behind(v[c], count[c]);
+        }
     }
-    float q = 0.0f;
+    uint64_t q = 0ull;
 #pragma unroll
     for (int c = 0; c < kRuns; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[c][j] = j < count[c] ? v[c][j] - mean : 0.0f;
-            q = fmaf(v[c][j], v[c][j], q);
-        }
-    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(q, part, slot + 1), static_cast<float>(N)), eps));
+        for (int j = 0; j < 4; ++j) q = fma_f2(v[c][j], v[c][j], q);
+    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(sum_pair(q), x, slot), n), eps));
+#pragma unroll
+    for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[c][j] = mul_f2(v[c][j], pack_f2(rstd, rstd));
+    return make_float2(mean, rstd);
+}
+// v w + b; w (the row's own copy, or read again) and b as they are wanted
+template <int kRuns>
+__device__ __forceinline__ void affine(uint64_t (&v)[kRuns][4], const uint64_t (&kept)[kRuns][4], bool keep, const float* w, const float* b,
+                                       const long long (&col)[kRuns], const int (&exist)[kRuns], bool wide) {
 #pragma unroll
     for (int c = 0; c < kRuns; ++c) {
-        float wv[8], bv[8];
-        load_vector8(w, col[c], count[c], wide, 1.0f, wv);
-        load_vector8(b, col[c], count[c], wide, 0.0f, bv);
+        if (w) {
+            uint64_t x[4];
+            if (!keep) load_vector_pairs(w, col[c], exist[c], wide, 1.0f, x);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[c][j] = fmaf(v[c][j] * rstd, wv[j], bv[j]);
+            for (int j = 0; j < 4; ++j) v[c][j] = mul_f2(v[c][j], keep ? kept[c][j] : x[j]);
+        }
+        if (b) {
+            uint64_t x[4];
+            load_vector_pairs(b, col[c], exist[c], wide, 0.0f, x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[c][j] = add_f2(v[c][j], x[j]);
+        }
     }
-    return make_float2(mean, rstd);
 }
 
 template <int kFormat>
@@ -82,138 +117,194 @@ __device__ __forceinline__ void store_codes8(uint8_t* dst, uint2 q, int count, b
     }
 }
 
-template <int kType, int kRuns, int kThreads>
-__global__ void __launch_bounds__(kThreads)
+// kRuns runs of eight columns a thread, up to kThreads threads a block; kAhead: the block goes on from row to row.
+template <int kType, int kRuns, int kThreads, bool kAhead>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 2 : 1)
 mip_norm_step_kernel(const StepArgs a) {
-    __shared__ float part[5][kMaxBlockRows][kMaxRowWarps];
+    __shared__ Exchange<kThreads> ex;
     pdl_wait();
     pdl_launch_dependents();
-    const long long row = static_cast<long long>(blockIdx.x) * blockDim.y + threadIdx.y;
-    const bool here = row < a.M;
     const bool wide = a.wide;
-    const bool gated = a.gate && here;
     const Dropout drop = dropout_of(a.bar, a.drop_scale, a.seed, a.counter, a.N);
+    const float n = static_cast<float>(a.N);
+    int slot = 0;
     long long col[kRuns];
-    int count[kRuns];
-    Eight<kType> x[kRuns], z[kRuns], g[kRuns];
+    int exist[kRuns];
+    uint64_t post_w[kRuns][4], pre_w[kRuns][4];
 #pragma unroll
     for (int c = 0; c < kRuns; ++c) {
         col[c] = 8ll * (static_cast<long long>(c) * blockDim.x + threadIdx.x);
-        const long long left = here ? a.N - col[c] : 0;
-        count[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
-        if (a.Z) z[c].load(a.Z, row * a.ldz + col[c], count[c], wide);
-        else z[c].clear();
-        if (a.X) x[c].load(a.X, row * a.ldx + col[c], count[c], wide);
-        else x[c].clear();
-        if (gated) g[c].load(a.gate, static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows) * a.ldgate + col[c], count[c], wide);
-    }
-    float v[kRuns][8];
-#pragma unroll
-    for (int c = 0; c < kRuns; ++c) z[c].values(v[c]);
-    float2 post = make_float2(0.0f, 0.0f), pre = post;
-    if (a.post != kNormNone) post = normalize<kRuns>(a.post, v, count, a.post_w, a.post_b, wide, col, a.N, a.eps, part, 0);
-#pragma unroll
-    for (int c = 0; c < kRuns; ++c) {
-        if (gated) {
-            float gv[8];
-            g[c].values(gv);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[c][j] *= gv[j];
-        }
-        if (drop.bar) drop.apply(drop.draw(row, col[c]), v[c]);
-        float xv[8];
-        x[c].values(xv);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[c][j] = fmaf(a.x_scale, xv[j], v[c][j]);
-        if (a.Y) {
-            Eight<kType> y;
-            y.set(v[c]);
-            y.store(a.Y, row * a.ldy + col[c], count[c], wide);
+        const long long left = a.N - col[c];
+        exist[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
+        if (kAhead) {
+            if (a.post_w) load_vector_pairs(a.post_w, col[c], exist[c], wide, 1.0f, post_w[c]);
+            if (a.pre_w) load_vector_pairs(a.pre_w, col[c], exist[c], wide, 1.0f, pre_w[c]);
         }
     }
-    if (a.pre != kNormNone) {
-        pre = normalize<kRuns>(a.pre, v, count, a.pre_w, a.pre_b, wide, col, a.N, a.eps, part, 2);
-        if (a.H) {
+    struct Row {
+        Eight<kType> x[kRuns], z[kRuns];
+    };
+    const auto load = [&](Row& r, long long row) {
 #pragma unroll
-            for (int c = 0; c < kRuns; ++c) {
-                Eight<kType> h;
-                h.set(v[c]);
-                h.store(a.H, row * a.ldh + col[c], count[c], wide);
+        for (int c = 0; c < kRuns; ++c) {
+            const int count = row < a.M ? exist[c] : 0;
+            if (a.Z) r.z[c].load(a.Z, row * a.ldz + col[c], count, wide);
+            else r.z[c].clear();
+            if (a.X) r.x[c].load(a.X, row * a.ldx + col[c], count, wide);
+            else r.x[c].clear();
+        }
+    };
+    const long long step = static_cast<long long>(gridDim.x) * blockDim.y;
+    long long base = static_cast<long long>(blockIdx.x) * blockDim.y;
+    Row cur;
+    load(cur, base + threadIdx.y);
+    for (; base < a.M; base += step) {
+        const long long row = base + threadIdx.y;
+        const bool here = row < a.M;
+        int count[kRuns];
+        Eight<kType> g[kRuns];
+        uint64_t v[kRuns][4];
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            count[c] = here ? exist[c] : 0;
+            if (a.gate) g[c].load(a.gate, (here ? static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows) : 0u) * a.ldgate + col[c], count[c], wide);
+            cur.z[c].pairs(v[c]);
+        }
+        Row next;
+        if (kAhead) load(next, row + step);
+        float2 post = make_float2(0.0f, 0.0f), pre = post;
+        if (a.post != kNormNone) {
+            post = normalize<kRuns>(a.post, v, count, n, a.eps, ex, slot);
+            affine<kRuns>(v, post_w, kAhead, a.post_w, a.post_b, col, exist, wide);
+        }
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            uint64_t t[4];
+            if (a.gate) {
+                g[c].pairs(t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[c][j] = mul_f2(v[c][j], t[j]);
+            }
+            if (drop.bar) drop.apply(drop.draw(row, col[c]), v[c]);
+            if (a.X) {
+                cur.x[c].pairs(t);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[c][j] = fma_f2(pack_f2(a.x_scale, a.x_scale), t[j], v[c][j]);
+            }
+            if (a.Y) {
+                Eight<kType> y;
+                y.set_pairs(v[c]);
+                y.store(a.Y, row * a.ldy + col[c], count[c], wide);
             }
         }
-        if (a.codes == kCodesS8) {
-            uint32_t top = 0u;
+        if (a.pre != kNormNone) {
+            pre = normalize<kRuns>(a.pre, v, count, n, a.eps, ex, slot);
+            affine<kRuns>(v, pre_w, kAhead, a.pre_w, a.pre_b, col, exist, wide);
+            if (a.H) {
 #pragma unroll
-            for (int c = 0; c < kRuns; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, j < count[c] ? magnitude_bits(v[c][j]) : 0u);
-            const float top_f = __uint_as_float(row_max(top, part, 4));
-            // (the rule of mipgemm_quantize_rows)
-            float scale = 0.0f, mult = 0.0f;
-            if (!(top_f <= 3.402823466e38f)) {
-                scale = __int_as_float(0x7FFFFFFF);
-            } else if (top_f >= 0x1p-119f) {
-                scale = __fdiv_rn(top_f, 127.0f);
-                mult = __fdiv_rn(127.0f, top_f);
-            }
-            if (here && threadIdx.x == 0) a.q_scale[row] = scale;
-#pragma unroll
-            for (int c = 0; c < kRuns; ++c) {
-                uint32_t q[2] = {0u, 0u};
-                if (mult != 0.0f) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) q[j / 4] |= (static_cast<uint32_t>(__float2int_rn(__fmul_rn(v[c][j], mult))) & 0xFFu) << (8 * (j & 3));
+                for (int c = 0; c < kRuns; ++c) {
+                    Eight<kType> h;
+                    h.set_pairs(v[c]);
+                    h.store(a.H, row * a.ldh + col[c], count[c], wide);
                 }
-                store_codes8(a.Q + row * a.ldq + col[c], make_uint2(q[0], q[1]), count[c], wide);
             }
-        } else if (a.codes != kCodesNone) {
-            // a block of 128 columns is what 16 neighbouring lanes hold
+            if (a.codes != kCodesNone) {
+                float h[kRuns][8];
+                uint32_t top[kRuns], most = 0u;
 #pragma unroll
-            for (int c = 0; c < kRuns; ++c) {
-                uint32_t top = 0u;
+                for (int c = 0; c < kRuns; ++c) {
+                    top[c] = 0u;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) top = max(top, j < count[c] ? magnitude_bits(v[c][j]) : 0u);
+                    for (int j = 0; j < 4; ++j) unpack_f2(v[c][j], h[c][2 * j], h[c][2 * j + 1]);
 #pragma unroll
-                for (int o = 8; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
-                const bool e4m3 = a.codes == kCodesE4M3;
-                const F8Scale s = e4m3 ? f8_scale<kE4M3>(__uint_as_float(top)) : f8_scale<kE5M2>(__uint_as_float(top));
-                if ((threadIdx.x & 15) == 0 && count[c] > 0) a.q_scale[(col[c] >> 7) * a.ldqs + row] = s.scale;
-                store_codes8(a.Q + row * a.ldq + col[c], e4m3 ? codes8<kE4M3>(v[c], s.mult) : codes8<kE5M2>(v[c], s.mult), count[c], wide);
+                    for (int j = 0; j < 8; ++j) top[c] = max(top[c], j < count[c] ? magnitude_bits(h[c][j]) : 0u);
+                    most = max(most, top[c]);
+                }
+                if (a.codes == kCodesS8) {
+                    const float top_f = __uint_as_float(row_max(most, ex, slot));
+                    // (the rule of mipgemm_quantize_rows)
+                    float scale = 0.0f, mult = 0.0f;
+                    if (!(top_f <= 3.402823466e38f)) {
+                        scale = __int_as_float(0x7FFFFFFF);
+                    } else if (top_f >= 0x1p-119f) {
+                        scale = __fdiv_rn(top_f, 127.0f);
+                        mult = __fdiv_rn(127.0f, top_f);
+                    }
+                    if (here && threadIdx.x == 0) a.q_scale[row] = scale;
+#pragma unroll
+                    for (int c = 0; c < kRuns; ++c) {
+                        uint32_t q[2] = {0u, 0u};
+                        if (mult != 0.0f) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) q[j / 4] |= (static_cast<uint32_t>(__float2int_rn(__fmul_rn(h[c][j], mult))) & 0xFFu) << (8 * (j & 3));
+                        }
+                        store_codes8(a.Q + row * a.ldq + col[c], make_uint2(q[0], q[1]), count[c], wide);
+                    }
+                } else {
+                    // a block of 128 columns is what 16 neighbouring lanes hold
+                    const bool e4m3 = a.codes == kCodesE4M3;
+#pragma unroll
+                    for (int c = 0; c < kRuns; ++c) {
+#pragma unroll
+                        for (int o = 8; o > 0; o >>= 1) top[c] = max(top[c], __shfl_xor_sync(~0u, top[c], o));
+                        const F8Scale s = e4m3 ? f8_scale<kE4M3>(__uint_as_float(top[c])) : f8_scale<kE5M2>(__uint_as_float(top[c]));
+                        if ((threadIdx.x & 15) == 0 && count[c] > 0) a.q_scale[(col[c] >> 7) * a.ldqs + row] = s.scale;
+                        store_codes8(a.Q + row * a.ldq + col[c], e4m3 ? codes8<kE4M3>(h[c], s.mult) : codes8<kE5M2>(h[c], s.mult), count[c], wide);
+                    }
+                }
             }
         }
-    }
-    if (a.stats && here && threadIdx.x == 0) {
-        float* s = a.stats + 4 * row;
-        s[0] = post.x; s[1] = post.y; s[2] = pre.x; s[3] = pre.y;
+        if (a.stats && here && threadIdx.x == 0) {
+            float* s = a.stats + 4 * row;
+            s[0] = post.x; s[1] = post.y; s[2] = pre.x; s[3] = pre.y;
+        }
+        if (kAhead) cur = next;
     }
 }
 
+struct StepShape {
+    int runs, threads, rows, blocks;     // blocks: 0, one for each `rows` rows; else they go on from row to row
+};
+// 16 columns a thread where there are rows enough to go on with; else eight, and more threads on a row.
+StepShape step_shape(long long M, long long N, int sm_count) {
+    StepShape s;
+    const bool many = M >= 4ll * sm_count && N <= 8192;
+    s.runs = many ? 2 : (N <= 4096 ? 1 : (N <= 8192 ? 2 : 4));
+    const long long per = 8ll * s.runs;
+    s.threads = static_cast<int>(((N + per - 1) / per + 31) / 32 * 32);
+    s.rows = std::max(1, std::min(kMaxBlockRows, (many ? 256 : 128) / s.threads));
+    s.blocks = many ? sm_count * (s.threads > 256 ? 1 : 2) : 0;
+    return s;
+}
+
 template <int kType>
-cudaError_t step_t(const StepArgs& a, int runs, const cudaLaunchConfig_t& cfg) {
-    if (runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512>, a);
-    if (runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512>, a);
-    if (cfg.blockDim.x <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512>, a);
-    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024>, a);
+cudaError_t step_t(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
+    if (s.blocks) {
+        if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true>, a);
+        return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true>, a);
+    }
+    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false>, a);
+    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false>, a);
+    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false>, a);
+    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false>, a);
 }
 
 }  // namespace
 
-cudaError_t launch_norm_step(int type, const StepArgs& a, cudaStream_t stream) {
-    const int runs = a.N <= 4096 ? 1 : (a.N <= 8192 ? 2 : 4);
-    const long long per = 8ll * runs;
-    const int threads = static_cast<int>(((a.N + per - 1) / per + 31) / 32 * 32);
-    const int rows = threads >= 128 ? 1 : 128 / threads;           // (at most kMaxBlockRows)
+cudaError_t launch_norm_step(int type, const StepArgs& a, int sm_count, cudaStream_t stream) {
+    const StepShape s = step_shape(a.M, a.N, sm_count);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((a.M + rows - 1) / rows));
-    cfg.blockDim = dim3(static_cast<unsigned>(threads), static_cast<unsigned>(rows));
+    const long long blocks = (a.M + s.rows - 1) / s.rows;
+    cfg.gridDim = dim3(static_cast<unsigned>(s.blocks ? std::min<long long>(s.blocks, blocks) : blocks));
+    cfg.blockDim = dim3(static_cast<unsigned>(s.threads), static_cast<unsigned>(s.rows));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
     cfg.attrs = attr;
     cfg.numAttrs = cfg.gridDim.x <= 128 ? 1 : 0;                   // (launched early only where the blocks are few, like the row kernels)
-    if (type == kF32) return step_t<kF32>(a, runs, cfg);
-    return type == kF16 ? step_t<kF16>(a, runs, cfg) : step_t<kBF16>(a, runs, cfg);
+    if (type == kF32) return step_t<kF32>(a, s, cfg);
+    return type == kF16 ? step_t<kF16>(a, s, cfg) : step_t<kBF16>(a, s, cfg);
 }
 
 }  // namespace mip

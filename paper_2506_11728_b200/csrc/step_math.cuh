@@ -16,19 +16,20 @@ constexpr int kCodesNone = 0, kCodesS8 = 1, kCodesE4M3 = 2, kCodesE5M2 = 3;
 __device__ __forceinline__ uint4 philox10(uint4 c, uint2 k) {
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
-        const uint32_t h0 = __umulhi(0xD2511F53u, c.x), l0 = 0xD2511F53u * c.x;
-        const uint32_t h1 = __umulhi(0xCD9E8D57u, c.z), l1 = 0xCD9E8D57u * c.z;
-        c = make_uint4(h1 ^ c.y ^ k.x, l1, h0 ^ c.w ^ k.y, l0);
+        // (one wide multiplication instead of two halves)
+        const uint64_t p0 = static_cast<uint64_t>(0xD2511F53u) * c.x, p1 = static_cast<uint64_t>(0xCD9E8D57u) * c.z;
+        c = make_uint4(static_cast<uint32_t>(p1 >> 32) ^ c.y ^ k.x, static_cast<uint32_t>(p1), static_cast<uint32_t>(p0 >> 32) ^ c.w ^ k.y,
+                       static_cast<uint32_t>(p0));
         k.x += 0x9E3779B9u;
         k.y += 0xBB67AE85u;
     }
     return c;
 }
 
-// The mask of eight neighbouring columns: one draw, 16 bits for each.  v[j] becomes v[j] * scale where the bits are `bar`
-// or more, 0 (whatever v[j] is) where they are below.
+// The mask of eight neighbouring columns: one draw, 16 bits for each.  An element becomes itself times `scale` where its bits
+// are the bar or more, 0 (whatever it is) where they are below.
 struct Dropout {
-    uint32_t bar;                        // 0: nothing is dropped
+    uint32_t bar;                        // shifted up by 16 bits; 0: nothing is dropped
     float scale;                         // 65536 / (65536 - bar)
     uint2 key;
     unsigned long long step;             // the caller's counter
@@ -37,17 +38,19 @@ struct Dropout {
         const unsigned long long g = static_cast<unsigned long long>(row) * groups + (static_cast<unsigned long long>(col) >> 3);
         return philox10(make_uint4(static_cast<uint32_t>(g), static_cast<uint32_t>(g >> 32), static_cast<uint32_t>(step), static_cast<uint32_t>(step >> 32)), key);
     }
-    __device__ __forceinline__ void apply(const uint4& bits, float (&v)[8]) const {
+    // (the high half of a word is compared with the low half still behind it: that changes nothing)
+    __device__ __forceinline__ void apply(const uint4& bits, uint64_t (&v)[4]) const {
         const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t r = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
-            v[j] = r >= bar ? v[j] * scale : 0.0f;
+        for (int j = 0; j < 4; ++j) {
+            float lo, hi;
+            unpack_f2(mul_f2(v[j], pack_f2(scale, scale)), lo, hi);
+            v[j] = pack_f2(w[j] << 16 >= bar ? lo : 0.0f, w[j] >= bar ? hi : 0.0f);
         }
     }
 };
 __device__ __forceinline__ Dropout dropout_of(uint32_t bar, float scale, unsigned long long seed, const unsigned long long* counter, long long N) {
-    return Dropout{bar, scale, make_uint2(static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)), bar && counter ? *counter : 0ull,
+    return Dropout{bar << 16, scale, make_uint2(static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)), bar && counter ? *counter : 0ull,
                    (static_cast<unsigned long long>(N) + 7) / 8};
 }
 
@@ -57,8 +60,31 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+__device__ __forceinline__ float sum_pair(uint64_t v) {
+    float a, b;
+    unpack_f2(v, a, b);
+    return a + b;
+}
+// Eight float32 of a vector that every row reads, as pairs.
+__device__ __forceinline__ void load_vector_pairs(const float* p, long long at, int count, bool wide, float fill, uint64_t (&v)[4]) {
+    float x[8];
+    load_vector8(p, at, count, wide, fill, x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = pack_f2(x[2 * j], x[2 * j + 1]);
+}
+// Elements that do not exist become 0.
+__device__ __forceinline__ void clear_behind(uint64_t (&v)[4], int count) {
+    if (count >= 8) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float a, b;
+        unpack_f2(v[j], a, b);
+        v[j] = pack_f2(2 * j < count ? a : 0.0f, 2 * j + 1 < count ? b : 0.0f);
+    }
+}
+
 // A multiple of 32 threads a row, up to 1024; blockDim.y rows side by side go through the same calls.
 constexpr int kMaxRowWarps = 32;
-constexpr int kMaxBlockRows = 4;         // rows per block where a row takes fewer than 128 threads
+constexpr int kMaxBlockRows = 8;         // rows side by side in a block
 
 }  // namespace mip
