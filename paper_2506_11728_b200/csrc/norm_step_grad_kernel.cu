@@ -29,8 +29,10 @@ constexpr int kMaxGradRows = 4, kMaxCluster = 8, kGradThreads = 512, kGradWarps 
 struct RowExchange {
     float2 share[2][kMaxGradRows][kMaxCluster * kGradWarps];
 };
+// (kFirst: the first value is wanted)
+template <bool kFirst>
 __device__ __forceinline__ float2 exchange(float2 v, RowExchange& x, int slot, int cluster, uint32_t rank) {
-    v.x = warp_sum(v.x);
+    if (kFirst) v.x = warp_sum(v.x);
     v.y = warp_sum(v.y);
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int shares = warps * cluster;
@@ -48,6 +50,16 @@ __device__ __forceinline__ float2 exchange(float2 v, RowExchange& x, int slot, i
         if (lane == 0) *at = v;
         __syncthreads();
     }
+    if (shares <= kGradWarps) {
+        const int i = lane & (kGradWarps - 1);
+        float2 s = i < shares ? x.share[slot][threadIdx.y][i] : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int o = kGradWarps / 2; o > 0; o >>= 1) {
+            if (kFirst) s.x += __shfl_xor_sync(~0u, s.x, o);
+            s.y += __shfl_xor_sync(~0u, s.y, o);
+        }
+        return s;
+    }
     float2 s = make_float2(0.0f, 0.0f);
     for (int i = lane; i < shares; i += 32) {
         const float2 t = x.share[slot][threadIdx.y][i];
@@ -58,10 +70,12 @@ __device__ __forceinline__ float2 exchange(float2 v, RowExchange& x, int slot, i
 }
 
 // kPre, kPost: there is a norm behind / in front of the sum; kMean: one of them subtracts its mean (and has a bias)
-template <int kType, bool kPre, bool kPost, bool kMean>
+template <int kType, bool kPre, bool kPost, bool kMean, bool kWide>
 __global__ void __launch_bounds__(kGradThreads, 1)
 mip_norm_step_grad_kernel(const StepGradArgs a) {
     constexpr bool kAhead = kType != kF32;       // (32-bit elements of two rows leave no registers for the sums)
+    constexpr bool wide = kWide;
+    constexpr int kSize = kType == kF32 ? 4 : 2;
     __shared__ RowExchange ex;
     __shared__ float rows_sum[kMaxGradRows - 1][8 * 64];
     pdl_wait();
@@ -70,30 +84,30 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
     const uint32_t rank = cluster > 1 ? cluster_ctarank() : 0u;
     const long long worker = blockIdx.x / static_cast<unsigned>(cluster);
     const int block_rows = blockDim.y;
-    const bool wide = a.wide;
     const long long col = 8ll * (static_cast<long long>(rank) * blockDim.x + threadIdx.x);
     const int exist = a.N <= col ? 0 : (a.N - col < 8 ? static_cast<int>(a.N - col) : 8);
     const Dropout drop = dropout_of(a.bar, a.drop_scale, a.seed, a.counter, a.N);
     const float inv_n = __fdiv_rn(1.0f, static_cast<float>(a.N));
     const bool gate_sum = a.dgate && a.gate_rows > 1, gate_each = a.dgate && a.gate_rows == 1;
-    float pre_w[8] = {}, pre_b[8] = {}, post_w[8] = {}, post_b[8] = {}, gate_s[8] = {};
+    uint64_t pre_w[4] = {}, pre_b[4] = {}, post_w[4] = {}, post_b[4] = {}, gate_s[4] = {};      // sums
 
     struct Row {
         Eight<kType> dy, dh, y, z;
         float4 st;
         int count;
     };
+    const auto at = [&](const void* p, long long row, long long ld) { return static_cast<const char*>(p) + (row * ld + col) * kSize; };
     const auto load = [&](Row& r, long long base, long long end) {
         const long long row = base + threadIdx.y;
         const bool here = row < end;
         r.count = here ? exist : 0;
-        if (a.dY) r.dy.load(a.dY, row * a.lddy + col, r.count, wide);
+        if (a.dY) r.dy.load(at(a.dY, row, a.lddy), 0, r.count, wide);
         else r.dy.clear();
         if (kPre) {
-            r.dh.load(a.dH, row * a.lddh + col, r.count, wide);
-            r.y.load(a.Y, row * a.ldy + col, r.count, wide);
+            r.dh.load(at(a.dH, row, a.lddh), 0, r.count, wide);
+            r.y.load(at(a.Y, row, a.ldy), 0, r.count, wide);
         }
-        if (kPost || a.Z) r.z.load(a.Z, row * a.ldz + col, r.count, wide);
+        if (kPost || a.Z) r.z.load(at(a.Z, row, a.ldz), 0, r.count, wide);
         else r.z.clear();
         r.st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if ((kPre || kPost) && here) {
@@ -101,98 +115,110 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
             r.st = make_float4(s[0], s[1], s[2], s[3]);
         }
     };
-    // (columns that lie behind the last one are not added up: their y^ may be anything)
+    Eight<kType> gate;
+    uint32_t gate_row = ~0u;
     int slot = 0;
+    // (x - mean) * rstd; columns that lie behind the last one are not added up: they are 0
+    const auto normalized = [&](uint64_t (&v)[4], float mean, float rstd, int count) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = mul_f2(kMean ? add_f2(v[j], pack_f2(-mean, -mean)) : v[j], pack_f2(rstd, rstd));
+        if (kMean || !kWide) clear_behind(v, count);
+    };
+    // sums over the row of g and g hat, and what a norm passes on: rstd (g - mean(g) - hat mean(g hat))
+    const auto through = [&](uint64_t (&g)[4], const uint64_t (&hat)[4], int kind, float rstd, const auto& take) {
+        uint64_t s = 0ull, u = 0ull;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (kMean) s = add_f2(s, g[j]);
+            u = fma_f2(g[j], hat[j], u);
+        }
+        const float2 e = exchange<kMean>(make_float2(kMean ? sum_pair(s) : 0.0f, sum_pair(u)), ex, slot ^= 1, cluster, rank);
+        const float mean = kMean && kind == kNormLayer ? -e.x * inv_n : 0.0f, slope = -e.y * inv_n;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) take(j, fma_f2(hat[j], pack_f2(slope, slope), kMean ? add_f2(g[j], pack_f2(mean, mean)) : g[j]), pack_f2(rstd, rstd));
+    };
     const auto process = [&](const Row& r, long long base) {
         const long long row = base + threadIdx.y;
-        float g[8], t[8], w[8];
-        r.dy.values(g);
+        if (a.gate && r.count) {                             // (read again where the row has another gate row than the last one)
+            const uint32_t i = a.gate_rows == 1 ? static_cast<uint32_t>(row)
+                               : (a.gate_rows >= a.M ? 0u : static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows));
+            if (i != gate_row) gate.load(a.gate, i * a.ldgate + col, exist, wide);
+            gate_row = i;
+        }
+        uint64_t g[4], t[4], w[4];
+        r.dy.pairs(g);
         if (kPre) {
-            float hat[8];
-            r.dh.values(t);
-            r.y.values(hat);
-            load_vector8(a.pre_w, col, exist, wide, 1.0f, w);
-            float2 s = make_float2(0.0f, 0.0f);
+            uint64_t hat[4];
+            r.dh.pairs(t);
+            r.y.pairs(hat);
+            load_vector_pairs(a.pre_w, col, exist, wide, 1.0f, w);
+            normalized(hat, r.st.z, r.st.w, r.count);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                hat[j] = j < r.count ? (hat[j] - r.st.z) * r.st.w : 0.0f;
-                pre_w[j] = fmaf(t[j], hat[j], pre_w[j]);
-                if (kMean) pre_b[j] += t[j];
-                t[j] *= w[j];
-                if (kMean) s.x += t[j];
-                s.y = fmaf(t[j], hat[j], s.y);
+            for (int j = 0; j < 4; ++j) {
+                pre_w[j] = fma_f2(t[j], hat[j], pre_w[j]);
+                if (kMean) pre_b[j] = add_f2(pre_b[j], t[j]);
+                t[j] = mul_f2(t[j], w[j]);
             }
-            s = exchange(s, ex, slot ^= 1, cluster, rank);
-            const float mean = kMean && a.pre == kNormLayer ? s.x * inv_n : 0.0f, slope = s.y * inv_n;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = fmaf(t[j] - mean - hat[j] * slope, r.st.w, g[j]);
+            through(t, hat, a.pre, r.st.w, [&](int j, uint64_t v, uint64_t rstd) { g[j] = fma_f2(v, rstd, g[j]); });
         }
         if (a.dX) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] = a.x_scale * g[j];
+            for (int j = 0; j < 4; ++j) t[j] = mul_f2(pack_f2(a.x_scale, a.x_scale), g[j]);
             Eight<kType> e;
-            e.set(t);
-            e.store(a.dX, row * a.lddx + col, r.count, wide);
+            e.set_pairs(t);
+            e.store(const_cast<char*>(at(a.dX, row, a.lddx)), 0, r.count, wide);
         }
-        if (drop.bar) {
-            uint64_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) u[j] = pack_f2(g[2 * j], g[2 * j + 1]);
-            drop.apply(drop.draw(row, col), u);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) unpack_f2(u[j], g[2 * j], g[2 * j + 1]);
-        }
-        float hat[8];
-        r.z.values(hat);
+        if (drop.bar) drop.apply(drop.draw(row, col), g);
+        uint64_t hat[4];
+        r.z.pairs(hat);
         if (kPost) {
-            load_vector8(a.post_w, col, exist, wide, 1.0f, w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) hat[j] = j < r.count ? (hat[j] - r.st.x) * r.st.y : 0.0f;
+            load_vector_pairs(a.post_w, col, exist, wide, 1.0f, w);
+            normalized(hat, r.st.x, r.st.y, r.count);
         }
         if (a.gate) {
             if (a.dgate) {
-                float b[8];
-                if (kPost) load_vector8(a.post_b, col, exist, wide, 0.0f, b);
+                uint64_t b[4];
+                if (kPost && kMean) load_vector_pairs(a.post_b, col, exist, wide, 0.0f, b);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) t[j] = g[j] * (kPost ? fmaf(hat[j], w[j], b[j]) : hat[j]);
+                for (int j = 0; j < 4; ++j) {
+                    uint64_t u = hat[j];
+                    if (kPost) u = kMean ? fma_f2(u, w[j], b[j]) : mul_f2(u, w[j]);
+                    t[j] = mul_f2(g[j], u);
+                }
                 if (gate_each) {
                     Eight<kType> e;
-                    e.set(t);
+                    e.set_pairs(t);
                     e.store(a.dgate, row * a.lddgate + col, r.count, wide);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) gate_s[j] += t[j];
+                    for (int j = 0; j < 4; ++j) gate_s[j] = add_f2(gate_s[j], t[j]);
                 }
             }
-            Eight<kType> e;
-            e.load(a.gate, (r.count ? static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows) : 0u) * a.ldgate + col, r.count, wide);
-            e.values(t);
+            if (r.count) {
+                gate.pairs(t);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] *= t[j];
+                for (int j = 0; j < 4; ++j) g[j] = mul_f2(g[j], t[j]);
+            }
         }
         if (kPost) {
-            float2 s = make_float2(0.0f, 0.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                post_w[j] = fmaf(g[j], hat[j], post_w[j]);
-                if (kMean) post_b[j] += g[j];
-                g[j] *= w[j];
-                if (kMean) s.x += g[j];
-                s.y = fmaf(g[j], hat[j], s.y);
+            for (int j = 0; j < 4; ++j) {
+                post_w[j] = fma_f2(g[j], hat[j], post_w[j]);
+                if (kMean) post_b[j] = add_f2(post_b[j], g[j]);
+                g[j] = mul_f2(g[j], w[j]);
             }
-            s = exchange(s, ex, slot ^= 1, cluster, rank);
-            const float mean = kMean && a.post == kNormLayer ? s.x * inv_n : 0.0f, slope = s.y * inv_n;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = (g[j] - mean - hat[j] * slope) * r.st.y;
+            through(g, hat, a.post, r.st.y, [&](int j, uint64_t v, uint64_t rstd) { g[j] = mul_f2(v, rstd); });
         }
         if (a.dZ) {
             Eight<kType> e;
-            e.set(g);
-            e.store(a.dZ, row * a.lddz + col, r.count, wide);
+            e.set_pairs(g);
+            e.store(const_cast<char*>(at(a.dZ, row, a.lddz)), 0, r.count, wide);
         }
     };
     // Adds the block's rows' sums up in the first one's registers.
-    const auto over_block = [&](float (&v)[8]) {
+    const auto over_block = [&](const uint64_t (&pairs)[4], float (&v)[8]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) unpack_f2(pairs[j], v[2 * j], v[2 * j + 1]);
         if (block_rows == 1) return;
         if (threadIdx.y > 0) {
 #pragma unroll
@@ -255,26 +281,28 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
             load(cur, b1, e1);
         }
         if (gate_sum) {
-            over_block(gate_s);
+            float v[8];
+            over_block(gate_s, v);
             if (a.parts > 1) {
-                put_sum(gate_s, a.gate_part + u * a.N);
+                put_sum(v, a.gate_part + u * a.N);
             } else if (threadIdx.y == 0) {
                 Eight<kType> e;
-                e.set(gate_s);
+                e.set(v);
                 e.store(a.dgate, u * a.lddgate + col, exist, wide);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) gate_s[j] = 0.0f;
+            for (int j = 0; j < 4; ++j) gate_s[j] = 0ull;
         }
     }
     if (a.sums == 0) return;
     float* plane = a.sum_part + worker * a.sums * a.N;
-    int at = 0;
-    const auto put = [&](float (&v)[8], const float* wanted) {
+    int place = 0;
+    const auto put = [&](const uint64_t (&pairs)[4], const float* wanted) {
         if (!wanted) return;
-        over_block(v);
-        put_sum(v, plane + at * a.N);
-        ++at;
+        float v[8];
+        over_block(pairs, v);
+        put_sum(v, plane + place * a.N);
+        ++place;
     };
     if (kPost) {
         put(post_w, a.dpost_w);
@@ -318,17 +346,21 @@ mip_norm_step_sums_kernel(const SumArgs a) {
     else store_element(a.dgate, (job - a.sums) * a.lddgate + col, a.type, s);
 }
 
-template <int kType, bool kPre, bool kPost>
+template <int kType, bool kPre, bool kPost, bool kWide>
 cudaError_t grad_mean(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
     if ((kPre && a.pre == kNormLayer) || (kPost && a.post == kNormLayer)) {
-        if constexpr (kPre || kPost) return cudaLaunchKernelEx(&cfg, mip_norm_step_grad_kernel<kType, kPre, kPost, true>, a);
+        if constexpr (kPre || kPost) return cudaLaunchKernelEx(&cfg, mip_norm_step_grad_kernel<kType, kPre, kPost, true, kWide>, a);
     }
-    return cudaLaunchKernelEx(&cfg, mip_norm_step_grad_kernel<kType, kPre, kPost, false>, a);
+    return cudaLaunchKernelEx(&cfg, mip_norm_step_grad_kernel<kType, kPre, kPost, false, kWide>, a);
+}
+template <int kType, bool kWide>
+cudaError_t grad_t(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
+    if (a.pre != kNormNone) return a.post != kNormNone ? grad_mean<kType, true, true, kWide>(a, cfg) : grad_mean<kType, true, false, kWide>(a, cfg);
+    return a.post != kNormNone ? grad_mean<kType, false, true, kWide>(a, cfg) : grad_mean<kType, false, false, kWide>(a, cfg);
 }
 template <int kType>
-cudaError_t grad_t(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
-    if (a.pre != kNormNone) return a.post != kNormNone ? grad_mean<kType, true, true>(a, cfg) : grad_mean<kType, true, false>(a, cfg);
-    return a.post != kNormNone ? grad_mean<kType, false, true>(a, cfg) : grad_mean<kType, false, false>(a, cfg);
+cudaError_t grad_wide(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
+    return a.wide ? grad_t<kType, true>(a, cfg) : grad_t<kType, false>(a, cfg);
 }
 
 struct GradShape {
@@ -383,7 +415,7 @@ cudaError_t launch_norm_step_grad(int type, StepGradArgs a, void* scratch, cudaS
         attr[1].val.programmaticStreamSerializationAllowed = pdl_allowed();
         cfg.attrs = s.cluster > 1 ? attr : attr + 1;
         cfg.numAttrs = s.cluster > 1 ? 1 : (cfg.gridDim.x <= 128 ? 1 : 0);
-        const cudaError_t e = type == kF32 ? grad_t<kF32>(a, cfg) : (type == kF16 ? grad_t<kF16>(a, cfg) : grad_t<kBF16>(a, cfg));
+        const cudaError_t e = type == kF32 ? grad_wide<kF32>(a, cfg) : (type == kF16 ? grad_wide<kF16>(a, cfg) : grad_wide<kBF16>(a, cfg));
         ++*launches;
         if (e != cudaSuccess) return e;
     }

@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, Exchange<kThreads>& x, i
 
 // v becomes (v - mean) / sqrt(var + eps); returns (mean, 1 / sqrt(var + eps)).
 template <int kRuns, int kThreads>
-__device__ __forceinline__ float2 normalize(int kind, uint64_t (&v)[kRuns][4], const int (&count)[kRuns], float n, float eps, Exchange<kThreads>& x, int& slot) {
+__device__ __forceinline__ float2 normalize(int kind, uint64_t (&v)[kRuns][4], const int (&count)[kRuns], float inv_n, float eps, Exchange<kThreads>& x, int& slot) {
     float mean = 0.0f;
     if (kind == kNormLayer) {
         uint64_t s = 0ull;
@@ -61,7 +61,7 @@ __device__ __forceinline__ float2 normalize(int kind, uint64_t (&v)[kRuns][4], c
         for (int c = 0; c < kRuns; ++c)
 #pragma unroll
             for (int j = 0; j < 4; ++j) s = add_f2(s, v[c][j]);        // (columns that do not exist hold 0)
-        mean = __fdiv_rn(row_sum(sum_pair(s), x, slot), n);
+        mean = row_sum(sum_pair(s), x, slot) * inv_n;
         const uint64_t m = pack_f2(-mean, -mean);
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
@@ -75,7 +75,7 @@ __device__ __forceinline__ float2 normalize(int kind, uint64_t (&v)[kRuns][4], c
     for (int c = 0; c < kRuns; ++c)
 #pragma unroll
         for (int j = 0; j < 4; ++j) q = fma_f2(v[c][j], v[c][j], q);
-    const float rstd = __frsqrt_rn(__fadd_rn(__fdiv_rn(row_sum(sum_pair(q), x, slot), n), eps));
+    const float rstd = rsqrtf(fmaf(row_sum(sum_pair(q), x, slot), inv_n, eps));
 #pragma unroll
     for (int c = 0; c < kRuns; ++c)
 #pragma unroll
@@ -118,15 +118,15 @@ __device__ __forceinline__ void store_codes8(uint8_t* dst, uint2 q, int count, b
 }
 
 // kRuns runs of eight columns a thread, up to kThreads threads a block; kAhead: the block goes on from row to row.
-template <int kType, int kRuns, int kThreads, bool kAhead>
+template <int kType, int kRuns, int kThreads, bool kAhead, bool kWide>
 __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 2 : 1)
 mip_norm_step_kernel(const StepArgs a) {
     __shared__ Exchange<kThreads> ex;
     pdl_wait();
     pdl_launch_dependents();
-    const bool wide = a.wide;
+    constexpr bool wide = kWide;
     const Dropout drop = dropout_of(a.bar, a.drop_scale, a.seed, a.counter, a.N);
-    const float n = static_cast<float>(a.N);
+    const float inv_n = __fdiv_rn(1.0f, static_cast<float>(a.N));
     int slot = 0;
     long long col[kRuns];
     int exist[kRuns];
@@ -144,37 +144,55 @@ mip_norm_step_kernel(const StepArgs a) {
     struct Row {
         Eight<kType> x[kRuns], z[kRuns];
     };
-    const auto load = [&](Row& r, long long row) {
+    constexpr int kSize = kType == kF32 ? 4 : 2;
+    const long long run = 8ll * blockDim.x;              // columns between a thread's runs
+    const long long step = static_cast<long long>(gridDim.x) * blockDim.y;
+    const long long first = static_cast<long long>(blockIdx.x) * blockDim.y + threadIdx.y;
+    // (addresses of the next row to read and of this row's outputs go on by a step's bytes)
+    const char* z_at = static_cast<const char*>(a.Z) + (first * a.ldz + col[0]) * kSize;
+    const char* x_at = static_cast<const char*>(a.X) + (first * a.ldx + col[0]) * kSize;
+    char* y_at = static_cast<char*>(a.Y) + (first * a.ldy + col[0]) * kSize;
+    char* h_at = static_cast<char*>(a.H) + (first * a.ldh + col[0]) * kSize;
+    const long long z_step = step * a.ldz * kSize, x_step = step * a.ldx * kSize, y_step = step * a.ldy * kSize, h_step = step * a.ldh * kSize;
+    const auto load = [&](Row& r, bool here) {
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
-            const int count = row < a.M ? exist[c] : 0;
-            if (a.Z) r.z[c].load(a.Z, row * a.ldz + col[c], count, wide);
+            const int count = here ? exist[c] : 0;
+            if (a.Z) r.z[c].load(z_at, c * run, count, wide);
             else r.z[c].clear();
-            if (a.X) r.x[c].load(a.X, row * a.ldx + col[c], count, wide);
+            if (a.X) r.x[c].load(x_at, c * run, count, wide);
             else r.x[c].clear();
         }
+        z_at += z_step;
+        x_at += x_step;
     };
-    const long long step = static_cast<long long>(gridDim.x) * blockDim.y;
-    long long base = static_cast<long long>(blockIdx.x) * blockDim.y;
     Row cur;
-    load(cur, base + threadIdx.y);
-    for (; base < a.M; base += step) {
-        const long long row = base + threadIdx.y;
+    load(cur, first < a.M);
+    Eight<kType> g[kRuns];
+    uint32_t gate_row = ~0u;
+    for (long long row = first; row - threadIdx.y < a.M; row += step, y_at += y_step, h_at += h_step) {
         const bool here = row < a.M;
         int count[kRuns];
-        Eight<kType> g[kRuns];
         uint64_t v[kRuns][4];
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
             count[c] = here ? exist[c] : 0;
-            if (a.gate) g[c].load(a.gate, (here ? static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows) : 0u) * a.ldgate + col[c], count[c], wide);
             cur.z[c].pairs(v[c]);
         }
+        if (a.gate && here) {                            // (read again where the row has another gate row than the last one)
+            const uint32_t i = a.gate_rows == 1 ? static_cast<uint32_t>(row)
+                               : (a.gate_rows >= a.M ? 0u : static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows));
+            if (i != gate_row) {
+#pragma unroll
+                for (int c = 0; c < kRuns; ++c) g[c].load(a.gate, i * a.ldgate + col[c], exist[c], wide);
+                gate_row = i;
+            }
+        }
         Row next;
-        if (kAhead) load(next, row + step);
+        if (kAhead) load(next, row + step < a.M);
         float2 post = make_float2(0.0f, 0.0f), pre = post;
         if (a.post != kNormNone) {
-            post = normalize<kRuns>(a.post, v, count, n, a.eps, ex, slot);
+            post = normalize<kRuns>(a.post, v, count, inv_n, a.eps, ex, slot);
             affine<kRuns>(v, post_w, kAhead, a.post_w, a.post_b, col, exist, wide);
         }
 #pragma unroll
@@ -194,18 +212,18 @@ mip_norm_step_kernel(const StepArgs a) {
             if (a.Y) {
                 Eight<kType> y;
                 y.set_pairs(v[c]);
-                y.store(a.Y, row * a.ldy + col[c], count[c], wide);
+                y.store(y_at, c * run, count[c], wide);
             }
         }
         if (a.pre != kNormNone) {
-            pre = normalize<kRuns>(a.pre, v, count, n, a.eps, ex, slot);
+            pre = normalize<kRuns>(a.pre, v, count, inv_n, a.eps, ex, slot);
             affine<kRuns>(v, pre_w, kAhead, a.pre_w, a.pre_b, col, exist, wide);
             if (a.H) {
 #pragma unroll
                 for (int c = 0; c < kRuns; ++c) {
                     Eight<kType> h;
                     h.set_pairs(v[c]);
-                    h.store(a.H, row * a.ldh + col[c], count[c], wide);
+                    h.store(h_at, c * run, count[c], wide);
                 }
             }
             if (a.codes != kCodesNone) {
@@ -277,16 +295,20 @@ StepShape step_shape(long long M, long long N, int sm_count) {
     return s;
 }
 
-template <int kType>
+template <int kType, bool kWide>
 cudaError_t step_t(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
     if (s.blocks) {
-        if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true>, a);
-        return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true>, a);
+        if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true, kWide>, a);
+        return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true, kWide>, a);
     }
-    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false>, a);
-    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false>, a);
-    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false>, a);
-    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false>, a);
+    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false, kWide>, a);
+    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false, kWide>, a);
+    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false, kWide>, a);
+    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false, kWide>, a);
+}
+template <int kType>
+cudaError_t step_wide(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
+    return a.wide ? step_t<kType, true>(a, s, cfg) : step_t<kType, false>(a, s, cfg);
 }
 
 }  // namespace
@@ -303,8 +325,8 @@ cudaError_t launch_norm_step(int type, const StepArgs& a, int sm_count, cudaStre
     attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
     cfg.attrs = attr;
     cfg.numAttrs = cfg.gridDim.x <= 128 ? 1 : 0;                   // (launched early only where the blocks are few, like the row kernels)
-    if (type == kF32) return step_t<kF32>(a, s, cfg);
-    return type == kF16 ? step_t<kF16>(a, s, cfg) : step_t<kBF16>(a, s, cfg);
+    if (type == kF32) return step_wide<kF32>(a, s, cfg);
+    return type == kF16 ? step_wide<kF16>(a, s, cfg) : step_wide<kBF16>(a, s, cfg);
 }
 
 }  // namespace mip
