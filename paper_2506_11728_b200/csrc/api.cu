@@ -2445,7 +2445,7 @@ int mipgemm_norm_step(int type, int post, int pre, int64_t M, int64_t N, float e
     a.Z = Z; a.ldz = ldz;
     a.post_w = post_weight; a.post_b = post_bias;
     a.gate = gate; a.ldgate = ldgate; a.gate_rows = gate_rows;
-    a.seed = seed; a.counter = reinterpret_cast<const unsigned long long*>(counter);
+    step_mask(a.mask, seed, reinterpret_cast<const unsigned long long*>(counter));
     a.pre_w = pre_weight; a.pre_b = pre_bias;
     a.Y = Y; a.ldy = ldy;
     a.H = H; a.ldh = ldh;
@@ -2471,7 +2471,7 @@ int mipgemm_norm_step_grad(int type, int post, int pre, int64_t M, int64_t N, co
     a.Z = Z; a.ldz = ldz;
     a.post_w = post_weight; a.post_b = post_bias;
     a.gate = gate; a.ldgate = ldgate; a.gate_rows = gate_rows;
-    a.seed = seed; a.counter = reinterpret_cast<const unsigned long long*>(counter);
+    step_mask(a.mask, seed, reinterpret_cast<const unsigned long long*>(counter));
     a.stats = stats;
     a.dX = dX; a.lddx = lddx;
     a.dZ = dZ; a.lddz = lddz;

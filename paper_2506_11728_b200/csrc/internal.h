@@ -307,6 +307,12 @@ cudaError_t f8_product_init();               // once per device
 cudaError_t launch_f8_product(const F8ProductParams& p, bool pair, bool vec, bool raw, int grid, cudaStream_t stream);
 cudaError_t launch_f8_finish(const F8ProductArgs& a, const PartialPlanes& s, cudaStream_t stream, int* launches);
 
+// Dropout: 16 bits of the generator below `bar` are dropped (0: nothing is), what is kept is multiplied with `scale`.
+struct StepMask {
+    uint32_t bar; float scale;
+    uint32_t keys[20];                   // of the generator's rounds
+    const unsigned long long* counter;
+};
 constexpr long long kStepColumns = 32768;    // the longest row of the step's kernels
 struct StepArgs {
     long long M, N;
@@ -318,9 +324,7 @@ struct StepArgs {
     const float* post_w;
     const float* post_b;
     const void* gate; long long ldgate, gate_rows;
-    uint32_t bar; float drop_scale;  // dropout: 16 bits below `bar` are dropped; 0: nothing is
-    unsigned long long seed;
-    const unsigned long long* counter;
+    StepMask mask;
     const float* pre_w;
     const float* pre_b;
     void* Y; long long ldy;
@@ -329,6 +333,7 @@ struct StepArgs {
     float* q_scale; long long ldqs;
     float* stats;
 };
+void step_mask(StepMask& m, unsigned long long seed, const unsigned long long* counter);      // keys and counter
 cudaError_t launch_norm_step(int type, const StepArgs& a, int sm_count, cudaStream_t stream);
 
 struct StepGradArgs {
@@ -344,9 +349,7 @@ struct StepGradArgs {
     const float* post_w;
     const float* post_b;
     const void* gate; long long ldgate, gate_rows;
-    uint32_t bar; float drop_scale;
-    unsigned long long seed;
-    const unsigned long long* counter;
+    StepMask mask;
     const float* stats;
     void* dX; long long lddx;
     void* dZ; long long lddz;

@@ -6,13 +6,15 @@
 // dw' = sum m z^, db' = sum m.  The rows' statistics come from the forward pass, so each norm needs one exchange; the mask
 // is drawn again from its counter.
 //
-// Workers (CTAs, or clusters of CTAs that share a row of more than 4096 columns) go through the rows and keep the column sums in
-// registers, eight columns a thread; a second kernel adds the workers' sums in a fixed order.  Rows are dealt in units that
-// lie within one gate row, so that a unit's sum is a share of one row of dgate.  While a row waits for its exchanges, the next
-// one's elements are on their way.
+// Workers (CTAs, or clusters of CTAs that share a row of more than 8192 columns) go through the rows, 16 columns a thread; a second
+// kernel adds the workers' column sums in a fixed order.  Rows are dealt in units that lie within one gate row, so that a
+// unit's sum is a share of one row of dgate.  The column sums lie in shared memory, where each thread has places of its own:
+// in registers (40 to 80 of a thread's) they left room for one block on an SM, whose warps waited for each row's exchanges
+// together; two blocks by turns, with the next row's elements on their way, fill those gaps.
 //
-// What bounds it: the bytes of dy, dh, y, z, dx and dz.
+// What bounds it: the bytes of dy, dh, y, z, dx and dz, and the instructions behind them.
 #include <algorithm>
+#include <atomic>
 
 #include "ptx.cuh"
 #include "step_math.cuh"
@@ -21,23 +23,24 @@ namespace mip {
 
 namespace {
 
-constexpr int kMaxGradRows = 4, kMaxCluster = 8, kGradThreads = 512, kGradWarps = kGradThreads / 32;
+constexpr int kGradThreads = 512, kBlockThreads = 256;       // most threads of a row's CTA; of a CTA with several rows side by side
+constexpr int kGradRuns = 2, kGradCols = 8 * kGradRuns;      // columns per thread
+constexpr int kMaxGradRows = kBlockThreads / 32, kMaxCluster = 4, kGradWarps = kGradThreads / 32;
+static_assert(kMaxCluster * kGradThreads * kGradCols >= kStepColumns && kMaxGradRows <= kMaxBlockRows, "rows");
 
 // Sums of two values over a row's threads, over the cluster's CTAs too: every warp leaves its share with every CTA, one
 // barrier, every warp adds the shares up in the same order.  Two slots by turns: a warp that writes a slot again has passed
 // the barrier of the other one, which all warps reach after reading this one.
-struct RowExchange {
-    float2 share[2][kMaxGradRows][kMaxCluster * kGradWarps];
-};
 // (kFirst: the first value is wanted)
 template <bool kFirst>
-__device__ __forceinline__ float2 exchange(float2 v, RowExchange& x, int slot, int cluster, uint32_t rank) {
+__device__ __forceinline__ float2 exchange(float2 v, float2* share, int cluster, uint32_t rank) {
     if (kFirst) v.x = warp_sum(v.x);
     v.y = warp_sum(v.y);
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int shares = warps * cluster;
     if (shares == 1) return v;
-    float2* at = &x.share[slot][threadIdx.y][rank * warps + warp];
+    float2* const row = share + threadIdx.y * shares;
+    float2* const at = row + rank * warps + warp;
     if (cluster > 1) {
         if (lane < cluster) {
             const uint32_t dst = mapa_u32(smem_u32(at), lane);
@@ -50,73 +53,110 @@ __device__ __forceinline__ float2 exchange(float2 v, RowExchange& x, int slot, i
         if (lane == 0) *at = v;
         __syncthreads();
     }
-    if (shares <= kGradWarps) {
-        const int i = lane & (kGradWarps - 1);
-        float2 s = i < shares ? x.share[slot][threadIdx.y][i] : make_float2(0.0f, 0.0f);
+    float2 s = make_float2(0.0f, 0.0f);
+    if (shares <= 8) {
+        if ((lane & 7) < shares) s = row[lane & 7];
 #pragma unroll
-        for (int o = kGradWarps / 2; o > 0; o >>= 1) {
+        for (int o = 4; o > 0; o >>= 1) {
             if (kFirst) s.x += __shfl_xor_sync(~0u, s.x, o);
             s.y += __shfl_xor_sync(~0u, s.y, o);
         }
         return s;
     }
-    float2 s = make_float2(0.0f, 0.0f);
     for (int i = lane; i < shares; i += 32) {
-        const float2 t = x.share[slot][threadIdx.y][i];
+        const float2 t = row[i];
         s.x += t.x;
         s.y += t.y;
     }
-    return make_float2(warp_sum(s.x), warp_sum(s.y));
+    return make_float2(kFirst ? warp_sum(s.x) : 0.0f, warp_sum(s.y));
 }
+
+// A thread's column sums of one vector: 16 bytes of neighbouring threads side by side.
+struct ColumnSums {
+    float4* at;                              // the thread's first place
+    int pitch;                               // threads of the block
+    __device__ __forceinline__ void clear() const {
+#pragma unroll
+        for (int k = 0; k < kGradCols / 4; ++k) at[k * pitch] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    // run c's eight columns: += v, or += v * w
+    template <typename F>
+    __device__ __forceinline__ void add(int c, const F& term) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float4* const p = at + (2 * c + h) * pitch;
+            const float4 s = *p;
+            float4 r;
+            unpack_f2(term(2 * h, pack_f2(s.x, s.y)), r.x, r.y);
+            unpack_f2(term(2 * h + 1, pack_f2(s.z, s.w)), r.z, r.w);
+            *p = r;
+        }
+    }
+};
 
 // kPre, kPost: there is a norm behind / in front of the sum; kMean: one of them subtracts its mean (and has a bias)
 template <int kType, bool kPre, bool kPost, bool kMean, bool kWide>
 __global__ void __launch_bounds__(kGradThreads, 1)
-mip_norm_step_grad_kernel(const StepGradArgs a) {
-    constexpr bool kAhead = kType != kF32;       // (32-bit elements of two rows leave no registers for the sums)
+mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
+    constexpr bool kAhead = kType != kF32;       // (32-bit elements of two rows do not fit the registers)
     constexpr bool wide = kWide;
-    constexpr int kSize = kType == kF32 ? 4 : 2;
-    __shared__ RowExchange ex;
-    __shared__ float rows_sum[kMaxGradRows - 1][8 * 64];
+    constexpr int kSize = kType == kF32 ? 4 : 2, kRuns = kGradRuns;
+    extern __shared__ float4 sums_smem[];        // column sums: of dpre_w, dpre_b, dpost_w, dpost_b, dgate
+    __shared__ float2 share[2][kMaxCluster * kGradWarps];
     pdl_wait();
     pdl_launch_dependents();
     const int cluster = a.cluster;
     const uint32_t rank = cluster > 1 ? cluster_ctarank() : 0u;
     const long long worker = blockIdx.x / static_cast<unsigned>(cluster);
-    const int block_rows = blockDim.y;
-    const long long col = 8ll * (static_cast<long long>(rank) * blockDim.x + threadIdx.x);
-    const int exist = a.N <= col ? 0 : (a.N - col < 8 ? static_cast<int>(a.N - col) : 8);
-    const Dropout drop = dropout_of(a.bar, a.drop_scale, a.seed, a.counter, a.N);
+    const int block_rows = blockDim.y, threads = blockDim.x * blockDim.y;
+    const long long run = 8ll * blockDim.x;                                // columns between a thread's runs
+    const long long col0 = static_cast<long long>(rank) * kRuns * run + 8ll * threadIdx.x;
+    int exist[kRuns];
+#pragma unroll
+    for (int c = 0; c < kRuns; ++c) {
+        const long long left = a.N - col0 - c * run;
+        exist[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
+    }
+    const Dropout drop(a.mask, a.N);
     const float inv_n = __fdiv_rn(1.0f, static_cast<float>(a.N));
     const bool gate_sum = a.dgate && a.gate_rows > 1, gate_each = a.dgate && a.gate_rows == 1;
-    uint64_t pre_w[4] = {}, pre_b[4] = {}, post_w[4] = {}, post_b[4] = {}, gate_s[4] = {};      // sums
+    // (vectors that no sum is kept of share the last place)
+    int places = 0;
+    const auto vector = [&](bool there) {
+        const ColumnSums s = {sums_smem + static_cast<long long>(places) * (kGradCols / 4) * threads + threadIdx.y * blockDim.x + threadIdx.x, threads};
+        if (there) {
+            s.clear();
+            ++places;
+        }
+        return s;
+    };
+    const ColumnSums pre_w = vector(kPre), pre_b = vector(kPre && kMean), post_w = vector(kPost), post_b = vector(kPost && kMean), gate_s = vector(gate_sum);
 
     struct Row {
-        Eight<kType> dy, dh, y, z;
+        Eight<kType> dy[kRuns], dh[kRuns], y[kRuns];
         float4 st;
-        int count;
+        bool here;
     };
-    const auto at = [&](const void* p, long long row, long long ld) { return static_cast<const char*>(p) + (row * ld + col) * kSize; };
+    const auto at = [&](const void* p, long long row, long long ld) { return static_cast<const char*>(p) + (row * ld + col0) * kSize; };
     const auto load = [&](Row& r, long long base, long long end) {
         const long long row = base + threadIdx.y;
-        const bool here = row < end;
-        r.count = here ? exist : 0;
-        if (a.dY) r.dy.load(at(a.dY, row, a.lddy), 0, r.count, wide);
-        else r.dy.clear();
-        if (kPre) {
-            r.dh.load(at(a.dH, row, a.lddh), 0, r.count, wide);
-            r.y.load(at(a.Y, row, a.ldy), 0, r.count, wide);
+        r.here = row < end;
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            const int count = r.here ? exist[c] : 0;
+            if (a.dY) r.dy[c].load(at(a.dY, row, a.lddy), c * run, count, wide);
+            else r.dy[c].clear();
+            if (kPre) {
+                r.dh[c].load(at(a.dH, row, a.lddh), c * run, count, wide);
+                r.y[c].load(at(a.Y, row, a.ldy), c * run, count, wide);
+            }
         }
-        if (kPost || a.Z) r.z.load(at(a.Z, row, a.ldz), 0, r.count, wide);
-        else r.z.clear();
         r.st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if ((kPre || kPost) && here) {
+        if ((kPre || kPost) && r.here) {
             const float* s = a.stats + 4 * row;
             r.st = make_float4(s[0], s[1], s[2], s[3]);
         }
     };
-    Eight<kType> gate;
-    uint32_t gate_row = ~0u;
     int slot = 0;
     // (x - mean) * rstd; columns that lie behind the last one are not added up: they are 0
     const auto normalized = [&](uint64_t (&v)[4], float mean, float rstd, int count) {
@@ -124,119 +164,142 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
         for (int j = 0; j < 4; ++j) v[j] = mul_f2(kMean ? add_f2(v[j], pack_f2(-mean, -mean)) : v[j], pack_f2(rstd, rstd));
         if (kMean || !kWide) clear_behind(v, count);
     };
-    // sums over the row of g and g hat, and what a norm passes on: rstd (g - mean(g) - hat mean(g hat))
-    const auto through = [&](uint64_t (&g)[4], const uint64_t (&hat)[4], int kind, float rstd, const auto& take) {
+    // what a norm passes on, but for rstd: g - mean(g) - hat mean(g hat)
+    const auto through = [&](uint64_t (&g)[kRuns][4], const uint64_t (&hat)[kRuns][4], int kind) {
         uint64_t s = 0ull, u = 0ull;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (kMean) s = add_f2(s, g[j]);
-            u = fma_f2(g[j], hat[j], u);
-        }
-        const float2 e = exchange<kMean>(make_float2(kMean ? sum_pair(s) : 0.0f, sum_pair(u)), ex, slot ^= 1, cluster, rank);
+        for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (kMean) s = add_f2(s, g[c][j]);
+                u = fma_f2(g[c][j], hat[c][j], u);
+            }
+        slot ^= 1;
+        const float2 e = exchange<kMean>(make_float2(kMean ? sum_pair(s) : 0.0f, sum_pair(u)), share[slot], cluster, rank);
         const float mean = kMean && kind == kNormLayer ? -e.x * inv_n : 0.0f, slope = -e.y * inv_n;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) take(j, fma_f2(hat[j], pack_f2(slope, slope), kMean ? add_f2(g[j], pack_f2(mean, mean)) : g[j]), pack_f2(rstd, rstd));
+        for (int c = 0; c < kRuns; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (kMean) g[c][j] = add_f2(g[c][j], pack_f2(mean, mean));
+                g[c][j] = fma_f2(hat[c][j], pack_f2(slope, slope), g[c][j]);
+            }
     };
+    const int gate_kind = a.gate_rows >= a.M ? 0 : (a.gate_rows == 1 ? 1 : 2);       // one row for all, one each, some share one
     const auto process = [&](const Row& r, long long base) {
         const long long row = base + threadIdx.y;
-        if (a.gate && r.count) {                             // (read again where the row has another gate row than the last one)
-            const uint32_t i = a.gate_rows == 1 ? static_cast<uint32_t>(row)
-                               : (a.gate_rows >= a.M ? 0u : static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows));
-            if (i != gate_row) gate.load(a.gate, i * a.ldgate + col, exist, wide);
-            gate_row = i;
+        int count[kRuns];
+        Eight<kType> z[kRuns], gate[kRuns];
+        uint32_t gate_row = gate_kind == 0 || !r.here ? 0u : static_cast<uint32_t>(row);
+        if (gate_kind == 2) gate_row /= static_cast<uint32_t>(a.gate_rows);
+        uint64_t g[kRuns][4], t[kRuns][4], hat[kRuns][4], w[4];
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            count[c] = r.here ? exist[c] : 0;
+            if (kPost || a.Z) z[c].load(at(a.Z, row, a.ldz), c * run, count[c], wide);
+            else z[c].clear();
+            if (a.gate) gate[c].load(a.gate, gate_row * a.ldgate + col0 + c * run, count[c], wide);
         }
-        uint64_t g[4], t[4], w[4];
-        r.dy.pairs(g);
+        // (drawn here, where the instructions fill the gaps of the first exchange)
+        uint4 bits[kRuns];
+        if (drop.bar) {
+#pragma unroll
+            for (int c = 0; c < kRuns; ++c) bits[c] = drop.draw(row, col0 + c * run);
+        }
         if (kPre) {
-            uint64_t hat[4];
-            r.dh.pairs(t);
-            r.y.pairs(hat);
-            load_vector_pairs(a.pre_w, col, exist, wide, 1.0f, w);
-            normalized(hat, r.st.z, r.st.w, r.count);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                pre_w[j] = fma_f2(t[j], hat[j], pre_w[j]);
-                if (kMean) pre_b[j] = add_f2(pre_b[j], t[j]);
-                t[j] = mul_f2(t[j], w[j]);
+            for (int c = 0; c < kRuns; ++c) {
+                r.dh[c].pairs(t[c]);
+                r.y[c].pairs(hat[c]);
+                load_vector_pairs(a.pre_w, col0 + c * run, exist[c], wide, 1.0f, w);
+                normalized(hat[c], r.st.z, r.st.w, count[c]);
+                pre_w.add(c, [&](int j, uint64_t s) { return fma_f2(t[c][j], hat[c][j], s); });
+                if (kMean) pre_b.add(c, [&](int j, uint64_t s) { return add_f2(t[c][j], s); });
+#pragma unroll
+                for (int j = 0; j < 4; ++j) t[c][j] = mul_f2(t[c][j], w[j]);
             }
-            through(t, hat, a.pre, r.st.w, [&](int j, uint64_t v, uint64_t rstd) { g[j] = fma_f2(v, rstd, g[j]); });
+            through(t, hat, a.pre);
         }
-        if (a.dX) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = mul_f2(pack_f2(a.x_scale, a.x_scale), g[j]);
-            Eight<kType> e;
-            e.set_pairs(t);
-            e.store(const_cast<char*>(at(a.dX, row, a.lddx)), 0, r.count, wide);
-        }
-        if (drop.bar) drop.apply(drop.draw(row, col), g);
-        uint64_t hat[4];
-        r.z.pairs(hat);
-        if (kPost) {
-            load_vector_pairs(a.post_w, col, exist, wide, 1.0f, w);
-            normalized(hat, r.st.x, r.st.y, r.count);
-        }
-        if (a.gate) {
-            if (a.dgate) {
-                uint64_t b[4];
-                if (kPost && kMean) load_vector_pairs(a.post_b, col, exist, wide, 0.0f, b);
+        for (int c = 0; c < kRuns; ++c) {
+            r.dy[c].pairs(g[c]);
+            if (kPre) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint64_t u = hat[j];
-                    if (kPost) u = kMean ? fma_f2(u, w[j], b[j]) : mul_f2(u, w[j]);
-                    t[j] = mul_f2(g[j], u);
+                for (int j = 0; j < 4; ++j) g[c][j] = fma_f2(t[c][j], pack_f2(r.st.w, r.st.w), g[c][j]);
+            }
+            if (a.dX) {
+                uint64_t x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = mul_f2(pack_f2(a.x_scale, a.x_scale), g[c][j]);
+                Eight<kType> e;
+                e.set_pairs(x);
+                e.store(const_cast<char*>(at(a.dX, row, a.lddx)), c * run, count[c], wide);
+            }
+            if (drop.bar) drop.apply(bits[c], g[c]);
+            z[c].pairs(hat[c]);
+            if (kPost) {
+                load_vector_pairs(a.post_w, col0 + c * run, exist[c], wide, 1.0f, w);
+                normalized(hat[c], r.st.x, r.st.y, count[c]);
+            }
+            if (a.gate) {
+                if (a.dgate) {
+                    uint64_t b[4];
+                    if (kPost && kMean) load_vector_pairs(a.post_b, col0 + c * run, exist[c], wide, 0.0f, b);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint64_t u = hat[c][j];
+                        if (kPost) u = kMean ? fma_f2(u, w[j], b[j]) : mul_f2(u, w[j]);
+                        t[c][j] = mul_f2(g[c][j], u);
+                    }
+                    if (gate_each) {
+                        Eight<kType> e;
+                        e.set_pairs(t[c]);
+                        e.store(a.dgate, row * a.lddgate + col0 + c * run, count[c], wide);
+                    } else {
+                        gate_s.add(c, [&](int j, uint64_t s) { return add_f2(t[c][j], s); });
+                    }
                 }
-                if (gate_each) {
-                    Eight<kType> e;
-                    e.set_pairs(t);
-                    e.store(a.dgate, row * a.lddgate + col, r.count, wide);
-                } else {
+                gate[c].pairs(t[c]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) gate_s[j] = add_f2(gate_s[j], t[j]);
-                }
+                for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], t[c][j]);
             }
-            if (r.count) {
-                gate.pairs(t);
+            if (kPost) {
+                post_w.add(c, [&](int j, uint64_t s) { return fma_f2(g[c][j], hat[c][j], s); });
+                if (kMean) post_b.add(c, [&](int j, uint64_t s) { return add_f2(g[c][j], s); });
 #pragma unroll
-                for (int j = 0; j < 4; ++j) g[j] = mul_f2(g[j], t[j]);
+                for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], w[j]);
             }
         }
-        if (kPost) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                post_w[j] = fma_f2(g[j], hat[j], post_w[j]);
-                if (kMean) post_b[j] = add_f2(post_b[j], g[j]);
-                g[j] = mul_f2(g[j], w[j]);
-            }
-            through(g, hat, a.post, r.st.y, [&](int j, uint64_t v, uint64_t rstd) { g[j] = mul_f2(v, rstd); });
-        }
+        if (kPost) through(g, hat, a.post);
         if (a.dZ) {
-            Eight<kType> e;
-            e.set_pairs(g);
-            e.store(const_cast<char*>(at(a.dZ, row, a.lddz)), 0, r.count, wide);
+#pragma unroll
+            for (int c = 0; c < kRuns; ++c) {
+                if (kPost) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], pack_f2(r.st.y, r.st.y));
+                }
+                Eight<kType> e;
+                e.set_pairs(g[c]);
+                e.store(const_cast<char*>(at(a.dZ, row, a.lddz)), c * run, count[c], wide);
+            }
         }
     };
-    // Adds the block's rows' sums up in the first one's registers.
-    const auto over_block = [&](const uint64_t (&pairs)[4], float (&v)[8]) {
+    // A vector's sums over the block's rows, in the first one's threads: eight columns of run c.
+    const auto over_block = [&](const ColumnSums& s, int c, float (&v)[8]) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) unpack_f2(pairs[j], v[2 * j], v[2 * j + 1]);
-        if (block_rows == 1) return;
-        if (threadIdx.y > 0) {
+        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+        for (int i = 0; i < block_rows; ++i) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) rows_sum[threadIdx.y - 1][8 * threadIdx.x + j] = v[j];
+            for (int h = 0; h < 2; ++h) {
+                const float4 x = s.at[(2 * c + h) * s.pitch + i * static_cast<int>(blockDim.x)];
+                v[4 * h] += x.x; v[4 * h + 1] += x.y; v[4 * h + 2] += x.z; v[4 * h + 3] += x.w;
+            }
         }
-        __syncthreads();
-        if (threadIdx.y == 0) {
-            for (int i = 0; i < block_rows - 1; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] += rows_sum[i][8 * threadIdx.x + j];
-        }
-        __syncthreads();
     };
-    const auto put_sum = [&](const float (&v)[8], float* dst) {
-        if (threadIdx.y != 0) return;
+    const auto put_sum = [&](const float (&v)[8], float* dst, int c) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (j < exist) dst[col + j] = v[j];
+            if (j < exist[c]) dst[col0 + c * run + j] = v[j];
     };
 
     // unit u: part u % parts of gate row u / parts (without a gate's sums: of all rows)
@@ -252,7 +315,7 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
     }
     long long begin, end;
     Row cur;
-    if (worker < a.units) {
+    if (kAhead && worker < a.units) {
         unit_rows(worker, begin, end);
         load(cur, begin, end);
     }
@@ -281,28 +344,38 @@ mip_norm_step_grad_kernel(const StepGradArgs a) {
             load(cur, b1, e1);
         }
         if (gate_sum) {
-            float v[8];
-            over_block(gate_s, v);
-            if (a.parts > 1) {
-                put_sum(v, a.gate_part + u * a.N);
-            } else if (threadIdx.y == 0) {
-                Eight<kType> e;
-                e.set(v);
-                e.store(a.dgate, u * a.lddgate + col, exist, wide);
-            }
+            if (block_rows > 1) __syncthreads();
+            if (threadIdx.y == 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) gate_s[j] = 0ull;
+                for (int c = 0; c < kRuns; ++c) {
+                    float v[8];
+                    over_block(gate_s, c, v);
+                    if (a.parts > 1) {
+                        put_sum(v, a.gate_part + u * a.N, c);
+                    } else {
+                        Eight<kType> e;
+                        e.set(v);
+                        e.store(a.dgate, u * a.lddgate + col0 + c * run, exist[c], wide);
+                    }
+                }
+            }
+            if (block_rows > 1) __syncthreads();
+            gate_s.clear();
         }
     }
     if (a.sums == 0) return;
+    if (block_rows > 1) __syncthreads();
+    if (threadIdx.y != 0) return;
     float* plane = a.sum_part + worker * a.sums * a.N;
-    int place = 0;
-    const auto put = [&](const uint64_t (&pairs)[4], const float* wanted) {
+    const auto put = [&](const ColumnSums& s, const float* wanted) {
         if (!wanted) return;
-        float v[8];
-        over_block(pairs, v);
-        put_sum(v, plane + place * a.N);
-        ++place;
+#pragma unroll
+        for (int c = 0; c < kRuns; ++c) {
+            float v[8];
+            over_block(s, c, v);
+            put_sum(v, plane, c);
+        }
+        plane += a.N;
     };
     if (kPost) {
         put(post_w, a.dpost_w);
@@ -346,12 +419,36 @@ mip_norm_step_sums_kernel(const SumArgs a) {
     else store_element(a.dgate, (job - a.sums) * a.lddgate + col, a.type, s);
 }
 
+// More shared memory than a kernel has without asking is asked for once per kernel and device, at its first launch there (which
+// loads it: that does not belong to a graph being captured).
+constexpr int kMostSums = 5 * kGradCols * 4 * kGradThreads;
+template <typename Kernel>
+cudaError_t grad_launch(Kernel kernel, std::atomic<unsigned long long>& asked, const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(asked.load(std::memory_order_acquire) & bit)) {
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        (void)cudaThreadExchangeStreamCaptureMode(&mode);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSums);
+        (void)cudaThreadExchangeStreamCaptureMode(&mode);
+        if (e != cudaSuccess) return e;
+        asked.fetch_or(bit, std::memory_order_release);
+    }
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+template <int kType, bool kPre, bool kPost, bool kMean, bool kWide>
+cudaError_t grad_one(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
+    static std::atomic<unsigned long long> asked{0};
+    return grad_launch(mip_norm_step_grad_kernel<kType, kPre, kPost, kMean, kWide>, asked, a, cfg);
+}
 template <int kType, bool kPre, bool kPost, bool kWide>
 cudaError_t grad_mean(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
     if ((kPre && a.pre == kNormLayer) || (kPost && a.post == kNormLayer)) {
-        if constexpr (kPre || kPost) return cudaLaunchKernelEx(&cfg, mip_norm_step_grad_kernel<kType, kPre, kPost, true, kWide>, a);
+        if constexpr (kPre || kPost) return grad_one<kType, kPre, kPost, true, kWide>(a, cfg);
     }
-    return cudaLaunchKernelEx(&cfg, mip_norm_step_grad_kernel<kType, kPre, kPost, false, kWide>, a);
+    return grad_one<kType, kPre, kPost, false, kWide>(a, cfg);
 }
 template <int kType, bool kWide>
 cudaError_t grad_t(const StepGradArgs& a, const cudaLaunchConfig_t& cfg) {
@@ -368,10 +465,16 @@ struct GradShape {
 };
 GradShape grad_shape(long long N) {
     GradShape s;
-    s.cluster = static_cast<int>((N + 8 * kGradThreads - 1) / (8 * kGradThreads));
-    s.threads = static_cast<int>(((N + 8 * s.cluster - 1) / (8 * s.cluster) + 31) / 32 * 32);
-    s.rows = s.threads >= 128 ? 1 : 128 / s.threads;             // (up to kMaxGradRows)
+    s.cluster = static_cast<int>((N + kGradCols * kGradThreads - 1) / (kGradCols * kGradThreads));
+    s.threads = static_cast<int>(((N + kGradCols * s.cluster - 1) / (kGradCols * s.cluster) + 31) / 32 * 32);
+    s.rows = s.threads >= kBlockThreads ? 1 : kBlockThreads / s.threads;
     return s;
+}
+size_t sums_bytes(const StepGradArgs& a, const GradShape& s) {
+    const bool mean = a.pre == kNormLayer || a.post == kNormLayer;
+    const int per_norm = mean ? 2 : 1;
+    const int vectors = (a.pre != kNormNone ? per_norm : 0) + (a.post != kNormNone ? per_norm : 0) + (a.dgate && a.gate_rows > 1 ? 1 : 0);
+    return static_cast<size_t>(vectors) * kGradCols * 4 * s.threads * s.rows;
 }
 
 }  // namespace
@@ -380,7 +483,7 @@ GradShape grad_shape(long long N) {
 size_t plan_norm_step_grad(StepGradArgs& a, int sm_count) {
     const GradShape s = grad_shape(a.N);
     a.cluster = s.cluster;
-    // (512 threads of up to 128 registers fill an SM)
+    // (512 threads of up to 128 registers fill an SM, and their sums' shared memory: 160 KB at most)
     const long long resident = std::max<long long>(1, static_cast<long long>(sm_count) * (kGradThreads / (s.threads * s.rows)) / s.cluster);
     const bool gate_sum = a.dgate && a.gate_rows > 1;
     const long long group_rows = gate_sum ? std::min(a.gate_rows, a.M) : a.M;
@@ -405,6 +508,7 @@ cudaError_t launch_norm_step_grad(int type, StepGradArgs a, void* scratch, cudaS
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(static_cast<unsigned>(a.workers * s.cluster));
         cfg.blockDim = dim3(static_cast<unsigned>(s.threads), static_cast<unsigned>(s.rows));
+        cfg.dynamicSmemBytes = sums_bytes(a, s);
         cfg.stream = stream;
         cudaLaunchAttribute attr[2];
         attr[0].id = cudaLaunchAttributeClusterDimension;

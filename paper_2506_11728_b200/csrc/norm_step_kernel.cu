@@ -117,15 +117,17 @@ __device__ __forceinline__ void store_codes8(uint8_t* dst, uint2 q, int count, b
     }
 }
 
-// kRuns runs of eight columns a thread, up to kThreads threads a block; kAhead: the block goes on from row to row.
-template <int kType, int kRuns, int kThreads, bool kAhead, bool kWide>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 2 : 1)
-mip_norm_step_kernel(const StepArgs a) {
+// kRuns runs of eight columns a thread, up to kThreads threads a block; kAhead: a row's elements are asked for while the one before
+// is worked on, and the norms' weights are kept.  kNorms: there may be norms; without them registers are few, and many blocks
+// on an SM do what reading ahead does.
+template <int kType, int kRuns, int kThreads, bool kAhead, bool kWide, bool kNorms>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (kNorms ? 2 : 4) : 1)
+mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
     __shared__ Exchange<kThreads> ex;
     pdl_wait();
     pdl_launch_dependents();
     constexpr bool wide = kWide;
-    const Dropout drop = dropout_of(a.bar, a.drop_scale, a.seed, a.counter, a.N);
+    const Dropout drop(a.mask, a.N);
     const float inv_n = __fdiv_rn(1.0f, static_cast<float>(a.N));
     int slot = 0;
     long long col[kRuns];
@@ -133,7 +135,7 @@ mip_norm_step_kernel(const StepArgs a) {
     uint64_t post_w[kRuns][4], pre_w[kRuns][4];
 #pragma unroll
     for (int c = 0; c < kRuns; ++c) {
-        col[c] = 8ll * (static_cast<long long>(c) * blockDim.x + threadIdx.x);
+        col[c] = 8ll * ((static_cast<long long>(blockIdx.y) * kRuns + c) * blockDim.x + threadIdx.x);
         const long long left = a.N - col[c];
         exist[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
         if (kAhead) {
@@ -142,7 +144,7 @@ mip_norm_step_kernel(const StepArgs a) {
         }
     }
     struct Row {
-        Eight<kType> x[kRuns], z[kRuns];
+        Eight<kType> x[kRuns], z[kRuns], g[kRuns];
     };
     constexpr int kSize = kType == kF32 ? 4 : 2;
     const long long run = 8ll * blockDim.x;              // columns between a thread's runs
@@ -154,7 +156,11 @@ mip_norm_step_kernel(const StepArgs a) {
     char* y_at = static_cast<char*>(a.Y) + (first * a.ldy + col[0]) * kSize;
     char* h_at = static_cast<char*>(a.H) + (first * a.ldh + col[0]) * kSize;
     const long long z_step = step * a.ldz * kSize, x_step = step * a.ldx * kSize, y_step = step * a.ldy * kSize, h_step = step * a.ldh * kSize;
-    const auto load = [&](Row& r, bool here) {
+    const int gate_kind = a.gate_rows >= a.M ? 0 : (a.gate_rows == 1 ? 1 : 2);       // one row for all, one each, some share one
+    const auto load = [&](Row& r, long long row) {
+        const bool here = row < a.M;
+        uint32_t gate_row = gate_kind == 0 || !here ? 0u : static_cast<uint32_t>(row);
+        if (gate_kind == 2) gate_row /= static_cast<uint32_t>(a.gate_rows);
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
             const int count = here ? exist[c] : 0;
@@ -162,14 +168,13 @@ mip_norm_step_kernel(const StepArgs a) {
             else r.z[c].clear();
             if (a.X) r.x[c].load(x_at, c * run, count, wide);
             else r.x[c].clear();
+            if (a.gate) r.g[c].load(a.gate, gate_row * a.ldgate + col[c], count, wide);
         }
         z_at += z_step;
         x_at += x_step;
     };
     Row cur;
-    load(cur, first < a.M);
-    Eight<kType> g[kRuns];
-    uint32_t gate_row = ~0u;
+    load(cur, first);
     for (long long row = first; row - threadIdx.y < a.M; row += step, y_at += y_step, h_at += h_step) {
         const bool here = row < a.M;
         int count[kRuns];
@@ -179,19 +184,10 @@ mip_norm_step_kernel(const StepArgs a) {
             count[c] = here ? exist[c] : 0;
             cur.z[c].pairs(v[c]);
         }
-        if (a.gate && here) {                            // (read again where the row has another gate row than the last one)
-            const uint32_t i = a.gate_rows == 1 ? static_cast<uint32_t>(row)
-                               : (a.gate_rows >= a.M ? 0u : static_cast<uint32_t>(row) / static_cast<uint32_t>(a.gate_rows));
-            if (i != gate_row) {
-#pragma unroll
-                for (int c = 0; c < kRuns; ++c) g[c].load(a.gate, i * a.ldgate + col[c], exist[c], wide);
-                gate_row = i;
-            }
-        }
         Row next;
-        if (kAhead) load(next, row + step < a.M);
+        if (kAhead) load(next, row + step);
         float2 post = make_float2(0.0f, 0.0f), pre = post;
-        if (a.post != kNormNone) {
+        if (kNorms && a.post != kNormNone) {
             post = normalize<kRuns>(a.post, v, count, inv_n, a.eps, ex, slot);
             affine<kRuns>(v, post_w, kAhead, a.post_w, a.post_b, col, exist, wide);
         }
@@ -199,7 +195,7 @@ mip_norm_step_kernel(const StepArgs a) {
         for (int c = 0; c < kRuns; ++c) {
             uint64_t t[4];
             if (a.gate) {
-                g[c].pairs(t);
+                cur.g[c].pairs(t);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[c][j] = mul_f2(v[c][j], t[j]);
             }
@@ -215,7 +211,7 @@ mip_norm_step_kernel(const StepArgs a) {
                 y.store(y_at, c * run, count[c], wide);
             }
         }
-        if (a.pre != kNormNone) {
+        if (kNorms && a.pre != kNormNone) {
             pre = normalize<kRuns>(a.pre, v, count, inv_n, a.eps, ex, slot);
             affine<kRuns>(v, pre_w, kAhead, a.pre_w, a.pre_b, col, exist, wide);
             if (a.H) {
@@ -272,39 +268,48 @@ mip_norm_step_kernel(const StepArgs a) {
                 }
             }
         }
-        if (a.stats && here && threadIdx.x == 0) {
+        if (a.stats && here && threadIdx.x == 0 && blockIdx.y == 0) {
             float* s = a.stats + 4 * row;
             s[0] = post.x; s[1] = post.y; s[2] = pre.x; s[3] = pre.y;
         }
         if (kAhead) cur = next;
+        else if (row - threadIdx.y + step < a.M) load(cur, row + step);
     }
 }
 
 struct StepShape {
     int runs, threads, rows, blocks;     // blocks: 0, one for each `rows` rows; else they go on from row to row
+    int parts;                           // of a row, each a block's
+    bool apart;                          // without norms
 };
-// 16 columns a thread where there are rows enough to go on with; else eight, and more threads on a row.
-StepShape step_shape(long long M, long long N, int sm_count) {
+// 16 columns a thread where there are rows enough to go on with; else eight, and more threads on a row.  Without norms nothing
+// holds a row together: blocks take 4096 columns of it.
+StepShape step_shape(const StepArgs& a, int sm_count) {
     StepShape s;
-    const bool many = M >= 4ll * sm_count && N <= 8192;
-    s.runs = many ? 2 : (N <= 4096 ? 1 : (N <= 8192 ? 2 : 4));
+    const long long M = a.M;
+    const bool apart = s.apart = a.post == kNormNone && a.pre == kNormNone;
+    s.parts = apart ? static_cast<int>((a.N + 4095) / 4096) : 1;
+    const long long N = apart ? std::min<long long>(a.N, 4096) : a.N;
+    const bool many = M * s.parts >= 4ll * sm_count && N <= 8192;
+    s.runs = many || apart ? 2 : (N <= 4096 ? 1 : (N <= 8192 ? 2 : 4));
     const long long per = 8ll * s.runs;
     s.threads = static_cast<int>(((N + per - 1) / per + 31) / 32 * 32);
-    s.rows = std::max(1, std::min(kMaxBlockRows, (many ? 256 : 128) / s.threads));
-    s.blocks = many ? sm_count * (s.threads > 256 ? 1 : 2) : 0;
+    s.rows = std::max(1, std::min(kMaxBlockRows, (many || apart ? 256 : 128) / s.threads));
+    s.blocks = many ? std::max(1, sm_count * (apart ? 8 : (s.threads > 256 ? 1 : 2)) / s.parts) : 0;
     return s;
 }
 
 template <int kType, bool kWide>
 cudaError_t step_t(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
+    if (s.apart) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, false, kWide, false>, a);
     if (s.blocks) {
-        if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true, kWide>, a);
-        return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true, kWide>, a);
+        if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true, kWide, true>, a);
+        return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true, kWide, true>, a);
     }
-    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false, kWide>, a);
-    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false, kWide>, a);
-    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false, kWide>, a);
-    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false, kWide>, a);
+    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false, kWide, true>, a);
+    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false, kWide, true>, a);
+    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false, kWide, true>, a);
+    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false, kWide, true>, a);
 }
 template <int kType>
 cudaError_t step_wide(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
@@ -313,18 +318,23 @@ cudaError_t step_wide(const StepArgs& a, const StepShape& s, const cudaLaunchCon
 
 }  // namespace
 
+void step_mask(StepMask& m, unsigned long long seed, const unsigned long long* counter) {
+    philox_keys(seed, m.keys);
+    m.counter = counter;
+}
+
 cudaError_t launch_norm_step(int type, const StepArgs& a, int sm_count, cudaStream_t stream) {
-    const StepShape s = step_shape(a.M, a.N, sm_count);
+    const StepShape s = step_shape(a, sm_count);
     cudaLaunchConfig_t cfg = {};
     const long long blocks = (a.M + s.rows - 1) / s.rows;
-    cfg.gridDim = dim3(static_cast<unsigned>(s.blocks ? std::min<long long>(s.blocks, blocks) : blocks));
+    cfg.gridDim = dim3(static_cast<unsigned>(s.blocks ? std::min<long long>(s.blocks, blocks) : blocks), static_cast<unsigned>(s.parts));
     cfg.blockDim = dim3(static_cast<unsigned>(s.threads), static_cast<unsigned>(s.rows));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = pdl_allowed();
     cfg.attrs = attr;
-    cfg.numAttrs = cfg.gridDim.x <= 128 ? 1 : 0;                   // (launched early only where the blocks are few, like the row kernels)
+    cfg.numAttrs = cfg.gridDim.x * cfg.gridDim.y <= 128 ? 1 : 0;                   // (launched early only where the blocks are few, like the row kernels)
     if (type == kF32) return step_wide<kF32>(a, s, cfg);
     return type == kF16 ? step_wide<kF16>(a, s, cfg) : step_wide<kBF16>(a, s, cfg);
 }

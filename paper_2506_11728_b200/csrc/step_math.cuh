@@ -12,16 +12,22 @@ constexpr int kNormNone = 0, kNormRms = 1, kNormLayer = 2;
 constexpr int kCodesNone = 0, kCodesS8 = 1, kCodesE4M3 = 2, kCodesE5M2 = 3;
 
 // Philox4x32-10 (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011): four words of 32 bits
-// from a counter of 128 and a key of 64.
-__device__ __forceinline__ uint4 philox10(uint4 c, uint2 k) {
+// from a counter of 128 and a key of 64.  The rounds' keys -- the key, raised by two constants from round to round -- come
+// worked out, as kernel arguments: an exclusive-or takes them from there.
+constexpr int kPhiloxRounds = 10;
+inline void philox_keys(unsigned long long seed, uint32_t (&keys)[2 * kPhiloxRounds]) {
+    for (int r = 0; r < kPhiloxRounds; ++r) {
+        keys[2 * r] = static_cast<uint32_t>(seed) + static_cast<uint32_t>(r) * 0x9E3779B9u;
+        keys[2 * r + 1] = static_cast<uint32_t>(seed >> 32) + static_cast<uint32_t>(r) * 0xBB67AE85u;
+    }
+}
+__device__ __forceinline__ uint4 philox(uint4 c, const uint32_t (&keys)[2 * kPhiloxRounds]) {
 #pragma unroll
-    for (int r = 0; r < 10; ++r) {
+    for (int r = 0; r < kPhiloxRounds; ++r) {
         // (one wide multiplication instead of two halves)
         const uint64_t p0 = static_cast<uint64_t>(0xD2511F53u) * c.x, p1 = static_cast<uint64_t>(0xCD9E8D57u) * c.z;
-        c = make_uint4(static_cast<uint32_t>(p1 >> 32) ^ c.y ^ k.x, static_cast<uint32_t>(p1), static_cast<uint32_t>(p0 >> 32) ^ c.w ^ k.y,
-                       static_cast<uint32_t>(p0));
-        k.x += 0x9E3779B9u;
-        k.y += 0xBB67AE85u;
+        c = make_uint4(static_cast<uint32_t>(p1 >> 32) ^ c.y ^ keys[2 * r], static_cast<uint32_t>(p1),
+                       static_cast<uint32_t>(p0 >> 32) ^ c.w ^ keys[2 * r + 1], static_cast<uint32_t>(p0));
     }
     return c;
 }
@@ -29,14 +35,15 @@ __device__ __forceinline__ uint4 philox10(uint4 c, uint2 k) {
 // The mask of eight neighbouring columns: one draw, 16 bits for each.  An element becomes itself times `scale` where its bits
 // are the bar or more, 0 (whatever it is) where they are below.
 struct Dropout {
+    const StepMask& m;                   // (kernel arguments)
     uint32_t bar;                        // shifted up by 16 bits; 0: nothing is dropped
-    float scale;                         // 65536 / (65536 - bar)
-    uint2 key;
     unsigned long long step;             // the caller's counter
     unsigned long long groups;           // of eight columns in a row
+    __device__ __forceinline__ Dropout(const StepMask& mask, long long N)
+        : m(mask), bar(mask.bar << 16), step(mask.bar && mask.counter ? *mask.counter : 0ull), groups((static_cast<unsigned long long>(N) + 7) / 8) {}
     __device__ __forceinline__ uint4 draw(long long row, long long col) const {
         const unsigned long long g = static_cast<unsigned long long>(row) * groups + (static_cast<unsigned long long>(col) >> 3);
-        return philox10(make_uint4(static_cast<uint32_t>(g), static_cast<uint32_t>(g >> 32), static_cast<uint32_t>(step), static_cast<uint32_t>(step >> 32)), key);
+        return philox(make_uint4(static_cast<uint32_t>(g), static_cast<uint32_t>(g >> 32), static_cast<uint32_t>(step), static_cast<uint32_t>(step >> 32)), m.keys);
     }
     // (the high half of a word is compared with the low half still behind it: that changes nothing)
     __device__ __forceinline__ void apply(const uint4& bits, uint64_t (&v)[4]) const {
@@ -44,16 +51,11 @@ struct Dropout {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float lo, hi;
-            unpack_f2(mul_f2(v[j], pack_f2(scale, scale)), lo, hi);
+            unpack_f2(mul_f2(v[j], pack_f2(m.scale, m.scale)), lo, hi);
             v[j] = pack_f2(w[j] << 16 >= bar ? lo : 0.0f, w[j] >= bar ? hi : 0.0f);
         }
     }
 };
-__device__ __forceinline__ Dropout dropout_of(uint32_t bar, float scale, unsigned long long seed, const unsigned long long* counter, long long N) {
-    return Dropout{bar << 16, scale, make_uint2(static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)), bar && counter ? *counter : 0ull,
-                   (static_cast<unsigned long long>(N) + 7) / 8};
-}
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
