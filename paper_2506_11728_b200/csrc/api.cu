@@ -223,7 +223,7 @@ int get_device(DeviceState** out) {
 // Kernels of the layer operators, set up on a device when one of the family is first launched there: setting an attribute
 // loads the kernel, and loading these with the plain products' made the first call of a program that never uses them
 // 8 to 20 ms longer (9 ms without them).
-constexpr int kFamilyLayer = 1, kFamilyFew = 2, kFamilyProduct = 4, kFamilyF8 = 8;
+constexpr int kFamilyLayer = 1, kFamilyFew = 2, kFamilyProduct = 4, kFamilyF8 = 8, kFamilyF8Few = 16;
 int family_ready(DeviceState* dev, int family) {
     if (dev->families.load(std::memory_order_acquire) & family) return MIPGEMM_OK;
     std::lock_guard<std::mutex> lock(g_mutex);
@@ -232,14 +232,15 @@ int family_ready(DeviceState* dev, int family) {
     cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
     (void)cudaThreadExchangeStreamCaptureMode(&mode);
     const cudaError_t e = family == kFamilyLayer ? layer_init()
-                          : (family == kFamilyFew ? stream_init() : (family == kFamilyProduct ? product_init() : f8_product_init()));
+                          : (family == kFamilyFew ? stream_init() : (family == kFamilyProduct ? product_init() : (family == kFamilyF8 ? f8_product_init() : f8_stream_init())));
     (void)cudaThreadExchangeStreamCaptureMode(&mode);
     if (e != cudaSuccess) return cuda_fail(e);
     dev->families.fetch_or(family, std::memory_order_release);
     if (log_enabled())
         std::fprintf(stderr, "mipgemm: set up %s kernels\n",
                      family == kFamilyLayer ? "dense layer"
-                     : (family == kFamilyFew ? "few-token layer" : (family == kFamilyProduct ? "product" : "8-bit floating-point product")));
+                     : (family == kFamilyFew ? "few-token layer" : (family == kFamilyProduct ? "product"
+                                                                       : (family == kFamilyF8 ? "8-bit floating-point product" : "few-token 8-bit floating-point product"))));
     return MIPGEMM_OK;
 }
 

@@ -49,12 +49,28 @@ int f8_dequantize_impl(int type, int format, int blocks, int64_t M, int64_t N, c
 
 struct F8Plan {
     int pair, grid, split;
+    int few;                             // 1: the few-token kernel
 };
+
+// Few tokens: as plan_stream of the 8-bit layer, K is split over the CTAs of a cluster while that leaves all CTAs resident at
+// once (two per SM), each CTA at least two k-blocks, and either a quarter of the SMs would go without or each still gets eight.
+F8Plan plan_f8_stream(const mip::F8ProductArgs& a, const DeviceState* dev) {
+    const long long tiles = (a.N + 127) / 128, k_blocks = f8_blocks(a.K);
+    F8Plan pl{0, 0, 1, 1};
+    while (pl.split < 8 && 2 * pl.split * tiles <= 2ll * dev->sm_count && k_blocks / (2 * pl.split) >= 2 &&
+           (4 * tiles * pl.split < 3 * dev->sm_count || k_blocks / (2 * pl.split) >= 8))
+        pl.split *= 2;
+    const Tuning tun = tuning_now();
+    if (tun.split_k == 1 || tun.split_k == 2 || tun.split_k == 4 || tun.split_k == 8) pl.split = tun.split_k;
+    pl.grid = static_cast<int>(tiles) * pl.split;
+    return pl;
+}
+int few_columns(long long M) { return M <= 16 ? 16 : (M <= 32 ? 32 : 64); }
 
 F8Plan plan_f8(const mip::F8ProductArgs& a, const DeviceState* dev) {
     const Tuning tun = tuning_now();
     const int k_blocks = static_cast<int>(f8_blocks(a.K));
-    F8Plan best{0, 1, 1};
+    F8Plan best{0, 1, 1, 0};
     double best_clk = 1e30;
     for (int pair = 0; pair <= 1; ++pair) {
         if (pair && dev->pair_clusters <= 0) continue;
@@ -73,7 +89,7 @@ F8Plan plan_f8(const mip::F8ProductArgs& a, const DeviceState* dev) {
             if (tun.split_k && split != tun.split_k) clk += kNotAsked;
             if (clk < best_clk) {
                 best_clk = clk;
-                best = F8Plan{pair, static_cast<int>(std::min(tiles * split, slots)) * (pair ? 2 : 1), split};
+                best = F8Plan{pair, static_cast<int>(std::min(tiles * split, slots)) * (pair ? 2 : 1), split, 0};
             }
         }
     }
@@ -120,36 +136,54 @@ int run_f8_product(const mip::F8ProductArgs& a, DeviceState* dev, cudaStream_t s
     if (!hit) {
         const Tuning tun = tuning_now();
         pl = plan_f8(a, dev);
+        const int k_blocks = static_cast<int>(f8_blocks(a.K));
+        int few_stages = 0;
+        if (a.M <= 64 && !a.a_order && tun.force_path != MIPGEMM_PATH_DENSE && tun.force_path != MIPGEMM_PATH_DENSE_PAIR) {
+            const F8Plan few = plan_f8_stream(a, dev);
+            few_stages = mip::f8_stream_stages(few_columns(a.M), (k_blocks + few.split - 1) / few.split);
+            if (few_stages) pl = few;
+        }
         std::memset(&p, 0, sizeof(p));
-        const int side = pl.pair ? 256 : 128;
         p.M = static_cast<int>(a.M);
         p.N = static_cast<int>(a.N);
         p.K = static_cast<int>(a.K);
         p.type = a.type;
-        p.k_blocks = static_cast<int>(f8_blocks(a.K));
-        p.block_n = p.out_n = side;
-        p.tiles_m = static_cast<int>((a.M + side - 1) / side);
-        p.tiles_n = static_cast<int>((a.N + side - 1) / side);
+        p.k_blocks = k_blocks;
         p.split = pl.split;
-        p.kb_share = (p.k_blocks + pl.split - 1) / pl.split;
-        p.plane_rows = static_cast<int>(round_up(a.M, 32));
-        p.stages = mip::f8_product_stages(a.type, pl.pair != 0, a.b_vec != 0, pl.split > 1);
-        if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
+        p.kb_share = (k_blocks + pl.split - 1) / pl.split;
         p.a_mn = a.a_order;
         p.b_mn = a.b_order;
-        p.a_rows = a.a_order ? mip::kBlockM : std::min(p.M, mip::kBlockM);
-        // D float32, the operands' formats, which of them are M/N-contiguous, 128 columns, the tile's rows
-        p.idesc = (1u << 4) | (static_cast<uint32_t>(a.a_format) << 7) | (static_cast<uint32_t>(a.b_format) << 10) | (static_cast<uint32_t>(a.a_order) << 15) |
-                  (static_cast<uint32_t>(a.b_order) << 16) | (128u >> 3 << 17) | (static_cast<uint32_t>(side >> 4) << 24);
         p.status = dev->status_word;
-        const size_t size = type_size(a.type);
-        p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;
-        p.c_tma = a.N * size % 16 == 0 && aligned16(a.C, a.ldc * static_cast<long long>(size)) ? 1 : 0;
-        int st = a.a_order ? encode_tiled_2d(&p.tmap_a, a.A, a.M, a.K, a.lda, 128, 128) : encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, p.a_rows);
+        int st;
+        if (pl.few) {
+            p.block_n = few_columns(a.M);
+            p.out_n = 128;
+            p.stages = few_stages;
+            // D float32; the weights are the 128-row operand, the tokens the columns
+            p.idesc = (1u << 4) | (static_cast<uint32_t>(a.b_format) << 7) | (static_cast<uint32_t>(a.a_format) << 10) |
+                      (static_cast<uint32_t>(a.b_order) << 15) | (static_cast<uint32_t>(p.block_n >> 3) << 17) | (128u >> 4 << 24);
+            st = encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, p.M);
+        } else {
+            const int side = pl.pair ? 256 : 128;
+            p.block_n = p.out_n = side;
+            p.tiles_m = static_cast<int>((a.M + side - 1) / side);
+            p.tiles_n = static_cast<int>((a.N + side - 1) / side);
+            p.plane_rows = static_cast<int>(round_up(a.M, 32));
+            p.stages = mip::f8_product_stages(a.type, pl.pair != 0, a.b_vec != 0, pl.split > 1);
+            if (tun.stages) p.stages = std::min(p.stages, std::max(tun.stages, 2));
+            p.a_rows = a.a_order ? mip::kBlockM : std::min(p.M, mip::kBlockM);
+            // D float32, the operands' formats, which of them are M/N-contiguous, 128 columns, the tile's rows
+            p.idesc = (1u << 4) | (static_cast<uint32_t>(a.a_format) << 7) | (static_cast<uint32_t>(a.b_format) << 10) | (static_cast<uint32_t>(a.a_order) << 15) |
+                      (static_cast<uint32_t>(a.b_order) << 16) | (128u >> 3 << 17) | (static_cast<uint32_t>(side >> 4) << 24);
+            const size_t size = type_size(a.type);
+            p.r_tma = a.R && aligned16(a.R, a.ldr * static_cast<long long>(size)) ? 1 : 0;
+            p.c_tma = a.N * size % 16 == 0 && aligned16(a.C, a.ldc * static_cast<long long>(size)) ? 1 : 0;
+            st = a.a_order ? encode_tiled_2d(&p.tmap_a, a.A, a.M, a.K, a.lda, 128, 128) : encode_tiled_2d(&p.tmap_a, a.A, a.K, a.M, a.lda, 128, p.a_rows);
+            if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.R, a.type, a.M, a.N, a.ldr);
+            if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
+        }
         if (st == MIPGEMM_OK)
             st = a.b_order ? encode_tiled_2d(&p.tmap_b0, a.B, a.N, a.K, a.ldb, 128, 128) : encode_tiled_2d(&p.tmap_b0, a.B, a.K, a.N, a.ldb, 128, 128);
-        if (st == MIPGEMM_OK && p.r_tma) st = encode_slots(&p.tmap_r, a.R, a.type, a.M, a.N, a.ldr);
-        if (st == MIPGEMM_OK && p.c_tma) st = encode_slots(&p.tmap_c, a.C, a.type, a.M, a.N, a.ldc);
         if (st != MIPGEMM_OK) return st;
         p.R = a.R; p.ldr = a.ldr;
         p.C = a.C; p.ldc = a.ldc;
@@ -175,11 +209,16 @@ int run_f8_product(const mip::F8ProductArgs& a, DeviceState* dev, cudaStream_t s
     p.sb_k = a.b_vec || a.b_order ? a.ldbs : 1;
     p.sb_n = a.b_vec || a.b_order ? 1 : a.ldbs;
     p.bias = a.bias;
-    const int ready = family_ready(dev, kFamilyF8);
+    const int ready = family_ready(dev, pl.few ? kFamilyF8Few : kFamilyF8);
     if (ready != MIPGEMM_OK) return ready;
     cudaError_t e;
     int launches = 1;
-    if (pl.split > 1) {
+    if (pl.few) {
+        // (a promise about the weights, not part of the plan; not about re-pitched copies, which the kernel before this one writes)
+        const size_t b_bytes = static_cast<size_t>(a.b_order ? a.K - 1 : a.N - 1) * a.ldb + (a.b_order ? a.N : a.K);
+        p.b_constant = as_passed && a.M <= 16 && (g_weights_constant.load() || inside_constant_range(a.B, b_bytes));
+        e = mip::launch_f8_stream(p, a.b_vec != 0, pl.grid, stream);
+    } else if (pl.split > 1) {
         mip::PartialPlanes planes{nullptr, pl.split, p.plane_rows, round_up(a.N, 32), 0};
         Scratch scratch(dev, stream);
         const int st = scratch.reserve(static_cast<size_t>(pl.split) * planes.plane_rows * planes.pitch * 4);
@@ -196,10 +235,10 @@ int run_f8_product(const mip::F8ProductArgs& a, DeviceState* dev, cudaStream_t s
     }
     g_launches += launches;
     if (e != cudaSuccess) return cuda_fail(e);
-    tl_last_path = (pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE) | (pl.split > 1 ? MIPGEMM_PATH_SPLITK : 0);
+    tl_last_path = (pl.few ? MIPGEMM_PATH_SKINNY : (pl.pair ? MIPGEMM_PATH_DENSE_PAIR : MIPGEMM_PATH_DENSE)) | (pl.split > 1 ? MIPGEMM_PATH_SPLITK : 0);
     if (log_enabled())
-        std::fprintf(stderr, "mipgemm: f8 product M=%d N=%d K=%d orders=%d%d -> dense %s stages=%d split=%d r_tma=%d c_tma=%d plan=%s\n", p.M, p.N, p.K,
-                     a.a_order, a.b_order, pl.pair ? "cta-pair" : "one-cta", p.stages, pl.split, p.r_tma, p.c_tma, hit ? "cached" : "new");
+        std::fprintf(stderr, "mipgemm: f8 product M=%d N=%d K=%d orders=%d%d -> %s stages=%d split=%d r_tma=%d c_tma=%d plan=%s\n", p.M, p.N, p.K,
+                     a.a_order, a.b_order, pl.few ? "few tokens" : (pl.pair ? "dense cta-pair" : "dense one-cta"), p.stages, pl.split, p.r_tma, p.c_tma, hit ? "cached" : "new");
     return MIPGEMM_OK;
 }
 

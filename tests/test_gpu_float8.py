@@ -132,7 +132,7 @@ KINDS = {  # a_order, b_order, b_blocks
     "forward": (0, 0, "squares"), "forward_rows": (0, 0, "rows"), "input_grad": (0, 1, "squares"), "weight_grad": (1, 1, "columns"),
     "a_columns": (1, 0, "squares"), "a_columns_rows": (1, 0, "rows"), "a_rows_columns": (0, 1, "columns"), "a_columns_squares": (1, 1, "squares"),
 }
-SIZES = [(1, 1, 1), (1, 128, 128), (3, 33, 17), (16, 256, 144), (100, 40, 129), (128, 128, 256), (129, 257, 200), (200, 520, 328),
+SIZES = [(1, 1, 1), (1, 128, 128), (3, 33, 17), (16, 256, 144), (17, 300, 2700), (33, 130, 1200), (64, 200, 5000), (5, 1000, 9000), (100, 40, 129), (128, 128, 256), (129, 257, 200), (200, 520, 328),
          (300, 300, 1000), (64, 1000, 40), (520, 640, 136), (8, 2048, 512), (2000, 24, 96), (40, 48, 0), (256, 264, 4096)]
 
 
@@ -169,7 +169,8 @@ def call(mg, kind, what, M, N, K, r, bias, R, C, a_fmt="e4m3", b_fmt="e4m3", ldr
     assert mg.mipgemm_device_status() == mg.OK
 
 
-FORMS = {"auto": {}, "pair": dict(force_path=2), "single": dict(force_path=1), "split": dict(force_path=1, split_k=3), "pair_split": dict(force_path=2, split_k=2)}
+FORMS = {"auto": {}, "pair": dict(force_path=2), "single": dict(force_path=1), "split": dict(force_path=1, split_k=3), "pair_split": dict(force_path=2, split_k=2),
+         "shares_1": dict(split_k=1), "shares_2": dict(split_k=2), "shares_8": dict(split_k=8)}
 
 
 @pytest.fixture(params=list(FORMS))
@@ -187,6 +188,8 @@ def test_small_integers_are_exact(mg, form, M, N, K, what, layout):
     counted twice or a wrong scale shows."""
     if layout == "padded" and form != "auto":
         pytest.skip("the forms differ in what they do with whole and with odd rows")
+    if form.startswith("shares") and M > 64:
+        pytest.skip("the few-token kernel's shares of K")
     rng, a, b, r = operands(M, N, K, what, layout, small=True)
     pad, shift = LAYOUTS[layout]
     C = u.Matrix(M, N, "f32", N + pad, shift)
@@ -297,6 +300,29 @@ def test_codes_and_products_make_a_layer_and_its_gradients(mg):
     assert (np.abs(vd - dy) <= 2.0 ** -3 * np.abs(dy) + np.abs(dy).max(axis=1, keepdims=True) * 2.0 ** -17 / 57344 * 1.01).all()
 
 
+@pytest.mark.parametrize("what", ["forward", "input_grad"])
+def test_constant_weights_fetched_early(mg, what):
+    """Under the promise the few-token kernel fetches weights before the kernel in front of it is over; tokens and scales are
+    still read behind it."""
+    import torch
+    M, N, K = 7, 640, 1500
+    rng, a, b, r = operands(M, N, K, what, "padded", 13, small=True)
+    C = [u.Matrix(M, N, "f32") for _ in range(6)]
+    buf = r["B"].buf
+    mg.mipgemm_register_constant_weights(buf)
+    try:
+        ao, bo, bb = KINDS[what]
+        for c in C:
+            r["A"].view.copy_(r["A"].view.clone())                     # (a kernel in front that writes the tokens)
+            mg.mipgemm_f8f8_product(0, 0, 0, ao, bo, mg.F8_BLOCKS[bb], M, N, K, r["A"].ptr, r["A"].ld, r["sa"], r["sa"].shape[1], r["B"].ptr,
+                                    r["B"].ld, r["sb"], r["sb"].shape[1], None, None, 0, c.ptr, N)
+        assert mg.mipgemm_device_status() == mg.OK and mg.mipgemm_last_path() & mg.PATH_MASK == mg.PATH_SKINNY
+    finally:
+        mg.mipgemm_unregister_constant_weights(buf)
+    assert all(np.array_equal(c.get(), a @ b) for c in C)
+    torch.cuda.synchronize()
+
+
 def test_captured_calls_use_their_own_scratch(mg):
     """Two graphs of calls that need scratch (odd pitches, K in shares), replayed on two streams at once."""
     import torch
@@ -327,8 +353,8 @@ def test_captured_calls_use_their_own_scratch(mg):
 def test_waits_that_run_out_are_reported(mg):
     """The signal that a block's products are ready is withheld: the kernel unwinds and says so; the next call is whole."""
     import torch
-    for M, N, path in ((300, 300, 2), (300, 300, 1)):
-        K = 600
+    for M, N, path in ((300, 300, 2), (300, 300, 1), (9, 300, 0)):
+        K = 1200
         rng, a, b, r = operands(M, N, K, "forward", "dense", 12, small=True)
         C = u.Matrix(M, N, "f32")
         mg.mipgemm_set_tuning(force_path=path)
@@ -341,7 +367,7 @@ def test_waits_that_run_out_are_reported(mg):
         finally:
             mg.mipgemm_debug_set()
             torch.cuda.synchronize()
-        mg.mipgemm_set_tuning(force_path=path, stages=3)               # (another plan: the kept one holds the test's limit)
+        mg.mipgemm_set_tuning(force_path=path, stages=3, split_k=1)    # (another plan: the kept one holds the test's limit)
         call(mg, "f32", "forward", M, N, K, r, None, None, C)
         assert np.array_equal(C.get(), a @ b)
         mg.mipgemm_set_tuning()
