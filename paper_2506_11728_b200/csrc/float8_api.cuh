@@ -65,7 +65,10 @@ F8Plan plan_f8_stream(const mip::F8ProductArgs& a, const DeviceState* dev) {
     pl.grid = static_cast<int>(tiles) * pl.split;
     return pl;
 }
-int few_columns(long long M) { return M <= 16 ? 16 : (M <= 32 ? 32 : 64); }
+// Up to so many tokens take it (us here / dense kernel: 16 x 14336 x 4096 11.4 / 15.4, 32 x 11008 x 4096 13.8 / 14.9, and with 64
+// tokens 64 x 4096 x 4096 11.4 / 10.4, 64 x 14336 x 4096 20.1 / 16.0).
+constexpr long long kFewTokens = 32;
+int few_columns(long long M) { return M <= 16 ? 16 : 32; }
 
 F8Plan plan_f8(const mip::F8ProductArgs& a, const DeviceState* dev) {
     const Tuning tun = tuning_now();
@@ -83,8 +86,15 @@ F8Plan plan_f8(const mip::F8ProductArgs& a, const DeviceState* dev) {
             if (split > 1 && (dev->lent || tiles * (split - 1) >= slots || k_blocks / split < 2)) break;
             const int share = (k_blocks + split - 1) / split;
             if ((k_blocks + share - 1) / share != split) continue;
+            // clocks of a k-block (measured: pairs 780, with a scale for each column 1200; single CTAs 480 and 620), but not less than
+            // its copies' latency over the stages on their way, which is longer where few row tiles share the weights (512 x 4096 x
+            // 14336 bf16: 128 single CTAs 61 us, 64 units of pairs with K in two shares 46); of a tile's outputs, which nothing hides
+            const int stages = mip::f8_product_stages(a.type, pair != 0, a.b_vec != 0, split > 1);
+            const double latency = ((a.M + side - 1) / side < 8 ? 3600.0 : 2000.0) / stages;
+            const double block = std::max(pair ? (a.b_vec ? 1200.0 : 780.0) : (a.b_vec ? 620.0 : 480.0), latency);
             const long long waves = (tiles * split + slots - 1) / slots;
-            double clk = static_cast<double>(waves) * (share * (pair ? 620.0 : 360.0) + (pair ? 4000.0 : 2500.0)) + (pair ? 1900.0 : 0.0);
+            double clk = static_cast<double>(waves) * (share * block + (a.type == MIPGEMM_TYPE_F32 ? (pair ? 8000.0 : 5500.0) : (pair ? 5000.0 : 4500.0))) + (pair ? 1900.0 : 0.0);
+            // (a launch, and the planes written and read at the L2's pace)
             if (split > 1) clk += 5500.0 + 8.0 * split * static_cast<double>(a.M) * a.N / 3500.0;
             if (tun.split_k && split != tun.split_k) clk += kNotAsked;
             if (clk < best_clk) {
@@ -138,7 +148,7 @@ int run_f8_product(const mip::F8ProductArgs& a, DeviceState* dev, cudaStream_t s
         pl = plan_f8(a, dev);
         const int k_blocks = static_cast<int>(f8_blocks(a.K));
         int few_stages = 0;
-        if (a.M <= 64 && !a.a_order && tun.force_path != MIPGEMM_PATH_DENSE && tun.force_path != MIPGEMM_PATH_DENSE_PAIR) {
+        if (a.M <= kFewTokens && !a.a_order && tun.force_path != MIPGEMM_PATH_DENSE && tun.force_path != MIPGEMM_PATH_DENSE_PAIR) {
             const F8Plan few = plan_f8_stream(a, dev);
             few_stages = mip::f8_stream_stages(few_columns(a.M), (k_blocks + few.split - 1) / few.split);
             if (few_stages) pl = few;

@@ -306,7 +306,7 @@ int f8_product_stages(int type, bool pair, bool vec, bool raw);
 cudaError_t f8_product_init();               // once per device
 cudaError_t launch_f8_product(const F8ProductParams& p, bool pair, bool vec, bool raw, int grid, cudaStream_t stream);
 // Few-token form: 128 columns of C on the accumulator's lanes, K split over a cluster (p.split), kb_share blocks per CTA;
-// block_n = 16, 32 or 64 tokens, tmap_a's boxes M rows high.
+// block_n = 16 or 32 tokens, tmap_a's boxes M rows high.
 int f8_stream_stages(int tokens, int kb_share);
 cudaError_t f8_stream_init();                // once per device
 cudaError_t launch_f8_stream(const F8ProductParams& p, bool vec, int grid, cudaStream_t stream);
