@@ -585,7 +585,8 @@ int mipgemm_norm_step(int type, int post, int pre, int64_t M, int64_t N, float e
  *   dX, dZ : M x N (written); each may be one of dY, dH, Y and Z (with the same pitch), not both the same
  *   dgate : as gate (written), summed over the rows that share a gate row
  *   dpost_weight, dpost_bias, dpre_weight, dpre_bias : N float32 (written), summed over all rows in binary32
- * M == 0 writes zeros to the four vectors.  Scratch memory: for the sums of the vectors and of dgate.
+ * M == 0 writes zeros to the four vectors.  Scratch memory: at most 8 bytes * N * (vectors wanted + 1) for each SM of the
+ * device, for the sums of the vectors and of dgate.
  */
 int mipgemm_norm_step_grad(int type, int post, int pre, int64_t M, int64_t N,
                            const void *dY, int64_t lddy, const void *dH, int64_t lddh,
@@ -652,7 +653,7 @@ int mipgemm_probe_i8_peak(int iters, int *grid_out, double *ops_per_launch,
 
 /*
  * A promise about the weights of the skinny-M (GEMV-like, paper Section 7.2 batch-1) calls, those of
- * mipgemm_*_linear, _gated and _gated_grad with as few tokens among them, process wide, off by default: with on != 0 the caller guarantees that the B operand of every later call with
+ * mipgemm_*_linear, _gated, _gated_grad and mipgemm_f8f8_product with as few tokens among them, process wide, off by default: with on != 0 the caller guarantees that the B operand of every later call with
  * M <= 16 is not written by any work still pending on the call's stream when it is enqueued (the
  * usual case: B holds inference weights).  The streaming kernel then starts fetching B while the
  * previous kernel on the stream is still draining (programmatic dependent launch); A is read and C is

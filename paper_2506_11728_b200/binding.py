@@ -347,9 +347,13 @@ def mipgemm_norm_step(type, post, pre, M, N, eps=1e-5, X=None, ldx=0, x_scale=1.
                       gate=None, ldgate=0, gate_rows=1, drop=0.0, seed=0, counter=None, pre_weight=None, pre_bias=None, Y=None, ldy=0,
                       H=None, ldh=0, codes=0, Q=None, ldq=0, q_scale=None, ldqs=0, stats=None, stream=None, check=True) -> int:
     """Y = x_scale * X + dropout(gate * post(Z)), H = pre(Y), as values and / or codes."""
-    return _check(_lib.mipgemm_norm_step(type, post, pre, M, N, eps, _ptr(X), ldx, x_scale, _ptr(Z), ldz, _ptr(post_weight), _ptr(post_bias),
-                                         _ptr(gate), ldgate, gate_rows, drop, seed, _ptr(counter), _ptr(pre_weight), _ptr(pre_bias),
-                                         _ptr(Y), ldy, _ptr(H), ldh, codes, _ptr(Q), ldq, _ptr(q_scale), ldqs, _ptr(stats),
+    # (None is passed on as it is: most of the pointers usually are)
+    return _check(_lib.mipgemm_norm_step(type, post, pre, M, N, eps, X if X is None else _ptr(X), ldx, x_scale, Z if Z is None else _ptr(Z), ldz,
+                                         post_weight if post_weight is None else _ptr(post_weight), post_bias if post_bias is None else _ptr(post_bias),
+                                         gate if gate is None else _ptr(gate), ldgate, gate_rows, drop, seed, counter if counter is None else _ptr(counter),
+                                         pre_weight if pre_weight is None else _ptr(pre_weight), pre_bias if pre_bias is None else _ptr(pre_bias),
+                                         Y if Y is None else _ptr(Y), ldy, H if H is None else _ptr(H), ldh, codes, Q if Q is None else _ptr(Q), ldq,
+                                         q_scale if q_scale is None else _ptr(q_scale), ldqs, stats if stats is None else _ptr(stats),
                                          _stream(stream)), check)
 
 

@@ -249,8 +249,12 @@ mip_f8_dequantize_kernel(int blocks, long long M, long long N, const uint8_t* Q,
             for (int j = 0; j < P::kLen; ++j) q[i][j] = r < M && c0 + P::col(j) < N ? src[P::col(j)] : 0u;
         }
     }
-    float by_col[P::kLen];
-    if (blocks == kBlocksColumns) {
+    // (all scales are asked for at once, beside the codes)
+    float by_col[P::kLen], by_row[P::kRuns];
+    if (blocks == kBlocksRows) {
+#pragma unroll
+        for (int i = 0; i < P::kRuns; ++i) by_row[i] = r0 + P::row(i) < M ? __ldg(scale + cb * lds + r0 + P::row(i)) : 0.0f;
+    } else if (blocks == kBlocksColumns) {
 #pragma unroll
         for (int j = 0; j < P::kLen; ++j) by_col[j] = c0 + P::col(j) < N ? __ldg(scale + rb * lds + c0 + P::col(j)) : 0.0f;
     } else if (blocks == kBlocksSquares) {
@@ -263,9 +267,8 @@ mip_f8_dequantize_kernel(int blocks, long long M, long long N, const uint8_t* Q,
         const long long r = r0 + P::row(i);
         if (r >= M) continue;
         if (blocks == kBlocksRows) {
-            const float s = __ldg(scale + cb * lds + r);
 #pragma unroll
-            for (int j = 0; j < P::kLen; ++j) by_col[j] = s;
+            for (int j = 0; j < P::kLen; ++j) by_col[j] = by_row[i];
         }
         if constexpr (kWide) {
             const long long c = c0 + P::col(0);
