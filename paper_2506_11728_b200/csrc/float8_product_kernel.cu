@@ -90,13 +90,13 @@ __device__ __forceinline__ uint64_t words_f2(uint32_t a, uint32_t b) {
 template <bool kPair, bool kVec, bool kWide, bool kRaw>
 __global__ void __launch_bounds__(kF8Threads, 1)
 mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
-    constexpr int kGroup = kPair ? 2 : 1;
+    constexpr int kCtas = kPair ? 2 : 1;
     // The tile's columns by halves (pair): 64 of each CTA's B tile, so that a half's 128 columns are two runs of 64.
     constexpr int kHalves = kPair ? 2 : 1;
     constexpr int kN = 128;                              // accumulator columns of an instruction
     constexpr int kDepth = 4 / kHalves;                  // blocks of products in tensor memory, for each half
     constexpr int kCols = kPair ? 128 : 64;              // columns per thread
-    constexpr int kRowsPerTile = kGroup * kBlockM;
+    constexpr int kRowsPerTile = kCtas * kBlockM;
     constexpr uint32_t a_bytes = kBlockM * 128, b_bytes = 128 * 128, stage_bytes = a_bytes + b_bytes;
     constexpr int kSlot = slot_bytes(kWide), kSlotBuffers = slot_buffers(kWide);
     const uint32_t cta_rank = kPair ? cluster_ctarank() : 0u;
@@ -150,8 +150,8 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         cluster_wait();
     }
     if (warp == 1) {
-        tmem_alloc<kGroup>(smem_u32(tmem_slot), 512);
-        tmem_relinquish<kGroup>();
+        tmem_alloc<kCtas>(smem_u32(tmem_slot), 512);
+        tmem_relinquish<kCtas>();
     }
     tc_fence_before();
     __syncthreads();
@@ -177,7 +177,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
             const bool side_a = warp == 0;
             const int mn = side_a ? p.a_mn : p.b_mn;
             // (fewer than 128 K-contiguous rows of A in all: only those are copied, as in the dense layer kernel)
-            const uint32_t tx_bytes = kGroup * (side_a ? static_cast<uint32_t>(p.a_rows) * 128u : b_bytes);
+            const uint32_t tx_bytes = kCtas * (side_a ? static_cast<uint32_t>(p.a_rows) * 128u : b_bytes);
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
                 const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
                 const int at = side_a ? tc.m0 + static_cast<int>(cta_rank) * kBlockM : tc.n0 + static_cast<int>(cta_rank) * 128;
@@ -222,7 +222,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                         if (elect_one()) {
 #pragma unroll
                             for (uint32_t k = 0; k < 4; ++k)
-                                mma_f8<kGroup>(tmem_base + buf * kN, a_desc + a_step * k, b_desc + b_half * h + b_step * k, idesc, k > 0 ? 1u : 0u);
+                                mma_f8<kCtas>(tmem_base + buf * kN, a_desc + a_step * k, b_desc + b_half * h + b_step * k, idesc, k > 0 ? 1u : 0u);
                             if (signal) commit_all<kPair>(bar_tfull + 8u * buf);
                             if (h == kHalves - 1) commit_all<kPair>(bar_empty + 8u * s);
                         }
@@ -238,7 +238,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
             // (The summing warps go from block to block in the time of two or three hundred instructions: what does not have to be
             // there is here.)  Loads are two blocks ahead.  Rows, columns and blocks behind the last read the last one's: nothing of
             // what they give is stored.
-            constexpr int kB = kVec ? kGroup * 4 : kHalves;
+            constexpr int kB = kVec ? kCtas * 4 : kHalves;
             uint32_t acc = 0, uses = 0, place = 0, tile_no = 0;
             bool ok = true;
             for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
@@ -557,7 +557,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     }
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc<kGroup>(tmem_base, 512);
+        tmem_dealloc<kCtas>(tmem_base, 512);
     }
     if (threadIdx.x == 0 && *abort_flag != 0) atomicOr(p.status, 1u);
 }

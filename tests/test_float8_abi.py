@@ -157,3 +157,13 @@ def test_step_gradient_formulas_against_differences():
                 down[at] -= e
                 d = (loss(dict(c, **{name: up})) - loss(dict(c, **{name: down}))) / (2 * e)
                 assert abs(d - got[grad][at]) < 1e-6 * (1 + abs(d)), (post, pre, name)
+
+
+def test_the_pair_kernel_allocates_behind_its_cluster_barrier():
+    """Read from the source, as for the other pair kernels: the allocation follows the barrier that shows both CTAs running."""
+    import os
+    import re
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2506_11728_b200", "csrc", "float8_product_kernel.cu")
+    text = re.sub(r"//[^\n]*", "", open(path).read())
+    found = re.findall(r"if \(kPair\) \{\s*__syncwarp\(\);\s*cluster_arrive\(\);\s*cluster_wait\(\);\s*\}\s*if \(warp == 1\) \{\s*tmem_alloc<kCtas>", text)
+    assert len(found) == 1 and len(re.findall(r"tmem_alloc<", text)) == 1
