@@ -685,7 +685,8 @@ int mipgemm_set_tuning(int block_n, int stages, int split_k, int force_path);
  * withholding a signal inside the kernel (never by faulting or trapping):
  *   flags bit 0 : the dense kernel's MMA warp never signals "accumulator ready", so the epilogue warps'
  *                 wait runs out; the skinny ring kernel's first CTA never loads the second 1 KB k-chunk
- *                 of its first unit, so its consumer warps' wait runs out.  C is left incomplete.
+ *                 of its first unit, so its consumer warps' wait runs out; the kernels of the 8-bit floating-point
+ *                 product never signal "products ready".  C is left incomplete.
  *   wait_budget_ns : limit of every wait in later launches (0 = the default 4 s).
  * Process-wide; returns MIPGEMM_OK or MIPGEMM_ERR_INVALID_ARG (unknown flag bits).
  */

@@ -6,7 +6,8 @@
 // lanes (shuffles), a column's in all warps (a 4 KB exchange in shared memory), a square in the whole CTA.  Magnitudes are
 // compared as bit patterns, where infinities and NaNs come out on top.
 //
-// What bounds it: the bytes (16-bit types, both axes: 2 in, 2 out per element).
+// What bounds it: the bytes (16384 x 4096 bf16: along the rows 34 us, 5.8 TB/s, squares 32, back 40 to 43), and for codes along both
+// axes the conversions beside them (57 us where their bytes take 41; along the columns alone 41).
 #include "float8_math.cuh"
 #include "internal.h"
 #include "ptx.cuh"

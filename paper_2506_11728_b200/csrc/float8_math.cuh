@@ -53,6 +53,13 @@ __device__ __forceinline__ uint32_t f8_codes4(float a, float b, float c, float d
 // The bits of |x|: they order like the magnitudes, with infinities and NaNs on top.
 __device__ __forceinline__ uint32_t magnitude_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
+// The larger magnitude; a NaN stays one.
+__device__ __forceinline__ float max_magnitude(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+
 // ---- elements as they lie, in words: 2 of 16 bits or 1 of 32 per word
 template <int kType>
 __device__ __forceinline__ float2 unpack_pair(uint32_t w) {          // 16-bit types

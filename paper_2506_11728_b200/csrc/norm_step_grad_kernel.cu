@@ -12,7 +12,8 @@
 // in registers (40 to 80 of a thread's) they left room for one block on an SM, whose warps waited for each row's exchanges
 // together; two blocks by turns, with the next row's elements on their way, fill those gaps.
 //
-// What bounds it: the bytes of dy, dh, y, z, dx and dz, and the instructions behind them.
+// What bounds it: the instructions (990 of a warp for 16 columns of a row with two norms, a gate and dropout) and their latencies,
+// beside the bytes of dy, dh, y, z, dx and dz: 16384 x 4096 bf16 240 us, the bytes 123.
 #include <algorithm>
 #include <atomic>
 

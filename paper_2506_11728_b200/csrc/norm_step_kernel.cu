@@ -11,6 +11,9 @@
 // rounds on every eight columns).  Hence packed arithmetic on pairs, 16 columns a thread (a row's exchanges cost a warp the same
 // whatever it holds), blocks that go on from row to row with the norms' weights in registers, and the next row's elements on
 // their way while a row waits for its exchanges.  With few rows each gets a block of its own and eight columns a thread.
+//
+// Measured, 16384 x 4096 bf16: two norms, a gate for each channel and dropout 132 us, without dropout 105 (the bytes: 82), x and z to y
+// and codes 101 (72); without norms, with dropout 80, without 69 to 76.
 #include <algorithm>
 
 #include "ptx.cuh"
@@ -103,10 +106,6 @@ __device__ __forceinline__ void affine(uint64_t (&v)[kRuns][4], const uint64_t (
     }
 }
 
-template <int kFormat>
-__device__ __forceinline__ uint2 codes8(const float (&v)[8], float mult) {
-    return make_uint2(f8_codes4<kFormat>(v[0], v[1], v[2], v[3], mult), f8_codes4<kFormat>(v[4], v[5], v[6], v[7], mult));
-}
 __device__ __forceinline__ void store_codes8(uint8_t* dst, uint2 q, int count, bool wide) {
     if (wide) {
         if (count > 0) *reinterpret_cast<uint2*>(dst) = q;
@@ -223,19 +222,21 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
                 }
             }
             if (a.codes != kCodesNone) {
-                float h[kRuns][8];
-                uint32_t top[kRuns], most = 0u;
+                float top[kRuns], most = 0.0f;
 #pragma unroll
                 for (int c = 0; c < kRuns; ++c) {
-                    top[c] = 0u;
+                    if (!kWide) clear_behind(v[c], count[c]);
+                    top[c] = 0.0f;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) unpack_f2(v[c][j], h[c][2 * j], h[c][2 * j + 1]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) top[c] = max(top[c], j < count[c] ? magnitude_bits(h[c][j]) : 0u);
-                    most = max(most, top[c]);
+                    for (int j = 0; j < 4; ++j) {
+                        float lo, hi;
+                        unpack_f2(v[c][j], lo, hi);
+                        top[c] = max_magnitude(max_magnitude(top[c], lo), hi);
+                    }
+                    most = max_magnitude(most, top[c]);
                 }
                 if (a.codes == kCodesS8) {
-                    const float top_f = __uint_as_float(row_max(most, ex, slot));
+                    const float top_f = __uint_as_float(row_max(magnitude_bits(most), ex, slot));
                     // (the rule of mipgemm_quantize_rows)
                     float scale = 0.0f, mult = 0.0f;
                     if (!(top_f <= 3.402823466e38f)) {
@@ -247,24 +248,43 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
                     if (here && threadIdx.x == 0) a.q_scale[row] = scale;
 #pragma unroll
                     for (int c = 0; c < kRuns; ++c) {
+                        float h[8];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) unpack_f2(mul_f2(v[c][j], pack_f2(mult, mult)), h[2 * j], h[2 * j + 1]);
                         uint32_t q[2] = {0u, 0u};
                         if (mult != 0.0f) {
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) q[j / 4] |= (static_cast<uint32_t>(__float2int_rn(__fmul_rn(h[c][j], mult))) & 0xFFu) << (8 * (j & 3));
+                            for (int j = 0; j < 8; ++j) q[j / 4] |= (static_cast<uint32_t>(__float2int_rn(h[j])) & 0xFFu) << (8 * (j & 3));
                         }
                         store_codes8(a.Q + row * a.ldq + col[c], make_uint2(q[0], q[1]), count[c], wide);
                     }
                 } else {
                     // a block of 128 columns is what 16 neighbouring lanes hold
-                    const bool e4m3 = a.codes == kCodesE4M3;
 #pragma unroll
                     for (int c = 0; c < kRuns; ++c) {
 #pragma unroll
-                        for (int o = 8; o > 0; o >>= 1) top[c] = max(top[c], __shfl_xor_sync(~0u, top[c], o));
-                        const F8Scale s = e4m3 ? f8_scale<kE4M3>(__uint_as_float(top[c])) : f8_scale<kE5M2>(__uint_as_float(top[c]));
-                        if ((threadIdx.x & 15) == 0 && count[c] > 0) a.q_scale[(col[c] >> 7) * a.ldqs + row] = s.scale;
-                        store_codes8(a.Q + row * a.ldq + col[c], e4m3 ? codes8<kE4M3>(h[c], s.mult) : codes8<kE5M2>(h[c], s.mult), count[c], wide);
+                        for (int o = 8; o > 0; o >>= 1) top[c] = max_magnitude(top[c], __shfl_xor_sync(~0u, top[c], o));
                     }
+                    const auto put = [&](auto format) {
+                        constexpr int kFormat = decltype(format)::value;
+#pragma unroll
+                        for (int c = 0; c < kRuns; ++c) {
+                            const F8Scale s = f8_scale<kFormat>(top[c]);
+                            if ((threadIdx.x & 15) == 0 && count[c] > 0) a.q_scale[(col[c] >> 7) * a.ldqs + row] = s.scale;
+                            uint32_t q[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float lo, hi;
+                                unpack_f2(mul_f2(v[c][j], pack_f2(s.mult, s.mult)), lo, hi);
+                                q[j] = f8_pair<kFormat>(lo, hi);
+                            }
+                            // (a multiplier of 0 stands for "codes 0": an infinity times 0 would be NaN)
+                            const uint2 w = s.mult == 0.0f ? make_uint2(0u, 0u) : make_uint2(q[0] | (q[1] << 16), q[2] | (q[3] << 16));
+                            store_codes8(a.Q + row * a.ldq + col[c], w, count[c], wide);
+                        }
+                    };
+                    if (a.codes == kCodesE4M3) put(std::integral_constant<int, kE4M3>{});
+                    else put(std::integral_constant<int, kE5M2>{});
                 }
             }
         }
