@@ -20,6 +20,7 @@ NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-Xcompiler", "-fPIC,-O3,-Wall",
     "--expt-relaxed-constexpr",
+    "--threads", "0",                  # the sources side by side
 ]
 
 

@@ -13,7 +13,7 @@
 // their way while a row waits for its exchanges.  With few rows each gets a block of its own and eight columns a thread.
 //
 // Measured, 16384 x 4096 bf16: two norms, a gate for each channel and dropout 132 us, without dropout 105 (the bytes: 82), x and z to y
-// and codes 101 (72); without norms, with dropout 80, without 69 to 76.
+// and codes 92 (72); without norms, with dropout 76, without 68.
 #include <algorithm>
 
 #include "ptx.cuh"
@@ -117,10 +117,10 @@ __device__ __forceinline__ void store_codes8(uint8_t* dst, uint2 q, int count, b
 }
 
 // kRuns runs of eight columns a thread, up to kThreads threads a block; kAhead: a row's elements are asked for while the one before
-// is worked on, and the norms' weights are kept.  kNorms: there may be norms; without them registers are few, and many blocks
-// on an SM do what reading ahead does.
-template <int kType, int kRuns, int kThreads, bool kAhead, bool kWide, bool kNorms>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (kNorms ? 2 : 4) : 1)
+// is worked on, and the norms' weights are kept.  kPost, kPre: there may be such a norm; without any, registers are few, and many
+// blocks on an SM do what reading ahead does.
+template <int kType, int kRuns, int kThreads, bool kAhead, bool kWide, bool kPost, bool kPre>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (kPost || kPre ? 2 : 4) : 1)
 mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
     __shared__ Exchange<kThreads> ex;
     pdl_wait();
@@ -138,8 +138,8 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
         const long long left = a.N - col[c];
         exist[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
         if (kAhead) {
-            if (a.post_w) load_vector_pairs(a.post_w, col[c], exist[c], wide, 1.0f, post_w[c]);
-            if (a.pre_w) load_vector_pairs(a.pre_w, col[c], exist[c], wide, 1.0f, pre_w[c]);
+            if (kPost && a.post_w) load_vector_pairs(a.post_w, col[c], exist[c], wide, 1.0f, post_w[c]);
+            if (kPre && a.pre_w) load_vector_pairs(a.pre_w, col[c], exist[c], wide, 1.0f, pre_w[c]);
         }
     }
     struct Row {
@@ -186,7 +186,7 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
         Row next;
         if (kAhead) load(next, row + step);
         float2 post = make_float2(0.0f, 0.0f), pre = post;
-        if (kNorms && a.post != kNormNone) {
+        if (kPost && a.post != kNormNone) {
             post = normalize<kRuns>(a.post, v, count, inv_n, a.eps, ex, slot);
             affine<kRuns>(v, post_w, kAhead, a.post_w, a.post_b, col, exist, wide);
         }
@@ -210,7 +210,7 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
                 y.store(y_at, c * run, count[c], wide);
             }
         }
-        if (kNorms && a.pre != kNormNone) {
+        if (kPre && a.pre != kNormNone) {
             pre = normalize<kRuns>(a.pre, v, count, inv_n, a.eps, ex, slot);
             affine<kRuns>(v, pre_w, kAhead, a.pre_w, a.pre_b, col, exist, wide);
             if (a.H) {
@@ -321,15 +321,21 @@ StepShape step_shape(const StepArgs& a, int sm_count) {
 
 template <int kType, bool kWide>
 cudaError_t step_t(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
-    if (s.apart) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, false, kWide, false>, a);
+    if (s.apart) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, false, kWide, false, false>, a);
     if (s.blocks) {
-        if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true, kWide, true>, a);
-        return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true, kWide, true>, a);
+        const bool post = a.post != kNormNone, pre = a.pre != kNormNone;
+        const auto many = [&](auto has_post, auto has_pre) {
+            constexpr bool kPost = decltype(has_post)::value, kPre = decltype(has_pre)::value;
+            if (s.threads <= 256) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 256, true, kWide, kPost, kPre>, a);
+            return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, true, kWide, kPost, kPre>, a);
+        };
+        if (post && pre) return many(std::true_type{}, std::true_type{});
+        return post ? many(std::true_type{}, std::false_type{}) : many(std::false_type{}, std::true_type{});
     }
-    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false, kWide, true>, a);
-    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false, kWide, true>, a);
-    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false, kWide, true>, a);
-    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false, kWide, true>, a);
+    if (s.runs == 1) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 1, 512, false, kWide, true, true>, a);
+    if (s.runs == 2) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 2, 512, false, kWide, true, true>, a);
+    if (s.threads <= 512) return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 512, false, kWide, true, true>, a);
+    return cudaLaunchKernelEx(&cfg, mip_norm_step_kernel<kType, 4, 1024, false, kWide, true, true>, a);
 }
 template <int kType>
 cudaError_t step_wide(const StepArgs& a, const StepShape& s, const cudaLaunchConfig_t& cfg) {
