@@ -72,25 +72,32 @@ __device__ __forceinline__ float2 exchange(float2 v, float2* share, int cluster,
     return make_float2(kFirst ? warp_sum(s.x) : 0.0f, warp_sum(s.y));
 }
 
-// A thread's column sums of one vector: 16 bytes of neighbouring threads side by side.
+// A thread's column sums of one vector, in shared memory: 16 bytes of neighbouring threads side by side.
 struct ColumnSums {
-    float4* at;                              // the thread's first place
-    int pitch;                               // threads of the block
+    uint32_t at, pitch;                      // the thread's first place; bytes of the block's threads' places
+    static __device__ __forceinline__ float4 get(uint32_t p) {
+        float4 v;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(p) : "memory");
+        return v;
+    }
+    static __device__ __forceinline__ void put(uint32_t p, float4 v) {
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(p), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+    }
     __device__ __forceinline__ void clear() const {
 #pragma unroll
-        for (int k = 0; k < kGradCols / 4; ++k) at[k * pitch] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = 0; k < kGradCols / 4; ++k) put(at + k * pitch, make_float4(0.0f, 0.0f, 0.0f, 0.0f));
     }
-    // run c's eight columns: += v, or += v * w
+    // run c's eight columns: term(j, sum) instead of the j-th pair
     template <typename F>
     __device__ __forceinline__ void add(int c, const F& term) const {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float4* const p = at + (2 * c + h) * pitch;
-            const float4 s = *p;
+            const uint32_t p = at + (2 * c + h) * pitch;
+            const float4 s = get(p);
             float4 r;
             unpack_f2(term(2 * h, pack_f2(s.x, s.y)), r.x, r.y);
             unpack_f2(term(2 * h + 1, pack_f2(s.z, s.w)), r.z, r.w);
-            *p = r;
+            put(p, r);
         }
     }
 };
@@ -124,7 +131,8 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
     // (vectors that no sum is kept of share the last place)
     int places = 0;
     const auto vector = [&](bool there) {
-        const ColumnSums s = {sums_smem + static_cast<long long>(places) * (kGradCols / 4) * threads + threadIdx.y * blockDim.x + threadIdx.x, threads};
+        const ColumnSums s = {smem_u32(sums_smem) + static_cast<uint32_t>(places * (kGradCols / 4) * threads + threadIdx.y * blockDim.x + threadIdx.x) * 16u,
+                              static_cast<uint32_t>(threads) * 16u};
         if (there) {
             s.clear();
             ++places;
@@ -292,7 +300,7 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
         for (int i = 0; i < block_rows; ++i) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float4 x = s.at[(2 * c + h) * s.pitch + i * static_cast<int>(blockDim.x)];
+                const float4 x = ColumnSums::get(s.at + (2 * c + h) * s.pitch + static_cast<uint32_t>(i) * blockDim.x * 16u);
                 v[4 * h] += x.x; v[4 * h + 1] += x.y; v[4 * h + 2] += x.z; v[4 * h + 3] += x.w;
             }
         }
