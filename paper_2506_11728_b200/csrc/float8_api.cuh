@@ -357,9 +357,11 @@ int norm_step_impl(int type, mip::StepArgs& a, float drop, void* stream_v) {
     if (!size_ok(a.M) || a.N < 0 || a.N > mip::kStepColumns || !(a.eps >= 0.0f)) return MIPGEMM_ERR_INVALID_ARG;
     if (!dropout_rate(drop, &a.mask.bar, &a.mask.scale)) return MIPGEMM_ERR_INVALID_ARG;
     a.wide = a.N % 8 == 0;
+    a.wide_vectors = true;
     if (!step_matrices_ok({{a.X, a.ldx}, {a.Z, a.ldz}, {a.gate, a.ldgate}, {a.Y, a.ldy}, {a.H, a.ldh}}, type, a.N, &a.wide) ||
-        !step_vectors_ok({a.post_w, a.post_b, a.pre_w, a.pre_b}, &a.wide))
+        !step_vectors_ok({a.post_w, a.post_b, a.pre_w, a.pre_b}, &a.wide_vectors))
         return MIPGEMM_ERR_INVALID_ARG;
+    a.wide = a.wide && a.wide_vectors;
     if (!aligned_to(a.stats, 4) || !aligned_to(a.q_scale, 4) || !aligned_to(a.mask.counter, 8) || (a.gate && a.gate_rows < 1)) return MIPGEMM_ERR_INVALID_ARG;
     // parts that nothing would read, or that something would miss
     if (!a.Z && (a.post != MIPGEMM_NORM_NONE || a.gate || a.mask.bar)) return MIPGEMM_ERR_INVALID_ARG;
@@ -391,10 +393,12 @@ int norm_step_grad_impl(int type, mip::StepGradArgs& a, float drop, void* stream
     if (!size_ok(a.M) || a.N < 0 || a.N > mip::kStepColumns) return MIPGEMM_ERR_INVALID_ARG;
     if (!dropout_rate(drop, &a.mask.bar, &a.mask.scale)) return MIPGEMM_ERR_INVALID_ARG;
     a.wide = a.N % 8 == 0;
+    a.wide_vectors = true;
     if (!step_matrices_ok({{a.dY, a.lddy}, {a.dH, a.lddh}, {a.Y, a.ldy}, {a.Z, a.ldz}, {a.gate, a.ldgate}, {a.dX, a.lddx}, {a.dZ, a.lddz}, {a.dgate, a.lddgate}},
                           type, a.N, &a.wide) ||
-        !step_vectors_ok({a.post_w, a.post_b, a.pre_w}, &a.wide))
+        !step_vectors_ok({a.post_w, a.post_b, a.pre_w}, &a.wide_vectors))
         return MIPGEMM_ERR_INVALID_ARG;
+    a.wide = a.wide && a.wide_vectors;
     for (const float* v : {a.stats, static_cast<const float*>(a.dpost_w), static_cast<const float*>(a.dpost_b), static_cast<const float*>(a.dpre_w),
                            static_cast<const float*>(a.dpre_b)})
         if (!aligned_to(v, 4)) return MIPGEMM_ERR_INVALID_ARG;
@@ -424,6 +428,7 @@ int norm_step_grad_impl(int type, mip::StepGradArgs& a, float drop, void* stream
         mip::StepArgs f = {};
         f.M = a.M; f.N = a.N;
         f.wide = a.wide;
+        f.wide_vectors = true;
         f.gate_rows = 1;
         if (a.dX) {
             f.X = a.dY; f.ldx = a.lddy;

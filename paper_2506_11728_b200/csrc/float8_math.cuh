@@ -87,7 +87,9 @@ __device__ __forceinline__ uint4 ld_once_v4(const void* p) {
     return r;
 }
 
-// Eight consecutive elements.  `wide`: 16-byte accesses, all eight exist; else element by element, `count` of them exist.
+// Eight consecutive elements.  `wide`: 16-byte accesses, all eight exist or none; else element by element, `count` of them exist.
+// Where there are many, a warp takes its 256 by turns instead, lane by lane, and brings them into order, or out of it, through
+// 256 elements of shared memory (load_spread and gather, scatter and store_spread: all lanes together).
 template <int kType>
 struct Eight {
     uint32_t w[kType == kF32 ? 8 : 4];
@@ -115,6 +117,75 @@ struct Eight {
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < (kType == kF32 ? 8 : 4); ++i) w[i] = 0u;
+    }
+    // The warp's elements lane, lane + 32, ...; `limit` of its 256 exist.  (A whole run, as nearly all are, without a question for
+    // each element.  16-bit elements one at a time: in words, of which every other row's are split at both ends, it took longer.)
+    template <bool kWhole>
+    __device__ __forceinline__ void load_spread_as(const void* base, int limit) {
+        const int lane = threadIdx.x & 31;
+        const auto get = [&](int i) -> uint32_t {
+            if (!kWhole && lane + 32 * i >= limit) return 0u;
+            if constexpr (kType == kF32) return static_cast<const uint32_t*>(base)[lane + 32 * i];
+            else return static_cast<const uint16_t*>(base)[lane + 32 * i];
+        };
+        if constexpr (kType == kF32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = get(i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = get(2 * i) | (get(2 * i + 1) << 16);
+        }
+    }
+    __device__ __forceinline__ void load_spread(const void* base, int limit) {
+        if (limit == 256) load_spread_as<true>(base, limit);
+        else load_spread_as<false>(base, limit);
+    }
+    template <bool kWhole>
+    __device__ __forceinline__ void store_spread_as(void* base, int limit) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!kWhole && lane + 32 * i >= limit) continue;
+            if constexpr (kType == kF32) static_cast<uint32_t*>(base)[lane + 32 * i] = w[i];
+            else static_cast<uint16_t*>(base)[lane + 32 * i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+        }
+    }
+    __device__ __forceinline__ void store_spread(void* base, int limit) const {
+        if (limit == 256) store_spread_as<true>(base, limit);
+        else store_spread_as<false>(base, limit);
+    }
+    // by turns -> in order, and back; buf: the warp's 256 elements of shared memory
+    __device__ __forceinline__ void gather(uint32_t* buf) {
+        const int lane = threadIdx.x & 31;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (kType == kF32) buf[lane + 32 * i] = w[i];
+            else reinterpret_cast<uint16_t*>(buf)[lane + 32 * i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+        }
+        __syncwarp();
+        const uint4* const q = reinterpret_cast<const uint4*>(buf) + lane * (kType == kF32 ? 2 : 1);
+#pragma unroll
+        for (int i = 0; i < (kType == kF32 ? 2 : 1); ++i) {
+            const uint4 x = q[i];
+            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+        }
+    }
+    __device__ __forceinline__ void scatter(uint32_t* buf) {
+        const int lane = threadIdx.x & 31;
+        __syncwarp();
+        uint4* const q = reinterpret_cast<uint4*>(buf) + lane * (kType == kF32 ? 2 : 1);
+#pragma unroll
+        for (int i = 0; i < (kType == kF32 ? 2 : 1); ++i) q[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+        __syncwarp();
+        if constexpr (kType == kF32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = buf[lane + 32 * i];
+        } else {
+            const uint16_t* const b = reinterpret_cast<const uint16_t*>(buf);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = b[lane + 64 * i] | (static_cast<uint32_t>(b[lane + 64 * i + 32]) << 16);
+        }
     }
     __device__ __forceinline__ void values(float (&v)[8]) const {
         if constexpr (kType == kF32) {
@@ -183,12 +254,12 @@ struct Eight {
     }
 };
 
-// Eight float32 of a vector that every row reads (cached), `fill` where it is absent.
+// Eight float32 of a vector that every row reads (cached), `fill` where it is absent.  `wide`: it lies on 16 bytes.
 __device__ __forceinline__ void load_vector8(const float* p, long long at, int count, bool wide, float fill, float (&v)[8]) {
     if (!p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fill;
-    } else if (wide) {
+    } else if (wide && (count == 0 || count == 8)) {
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
         if (count > 0) {
             a = __ldg(reinterpret_cast<const float4*>(p + at));

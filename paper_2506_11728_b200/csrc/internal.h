@@ -322,7 +322,7 @@ constexpr long long kStepColumns = 32768;    // the longest row of the step's ke
 struct StepArgs {
     long long M, N;
     int post, pre, codes;
-    bool wide;                       // 16-byte accesses everywhere (8 bytes of codes)
+    bool wide, wide_vectors;         // 16-byte accesses everywhere (8 bytes of codes), of the vectors at least
     float eps, x_scale;
     const void* X; long long ldx;    // may be NULL, like most of what follows
     const void* Z; long long ldz;
@@ -344,7 +344,7 @@ cudaError_t launch_norm_step(int type, const StepArgs& a, int sm_count, cudaStre
 struct StepGradArgs {
     long long M, N;
     int post, pre;
-    bool wide;
+    bool wide, wide_vectors;
     float x_scale;
     const void* dY; long long lddy;
     const void* dH; long long lddh;

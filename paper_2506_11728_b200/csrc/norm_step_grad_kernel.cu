@@ -109,6 +109,9 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
     constexpr bool kAhead = kType != kF32;       // (32-bit elements of two rows do not fit the registers)
     constexpr bool wide = kWide;
     constexpr int kSize = kType == kF32 ? 4 : 2, kRuns = kGradRuns;
+    __shared__ alignas(16) uint32_t spread[kWide ? 1 : kGradWarps][kWide ? 4 : (kType == kF32 ? 256 : 128)];
+    uint32_t* const buf = spread[kWide ? 0 : (threadIdx.y * blockDim.x + threadIdx.x) >> 5];
+    const bool vectors = kWide || a.wide_vectors;
     extern __shared__ float4 sums_smem[];        // column sums: of dpre_w, dpre_b, dpost_w, dpost_b, dgate
     __shared__ float2 share[2][kMaxCluster * kGradWarps];
     pdl_wait();
@@ -119,11 +122,12 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
     const int block_rows = blockDim.y, threads = blockDim.x * blockDim.y;
     const long long run = 8ll * blockDim.x;                                // columns between a thread's runs
     const long long col0 = static_cast<long long>(rank) * kRuns * run + 8ll * threadIdx.x;
-    int exist[kRuns];
+    int exist[kRuns], warp_exist[kRuns];                 // of the thread's run, of its warp's
 #pragma unroll
     for (int c = 0; c < kRuns; ++c) {
         const long long left = a.N - col0 - c * run;
-        exist[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
+        exist[c] = left <= 0 ? 0 : (kWide || left >= 8 ? 8 : static_cast<int>(left));
+        warp_exist[c] = static_cast<int>(min(max(left + 8 * (threadIdx.x & 31), 0ll), 256ll));
     }
     const Dropout drop(a.mask, a.N);
     const float inv_n = __fdiv_rn(1.0f, static_cast<float>(a.N));
@@ -152,12 +156,12 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
         r.here = row < end;
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
-            const int count = r.here ? exist[c] : 0;
-            if (a.dY) r.dy[c].load(at(a.dY, row, a.lddy), c * run, count, wide);
+            const int count = r.here ? exist[c] : 0, limit = r.here ? warp_exist[c] : 0;
+            if (a.dY) load_run<kWide>(r.dy[c], at(a.dY, row, a.lddy) + c * run * kSize, count, limit);
             else r.dy[c].clear();
             if (kPre) {
-                r.dh[c].load(at(a.dH, row, a.lddh), c * run, count, wide);
-                r.y[c].load(at(a.Y, row, a.ldy), c * run, count, wide);
+                load_run<kWide>(r.dh[c], at(a.dH, row, a.lddh) + c * run * kSize, count, limit);
+                load_run<kWide>(r.y[c], at(a.Y, row, a.ldy) + c * run * kSize, count, limit);
             }
         }
         r.st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -197,7 +201,7 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
     const int gate_kind = a.gate_rows >= a.M ? 0 : (a.gate_rows == 1 ? 1 : 2);       // one row for all, one each, some share one
     const auto process = [&](const Row& r, long long base) {
         const long long row = base + threadIdx.y;
-        int count[kRuns];
+        int count[kRuns], limit[kRuns];
         Eight<kType> z[kRuns], gate[kRuns];
         uint32_t gate_row = gate_kind == 0 || !r.here ? 0u : static_cast<uint32_t>(row);
         if (gate_kind == 2) gate_row /= static_cast<uint32_t>(a.gate_rows);
@@ -205,9 +209,10 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
             count[c] = r.here ? exist[c] : 0;
-            if (kPost || a.Z) z[c].load(at(a.Z, row, a.ldz), c * run, count[c], wide);
+            limit[c] = r.here ? warp_exist[c] : 0;
+            if (kPost || a.Z) load_run<kWide>(z[c], at(a.Z, row, a.ldz) + c * run * kSize, count[c], limit[c]);
             else z[c].clear();
-            if (a.gate) gate[c].load(a.gate, gate_row * a.ldgate + col0 + c * run, count[c], wide);
+            if (a.gate) load_run<kWide>(gate[c], at(a.gate, gate_row, a.ldgate) + c * run * kSize, count[c], limit[c]);
         }
         // (drawn here, where the instructions fill the gaps of the first exchange)
         uint4 bits[kRuns];
@@ -218,9 +223,9 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
         if (kPre) {
 #pragma unroll
             for (int c = 0; c < kRuns; ++c) {
-                r.dh[c].pairs(t[c]);
-                r.y[c].pairs(hat[c]);
-                load_vector_pairs(a.pre_w, col0 + c * run, exist[c], wide, 1.0f, w);
+                run_pairs<kWide>(r.dh[c], buf, t[c]);
+                run_pairs<kWide>(r.y[c], buf, hat[c]);
+                load_vector_pairs(a.pre_w, col0 + c * run, exist[c], vectors, 1.0f, w);
                 normalized(hat[c], r.st.z, r.st.w, count[c]);
                 pre_w.add(c, [&](int j, uint64_t s) { return fma_f2(t[c][j], hat[c][j], s); });
                 if (kMean) pre_b.add(c, [&](int j, uint64_t s) { return add_f2(t[c][j], s); });
@@ -231,7 +236,7 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
         }
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
-            r.dy[c].pairs(g[c]);
+            run_pairs<kWide>(r.dy[c], buf, g[c]);
             if (kPre) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) g[c][j] = fma_f2(t[c][j], pack_f2(r.st.w, r.st.w), g[c][j]);
@@ -240,20 +245,18 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
                 uint64_t x[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = mul_f2(pack_f2(a.x_scale, a.x_scale), g[c][j]);
-                Eight<kType> e;
-                e.set_pairs(x);
-                e.store(const_cast<char*>(at(a.dX, row, a.lddx)), c * run, count[c], wide);
+                store_run<kWide, kType>(x, const_cast<char*>(at(a.dX, row, a.lddx)) + c * run * kSize, count[c], limit[c], buf);
             }
             if (drop.bar) drop.apply(bits[c], g[c]);
-            z[c].pairs(hat[c]);
+            run_pairs<kWide>(z[c], buf, hat[c]);
             if (kPost) {
-                load_vector_pairs(a.post_w, col0 + c * run, exist[c], wide, 1.0f, w);
+                load_vector_pairs(a.post_w, col0 + c * run, exist[c], vectors, 1.0f, w);
                 normalized(hat[c], r.st.x, r.st.y, count[c]);
             }
             if (a.gate) {
                 if (a.dgate) {
                     uint64_t b[4];
-                    if (kPost && kMean) load_vector_pairs(a.post_b, col0 + c * run, exist[c], wide, 0.0f, b);
+                    if (kPost && kMean) load_vector_pairs(a.post_b, col0 + c * run, exist[c], vectors, 0.0f, b);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint64_t u = hat[c][j];
@@ -261,14 +264,12 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
                         t[c][j] = mul_f2(g[c][j], u);
                     }
                     if (gate_each) {
-                        Eight<kType> e;
-                        e.set_pairs(t[c]);
-                        e.store(a.dgate, row * a.lddgate + col0 + c * run, count[c], wide);
+                        store_run<kWide, kType>(t[c], const_cast<char*>(at(a.dgate, row, a.lddgate)) + c * run * kSize, count[c], limit[c], buf);
                     } else {
                         gate_s.add(c, [&](int j, uint64_t s) { return add_f2(t[c][j], s); });
                     }
                 }
-                gate[c].pairs(t[c]);
+                run_pairs<kWide>(gate[c], buf, t[c]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], t[c][j]);
             }
@@ -287,9 +288,7 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], pack_f2(r.st.y, r.st.y));
                 }
-                Eight<kType> e;
-                e.set_pairs(g[c]);
-                e.store(const_cast<char*>(at(a.dZ, row, a.lddz)), c * run, count[c], wide);
+                store_run<kWide, kType>(g[c], const_cast<char*>(at(a.dZ, row, a.lddz)) + c * run * kSize, count[c], limit[c], buf);
             }
         }
     };

@@ -120,26 +120,30 @@ __device__ __forceinline__ void store_codes8(uint8_t* dst, uint2 q, int count, b
 // is worked on, and the norms' weights are kept.  kPost, kPre: there may be such a norm; without any, registers are few, and many
 // blocks on an SM do what reading ahead does.
 template <int kType, int kRuns, int kThreads, bool kAhead, bool kWide, bool kPost, bool kPre>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (kPost || kPre ? 2 : 4) : 1)
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? (kPost || kPre ? 2 : (kWide || kType != kF32 ? 4 : 3)) : 1)
 mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
     __shared__ Exchange<kThreads> ex;
     pdl_wait();
     pdl_launch_dependents();
     constexpr bool wide = kWide;
+    __shared__ alignas(16) uint32_t spread[kWide ? 1 : kThreads / 32][kWide ? 4 : (kType == kF32 ? 256 : 128)];
+    uint32_t* const buf = spread[kWide ? 0 : (threadIdx.y * blockDim.x + threadIdx.x) >> 5];
+    const bool vectors = kWide || a.wide_vectors;
     const Dropout drop(a.mask, a.N);
     const float inv_n = __fdiv_rn(1.0f, static_cast<float>(a.N));
     int slot = 0;
     long long col[kRuns];
-    int exist[kRuns];
+    int exist[kRuns], warp_exist[kRuns];                 // of the thread's run, of its warp's
     uint64_t post_w[kRuns][4], pre_w[kRuns][4];
 #pragma unroll
     for (int c = 0; c < kRuns; ++c) {
         col[c] = 8ll * ((static_cast<long long>(blockIdx.y) * kRuns + c) * blockDim.x + threadIdx.x);
         const long long left = a.N - col[c];
-        exist[c] = left <= 0 ? 0 : (left < 8 ? static_cast<int>(left) : 8);
+        exist[c] = left <= 0 ? 0 : (kWide || left >= 8 ? 8 : static_cast<int>(left));
+        warp_exist[c] = static_cast<int>(min(max(left + 8 * (threadIdx.x & 31), 0ll), 256ll));
         if (kAhead) {
-            if (kPost && a.post_w) load_vector_pairs(a.post_w, col[c], exist[c], wide, 1.0f, post_w[c]);
-            if (kPre && a.pre_w) load_vector_pairs(a.pre_w, col[c], exist[c], wide, 1.0f, pre_w[c]);
+            if (kPost && a.post_w) load_vector_pairs(a.post_w, col[c], exist[c], vectors, 1.0f, post_w[c]);
+            if (kPre && a.pre_w) load_vector_pairs(a.pre_w, col[c], exist[c], vectors, 1.0f, pre_w[c]);
         }
     }
     struct Row {
@@ -160,14 +164,16 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
         const bool here = row < a.M;
         uint32_t gate_row = gate_kind == 0 || !here ? 0u : static_cast<uint32_t>(row);
         if (gate_kind == 2) gate_row /= static_cast<uint32_t>(a.gate_rows);
+        const char* const g_at = static_cast<const char*>(a.gate) + (gate_row * a.ldgate + col[0]) * kSize;
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
             const int count = here ? exist[c] : 0;
-            if (a.Z) r.z[c].load(z_at, c * run, count, wide);
+            const int limit = here ? warp_exist[c] : 0;
+            if (a.Z) load_run<kWide>(r.z[c], z_at + c * run * kSize, count, limit);
             else r.z[c].clear();
-            if (a.X) r.x[c].load(x_at, c * run, count, wide);
+            if (a.X) load_run<kWide>(r.x[c], x_at + c * run * kSize, count, limit);
             else r.x[c].clear();
-            if (a.gate) r.g[c].load(a.gate, gate_row * a.ldgate + col[c], count, wide);
+            if (a.gate) load_run<kWide>(r.g[c], g_at + c * run * kSize, count, limit);
         }
         z_at += z_step;
         x_at += x_step;
@@ -181,44 +187,39 @@ mip_norm_step_kernel(const __grid_constant__ StepArgs a) {
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
             count[c] = here ? exist[c] : 0;
-            cur.z[c].pairs(v[c]);
+            run_pairs<kWide>(cur.z[c], buf, v[c]);
         }
         Row next;
         if (kAhead) load(next, row + step);
         float2 post = make_float2(0.0f, 0.0f), pre = post;
         if (kPost && a.post != kNormNone) {
             post = normalize<kRuns>(a.post, v, count, inv_n, a.eps, ex, slot);
-            affine<kRuns>(v, post_w, kAhead, a.post_w, a.post_b, col, exist, wide);
+            affine<kRuns>(v, post_w, kAhead, a.post_w, a.post_b, col, exist, vectors);
         }
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
             uint64_t t[4];
             if (a.gate) {
-                cur.g[c].pairs(t);
+                run_pairs<kWide>(cur.g[c], buf, t);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[c][j] = mul_f2(v[c][j], t[j]);
             }
             if (drop.bar) drop.apply(drop.draw(row, col[c]), v[c]);
             if (a.X) {
-                cur.x[c].pairs(t);
+                run_pairs<kWide>(cur.x[c], buf, t);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[c][j] = fma_f2(pack_f2(a.x_scale, a.x_scale), t[j], v[c][j]);
             }
-            if (a.Y) {
-                Eight<kType> y;
-                y.set_pairs(v[c]);
-                y.store(y_at, c * run, count[c], wide);
-            }
+            if (a.Y)
+                store_run<kWide, kType>(v[c], y_at + c * run * kSize, count[c], here ? warp_exist[c] : 0, buf);
         }
         if (kPre && a.pre != kNormNone) {
             pre = normalize<kRuns>(a.pre, v, count, inv_n, a.eps, ex, slot);
-            affine<kRuns>(v, pre_w, kAhead, a.pre_w, a.pre_b, col, exist, wide);
+            affine<kRuns>(v, pre_w, kAhead, a.pre_w, a.pre_b, col, exist, vectors);
             if (a.H) {
 #pragma unroll
                 for (int c = 0; c < kRuns; ++c) {
-                    Eight<kType> h;
-                    h.set_pairs(v[c]);
-                    h.store(h_at, c * run, count[c], wide);
+                    store_run<kWide, kType>(v[c], h_at + c * run * kSize, count[c], here ? warp_exist[c] : 0, buf);
                 }
             }
             if (a.codes != kCodesNone) {

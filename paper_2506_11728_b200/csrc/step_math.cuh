@@ -85,6 +85,29 @@ __device__ __forceinline__ void clear_behind(uint64_t (&v)[4], int count) {
     }
 }
 
+// A run of eight columns of a thread whose own address is `at`; `limit` of its warp's 256 columns exist.
+template <bool kWide, int kType>
+__device__ __forceinline__ void load_run(Eight<kType>& e, const void* at, int count, int limit) {
+    if constexpr (kWide) e.load(at, 0, count, true);
+    else e.load_spread(static_cast<const char*>(at) - (threadIdx.x & 31) * (kType == kF32 ? 32 : 16), limit);
+}
+template <bool kWide, int kType>
+__device__ __forceinline__ void run_pairs(Eight<kType> e, uint32_t* buf, uint64_t (&v)[4]) {
+    if constexpr (!kWide) e.gather(buf);
+    e.pairs(v);
+}
+template <bool kWide, int kType>
+__device__ __forceinline__ void store_run(const uint64_t (&v)[4], void* at, int count, int limit, uint32_t* buf) {
+    Eight<kType> e;
+    e.set_pairs(v);
+    if constexpr (kWide) {
+        e.store(at, 0, count, true);
+    } else {
+        e.scatter(buf);
+        e.store_spread(static_cast<char*>(at) - (threadIdx.x & 31) * (kType == kF32 ? 32 : 16), limit);
+    }
+}
+
 // A multiple of 32 threads a row, up to 1024; blockDim.y rows side by side go through the same calls.
 constexpr int kMaxRowWarps = 32;
 constexpr int kMaxBlockRows = 8;         // rows side by side in a block

@@ -421,3 +421,61 @@ def test_gradients_against_differences(mg):
             curve = abs((l64[0] - l64[1]) / (2 * e) - exact)
             noise = 2 * 128 * 2.0 ** -24 * (np.abs(dy).sum() * 4 + np.abs(dh).sum() * 4) / (2 * e) / 16
             assert abs(slope - exact) <= curve + noise + 1e-3 * abs(exact), (post, pre, name)
+
+
+# ------------------------------------------------------------------------------------------------ rows that lie on no boundary
+def placed(t, pitch, shift):
+    """A copy of `t` whose rows are `pitch` elements apart, the first one `shift` elements into its memory."""
+    import torch
+    room = torch.full((t.shape[0] * pitch + 64,), 7.0, dtype=t.dtype, device="cuda")
+    at = room[shift:shift + t.shape[0] * pitch].view(t.shape[0], pitch)
+    at[:, :t.shape[1]].copy_(t)
+    return at
+
+
+@pytest.mark.parametrize("kind", u.TYPES)
+@pytest.mark.parametrize("post,pre,gate_rows,drop", [("rms", "rms", 0, 0.1), ("layer", "rms", 1, 0.0), ("none", "layer", 50, 0.2), ("rms", "none", 1400, 0.0), ("none", "none", 1, 0.3)])
+@pytest.mark.parametrize("M,N", [(1300, 1000), (700, 520), (610, 8192), (5, 1000), (3, 20000)])
+def test_where_rows_lie_changes_no_bit(mg, M, N, post, pre, gate_rows, drop, kind):
+    """Many rows and few, at 16-byte boundaries and at none, in place and not: one arithmetic, so the same bits."""
+    import torch
+    torch.manual_seed(M + N)
+    dtype = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}[kind]
+    new = lambda rows: torch.randn(rows, N, device="cuda").to(dtype)
+    x, z, dy, dh = (new(M) for _ in range(4))
+    gate = new((M + gate_rows - 1) // gate_rows) if gate_rows else None
+    post_w, pre_w = torch.randn(N + 1, device="cuda"), torch.randn(N + 1, device="cuda")
+    seen = []
+    for pitch, shift, in_place in ((N, 0, False), (N + 1, 1, False), (N + 3, 2, True), (N + 8, 0, True)):
+        put = lambda t: placed(t, pitch, shift)
+        X, Z, DY, DH = (put(t) for t in (x, z, dy, dh))
+        Y = X if in_place else put(torch.zeros_like(x))
+        H = put(torch.zeros_like(x))
+        stats = torch.zeros(M, 4, device="cuda")
+        w = {}
+        for name, v, there in (("post_weight", post_w, post != "none"), ("pre_weight", pre_w, pre != "none")):
+            if there:
+                w[name] = v[:N] if pitch % 8 == 0 else torch.cat([v[:1], v[:N]])[1:]
+        g = put(gate) if gate_rows else None
+        shared = dict(w, Z=Z, ldz=pitch, gate=g, ldgate=pitch if gate_rows else 0, gate_rows=gate_rows or 1, drop=drop, seed=3)
+        norms = (mg.TYPES[kind], mg.NORMS[post], mg.NORMS[pre], M, N)
+        mg.mipgemm_norm_step(*norms, EPS, X=X, ldx=pitch, Y=Y, ldy=pitch, **({"H": H, "ldh": pitch} if pre != "none" else {}), stats=stats, **shared)
+        out = [Y[:, :N].clone(), H[:, :N].clone(), stats.clone()]
+        back, sums = {}, {}
+        if pre != "none":
+            back.update(dH=DH, lddh=pitch, Y=Y, ldy=pitch)
+            sums["dpre_weight"] = torch.zeros(N, device="cuda")
+        if post != "none":
+            sums["dpost_weight"] = torch.zeros(N, device="cuda")
+        dg = put(torch.zeros_like(gate)) if gate_rows else None
+        if gate_rows:
+            back.update(dgate=dg, lddgate=pitch)
+        dx, dz = (DY, Z) if in_place else (put(torch.zeros_like(x)), put(torch.zeros_like(x)))
+        mg.mipgemm_norm_step_grad(*norms, dY=DY, lddy=pitch, stats=stats, dX=dx, lddx=pitch, dZ=dz, lddz=pitch, **back, **sums, **shared)
+        out += [dx[:, :N].clone(), dz[:, :N].clone(), *sums.values()] + ([dg[:, :N].clone()] if gate_rows else [])
+        for t in (Y, H, dx, dz):
+            behind = t[:, N:]
+            assert bool((behind == 7.0).all())
+        seen.append(out)
+    for other in seen[1:]:
+        assert all(torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(seen[0], other))
