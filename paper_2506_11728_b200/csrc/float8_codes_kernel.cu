@@ -43,7 +43,7 @@ struct Tile {
             if constexpr (kWide) {
                 const long long c = c0 + P::col(0);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) e[i][h].load(X, r * ldx + c + 8 * h, r < M && c + 8 * h < N ? 8 : 0, true);
+                for (int h = 0; h < 2; ++h) e[i][h].load(X, r * ldx + c + 8 * h, r < M && c + 8 * h < N ? 8 : 0);
             } else {
                 float v[8] = {};
 #pragma unroll

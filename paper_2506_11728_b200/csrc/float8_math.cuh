@@ -87,33 +87,23 @@ __device__ __forceinline__ uint4 ld_once_v4(const void* p) {
     return r;
 }
 
-// Eight consecutive elements.  `wide`: 16-byte accesses, all eight exist or none; else element by element, `count` of them exist.
-// Where there are many, a warp takes its 256 by turns instead, lane by lane, and brings them into order, or out of it, through
-// 256 elements of shared memory (load_spread and gather, scatter and store_spread: all lanes together).
+// Eight consecutive elements.  load, and store where `wide`: 16-byte accesses, all eight exist or none; store else: element by
+// element, `count` of them exist.  Where rows lie on no 16-byte boundary a warp takes its 256 by turns, lane by lane, and brings
+// them into order, or out of it, through 256 elements of shared memory (load_spread and gather, scatter and store_spread: all
+// lanes together).
 template <int kType>
 struct Eight {
     uint32_t w[kType == kF32 ? 8 : 4];
-    __device__ __forceinline__ void load(const void* base, long long at, int count, bool wide) {
-        if (wide) {
+    __device__ __forceinline__ void load(const void* base, long long at, int count) {
+        if (count > 0) {
             const char* p = static_cast<const char*>(base) + at * (kType == kF32 ? 4 : 2);
-            if (count > 0) {
-                *reinterpret_cast<uint4*>(w) = ld_once_v4(p);
-                if constexpr (kType == kF32) *reinterpret_cast<uint4*>(w + 4) = ld_once_v4(p + 16);
-            } else {
-                clear();
-            }
-        } else if constexpr (kType == kF32) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = i < count ? static_cast<const uint32_t*>(base)[at + i] : 0u;
+            for (int i = 0; i < (kType == kF32 ? 2 : 1); ++i) put(i, ld_once_v4(p + 16 * i));
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = 2 * i < count ? static_cast<const uint16_t*>(base)[at + 2 * i] : 0u;
-                const uint32_t hi = 2 * i + 1 < count ? static_cast<const uint16_t*>(base)[at + 2 * i + 1] : 0u;
-                w[i] = lo | (hi << 16);
-            }
+            clear();
         }
     }
+    __device__ __forceinline__ void put(int i, uint4 x) { w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w; }
     __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int i = 0; i < (kType == kF32 ? 8 : 4); ++i) w[i] = 0u;
@@ -166,10 +156,7 @@ struct Eight {
         __syncwarp();
         const uint4* const q = reinterpret_cast<const uint4*>(buf) + lane * (kType == kF32 ? 2 : 1);
 #pragma unroll
-        for (int i = 0; i < (kType == kF32 ? 2 : 1); ++i) {
-            const uint4 x = q[i];
-            w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-        }
+        for (int i = 0; i < (kType == kF32 ? 2 : 1); ++i) put(i, q[i]);
     }
     __device__ __forceinline__ void scatter(uint32_t* buf) {
         const int lane = threadIdx.x & 31;

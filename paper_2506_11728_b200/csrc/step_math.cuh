@@ -85,10 +85,11 @@ __device__ __forceinline__ void clear_behind(uint64_t (&v)[4], int count) {
     }
 }
 
-// A run of eight columns of a thread whose own address is `at`; `limit` of its warp's 256 columns exist.
+// A run of eight columns of a thread whose own address is `at`; `limit` of its warp's 256 columns exist.  All lanes together, and
+// `buf` is the warp's own; run_pairs brings what load_run took into order.
 template <bool kWide, int kType>
 __device__ __forceinline__ void load_run(Eight<kType>& e, const void* at, int count, int limit) {
-    if constexpr (kWide) e.load(at, 0, count, true);
+    if constexpr (kWide) e.load(at, 0, count);
     else e.load_spread(static_cast<const char*>(at) - (threadIdx.x & 31) * (kType == kF32 ? 32 : 16), limit);
 }
 template <bool kWide, int kType>
