@@ -37,7 +37,7 @@ constexpr int all_slot_bytes(bool wide) { return kSumWarps * slot_buffers(wide) 
 // `depth` blocks before are ready, which says that those of another `depth` blocks before have been summed.
 constexpr int scale_bytes(bool pair, bool vec) { return vec ? (pair ? 1536 : 1024) : (pair ? 1024 : 512); }
 constexpr int scale_places(bool pair) { return pair ? 4 : 8; }
-constexpr int kBiasBytes = kSumWarps * 128;                              // 32 columns for each summing warp
+constexpr int kOwnBytes = 128 + 16;                                      // of a summing warp: bias of 32 columns, where its tile lies
 // Registers per thread: the sums take 128 of those of a pair's summing warps.  The block is launched with kLaunchRegs a thread; the
 // four other warps give theirs up (checked against the compiled kernel before its first launch).
 constexpr int kLaunchRegs = 168, kFewRegs = 120, kManyRegs = 192;
@@ -113,12 +113,12 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
     uint8_t* smem = smem_raw + pad;
     const uint32_t smem_base = raw_addr + pad;
-    // shared memory: [stages x (A | B)] [slots of the summing warps] [scales] [bias] [control block]
+    // shared memory: [stages x (A | B)] [slots of the summing warps] [scales] [summing warps' own] [control block]
     const uint32_t slots = smem_base + p.stages * stage_bytes;
     const uint32_t scales = slots + (kRaw ? 0u : all_slot_bytes(kWide));
     constexpr uint32_t kScaleBytes = scale_bytes(kPair, kVec), kPlaces = scale_places(kPair);
-    const uint32_t bias_at = scales + kPlaces * kScaleBytes;
-    const uint32_t ctrl = bias_at + kBiasBytes;
+    const uint32_t own = scales + kPlaces * kScaleBytes;
+    const uint32_t ctrl = own + kSumWarps * kOwnBytes;
     const uint32_t bar_full = ctrl, bar_empty = ctrl + 8u * kMaxF8Stages;
     const uint32_t bar_tfull = ctrl + 16u * kMaxF8Stages, bar_tempty = bar_tfull + 32u, bar_drain = bar_tempty + 32u;
     const uint32_t bar_in = bar_drain + 8u;              // kSumWarps x kSlotBuffers: a slot's tile has arrived
@@ -126,8 +126,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl_ptr);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(tmem_slot + 1);
     const UnwindWords unwind = {bar_in + 8u * kSumWarps * kSlotBuffers + 8u};
-    static_assert(16 * kMaxF8Stages + 72 + 8 * kSumWarps * slot_buffers(false) + 8 + UnwindWords::kBytes <= 448, "control block");
-    const uint32_t info = ctrl + 448u;                   // m0, n0 and first plane row of the last four tiles
+    static_assert(16 * kMaxF8Stages + 72 + 8 * kSumWarps * slot_buffers(false) + 8 + UnwindWords::kBytes <= kCtrlBytes, "control block");
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int lane = threadIdx.x & 31;
@@ -239,18 +238,15 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                 }
             }
         } else if (warp == 3) {
-            // -------------------------------------------------------- scales, and where the tiles lie
+            // -------------------------------------------------------- scales
             // (The summing warps go from block to block in the time of two or three hundred instructions: what does not have to be
             // there is here.)  Loads are two blocks ahead.  Rows, columns and blocks behind the last read the last one's: nothing of
             // what they give is stored.
             constexpr int kB = kVec ? kCtas * 4 : kHalves;
-            uint32_t acc = 0, uses = 0, place = 0, tile_no = 0;
+            uint32_t acc = 0, uses = 0, place = 0;
             bool ok = true;
-            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
+            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
                 const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
-                if (lane == 0)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};"
-                                 ::"r"(info + (tile_no & 3u) * 16u), "r"(tc.m0), "r"(tc.n0), "r"(tc.plane) : "memory");
                 int row[4];
                 long long col[kB];
 #pragma unroll
@@ -314,7 +310,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         if constexpr (kPair) regs_inc<kManyRegs>();
         const int e = warp - 4, q = warp & 3, half = e >> 2;
         const uint32_t my_slots = slots + static_cast<uint32_t>(e) * kSlotBuffers * kSlot;
-        const uint32_t my_bias = bias_at + static_cast<uint32_t>(e) * 128u;
+        const uint32_t my_bias = own + static_cast<uint32_t>(e * kOwnBytes), my_tile = my_bias + 128u;
         const uint32_t my_bar = bar_in + 8u * static_cast<uint32_t>(e * kSlotBuffers);
         // (pair: this half's buffers, 128 columns each; else half the columns of all)
         const uint32_t t_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(kPair ? half * kDepth * kN : half * kCols);
@@ -328,15 +324,22 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         const uint32_t my_scale = scales + static_cast<uint32_t>(q * 32 + lane) * (kVec || !kPair ? 4u : 8u);
         const uint32_t my_cols = scales + 512u + static_cast<uint32_t>(half * kCols) * 4u;
         const bool f16 = p.type == kF16, has_r = p.R != nullptr, r_tma = !kRaw && p.r_tma != 0, c_tma = p.c_tma != 0;
-        uint32_t acc = 0, acc_phase = 0, place = 0, tile_no = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
+        uint32_t acc = 0, acc_phase = 0, place = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
         bool ok = true;
-        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+            // Where the tile lies is worked out before there are sums and kept in a place of the warp's own (registers are short, and
+            // no other warp may write it: the scales' warp, for one, is whole tiles ahead where K is short).
+            {
+                const LayerTile at = decode_tile(p, unit, kRowsPerTile);
+                __syncwarp();                                      // (all lanes have read the last one's)
+                if (lane == 0) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};" ::"r"(my_tile), "r"(at.m0), "r"(at.n0), "r"(at.plane) : "memory");
+                __syncwarp();
+            }
             struct { int m0, n0, plane; } tc = {};
             int row0 = 0;
-            const auto read_info = [&] {
+            const auto read_tile = [&] {
                 int none;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                             : "=r"(tc.m0), "=r"(tc.n0), "=r"(tc.plane), "=r"(none) : "r"(info + (tile_no & 3u) * 16u) : "memory");
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(tc.m0), "=r"(tc.n0), "=r"(tc.plane), "=r"(none) : "r"(my_tile) : "memory");
                 row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
             };
             const auto run_ok = [&](int c) { return row0 < p.M && tc.n0 + run_col(c) < p.N; };       // (warp-uniform)
@@ -409,7 +412,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                 if (++acc == kDepth) { acc = 0; acc_phase ^= 1u; }
                 if (++place == kPlaces) place = 0;
                 if (r_tma && i == 0) {
-                    read_info();
+                    read_tile();
                     if (run_ok(0)) {
                         if (elect_one()) tma_store_wait_read<0>();
                         __syncwarp();
@@ -418,7 +421,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                 }
             }
             if (!ok) break;
-            read_info();
+            read_tile();
             if constexpr (kRaw) {
                 // (planes have whole blocks of 32 rows and columns)
                 float* out = static_cast<float*>(p.C) + static_cast<long long>(tc.plane + row0 + lane) * p.ldc + tc.n0;
@@ -616,7 +619,7 @@ cudaError_t launch_form(const F8ProductParams& p, bool raw, const cudaLaunchConf
 }
 
 size_t smem_of(int type, bool pair, bool vec, bool raw, int stages) {
-    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : all_slot_bytes(type == kF32)) + scale_places(pair) * scale_bytes(pair, vec) + kBiasBytes + kCtrlBytes + 1024;
+    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : all_slot_bytes(type == kF32)) + scale_places(pair) * scale_bytes(pair, vec) + kSumWarps * kOwnBytes + kCtrlBytes + 1024;
 }
 
 }  // namespace

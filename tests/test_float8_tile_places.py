@@ -1,0 +1,43 @@
+"""How far apart the warps of the dense 8-bit floating-point product may be, by a model of its barriers on the CPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+PAIR, SINGLE = ("2", "2"), ("4", "1")            # blocks in tensor memory for each half, halves
+
+
+@pytest.fixture(scope="module")
+def model(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("tiles") / "model")
+    cxx = shutil.which("g++") or shutil.which("c++")
+    assert cxx, "no C++ compiler"
+    subprocess.run([cxx, "-O2", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-o", exe, os.path.join(HERE, "tile_places_model.cpp")], check=True)
+    return lambda *args: [int(v) for v in subprocess.run([exe, *args], check=True, capture_output=True, text=True).stdout.split()]
+
+
+@pytest.mark.parametrize("form,blocks", [(PAIR, "1"), (SINGLE, "1"), (SINGLE, "2")])
+def test_the_scales_warp_is_whole_tiles_ahead_where_k_is_short(model, form, blocks):
+    """So tile positions cannot come from it by a ring of four: a tile's would be that of another one when its outputs are stored."""
+    moved, stuck, tiles = model(*form, blocks, "4", "1")
+    assert moved > 0 and stuck == 0 and tiles > 0
+
+
+@pytest.mark.parametrize("form,ring", [(PAIR, "6"), (SINGLE, "10")])
+def test_how_far_it_is_ahead(model, form, ring):
+    """2 * depth + 1 tiles at the most."""
+    for seed in ("1", "2"):
+        assert model(*form, "1", ring, seed)[:2] == [0, 0]
+    assert model(*form, "1", str(int(ring) - 1), "1")[0] > 0
+
+
+def test_positions_are_kept_by_the_warps_that_read_them():
+    """Read from the source: a summing warp works its tile's position out itself and keeps it at an address of its own."""
+    import re
+    path = os.path.join(os.path.dirname(HERE), "paper_2506_11728_b200", "csrc", "float8_product_kernel.cu")
+    text = re.sub(r"//[^\n]*", "", open(path).read())
+    scales, sums = text.split("else if (warp == 3)")[1].split("regs_inc<kManyRegs>")[:2]
+    assert "my_tile = my_bias + 128u" in sums and "own + static_cast<uint32_t>(e * kOwnBytes)" in sums
+    assert "decode_tile" in sums and "tc.m0" in scales and not re.search(r"st\.shared[^;]*tc\.m0", scales)
