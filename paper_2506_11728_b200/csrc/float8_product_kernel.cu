@@ -34,7 +34,8 @@ constexpr int slot_buffers(bool wide) { return wide ? 2 : 3; }           // per 
 constexpr int all_slot_bytes(bool wide) { return kSumWarps * slot_buffers(wide) * slot_bytes(wide); }
 // Scales of a k-block: of the tile's 128 rows times those of its squares (each half's two), or of the rows and of the columns.
 // As many blocks as there are buffers of products for a half, twice: a block's place is written when the products of one
-// `depth` blocks before are ready, which says that those of another `depth` blocks before have been summed.
+// `depth` blocks before are ready, which says that the buffers of another `depth` blocks before have been given back; nothing
+// reads a block's scales behind that.
 constexpr int scale_bytes(bool pair, bool vec) { return vec ? (pair ? 1536 : 1024) : (pair ? 1024 : 512); }
 constexpr int scale_places(bool pair) { return pair ? 4 : 8; }
 constexpr int kOwnBytes = 128 + 16;                                      // of a summing warp: bias of 32 columns, where its tile lies
@@ -382,11 +383,19 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                 }
 #pragma unroll
                 for (int c = 0; c < kCols / 16; ++c) {
+                    const uint32_t cols_at = my_cols + at + static_cast<uint32_t>(16 * c) * 4u;
+                    const bool last = c + 1 == kCols / 16;
+                    float b_s[4][4];                               // (of the last run; before it there are no registers for all of a run's)
+                    if (kVec && last) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) lds_f4(cols_at + 16u * j, b_s[j]);
+                    }
                     tmem_ld_wait_for_16(v[c & 1]);
-                    if (c + 1 < kCols / 16) {
+                    if (!last) {
                         tmem_ld_32x16(t_at + 16 * (c + 1), v[(c + 1) & 1]);
                     } else {
-                        // the buffer is the tensor core's again: its last columns are in registers
+                        // the buffer is the tensor core's again, and the scales' place the scales' warp's: what is left of both is
+                        // in registers
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) {
@@ -399,8 +408,8 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                         const uint64_t x0 = words_f2(v[c & 1][j], v[c & 1][j + 1]), x1 = words_f2(v[c & 1][j + 2], v[c & 1][j + 3]);
                         uint64_t* to = &sum[8 * c + j / 2];
                         if constexpr (kVec) {
-                            float b[4];
-                            lds_f4(my_cols + at + static_cast<uint32_t>(16 * c + j) * 4u, b);
+                            float (&b)[4] = b_s[j / 4];
+                            if (!last) lds_f4(cols_at + 4u * j, b);
                             to[0] = fma_f2(mul_f2(x0, pack_f2(b[0], b[1])), s2[0], to[0]);
                             to[1] = fma_f2(mul_f2(x1, pack_f2(b[2], b[3])), s2[0], to[1]);
                         } else {

@@ -21,7 +21,7 @@ def model(tmp_path_factory):
 @pytest.mark.parametrize("form,blocks", [(PAIR, "1"), (SINGLE, "1"), (SINGLE, "2")])
 def test_the_scales_warp_is_whole_tiles_ahead_where_k_is_short(model, form, blocks):
     """So tile positions cannot come from it by a ring of four: a tile's would be that of another one when its outputs are stored."""
-    moved, stuck, tiles = model(*form, blocks, "4", "1")
+    moved, stuck, tiles, _ = model(*form, blocks, "4", "1")
     assert moved > 0 and stuck == 0 and tiles > 0
 
 
@@ -41,3 +41,28 @@ def test_positions_are_kept_by_the_warps_that_read_them():
     scales, sums = text.split("else if (warp == 3)")[1].split("regs_inc<kManyRegs>")[:2]
     assert "my_tile = my_bias + 128u" in sums and "own + static_cast<uint32_t>(e * kOwnBytes)" in sums
     assert "decode_tile" in sums and "tc.m0" in scales and not re.search(r"st\.shared[^;]*tc\.m0", scales)
+
+
+@pytest.mark.parametrize("form", [PAIR, SINGLE])
+@pytest.mark.parametrize("blocks", ["1", "3"])
+def test_scales_are_read_before_their_place_is_given_back(model, form, blocks):
+    """In front of the buffer's return, twice as many places as buffers do; behind it, the next block's scales may be there."""
+    places = str(2 * int(form[0]))
+    for seed in ("1", "2"):
+        _, stuck, _, wrong = model(*form, blocks, "64", seed, places, "0")
+        assert stuck == 0 and wrong == 0
+    assert model(*form, blocks, "64", "1", places, "1")[3] > 0
+    assert model(*form, blocks, "64", "1", str(int(places) - 1), "0")[3] > 0
+
+
+def test_the_kernel_reads_them_so():
+    """Read from the source: behind a block's return of its buffer, column scales come from registers alone."""
+    import re
+    path = os.path.join(os.path.dirname(HERE), "paper_2506_11728_b200", "csrc", "float8_product_kernel.cu")
+    text = re.sub(r"//[^\n]*", "", open(path).read())
+    assert re.search(r"scale_places\(bool pair\) \{ return pair \? 4 : 8; \}", text) and "kDepth = 4 / kHalves" in text
+    block = text.split("for (int c = 0; c < kCols / 16; ++c) {")[1].split("if (++acc == kDepth)")[0]
+    front, back = block.split("mbar_arrive_cluster(my_tempty")
+    assert "if (kVec && last)" in front and "lds_f4(cols_at + 16u * j, b_s[j])" in front
+    assert [m for m in re.findall(r"[^;{}]*lds_f4\([^;]*;", back)] == [m for m in re.findall(r"[^;{}]*if \(!last\) lds_f4\([^;]*;", back)]
+    assert len(re.findall(r"lds_f4", back)) == 1 and "ld.shared" not in back

@@ -55,7 +55,7 @@ def product(mg, M, N, K, what, kind, residual, seed=0):
 
 
 @pytest.mark.parametrize("K", [1, 64, 100, 128, 129, 200, 256, 257])
-@pytest.mark.parametrize("what", ["forward"])
+@pytest.mark.parametrize("what", ["forward", "weight_grad"])
 @pytest.mark.parametrize("form,M,N", [("pair", 8190, 8448), ("pair", 8190, 8450), ("single", 8190, 4224)])
 def test_every_tile_is_stored_at_its_place(mg, form, M, N, what, K):
     """14 tiles a CTA or pair; rows of C at 16-byte boundaries (stored by TMA) and at none."""
@@ -67,7 +67,9 @@ def test_every_tile_is_stored_at_its_place(mg, form, M, N, what, K):
         assert torch.equal(C, want), (kind, residual)
 
 
-@pytest.mark.parametrize("M,N,K,what", [(16384, 4096, 64, "forward"), (100, 128256, 128, "forward"), (100, 128250, 256, "forward")])
+@pytest.mark.parametrize("M,N,K,what", [(16384, 4096, 64, "forward"), (8192, 8192, 128, "forward_rows"), (100, 128256, 128, "forward"), (100, 128250, 256, "forward"),
+                                        (11008, 4096, 100, "weight_grad"), (14336, 4096, 1, "weight_grad"), (40, 100000, 200, "forward_rows"),
+                                        (130, 60000, 129, "weight_grad")])
 def test_short_sums_as_they_are_planned(mg, M, N, K, what):
     import torch
     for kind, residual in (("f32", "own"), ("bf16", None)):
