@@ -38,7 +38,12 @@ constexpr int all_slot_bytes(bool wide) { return kSumWarps * slot_buffers(wide) 
 // reads a block's scales behind that.
 constexpr int scale_bytes(bool pair, bool vec) { return vec ? (pair ? 1536 : 1024) : (pair ? 1024 : 512); }
 constexpr int scale_places(bool pair) { return pair ? 4 : 8; }
-constexpr int kOwnBytes = 128 + 16;                                      // of a summing warp: bias of 32 columns, where its tile lies
+constexpr int kBiasBytes = kSumWarps * 128;                              // 32 columns for each summing warp
+// Where the last tiles lie, from the scales' warp to the summing warps, which look behind a tile's last block.  A tile's position is
+// written before any wait for the tile: with the wait for the block in front of it the buffers up to 2 * depth blocks before that one
+// had been given back, and where a tile is one block, the tile behind those is still to be looked up.
+constexpr int tile_places(bool pair) { return pair ? 8 : 16; }
+constexpr int tile_bytes(bool pair) { return 16 * tile_places(pair); }
 // Registers per thread: the sums take 128 of those of a pair's summing warps.  The block is launched with kLaunchRegs a thread; the
 // four other warps give theirs up (checked against the compiled kernel before its first launch).
 constexpr int kLaunchRegs = 168, kFewRegs = 120, kManyRegs = 192;
@@ -114,12 +119,15 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
     const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
     uint8_t* smem = smem_raw + pad;
     const uint32_t smem_base = raw_addr + pad;
-    // shared memory: [stages x (A | B)] [slots of the summing warps] [scales] [summing warps' own] [control block]
+    // shared memory: [stages x (A | B)] [slots of the summing warps] [scales] [bias] [control block] [tile positions]
     const uint32_t slots = smem_base + p.stages * stage_bytes;
     const uint32_t scales = slots + (kRaw ? 0u : all_slot_bytes(kWide));
     constexpr uint32_t kScaleBytes = scale_bytes(kPair, kVec), kPlaces = scale_places(kPair);
-    const uint32_t own = scales + kPlaces * kScaleBytes;
-    const uint32_t ctrl = own + kSumWarps * kOwnBytes;
+    const uint32_t bias_at = scales + kPlaces * kScaleBytes;
+    const uint32_t ctrl = bias_at + kBiasBytes;
+    const uint32_t tile_at = ctrl + kCtrlBytes;          // m0, n0 and first plane row
+    constexpr uint32_t kTilePlaces = tile_places(kPair);
+    static_assert(kTilePlaces >= 2 * kDepth + 2 && (kTilePlaces & (kTilePlaces - 1)) == 0, "tile positions");
     const uint32_t bar_full = ctrl, bar_empty = ctrl + 8u * kMaxF8Stages;
     const uint32_t bar_tfull = ctrl + 16u * kMaxF8Stages, bar_tempty = bar_tfull + 32u, bar_drain = bar_tempty + 32u;
     const uint32_t bar_in = bar_drain + 8u;              // kSumWarps x kSlotBuffers: a slot's tile has arrived
@@ -239,15 +247,18 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
                 }
             }
         } else if (warp == 3) {
-            // -------------------------------------------------------- scales
+            // -------------------------------------------------------- scales, and where the tiles lie
             // (The summing warps go from block to block in the time of two or three hundred instructions: what does not have to be
             // there is here.)  Loads are two blocks ahead.  Rows, columns and blocks behind the last read the last one's: nothing of
             // what they give is stored.
             constexpr int kB = kVec ? kCtas * 4 : kHalves;
-            uint32_t acc = 0, uses = 0, place = 0;
+            uint32_t acc = 0, uses = 0, place = 0, tile_no = 0;
             bool ok = true;
-            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
+            for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
                 const LayerTile tc = decode_tile(p, unit, kRowsPerTile);
+                if (lane == 0)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};"
+                                 ::"r"(tile_at + (tile_no & (kTilePlaces - 1)) * 16u), "r"(tc.m0), "r"(tc.n0), "r"(tc.plane) : "memory");
                 int row[4];
                 long long col[kB];
 #pragma unroll
@@ -311,7 +322,7 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         if constexpr (kPair) regs_inc<kManyRegs>();
         const int e = warp - 4, q = warp & 3, half = e >> 2;
         const uint32_t my_slots = slots + static_cast<uint32_t>(e) * kSlotBuffers * kSlot;
-        const uint32_t my_bias = own + static_cast<uint32_t>(e * kOwnBytes), my_tile = my_bias + 128u;
+        const uint32_t my_bias = bias_at + static_cast<uint32_t>(e) * 128u;
         const uint32_t my_bar = bar_in + 8u * static_cast<uint32_t>(e * kSlotBuffers);
         // (pair: this half's buffers, 128 columns each; else half the columns of all)
         const uint32_t t_base = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(kPair ? half * kDepth * kN : half * kCols);
@@ -325,22 +336,15 @@ mip_f8_product_kernel(const __grid_constant__ F8ProductParams p) {
         const uint32_t my_scale = scales + static_cast<uint32_t>(q * 32 + lane) * (kVec || !kPair ? 4u : 8u);
         const uint32_t my_cols = scales + 512u + static_cast<uint32_t>(half * kCols) * 4u;
         const bool f16 = p.type == kF16, has_r = p.R != nullptr, r_tma = !kRaw && p.r_tma != 0, c_tma = p.c_tma != 0;
-        uint32_t acc = 0, acc_phase = 0, place = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
+        uint32_t acc = 0, acc_phase = 0, place = 0, tile_no = 0, loads = 0, taken = 0;     // tile loads asked for, and waited for
         bool ok = true;
-        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride) {
-            // Where the tile lies is worked out before there are sums and kept in a place of the warp's own (registers are short, and
-            // no other warp may write it: the scales' warp, for one, is whole tiles ahead where K is short).
-            {
-                const LayerTile at = decode_tile(p, unit, kRowsPerTile);
-                __syncwarp();                                      // (all lanes have read the last one's)
-                if (lane == 0) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};" ::"r"(my_tile), "r"(at.m0), "r"(at.n0), "r"(at.plane) : "memory");
-                __syncwarp();
-            }
+        for (int unit = first_unit; unit < total_units && ok; unit += unit_stride, ++tile_no) {
             struct { int m0, n0, plane; } tc = {};
             int row0 = 0;
             const auto read_tile = [&] {
                 int none;
-                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(tc.m0), "=r"(tc.n0), "=r"(tc.plane), "=r"(none) : "r"(my_tile) : "memory");
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(tc.m0), "=r"(tc.n0), "=r"(tc.plane), "=r"(none) : "r"(tile_at + (tile_no & (kTilePlaces - 1)) * 16u) : "memory");
                 row0 = tc.m0 + static_cast<int>(cta_rank) * kBlockM + q * 32;
             };
             const auto run_ok = [&](int c) { return row0 < p.M && tc.n0 + run_col(c) < p.N; };       // (warp-uniform)
@@ -628,7 +632,7 @@ cudaError_t launch_form(const F8ProductParams& p, bool raw, const cudaLaunchConf
 }
 
 size_t smem_of(int type, bool pair, bool vec, bool raw, int stages) {
-    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : all_slot_bytes(type == kF32)) + scale_places(pair) * scale_bytes(pair, vec) + kSumWarps * kOwnBytes + kCtrlBytes + 1024;
+    return static_cast<size_t>(stages) * 32768 + (raw ? 0 : all_slot_bytes(type == kF32)) + scale_places(pair) * scale_bytes(pair, vec) + kBiasBytes + kCtrlBytes + tile_bytes(pair) + 1024;
 }
 
 }  // namespace

@@ -33,14 +33,15 @@ def test_how_far_it_is_ahead(model, form, ring):
     assert model(*form, "1", str(int(ring) - 1), "1")[0] > 0
 
 
-def test_positions_are_kept_by_the_warps_that_read_them():
-    """Read from the source: a summing warp works its tile's position out itself and keeps it at an address of its own."""
+@pytest.mark.parametrize("form,ring", [(PAIR, "8"), (SINGLE, "16")])
+@pytest.mark.parametrize("blocks", ["1", "2", "3"])
+def test_the_kernels_ring_is_deep_enough(model, form, ring, blocks):
     import re
     path = os.path.join(os.path.dirname(HERE), "paper_2506_11728_b200", "csrc", "float8_product_kernel.cu")
     text = re.sub(r"//[^\n]*", "", open(path).read())
-    scales, sums = text.split("else if (warp == 3)")[1].split("regs_inc<kManyRegs>")[:2]
-    assert "my_tile = my_bias + 128u" in sums and "own + static_cast<uint32_t>(e * kOwnBytes)" in sums
-    assert "decode_tile" in sums and "tc.m0" in scales and not re.search(r"st\.shared[^;]*tc\.m0", scales)
+    assert re.search(r"tile_places\(bool pair\) \{ return pair \? 8 : 16; \}", text) and "kTilePlaces >= 2 * kDepth + 2" in text
+    assert len(re.findall(r"tile_at \+ \(tile_no & \(kTilePlaces - 1\)\)", text)) == 2          # written, read
+    assert model(*form, blocks, ring, "3")[:2] == [0, 0]
 
 
 @pytest.mark.parametrize("form", [PAIR, SINGLE])
