@@ -177,8 +177,9 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
         for (int j = 0; j < 4; ++j) v[j] = mul_f2(kMean ? add_f2(v[j], pack_f2(-mean, -mean)) : v[j], pack_f2(rstd, rstd));
         if (kMean || !kWide) clear_behind(v, count);
     };
-    // what a norm passes on, but for rstd: g - mean(g) - hat mean(g hat)
-    const auto through = [&](uint64_t (&g)[kRuns][4], const uint64_t (&hat)[kRuns][4], int kind) {
+    // what a norm passes on, but for rstd: g - mean(g) - hat mean(g hat); columns behind the last one stay 0 (the other norm sums over
+    // them)
+    const auto through = [&](uint64_t (&g)[kRuns][4], const uint64_t (&hat)[kRuns][4], int kind, const int (&count)[kRuns]) {
         uint64_t s = 0ull, u = 0ull;
 #pragma unroll
         for (int c = 0; c < kRuns; ++c)
@@ -191,12 +192,15 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
         const float2 e = exchange<kMean>(make_float2(kMean ? sum_pair(s) : 0.0f, sum_pair(u)), share[slot], cluster, rank);
         const float mean = kMean && kind == kNormLayer ? -e.x * inv_n : 0.0f, slope = -e.y * inv_n;
 #pragma unroll
-        for (int c = 0; c < kRuns; ++c)
+        for (int c = 0; c < kRuns; ++c) {
+            const float m = kWide && count[c] == 0 ? 0.0f : mean;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (kMean) g[c][j] = add_f2(g[c][j], pack_f2(mean, mean));
+                if (kMean) g[c][j] = add_f2(g[c][j], pack_f2(m, m));
                 g[c][j] = fma_f2(hat[c][j], pack_f2(slope, slope), g[c][j]);
             }
+            if (kMean && !kWide) clear_behind(g[c], count[c]);
+        }
     };
     const int gate_kind = a.gate_rows >= a.M ? 0 : (a.gate_rows == 1 ? 1 : 2);       // one row for all, one each, some share one
     const auto process = [&](const Row& r, long long base) {
@@ -232,7 +236,7 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) t[c][j] = mul_f2(t[c][j], w[j]);
             }
-            through(t, hat, a.pre);
+            through(t, hat, a.pre, count);
         }
 #pragma unroll
         for (int c = 0; c < kRuns; ++c) {
@@ -280,7 +284,7 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
                 for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], w[j]);
             }
         }
-        if (kPost) through(g, hat, a.post);
+        if (kPost) through(g, hat, a.post, count);
         if (a.dZ) {
 #pragma unroll
             for (int c = 0; c < kRuns; ++c) {
