@@ -583,7 +583,8 @@ int mipgemm_norm_step(int type, int post, int pre, int64_t M, int64_t N, float e
  * and dH of H (with a pre norm only).  Y, Z, gate, the weights, drop, seed and counter as in the forward pass; stats as it
  * left them.  Every output may be NULL:
  *   dX, dZ : M x N (written); each may be one of dY, dH, Y and Z (with the same pitch), not both the same
- *   dgate : as gate (written), summed over the rows that share a gate row
+ *   dgate : as gate (written), summed over the rows that share a gate row.  Dropped places add 0 to it and get 0 in
+ *       dZ, whatever stands there in Z, the gate and the gradients
  *   dpost_weight, dpost_bias, dpre_weight, dpre_bias : N float32 (written), summed over all rows in binary32
  * M == 0 writes zeros to the four vectors.  Scratch memory: at most 8 bytes * N * (vectors wanted + 1) for each SM of the
  * device, for the sums of the vectors and of dgate.

@@ -251,31 +251,53 @@ mip_norm_step_grad_kernel(const __grid_constant__ StepGradArgs a) {
                 for (int j = 0; j < 4; ++j) x[j] = mul_f2(pack_f2(a.x_scale, a.x_scale), g[c][j]);
                 store_run<kWide, kType>(x, const_cast<char*>(at(a.dX, row, a.lddx)) + c * run * kSize, count[c], limit[c], buf);
             }
-            if (drop.bar) drop.apply(bits[c], g[c]);
             run_pairs<kWide>(z[c], buf, hat[c]);
             if (kPost) {
                 load_vector_pairs(a.post_w, col0 + c * run, exist[c], vectors, 1.0f, w);
                 normalized(hat[c], r.st.x, r.st.y, count[c]);
             }
-            if (a.gate) {
-                if (a.dgate) {
-                    uint64_t b[4];
-                    if (kPost && kMean) load_vector_pairs(a.post_b, col0 + c * run, exist[c], vectors, 0.0f, b);
+            if (!a.gate) {
+                if (drop.bar) drop.apply(bits[c], g[c]);
+            } else {
+                // The mask is taken from the products, not from what is multiplied: 0 times an infinity or a NaN that stands at a dropped
+                // place would be a NaN.  Both products in one go share its comparisons (16384 x 4096 bf16, rms norms, gate for each channel
+                // 238 us, one by one 246); with a bias behind the block there are no registers for both (layer norms 345, one by one 317).
+                constexpr bool kBoth = !(kPost && kMean);
+                const uint32_t draws[4] = {bits[c].x, bits[c].y, bits[c].z, bits[c].w};
+                uint64_t b[4];
+                const auto products = [&](auto masked, auto of_gate, auto of_z) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        uint64_t u = hat[c][j];
-                        if (kPost) u = kMean ? fma_f2(u, w[j], b[j]) : mul_f2(u, w[j]);
-                        t[c][j] = mul_f2(g[c][j], u);
+                        const uint64_t k = masked ? drop.scaled(g[c][j]) : g[c][j];
+                        const bool lo = !masked || draws[j] << 16 >= drop.bar, hi = !masked || draws[j] >= drop.bar;
+                        if (of_gate) {
+                            uint64_t u = hat[c][j];
+                            if (kPost) u = kMean ? fma_f2(u, w[j], b[j]) : mul_f2(u, w[j]);
+                            t[c][j] = mul_f2(k, u);
+                            if (masked) t[c][j] = Dropout::where(lo, hi, t[c][j]);
+                        }
+                        if (of_z) {
+                            g[c][j] = mul_f2(k, b[j]);
+                            if (masked) g[c][j] = Dropout::where(lo, hi, g[c][j]);
+                        }
                     }
+                };
+                const auto gate_products = [&](auto of_gate, auto of_z) {
+                    if (drop.bar) products(std::true_type{}, of_gate, of_z);
+                    else products(std::false_type{}, of_gate, of_z);
+                };
+                if (kBoth) run_pairs<kWide>(gate[c], buf, b);
+                if (a.dgate) {
+                    if (!kBoth) load_vector_pairs(a.post_b, col0 + c * run, exist[c], vectors, 0.0f, b);
+                    gate_products(std::true_type{}, std::bool_constant<kBoth>{});
                     if (gate_each) {
                         store_run<kWide, kType>(t[c], const_cast<char*>(at(a.dgate, row, a.lddgate)) + c * run * kSize, count[c], limit[c], buf);
                     } else {
                         gate_s.add(c, [&](int j, uint64_t s) { return add_f2(t[c][j], s); });
                     }
                 }
-                run_pairs<kWide>(gate[c], buf, t[c]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) g[c][j] = mul_f2(g[c][j], t[c][j]);
+                if (!kBoth) run_pairs<kWide>(gate[c], buf, b);
+                if (!kBoth || !a.dgate) gate_products(std::false_type{}, std::true_type{});
             }
             if (kPost) {
                 post_w.add(c, [&](int j, uint64_t s) { return fma_f2(g[c][j], hat[c][j], s); });

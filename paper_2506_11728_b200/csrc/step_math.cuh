@@ -45,15 +45,19 @@ struct Dropout {
         const unsigned long long g = static_cast<unsigned long long>(row) * groups + (static_cast<unsigned long long>(col) >> 3);
         return philox(make_uint4(static_cast<uint32_t>(g), static_cast<uint32_t>(g >> 32), static_cast<uint32_t>(step), static_cast<uint32_t>(step >> 32)), m.keys);
     }
-    // (the high half of a word is compared with the low half still behind it: that changes nothing)
+    // A pair without its dropped elements.  (The high half of a word is compared with the low half still behind it: that changes
+    // nothing.)
+    static __device__ __forceinline__ uint64_t where(bool keep_lo, bool keep_hi, uint64_t v) {
+        float lo, hi;
+        unpack_f2(v, lo, hi);
+        return pack_f2(keep_lo ? lo : 0.0f, keep_hi ? hi : 0.0f);
+    }
+    __device__ __forceinline__ uint64_t kept(uint32_t word, uint64_t v) const { return where(word << 16 >= bar, word >= bar, v); }
+    __device__ __forceinline__ uint64_t scaled(uint64_t v) const { return mul_f2(v, pack_f2(m.scale, m.scale)); }
     __device__ __forceinline__ void apply(const uint4& bits, uint64_t (&v)[4]) const {
         const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float lo, hi;
-            unpack_f2(mul_f2(v[j], pack_f2(m.scale, m.scale)), lo, hi);
-            v[j] = pack_f2(w[j] << 16 >= bar ? lo : 0.0f, w[j] >= bar ? hi : 0.0f);
-        }
+        for (int j = 0; j < 4; ++j) v[j] = kept(w[j], scaled(v[j]));
     }
 };
 __device__ __forceinline__ float warp_sum(float v) {

@@ -29,3 +29,38 @@ def test_backward_without_weights(mg, M, N, layout, left_out):
             for name in left_out:
                 c[name] = None
             base.check_grad(mg, c, kind, layout, M, N, rng)
+
+
+@pytest.mark.parametrize("layout", ["dense", "odd"])
+@pytest.mark.parametrize("kind", u.TYPES)
+@pytest.mark.parametrize("gate_rows", [1, 3, 1000])
+@pytest.mark.parametrize("M,N", [(30, 40), (700, 24), (9, 1001), (4, 8200)])
+def test_gradients_of_dropped_places_are_zero_whatever_was_there(mg, M, N, gate_rows, kind, layout):
+    """Infinities and NaNs in z, the gate and the gradient, at dropped places alone: they reach nothing."""
+    rng = np.random.default_rng([M, N, gate_rows, 22])
+    c = base.case(rng, M, N, kind, "none", "none", gate_rows, 0.4)
+    off = c["mask"] == 0
+    dy = u.rounded(rng.standard_normal((M, N)), kind)
+    clean = {k: np.where(off, 0, v) for k, v in (("z", c["z"]), ("dy", dy))}
+    st = np.zeros((M, 4))
+    for spoiled in ("z", "gate", "dy"):
+        d, g = dict(c), dy
+        bad = np.where(rng.random((M, N)) < 0.5, np.nan, np.where(rng.random((M, N)) < 0.5, np.inf, -np.inf))
+        if spoiled == "z":
+            d["z"] = np.where(off, bad, c["z"])
+        elif spoiled == "dy":
+            g = np.where(off, bad, dy)
+        elif gate_rows == 1:
+            d["gate"] = np.where(off, bad, c["gate"])
+        else:
+            continue
+        y = f.step(dict(c, z=clean["z"]))[0]
+        got = base.backward(mg, d, kind, layout, M, N, y, st, g, None, without=("dX",) if spoiled == "dy" else ())
+        want, size = (fn(dict(c, z=clean["z"]), y, st, clean["dy"] if spoiled == "dy" else dy, None) for fn in (f.step_grad, base.grad_sizes))
+        for name, ref in (("dX", "dx"), ("dZ", "dz"), ("dgate", "dgate")):
+            if name not in got:
+                continue
+            extra = M * 2.0 ** -24 * size[name] if name == "dgate" else 0
+            tol = base.arithmetic(N) * size[name] + extra + u.ROUND[kind] * np.abs(want[ref]) * 1.01 + u.TINY[kind]
+            assert (np.abs(got[name] - want[ref]) <= tol).all(), (spoiled, name)
+        assert (got["dZ"][off] == 0).all()
