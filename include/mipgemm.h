@@ -586,8 +586,8 @@ int mipgemm_norm_step(int type, int post, int pre, int64_t M, int64_t N, float e
  *   dgate : as gate (written), summed over the rows that share a gate row.  Dropped places add 0 to it and get 0 in
  *       dZ, whatever stands there in Z, the gate and the gradients
  *   dpost_weight, dpost_bias, dpre_weight, dpre_bias : N float32 (written), summed over all rows in binary32
- * M == 0 writes zeros to the four vectors.  Scratch memory: at most 8 bytes * N * (vectors wanted + 1) for each SM of the
- * device, for the sums of the vectors and of dgate.
+ * M == 0 writes zeros to the four vectors.  Scratch memory, for the sums of the vectors and of dgate: at most 12 bytes * N * (vectors
+ * wanted + 1) for each SM of the device; a lent buffer of 8 bytes * N * (vectors wanted + 1) for each SM is enough.
  */
 int mipgemm_norm_step_grad(int type, int post, int pre, int64_t M, int64_t N,
                            const void *dY, int64_t lddy, const void *dH, int64_t lddh,

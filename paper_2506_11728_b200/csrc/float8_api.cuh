@@ -444,7 +444,9 @@ int norm_step_grad_impl(int type, mip::StepGradArgs& a, float drop, void* stream
         ++g_launches;
         return e == cudaSuccess ? MIPGEMM_OK : cuda_fail(e);
     }
-    const size_t need = a.M > 0 ? mip::plan_norm_step_grad(a, dev->sm_count) : 0;
+    size_t need = a.M > 0 ? mip::plan_norm_step_grad(a, dev->sm_count, mip::kMostWorkers) : 0;
+    // (a lent buffer need not hold more than two workers' sums for each SM)
+    if (dev->lent && need > dev->lent_bytes) need = mip::plan_norm_step_grad(a, dev->sm_count, mip::kFewWorkers);
     Scratch scratch(dev, stream);
     if ((st = scratch.reserve(need)) != MIPGEMM_OK) return st;
     int launches = 0;

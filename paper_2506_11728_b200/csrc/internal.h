@@ -370,7 +370,8 @@ struct StepGradArgs {
     float* sum_part;
     float* gate_part;
 };
-size_t plan_norm_step_grad(StepGradArgs& a, int sm_count);       // bytes of scratch
+constexpr int kMostWorkers = 3, kFewWorkers = 2;                 // on an SM: as many as there may be, as all sizes can do with
+size_t plan_norm_step_grad(StepGradArgs& a, int sm_count, int per_sm);       // bytes of scratch
 cudaError_t launch_norm_step_grad(int type, StepGradArgs a, void* scratch, cudaStream_t stream, int* launches);
 
 // Auxiliary kernels.

@@ -513,12 +513,15 @@ size_t sums_bytes(const StepGradArgs& a, const GradShape& s) {
 
 }  // namespace
 
-// How the rows are dealt: fills a's cluster, workers, units, parts and part_rows; returns the scratch bytes needed.
-size_t plan_norm_step_grad(StepGradArgs& a, int sm_count) {
+// How the rows are dealt: fills a's cluster, workers, units, parts and part_rows; returns the scratch bytes needed: no more than
+// `per_sm` planes of N float32 for each SM and vector.
+size_t plan_norm_step_grad(StepGradArgs& a, int sm_count, int per_sm) {
     const GradShape s = grad_shape(a.N);
     a.cluster = s.cluster;
-    // (512 threads of up to 128 registers fill an SM, and their sums' shared memory: 160 KB at most)
-    const long long resident = std::max<long long>(1, static_cast<long long>(sm_count) * (kGradThreads / (s.threads * s.rows)) / s.cluster);
+    // (512 threads of up to 128 registers fill an SM, and their sums' shared memory: 160 KB at most; three CTAs are those of rows of 2049
+    // to 2560 columns: with two 16384 x 2560 bf16 156 -> 192 us)
+    const int here = std::min(per_sm, kGradThreads / (s.threads * s.rows));
+    const long long resident = std::max<long long>(1, static_cast<long long>(sm_count) * here / s.cluster);
     const bool gate_sum = a.dgate && a.gate_rows > 1;
     const long long group_rows = gate_sum ? std::min(a.gate_rows, a.M) : a.M;
     const long long groups = (a.M + group_rows - 1) / group_rows;

@@ -64,3 +64,22 @@ def test_gradients_of_dropped_places_are_zero_whatever_was_there(mg, M, N, gate_
             tol = base.arithmetic(N) * size[name] + extra + u.ROUND[kind] * np.abs(want[ref]) * 1.01 + u.TINY[kind]
             assert (np.abs(got[name] - want[ref]) <= tol).all(), (spoiled, name)
         assert (got["dZ"][off] == 0).all()
+
+
+@pytest.mark.parametrize("N", [24, 1000, 2049, 2304, 2560, 2561, 5000, 9000])
+def test_a_lent_buffer_of_the_documented_size_is_enough(mg, N):
+    """8 bytes * N * (vectors wanted + 1) for each SM, whatever the row's length, with and without sums of a gate; the sums are those
+    of the library's own scratch up to their order."""
+    import torch
+    rng = np.random.default_rng([N, 23])
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    M = 6 * sms                          # (rows for two, three or six workers on an SM, without a remainder)
+    for gate_rows, vectors in ((0, 4), (M, 4), (M // 2, 4), (M, 0)):
+        names = ("dpost_weight", "dpost_bias", "dpre_weight", "dpre_bias")
+        c = base.case(rng, M, N, "bf16", "layer", "layer", gate_rows, 0.0)
+        room = torch.empty(8 * N * (vectors + 1) * sms, dtype=torch.uint8, device="cuda")
+        assert mg.mipgemm_set_workspace(room, room.numel()) == mg.OK
+        try:
+            base.check_grad(mg, c, "bf16", "dense", M, N, rng, without=() if vectors else names)
+        finally:
+            mg.mipgemm_set_workspace(None, 0)
