@@ -407,6 +407,7 @@ int norm_step_grad_impl(int type, mip::StepGradArgs& a, float drop, void* stream
     if ((!post && (a.post_w || a.post_b || a.dpost_w || a.dpost_b)) || (!pre && (a.pre_w || a.dpre_w || a.dpre_b || a.dH))) return MIPGEMM_ERR_INVALID_ARG;
     if ((a.post != MIPGEMM_NORM_LAYER && (a.post_b || a.dpost_b)) || (a.pre != MIPGEMM_NORM_LAYER && a.dpre_b)) return MIPGEMM_ERR_INVALID_ARG;
     if (!a.dX && !a.dZ && !a.dgate && !a.dpost_w && !a.dpost_b && !a.dpre_w && !a.dpre_b) return MIPGEMM_ERR_INVALID_ARG;
+    if (a.dX && a.dX == a.dZ) return MIPGEMM_ERR_INVALID_ARG;
     if (a.N == 0) return MIPGEMM_OK;
     if (a.M > 0) {
         if ((pre && (!a.dH || !a.Y)) || (!pre && !a.dY) || ((post || pre) && !a.stats)) return MIPGEMM_ERR_INVALID_ARG;
