@@ -524,8 +524,10 @@ int mipgemm_f8_dequantize(int type, int format, int blocks, int64_t M, int64_t N
  *   residual : M x N of the call's type, ldr >= N, or NULL; may be C itself (with ldr == ldc): C += ...
  *   C : M x N of the call's type, ldc >= N (written)
  * A block's products are summed on the tensor cores in binary32, the blocks' sums in binary32 behind their scales, in the
- * order of k or in equal shares of it; the error stays below (K + 8) 2^-23 of the sum of the magnitudes.  Scratch memory: as for
- * mipgemm_s8s8_linear.
+ * order of k or in equal shares of it; the error stays below (K + 8) 2^-23 of the sum of the magnitudes, as long as every product
+ * a_scale b_scale, and every block's sum times its b_scale, is 0 or within binary32's normal range (2^-126 to 2^128: what is
+ * multiplied first depends on the form; beyond it a term may come out as 0, an infinity or a NaN although the exact one is none).
+ * Scratch memory: as for mipgemm_s8s8_linear.
  */
 int mipgemm_f8f8_product(int type, int a_format, int b_format, int a_order, int b_order, int b_blocks,
                          int64_t M, int64_t N, int64_t K,
