@@ -75,3 +75,35 @@ def test_short_sums_as_they_are_planned(mg, M, N, K, what):
     for kind, residual in (("f32", "own"), ("bf16", None)):
         C, want, _ = product(mg, M, N, K, what, kind, residual, 1)
         assert torch.equal(C, want), (kind, residual)
+
+
+@pytest.mark.parametrize("formats", [("e4m3", "e4m3"), ("e5m2", "e4m3"), ("e4m3", "e5m2")])
+@pytest.mark.parametrize("what", ["forward", "forward_rows", "input_grad", "weight_grad"])
+@pytest.mark.parametrize("form,M,N,K", [("pair", 6000, 5128, 700), ("single", 4000, 3001, 1300), ("pair", 5129, 6001, 389)])
+def test_every_element_of_many_tiles(mg, form, M, N, K, what, formats):
+    """Codes over the formats' whole range, any scales, several tiles a CTA and several blocks of K: the documented bound, against 64 bits."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(M + K)
+    orders = {"forward": (0, 0, "squares"), "forward_rows": (0, 0, "rows"), "input_grad": (0, 1, "squares"), "weight_grad": (1, 1, "columns")}
+    ao, bo, bb = orders[what]
+    mats = []
+    for rows, cols, blocks, fmt in (((K, M) if ao else (M, K)) + ("columns" if ao else "rows", formats[0]), ((K, N) if bo else (N, K)) + (bb, formats[1])):
+        pitch = (cols + 15) // 16 * 16
+        q = torch.zeros(rows, pitch, dtype=torch.uint8, device="cuda")
+        v = (torch.randn(rows, cols, generator=g, device="cuda") * f.LARGEST[fmt] / 5).clamp_(-f.LARGEST[fmt], f.LARGEST[fmt]).to(f.f8_type(fmt))
+        q[:, :cols] = v.view(torch.uint8)
+        s = (torch.rand(f.scale_shape(blocks, rows, cols), generator=g, device="cuda") + 0.5) / f.LARGEST[fmt]
+        d = s.double().repeat_interleave(128, 0)
+        d = d[:cols].t() if blocks == "rows" else (d[:rows] if blocks == "columns" else d[:rows].repeat_interleave(128, 1)[:, :cols])
+        mats.append((q, pitch, s, v.double() * d))
+    (A, lda, sa, a), (B, ldb, sb, b) = mats
+    a, b = a.t() if ao else a, b if bo else b.t()
+    want, total = a @ b, a.abs() @ b.abs()
+    mg.mipgemm_set_tuning(force_path=2 if form == "pair" else 1)
+    for kind, half, tiny in (("f32", 2.0 ** -24, 2.0 ** -149), ("bf16", 2.0 ** -8, 2.0 ** -134)):
+        C = torch.full((M, N), float("nan"), dtype=torch.float32 if kind == "f32" else torch.bfloat16, device="cuda")
+        mg.mipgemm_f8f8_product(mg.TYPES[kind], mg.F8_FORMATS[formats[0]], mg.F8_FORMATS[formats[1]], ao, bo, mg.F8_BLOCKS[bb], M, N, K, A, lda, sa, sa.shape[1],
+                                B, ldb, sb, sb.shape[1], None, None, 0, C, N)
+        assert mg.mipgemm_device_status() == mg.OK
+        tol = total * (K + 8) * 2.0 ** -23 + half * want.abs() * 1.01 + tiny
+        assert bool(((C.double() - want).abs() <= tol).all()), kind
