@@ -88,7 +88,10 @@ F8Plan plan_f8(const mip::F8ProductArgs& a, const DeviceState* dev) {
             if ((k_blocks + share - 1) / share != split) continue;
             // clocks of a k-block (measured: pairs 780, with a scale for each column 1200; single CTAs 480 and 620), but not less than
             // its copies' latency over the stages on their way, which is longer where few row tiles share the weights (512 x 4096 x
-            // 14336 bf16: 128 single CTAs 61 us, 64 units of pairs with K in two shares 46); of a tile's outputs, which nothing hides
+            // 14336 bf16: 128 single CTAs 57 us, 64 units of pairs with K in two shares 45; 256 x 4096 x 14336: 28 and, in four shares, 25;
+            // from eight row tiles, 1024 x 4096 x 14336: pairs whole 64, in two shares 85); of a tile's outputs, which nothing hides.
+            // Of 32 sizes (64 to 4096 rows, both kinds of scales) 24 get a form within 5 % of the best one; furthest off are 1024 x 1024 x
+            // 8192 (23.1 us, pairs in four shares 19.1) and, with column scales, 2048 x 2048 x 512 (11.0, single CTAs 9.0).
             const int stages = mip::f8_product_stages(a.type, pair != 0, a.b_vec != 0, split > 1);
             const double latency = ((a.M + side - 1) / side < 8 ? 3600.0 : 2000.0) / stages;
             const double block = std::max(pair ? (a.b_vec ? 1200.0 : 780.0) : (a.b_vec ? 620.0 : 480.0), latency);

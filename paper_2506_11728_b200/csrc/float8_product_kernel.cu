@@ -15,7 +15,8 @@
 // What bounds it.  Squares: 8192 x 4096 x 4096 bf16 131 to 136 us (2060 TFLOP/s); without a tile's outputs, which nothing hides as the
 // sums' registers are taken until then, 111, without the sums 92.  16384 x 4096 x 11008: 717 us after a pause, 773 in a row of calls
 // (power).  A scale for each column: two packed operations for two elements make a block 512 clocks of the summing warps' pipes at
-// least, 1200 with their waits (11008 x 4096 x 8192 float32, added to: 575 us).
+// least, 1200 with their waits (11008 x 4096 x 8192 float32, added to: 568 us).  Few blocks of K: a tile's
+// outputs (16384 x 4096 x 64 bf16 70 us, float32 57, their bytes 21 and 41).
 //
 // Every wait is bounded, with the unwinding of the dense layer kernel.
 #include <algorithm>

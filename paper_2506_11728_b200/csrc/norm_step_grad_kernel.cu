@@ -12,8 +12,10 @@
 // in registers (40 to 80 of a thread's) they left room for one block on an SM, whose warps waited for each row's exchanges
 // together; two blocks by turns, with the next row's elements on their way, fill those gaps.
 //
-// What bounds it: the instructions (990 of a warp for 16 columns of a row with two norms, a gate and dropout) and their latencies,
-// beside the bytes of dy, dh, y, z, dx and dz: 16384 x 4096 bf16 234 us, the bytes 123.
+// What bounds it: the instructions (1000 of a warp for 16 columns of a row with two norms, a gate and dropout) and their latencies,
+// beside the bytes of dy, dh, y, z, dx and dz: 16384 x 4096 bf16 238 to 241 us, the bytes 123.  Gate rows that few rows share leave most
+// of a CTA's rows side by side idle (16384 x 1024, a gate for 2 rows 143 us, for each row 69); rows that take a whole cluster wait for
+// its barriers (4096 x 16384 337 us, 4096 x 32768 1111, the bytes 246).
 #include <algorithm>
 #include <atomic>
 
